@@ -147,7 +147,7 @@ def work(case):
     b = 12.0 * n + feat + 4.0 * H * R + 8.0 * (n + 1) + 4.0 * E + 4.0 * E * H + 4.0 * n * H + 4.0 * n * (c["graph"] == "packed")
     f = E * H * (2.0 * c["dk"] + 2.0 * R + 20) + E * (8.0 * R + 20)
     if train:  # the transposed graph, the weights' gradient, and those of features, radial weights and positions
-        b += 8.0 * (n + 1) + 4.0 * E + 4.0 * E * H + feat + 4.0 * H * R + 12.0 * n
+        b += 8.0 * (n + 1) + 8.0 * E + 4.0 * E * H + feat + 4.0 * H * R + 12.0 * n
         f += E * H * (4.0 * c["dk"] + 4.0 * R + 20) + E * (8.0 * R + 30)
     return {"bytes": b, "flops": f}
 
@@ -281,10 +281,10 @@ def _own_attention(s):
     alpha, lse = e2f.e2f_attention_forward(ctx, s["pos"], s["rp"], s["ci"], c["cutoff"], **kw)
     out = {"alpha": alpha, "lse": lse}
     if c["kind"] == "train":
-        row_t, perm = e2f.e2f_transpose_graph(ctx, c["n"], s["rp"], s["ci"])
+        row_t, col_t, perm = e2f.e2f_transpose_graph(ctx, c["n"], s["rp"], s["ci"])
         gq, gk, gw, gp = e2f.e2f_attention_backward(ctx, s["pos"], s["rp"], s["ci"], c["cutoff"], alpha, lse, s["ga"],
-                                                    row_t, perm, **kw)
-        out.update(row_t=row_t, perm=perm, grad_q=gq, grad_k=gk, grad_w=gw, grad_pos=gp)
+                                                    row_t, col_t, perm, **kw)
+        out.update(row_t=row_t, col_t=col_t, perm=perm, grad_q=gq, grad_k=gk, grad_w=gw, grad_pos=gp)
     return out
 
 
@@ -316,7 +316,7 @@ def _plain_attention(s):
     c = s["case"]
     n, H, dk, R, cap, rc = c["n"], c["H"], c["dk"], c["R"], c["cap"], c["cutoff"]
     i, j = _rows(s)
-    every, E, share = (s["rp"], s["ci"]), i.numel(), H // c["Hk"]
+    recv, send, E, share = i, j, i.numel(), H // c["Hk"]
     if s["gid"] is not None:  # the edges of one graph alone
         at = (s["gid"][i] == s["gid"][j]).nonzero()[:, 0]
         i, j = i[at], j[at]
@@ -347,7 +347,7 @@ def _plain_attention(s):
     out = {"alpha": whole, "lse": lse}
     if c["kind"] != "train":
         return out
-    col, perm = torch.sort(every[1].long(), stable=True)
+    col, perm = torch.sort(send, stable=True)
     row_t = torch.zeros(n + 1, dtype=torch.long, device=DEV)
     row_t[1:] = torch.bincount(col, minlength=n).cumsum(0)
     ga = s["ga"] if s["gid"] is None else s["ga"][at]
@@ -365,8 +365,8 @@ def _plain_attention(s):
         dd = dd + ((ds @ s["w"]) * basis * z).sum(1) * (-2.0 * (R - 1) / rc)
     f = v * torch.where(d > 0, dd / d, 0.0)[:, None]
     grad_pos = torch.zeros_like(s["pos"]).index_add(0, i, f).index_add(0, j, -f)
-    out.update(row_t=row_t, perm=perm.int(), grad_q=grad_q.to(s["q"].dtype), grad_k=grad_k.to(s["k"].dtype),
-               grad_w=grad_w, grad_pos=grad_pos)
+    out.update(row_t=row_t, col_t=recv[perm].int(), perm=perm.int(), grad_q=grad_q.to(s["q"].dtype),
+               grad_k=grad_k.to(s["k"].dtype), grad_w=grad_w, grad_pos=grad_pos)
     return out
 
 
@@ -473,9 +473,9 @@ def _exact_attention(s):
     out = {"alpha": alpha.detach(), "lse": (top + total.log()).detach()}
     if train:
         (alpha * s["ga"].double()).sum().backward()
-        order = s["ci"].cpu().numpy().argsort(kind="stable")
-        out.update(row_t=torch.cat([s["rp"][:1], torch.bincount(s["ci"].long(), minlength=n).cumsum(0)]),
-                   perm=torch.from_numpy(order).int().to(DEV), grad_q=q.grad, grad_k=k.grad,
+        order = torch.from_numpy(s["ci"].cpu().numpy().argsort(kind="stable")).to(DEV)
+        out.update(col_t=torch.arange(n, device=DEV).repeat_interleave(counts)[order].int(), row_t=torch.cat([s["rp"][:1], torch.bincount(s["ci"].long(), minlength=n).cumsum(0)]),
+                   perm=order.int(), grad_q=q.grad, grad_k=k.grad,
                    grad_w=None if w is None else w.grad, grad_pos=pos.grad)
     return out
 
