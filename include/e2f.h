@@ -124,6 +124,140 @@ e2f_status e2f_attention_weights(e2f_ctx* ctx, const float* pos, const float* q,
                                  const int64_t* row_ptr, const int32_t* col_idx, int64_t n_edges, float* alpha,
                                  void* stream);
 
+/* The transposed graph: the edges by their sender.  rowT_ptr [n+1]; colT
+ * [n_edges]: the receivers of sender j's edges at rowT_ptr[j] .. rowT_ptr[j+1],
+ * and perm [n_edges] where each stands in the graph's own order, ascending.
+ * Made once for a graph and used by the backward of every layer on it.
+ * Senders outside [0, n) are taken as the nearest atom (e2f_validate_graph
+ * finds them).  workspace: e2f_transpose_graph_workspace_size bytes, 256-byte
+ * aligned (E2F_ECAPACITY below).  Asynchronous, no allocation, can be captured
+ * in a HIP graph; deterministic. */
+e2f_status e2f_transpose_graph_workspace_size(e2f_ctx* ctx, int32_t n, int64_t n_edges, size_t* bytes);
+e2f_status e2f_transpose_graph(e2f_ctx* ctx, int32_t n, const int64_t* row_ptr, const int32_t* col_idx,
+                               int64_t n_edges, int64_t* rowT_ptr, int32_t* colT, int32_t* perm, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+typedef struct {
+  int32_t heads;    /* H, 1..64 */
+  int32_t k_heads;  /* heads of k, a divisor of H: head h reads k's head h / (H / k_heads) */
+  int32_t dk;       /* features of a head, 0 (no product) .. 256 */
+  int32_t n_rbf;    /* radial functions, 0 (none) or 2..32 */
+  float cutoff;     /* of the envelope and the radial functions */
+  float scale;      /* of the product, usually dk^-0.5 */
+  float cap;        /* the scores' bound; 0: none */
+  e2f_dtype dtype;  /* of q, k and their gradients */
+  int64_t ldq, ldk; /* elements from one atom's q (k) to the next's, at least heads dk (k_heads dk):
+                       q and k may be columns of one projection; 0: packed */
+} e2f_attention_params;
+
+/* Attention weights of the graph's edges from capped scores, under a mask by
+ * graph.  For the edge e = (i, j) of row i and head h, d = |r_i - r_j|:
+ *   x = scale sum_t q[i][h][t] k[j][h / (H / k_heads)][t]
+ *       + sum_r rbf_w[h][r] exp(-((d - mu_r)/sigma)^2),   mu_r, sigma as for e2f_attention_weights,
+ *   s = cap tanh(x / cap)  (s = x with cap = 0),
+ *   alpha[e][h] = (cos(pi d / cutoff) + 1)/2 * exp(s - lse[i][h]),  the envelope 0 for d >= cutoff,
+ *   lse[i][h] = log(sum over row i of exp(s)).
+ * graph_id [n] or NULL: an edge between atoms of different ids has alpha = 0,
+ * takes no part in the sums, and what its sender holds is not looked at; a row
+ * left without an edge has lse = -infinity.  q [n][H][dk], k [n][k_heads][dk]
+ * (unused if dk = 0); rbf_w float32 [H][n_rbf]; alpha float32 [n_edges][H];
+ * lse float32 [n][H], kept for the backward.  Sums and statistics are float32.
+ * Without a cap, for float32 features and one graph the weights are those of
+ * e2f_attention_weights with q scaled.  The CSR is trusted for values but read
+ * with clamped indices.  Asynchronous, no allocation, can be captured in a HIP
+ * graph; deterministic. */
+e2f_status e2f_attention_forward(e2f_ctx* ctx, const e2f_attention_params* params, const float* pos,
+                                 const int32_t* graph_id, const void* q, const void* k, int32_t n,
+                                 const float* rbf_w, const int64_t* row_ptr, const int32_t* col_idx, int64_t n_edges,
+                                 float* alpha, float* lse, void* stream);
+/* Backward of e2f_attention_forward (same parameters and inputs, its alpha and
+ * lse): the vector-Jacobian products for grad_alpha [n_edges][H] (of the edges
+ * between different graphs not looked at), e.g. e2f_wigner6j_conv_backward's:
+ *   grad_q [n][H][dk], grad_k [n][k_heads][dk] of the parameters' dtype, packed (the
+ *     heads that share a head of k summed);
+ *   grad_rbf_w float32 [H][n_rbf];
+ *   grad_pos float32 [n][3]: through distances and envelope, the graph held fixed; an
+ *     edge of length 0 adds nothing.  The whole gradient of a layer's positions is
+ *     this plus e2f_wigner6j_conv_backward's.
+ * Any of them may be NULL (not all).  rowT_ptr, colT, perm: e2f_transpose_graph's,
+ * needed for grad_k and grad_pos (else NULL).  workspace:
+ * e2f_attention_backward_workspace_size bytes, 256-byte aligned (E2F_ECAPACITY
+ * below).  Outputs must not overlap inputs.  Asynchronous, no allocation, can be
+ * captured in a HIP graph; deterministic. */
+e2f_status e2f_attention_backward_workspace_size(e2f_ctx* ctx, const e2f_attention_params* params, int32_t n,
+                                                 int64_t n_edges, size_t* bytes);
+e2f_status e2f_attention_backward(e2f_ctx* ctx, const e2f_attention_params* params, const float* pos,
+                                  const int32_t* graph_id, const void* q, const void* k, int32_t n,
+                                  const float* rbf_w, const int64_t* row_ptr, const int32_t* col_idx,
+                                  int64_t n_edges, const int64_t* rowT_ptr, const int32_t* colT, const int32_t* perm,
+                                  const float* alpha, const float* lse, const float* grad_alpha, void* grad_q,
+                                  void* grad_k, float* grad_rbf_w, float* grad_pos, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+typedef struct {
+  int lmax;              /* L, 0..6; 0: plain activations [N][C] */
+  int32_t channels;      /* C, a multiple of 4, <= 1024 */
+  int32_t gates;         /* gates of a channel: 0 (none), 1 (of all degrees) or L + 1 (one each) */
+  float eps;             /* added to the mean square, >= 0 */
+  e2f_dtype dtype;       /* of x, block, gate, out, normed and their gradients */
+  const float* post_w;   /* device [(L+1)][C], or NULL: the block's output is taken without a norm */
+  const float* res_scale;/* device [(L+1)][C], or NULL: ones */
+  const float* pre_w;    /* device [(L+1)][C], or NULL: no norm after the sum */
+} e2f_norm_params;
+
+/* The norms after a block and before the next one, with the block's gate, scale
+ * and residual sum, in one pass.  With rms(v)^2 = the mean over the degrees of the mean
+ * over (m, c) of v^2, plus eps (so rotations leave it alone; lmax = 0: the mean square
+ * of the channels):
+ *   out[i][l,m][c]    = x + res_scale[l][c] sigmoid(gate[i][l][c]) post_w[l][c] block / rms(block_i)
+ *   normed[i][l,m][c] = pre_w[l][c] out / rms(out_i)
+ * x, block, out, normed [n][(L+1)^2][C]; gate [n][gates][C] (NULL with gates = 0).
+ * block NULL: out = x, which is not written (out NULL), the norm before a first
+ * block.  normed NULL without pre_w.  rstd float32 [n][2] or NULL: 1/rms(block) and
+ * 1/rms(out) (1 for a norm that is not taken), kept for the backward.  Statistics and
+ * all between loads and stores are float32; out is rounded once and normed is taken of
+ * the sum before that rounding.  Outputs must not overlap inputs (E2F_EINVAL).
+ * Asynchronous, no allocation, can be captured in a HIP graph; deterministic. */
+e2f_status e2f_block_norm_forward(e2f_ctx* ctx, const e2f_norm_params* params, const void* x, const void* block,
+                                  const void* gate, int32_t n, void* out, void* normed, float* rstd, void* stream);
+/* Backward of e2f_block_norm_forward (same parameters and inputs, its rstd): the
+ * vector-Jacobian products for grad_out (the gradient of out, or of x's further use
+ * without a block; NULL: zero) and grad_normed (NULL: zero; only with pre_w):
+ *   grad_x, grad_block, grad_gate like x, block and gate; grad_post_w, grad_res_scale,
+ *   grad_pre_w float32 [(L+1)][C], summed over the atoms.
+ * Any of them may be NULL (not all); those of inputs that the parameters leave out must
+ * be.  workspace: e2f_block_norm_workspace_size bytes, 256-byte aligned (E2F_ECAPACITY
+ * below); not needed without the gradients of weights.  Outputs must not overlap inputs (E2F_EINVAL).
+ * Asynchronous, no allocation, can be captured in a HIP graph; deterministic. */
+e2f_status e2f_block_norm_workspace_size(e2f_ctx* ctx, const e2f_norm_params* params, int32_t n, size_t* bytes);
+e2f_status e2f_block_norm_backward(e2f_ctx* ctx, const e2f_norm_params* params, const void* x, const void* block,
+                                   const void* gate, const float* rstd, int32_t n, const void* grad_out,
+                                   const void* grad_normed, void* grad_x, void* grad_block, void* grad_gate,
+                                   float* grad_post_w, float* grad_res_scale, float* grad_pre_w, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/* The norm over all values of `count` tensors, e.g. the gradients of a training step:
+ * *sumsq (device, float64) = the sum of their squares, *norm (device) = its root; either
+ * may be NULL (not both).  tensors, sizes (values), dtypes (E2F_F32 or E2F_BF16): host
+ * arrays of `count`, read before the call returns; a tensor of no values may be NULL;
+ * addresses need an element's alignment.  Sums are float64.  Several GPUs that hold
+ * parts of the gradients add their sumsq before e2f_grad_clip.  workspace:
+ * e2f_grad_norm_workspace_size bytes, 256-byte aligned (E2F_ECAPACITY below).
+ * Asynchronous, no allocation, can be captured in a HIP graph; deterministic. */
+e2f_status e2f_grad_norm_workspace_size(e2f_ctx* ctx, int32_t count, const int64_t* sizes /* host */, size_t* bytes);
+e2f_status e2f_grad_norm(e2f_ctx* ctx, int32_t count, const void* const* tensors /* host */,
+                         const int64_t* sizes /* host */, const int32_t* dtypes /* host */, double* sumsq,
+                         float* norm, void* workspace, size_t workspace_bytes, void* stream);
+/* outs[t] = tensors[t] min(1, max_norm / (sqrt(*sumsq) + 1e-6)) for every tensor, the
+ * factor rounded to float32 (a norm that is infinite gives 0, NaN gives NaN: the caller
+ * that wants to skip such a step looks at the norm).  outs[t] may be tensors[t] (nothing
+ * is then written where the factor is 1); apart from that no out may overlap another
+ * tensor (E2F_EINVAL).  max_norm > 0.  Asynchronous, no allocation, can be captured in
+ * a HIP graph. */
+e2f_status e2f_grad_clip(e2f_ctx* ctx, int32_t count, const void* const* tensors /* host */,
+                         void* const* outs /* host */, const int64_t* sizes /* host */,
+                         const int32_t* dtypes /* host */, const double* sumsq, float max_norm, void* stream);
+
 /* Real regular solid harmonics (Def. 2.1) of p_i = pos_i - origins[origin_id[i]]
  * (origin 0 if origin_id is NULL; the zero vector if origins is NULL),
  * evaluated in float64 and rounded: out [N][(lmax+1)^2] float32. */

@@ -9,6 +9,7 @@
 #include <cstdlib>
 #include <algorithm>
 #include <cstring>
+#include <exception>
 #include <limits>
 #include <map>
 #include <string>
@@ -1428,6 +1429,390 @@ e2f_status e2f_wigner6j_conv_forward_global(e2f_ctx* ctx, const e2f_conv_params*
   E2F_TIMED("tile_plan", launch_iota(n, order, s));
   E2F_TIMED("recouple", launch_recouple(t, R, M32, true, order, n, C, dh, y, s));
   if (mixing) E2F_TIMED("mix", launch_mix(L, y, p->mix_w, p->mix_dtype == E2F_BF16, n, C, out, s));
+  return E2F_OK;
+}
+
+// ---- the operators around the convolution: capped attention, norms, clipping
+namespace {
+
+e2f_status check_workspace(const void* ws, size_t have, size_t need) {
+  if (need == 0) return E2F_OK;
+  if (!ws || have < need) return fail(E2F_ECAPACITY, "workspace of %zu bytes is required", need);
+  if ((uintptr_t)ws % 256) return fail(E2F_EINVAL, "workspace must be 256-byte aligned");
+  return E2F_OK;
+}
+
+struct TransposeLayout {
+  size_t cnt, sums, rank, list, total;
+};
+TransposeLayout transpose_layout(int32_t n, int64_t E) {
+  TransposeLayout t;
+  t.cnt = 0;
+  t.sums = al256(sizeof(int32_t) * (size_t)n);
+  t.rank = t.sums + al256(sizeof(int64_t) * (size_t)transpose_scan_blocks(n));
+  t.list = t.rank + al256(sizeof(int32_t) * (size_t)E);
+  t.total = t.list + al256(sizeof(int32_t) * (size_t)E);
+  return t;
+}
+
+e2f_status check_edges(e2f_ctx* ctx, int32_t n, int64_t n_edges) {
+  if (!ctx) return fail(E2F_EINVAL, "ctx is NULL");
+  if (n < 0 || n_edges < 0) return fail(E2F_EINVAL, "n or n_edges < 0");
+  if (n == 0 && n_edges > 0) return fail(E2F_EINVAL, "edges without atoms");
+  if (n_edges > std::numeric_limits<int32_t>::max()) return fail(E2F_EUNSUPPORTED, "more than 2^31-1 edges");
+  return E2F_OK;
+}
+
+e2f_status check_attention(e2f_ctx* ctx, const e2f_attention_params* p, int32_t n, int64_t n_edges) {
+  if (e2f_status rs = check_edges(ctx, n, n_edges); rs != E2F_OK) return rs;
+  if (!p) return fail(E2F_EINVAL, "params is NULL");
+  if (p->heads < 1) return fail(E2F_EINVAL, "heads = %d < 1", p->heads);
+  if (p->heads > 64) return fail(E2F_EUNSUPPORTED, "heads = %d > 64", p->heads);
+  if (p->k_heads < 1 || p->heads % p->k_heads)
+    return fail(E2F_EINVAL, "k_heads = %d must divide heads = %d", p->k_heads, p->heads);
+  if (p->dk < 0 || p->n_rbf < 0 || p->n_rbf == 1)
+    return fail(E2F_EINVAL, "dk >= 0 and n_rbf = 0 or >= 2 are required");
+  if (p->dk > kAttnMaxDk) return fail(E2F_EUNSUPPORTED, "dk = %d > %d", p->dk, kAttnMaxDk);
+  if (p->n_rbf > kAttnMaxRbf) return fail(E2F_EUNSUPPORTED, "n_rbf = %d > %d", p->n_rbf, kAttnMaxRbf);
+  if (!finite_pos(p->cutoff)) return fail(E2F_EINVAL, "cutoff must be finite and positive");
+  if (!std::isfinite(p->scale)) return fail(E2F_EINVAL, "scale must be finite");
+  if (!std::isfinite(p->cap) || p->cap < 0.0f) return fail(E2F_EINVAL, "cap must be finite and >= 0");
+  if ((int)p->dtype != E2F_F32 && (int)p->dtype != E2F_BF16) return fail(E2F_EINVAL, "dtype %d", (int)p->dtype);
+  if ((p->ldq && p->ldq < (int64_t)p->heads * p->dk) || (p->ldk && p->ldk < (int64_t)p->k_heads * p->dk))
+    return fail(E2F_EINVAL, "ldq or ldk is smaller than an atom's features");
+  return E2F_OK;
+}
+
+AttnArgs attention_args(const e2f_attention_params* p, const float* pos, const int32_t* gid, const void* q,
+                        const void* k, int32_t n, const float* w, const int64_t* row_ptr, const int32_t* col,
+                        int64_t E) {
+  AttnArgs a{};
+  a.pos = pos, a.gid = gid, a.q = q, a.k = k, a.w = w, a.row_ptr = row_ptr, a.col = col;
+  a.E = E;
+  a.ldq = p->ldq ? p->ldq : (int64_t)p->heads * p->dk;
+  a.ldk = p->ldk ? p->ldk : (int64_t)p->k_heads * p->dk;
+  a.n = n, a.H = p->heads, a.Hk = p->k_heads, a.dk = p->dk, a.R = p->n_rbf;
+  a.rc = p->cutoff, a.scale = p->scale, a.cap = p->cap;
+  a.bf16 = p->dtype == E2F_BF16;
+  return a;
+}
+
+// the inputs that both directions read
+e2f_status check_attention_inputs(const e2f_attention_params* p, const float* pos, const void* q, const void* k,
+                                  int32_t n, const float* rbf_w, const int64_t* row_ptr, const int32_t* col_idx,
+                                  int64_t n_edges) {
+  if (n > 0 && (!pos || !row_ptr)) return fail(E2F_EINVAL, "pos and row_ptr are required");
+  if (n > 0 && p->dk > 0 && (!q || !k)) return fail(E2F_EINVAL, "q and k are required with dk > 0");
+  if (p->n_rbf > 0 && !rbf_w) return fail(E2F_EINVAL, "rbf_w is required with n_rbf > 0");
+  if (n_edges > 0 && !col_idx) return fail(E2F_EINVAL, "col_idx is required");
+  return E2F_OK;
+}
+
+struct AttnLayout {
+  size_t ds, edge, part, total;
+};
+AttnLayout attention_layout(const e2f_attention_params* p, int64_t E) {
+  AttnLayout l;
+  l.ds = 0;
+  l.edge = al256(sizeof(float) * (size_t)E * p->heads);
+  l.part = l.edge + al256(sizeof(float) * 4 * (size_t)E);
+  l.total = l.part + al256(sizeof(float) * (size_t)kAttnParts * p->heads * p->n_rbf);
+  return l;
+}
+
+e2f_status check_norm(e2f_ctx* ctx, const e2f_norm_params* p, int32_t n) {
+  if (!ctx) return fail(E2F_EINVAL, "ctx is NULL");
+  if (!p) return fail(E2F_EINVAL, "params is NULL");
+  if (n < 0) return fail(E2F_EINVAL, "n < 0");
+  if (p->lmax < 0) return fail(E2F_EINVAL, "lmax = %d < 0", p->lmax);
+  if (p->lmax > kMaxL) return fail(E2F_EUNSUPPORTED, "lmax = %d > %d", p->lmax, kMaxL);
+  if (p->channels < 4 || p->channels % 4 || p->channels > 1024)
+    return fail(E2F_EUNSUPPORTED, "channels %d must be a multiple of 4 in 4..1024", p->channels);
+  if (p->gates != 0 && p->gates != 1 && p->gates != p->lmax + 1)
+    return fail(E2F_EINVAL, "gates = %d must be 0, 1 or lmax + 1", p->gates);
+  if (!std::isfinite(p->eps) || p->eps < 0.0f) return fail(E2F_EINVAL, "eps must be finite and >= 0");
+  if ((int)p->dtype != E2F_F32 && (int)p->dtype != E2F_BF16) return fail(E2F_EINVAL, "dtype %d", (int)p->dtype);
+  return E2F_OK;
+}
+
+e2f_status check_norm_inputs(const e2f_norm_params* p, const void* x, const void* block, const void* gate, int32_t n) {
+  if (n > 0 && !x) return fail(E2F_EINVAL, "x is required");
+  if (n > 0 && p->gates > 0 && !gate) return fail(E2F_EINVAL, "gate is required with gates > 0");
+  if (p->gates == 0 && gate) return fail(E2F_EINVAL, "gate without gates");
+  if (!block && (p->gates || p->post_w || p->res_scale) && n > 0)
+    return fail(E2F_EINVAL, "gates, post_w and res_scale need a block");
+  return E2F_OK;
+}
+
+struct Span {
+  const char* lo;
+  size_t bytes;
+};
+bool overlap(const Span& a, const Span& b) {
+  return a.lo && b.lo && a.bytes && b.bytes && a.lo < b.lo + b.bytes && b.lo < a.lo + a.bytes;
+}
+
+e2f_status check_tensors(e2f_ctx* ctx, int32_t count, const int64_t* sizes, const int32_t* dtypes,
+                         const void* const* tensors, int64_t* total) {
+  if (!ctx) return fail(E2F_EINVAL, "ctx is NULL");
+  if (count < 0) return fail(E2F_EINVAL, "count < 0");
+  if (count > 0 && (!sizes || !dtypes || !tensors)) return fail(E2F_EINVAL, "tensors, sizes and dtypes are required");
+  *total = 0;
+  for (int i = 0; i < count; ++i) {
+    if (sizes[i] < 0 || sizes[i] > (int64_t)1 << 40) return fail(E2F_EINVAL, "size of tensor %d", i);
+    if (dtypes[i] != E2F_F32 && dtypes[i] != E2F_BF16) return fail(E2F_EINVAL, "dtype of tensor %d", i);
+    if (sizes[i] > 0 && !tensors[i]) return fail(E2F_EINVAL, "tensor %d is NULL", i);
+    if ((uintptr_t)tensors[i] % (dtypes[i] == E2F_BF16 ? 2 : 4)) return fail(E2F_EINVAL, "alignment of tensor %d", i);
+    *total += sizes[i];
+  }
+  if (*total > (int64_t)1 << 44) return fail(E2F_EUNSUPPORTED, "more than 2^44 values");
+  return E2F_OK;
+}
+
+// a partial sum for every chunk of every tensor
+size_t grad_norm_bytes(int32_t count, const int64_t* sizes, int64_t total) {
+  const int64_t chunk = grad_chunk(total);
+  int64_t parts = 0;
+  for (int i = 0; i < count; ++i) parts += (sizes[i] + chunk - 1) / chunk;
+  return al256(sizeof(double) * (size_t)std::max<int64_t>(parts, 1));
+}
+
+}  // namespace
+
+e2f_status e2f_transpose_graph_workspace_size(e2f_ctx* ctx, int32_t n, int64_t n_edges, size_t* bytes) {
+  if (e2f_status rs = check_edges(ctx, n, n_edges); rs != E2F_OK) return rs;
+  if (!bytes) return fail(E2F_EINVAL, "bytes is NULL");
+  *bytes = transpose_layout(n, n_edges).total;
+  return E2F_OK;
+}
+
+e2f_status e2f_transpose_graph(e2f_ctx* ctx, int32_t n, const int64_t* row_ptr, const int32_t* col_idx,
+                               int64_t n_edges, int64_t* rowT_ptr, int32_t* colT, int32_t* perm, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  if (e2f_status rs = check_edges(ctx, n, n_edges); rs != E2F_OK) return rs;
+  if (!rowT_ptr) return fail(E2F_EINVAL, "rowT_ptr is required");
+  if (n > 0 && !row_ptr) return fail(E2F_EINVAL, "row_ptr is required");
+  if (n_edges > 0 && (!col_idx || !colT || !perm)) return fail(E2F_EINVAL, "col_idx, colT and perm are required");
+  const TransposeLayout t = transpose_layout(n, n_edges);
+  if (e2f_status rs = check_workspace(workspace, workspace_bytes, t.total); rs != E2F_OK) return rs;
+  if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
+  hipStream_t s = (hipStream_t)stream;
+  DeviceGuard g(ctx->device);
+  char* ws = (char*)workspace;
+  E2F_TIMED("transpose", launch_transpose(row_ptr, col_idx, n, n_edges, (int32_t*)(ws + t.cnt),
+                                          (int64_t*)(ws + t.sums), (int32_t*)(ws + t.rank), (int32_t*)(ws + t.list),
+                                          rowT_ptr, colT, perm, s));
+  return E2F_OK;
+}
+
+e2f_status e2f_attention_forward(e2f_ctx* ctx, const e2f_attention_params* p, const float* pos,
+                                 const int32_t* graph_id, const void* q, const void* k, int32_t n,
+                                 const float* rbf_w, const int64_t* row_ptr, const int32_t* col_idx, int64_t n_edges,
+                                 float* alpha, float* lse, void* stream) {
+  if (e2f_status rs = check_attention(ctx, p, n, n_edges); rs != E2F_OK) return rs;
+  if (e2f_status rs = check_attention_inputs(p, pos, q, k, n, rbf_w, row_ptr, col_idx, n_edges); rs != E2F_OK)
+    return rs;
+  if (n_edges > 0 && !alpha) return fail(E2F_EINVAL, "alpha is required");
+  if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
+  if (n == 0) return E2F_OK;
+  hipStream_t s = (hipStream_t)stream;
+  DeviceGuard g(ctx->device);
+  E2F_TIMED("attention", launch_att_forward(attention_args(p, pos, graph_id, q, k, n, rbf_w, row_ptr, col_idx,
+                                                           n_edges), alpha, lse, s));
+  return E2F_OK;
+}
+
+e2f_status e2f_attention_backward_workspace_size(e2f_ctx* ctx, const e2f_attention_params* p, int32_t n,
+                                                 int64_t n_edges, size_t* bytes) {
+  if (e2f_status rs = check_attention(ctx, p, n, n_edges); rs != E2F_OK) return rs;
+  if (!bytes) return fail(E2F_EINVAL, "bytes is NULL");
+  *bytes = attention_layout(p, n_edges).total;
+  return E2F_OK;
+}
+
+e2f_status e2f_attention_backward(e2f_ctx* ctx, const e2f_attention_params* p, const float* pos,
+                                  const int32_t* graph_id, const void* q, const void* k, int32_t n,
+                                  const float* rbf_w, const int64_t* row_ptr, const int32_t* col_idx,
+                                  int64_t n_edges, const int64_t* rowT_ptr, const int32_t* colT, const int32_t* perm,
+                                  const float* alpha, const float* lse, const float* grad_alpha, void* grad_q,
+                                  void* grad_k, float* grad_rbf_w, float* grad_pos, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  if (e2f_status rs = check_attention(ctx, p, n, n_edges); rs != E2F_OK) return rs;
+  if (!grad_q && !grad_k && !grad_rbf_w && !grad_pos) return fail(E2F_EINVAL, "no gradient is requested");
+  if (e2f_status rs = check_attention_inputs(p, pos, q, k, n, rbf_w, row_ptr, col_idx, n_edges); rs != E2F_OK)
+    return rs;
+  if ((grad_q || grad_k) && p->dk == 0) return fail(E2F_EINVAL, "grad_q and grad_k need dk > 0");
+  if (grad_rbf_w && p->n_rbf == 0) return fail(E2F_EINVAL, "grad_rbf_w needs n_rbf > 0");
+  if (n > 0 && !lse) return fail(E2F_EINVAL, "lse is required");
+  if (n_edges > 0 && (!alpha || !grad_alpha)) return fail(E2F_EINVAL, "alpha and grad_alpha are required");
+  if ((grad_k || grad_pos) && n > 0 && (!rowT_ptr || (n_edges > 0 && (!colT || !perm))))
+    return fail(E2F_EINVAL, "grad_k and grad_pos need the transposed graph");
+  const AttnLayout l = attention_layout(p, n_edges);
+  if (e2f_status rs = check_workspace(workspace, workspace_bytes, l.total); rs != E2F_OK) return rs;
+  if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
+  hipStream_t s = (hipStream_t)stream;
+  DeviceGuard g(ctx->device);
+  char* ws = (char*)workspace;
+  AttnGrad d{};
+  d.alpha = alpha, d.lse = lse, d.galpha = grad_alpha, d.rowT = rowT_ptr, d.colT = colT, d.perm = perm;
+  d.ds = (float*)(ws + l.ds), d.edge = (float*)(ws + l.edge), d.part = (float*)(ws + l.part);
+  d.gq = grad_q, d.gk = grad_k, d.gw = grad_rbf_w, d.gpos = grad_pos;
+  E2F_TIMED("attention_grad", launch_att_backward(attention_args(p, pos, graph_id, q, k, n, rbf_w, row_ptr, col_idx,
+                                                                 n_edges), d, s));
+  return E2F_OK;
+}
+
+e2f_status e2f_block_norm_forward(e2f_ctx* ctx, const e2f_norm_params* p, const void* x, const void* block,
+                                  const void* gate, int32_t n, void* out, void* normed, float* rstd, void* stream) {
+  if (e2f_status rs = check_norm(ctx, p, n); rs != E2F_OK) return rs;
+  if (e2f_status rs = check_norm_inputs(p, x, block, gate, n); rs != E2F_OK) return rs;
+  if (n > 0 && (out != nullptr) != (block != nullptr)) return fail(E2F_EINVAL, "out goes with block");
+  if (n > 0 && (normed != nullptr) != (p->pre_w != nullptr)) return fail(E2F_EINVAL, "normed goes with pre_w");
+  if (n > 0 && !out && !normed) return fail(E2F_EINVAL, "neither a block nor pre_w: nothing to compute");
+  const size_t el = p->dtype == E2F_BF16 ? 2 : 4, all = el * (size_t)n * nk_of(p->lmax) * p->channels;
+  const Span in[3] = {{(const char*)x, all}, {(const char*)block, all},
+                      {(const char*)gate, el * (size_t)n * p->gates * p->channels}};
+  const Span to[3] = {{(const char*)out, all}, {(const char*)normed, all},
+                      {(const char*)rstd, sizeof(float) * 2 * (size_t)n}};
+  for (int i = 0; i < 3; ++i) {
+    for (int j = 0; j < 3; ++j)
+      if (overlap(to[i], in[j])) return fail(E2F_EINVAL, "an output overlaps an input");
+    for (int j = 0; j < i; ++j)
+      if (overlap(to[i], to[j])) return fail(E2F_EINVAL, "two outputs overlap");
+  }
+  if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
+  if (n == 0) return E2F_OK;
+  hipStream_t s = (hipStream_t)stream;
+  DeviceGuard g(ctx->device);
+  const NormArgs a{x, block, gate, p->post_w, p->res_scale, p->pre_w, n, p->channels, p->gates, p->eps};
+  E2F_TIMED("block_norm", launch_norm_forward(p->lmax, p->dtype == E2F_BF16, a, out, normed, rstd, s));
+  return E2F_OK;
+}
+
+e2f_status e2f_block_norm_workspace_size(e2f_ctx* ctx, const e2f_norm_params* p, int32_t n, size_t* bytes) {
+  if (e2f_status rs = check_norm(ctx, p, n); rs != E2F_OK) return rs;
+  if (!bytes) return fail(E2F_EINVAL, "bytes is NULL");
+  *bytes = al256(sizeof(float) * 2 * (size_t)norm_parts(p->lmax, p->channels, p->dtype == E2F_BF16, n) *
+                 (p->lmax + 1) * p->channels);
+  return E2F_OK;
+}
+
+e2f_status e2f_block_norm_backward(e2f_ctx* ctx, const e2f_norm_params* p, const void* x, const void* block,
+                                   const void* gate, const float* rstd, int32_t n, const void* grad_out,
+                                   const void* grad_normed, void* grad_x, void* grad_block, void* grad_gate,
+                                   float* grad_post_w, float* grad_res_scale, float* grad_pre_w, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+  if (e2f_status rs = check_norm(ctx, p, n); rs != E2F_OK) return rs;
+  if (e2f_status rs = check_norm_inputs(p, x, block, gate, n); rs != E2F_OK) return rs;
+  const bool weights = grad_post_w || grad_res_scale || grad_pre_w;
+  if (!grad_x && !grad_block && !grad_gate && !weights) return fail(E2F_EINVAL, "no gradient is requested");
+  if (n > 0 && !rstd) return fail(E2F_EINVAL, "rstd is required");
+  if (n > 0 && (grad_block || grad_gate || grad_post_w || grad_res_scale) && !block)
+    return fail(E2F_EINVAL, "grad_block, grad_gate, grad_post_w and grad_res_scale need a block");
+  if ((grad_gate && !p->gates) || (grad_post_w && !p->post_w) || (grad_res_scale && !p->res_scale) ||
+      (grad_pre_w && !p->pre_w))
+    return fail(E2F_EINVAL, "the gradient of an input that is not there");
+  if (grad_normed && !p->pre_w) return fail(E2F_EINVAL, "grad_normed without pre_w");
+  size_t need = 0;
+  if (weights) {
+    if (e2f_status rs = e2f_block_norm_workspace_size(ctx, p, n, &need); rs != E2F_OK) return rs;
+    if (e2f_status rs = check_workspace(workspace, workspace_bytes, need); rs != E2F_OK) return rs;
+  }
+  const size_t el = p->dtype == E2F_BF16 ? 2 : 4, all = el * (size_t)n * nk_of(p->lmax) * p->channels;
+  const size_t gates = el * (size_t)n * p->gates * p->channels, w = sizeof(float) * (p->lmax + 1) * p->channels;
+  const Span in[9] = {{(const char*)x, all}, {(const char*)block, all}, {(const char*)gate, gates},
+                      {(const char*)grad_out, all}, {(const char*)grad_normed, all},
+                      {(const char*)rstd, sizeof(float) * 2 * (size_t)n}, {(const char*)p->post_w, w},
+                      {(const char*)p->res_scale, w}, {(const char*)p->pre_w, w}};
+  const Span to[6] = {{(const char*)grad_x, all}, {(const char*)grad_block, all}, {(const char*)grad_gate, gates},
+                      {(const char*)grad_post_w, w}, {(const char*)grad_res_scale, w}, {(const char*)grad_pre_w, w}};
+  for (int i = 0; i < 6; ++i) {
+    for (int j = 0; j < 9; ++j)
+      if (overlap(to[i], in[j])) return fail(E2F_EINVAL, "an output overlaps an input");
+    for (int j = 0; j < i; ++j)
+      if (overlap(to[i], to[j])) return fail(E2F_EINVAL, "two outputs overlap");
+  }
+  if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
+  hipStream_t s = (hipStream_t)stream;
+  DeviceGuard g(ctx->device);
+  const NormArgs a{x, block, gate, p->post_w, p->res_scale, p->pre_w, n, p->channels, p->gates, p->eps};
+  const NormGrad d{rstd, grad_out, grad_normed, grad_x, grad_block, grad_gate, weights ? (float*)workspace : nullptr,
+                   grad_post_w, grad_res_scale, grad_pre_w};
+  E2F_TIMED("block_norm_grad", launch_norm_backward(p->lmax, p->dtype == E2F_BF16, a, d, s));
+  return E2F_OK;
+}
+
+e2f_status e2f_grad_norm_workspace_size(e2f_ctx* ctx, int32_t count, const int64_t* sizes, size_t* bytes) {
+  if (!ctx) return fail(E2F_EINVAL, "ctx is NULL");
+  if (count < 0 || (count > 0 && !sizes)) return fail(E2F_EINVAL, "sizes are required");
+  if (!bytes) return fail(E2F_EINVAL, "bytes is NULL");
+  int64_t total = 0;
+  for (int i = 0; i < count; ++i) {
+    if (sizes[i] < 0 || sizes[i] > (int64_t)1 << 40) return fail(E2F_EINVAL, "size of tensor %d", i);
+    total += sizes[i];
+  }
+  *bytes = grad_norm_bytes(count, sizes, total);
+  return E2F_OK;
+}
+
+e2f_status e2f_grad_norm(e2f_ctx* ctx, int32_t count, const void* const* tensors, const int64_t* sizes,
+                         const int32_t* dtypes, double* sumsq, float* norm, void* workspace, size_t workspace_bytes,
+                         void* stream) {
+  int64_t total = 0;
+  if (e2f_status rs = check_tensors(ctx, count, sizes, dtypes, tensors, &total); rs != E2F_OK) return rs;
+  if (!sumsq && !norm) return fail(E2F_EINVAL, "sumsq or norm is required");
+  if (e2f_status rs = check_workspace(workspace, workspace_bytes, grad_norm_bytes(count, sizes, total)); rs != E2F_OK)
+    return rs;
+  if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
+  hipStream_t s = (hipStream_t)stream;
+  DeviceGuard g(ctx->device);
+  E2F_TIMED("grad_norm", launch_grad_norm(count, tensors, sizes, dtypes, total, (double*)workspace, sumsq, norm, s));
+  return E2F_OK;
+}
+
+e2f_status e2f_grad_clip(e2f_ctx* ctx, int32_t count, const void* const* tensors, void* const* outs,
+                         const int64_t* sizes, const int32_t* dtypes, const double* sumsq, float max_norm,
+                         void* stream) {
+  int64_t total = 0;
+  if (e2f_status rs = check_tensors(ctx, count, sizes, dtypes, tensors, &total); rs != E2F_OK) return rs;
+  if (e2f_status rs = check_tensors(ctx, count, sizes, dtypes, (const void* const*)outs, &total); rs != E2F_OK)
+    return rs;
+  if (!sumsq) return fail(E2F_EINVAL, "sumsq is required");
+  if (!finite_pos(max_norm)) return fail(E2F_EINVAL, "max_norm must be finite and positive");
+  // no output overlaps another tensor: sorted by address, each range ends before the next begins, unless
+  // both are only read or they are one tensor's, in place
+  struct Range {
+    const char* lo;
+    const char* hi;
+    int tensor;
+    bool out;
+  };
+  try {
+    std::vector<Range> r;
+    r.reserve(2 * (size_t)count);
+    for (int i = 0; i < count; ++i) {
+      if (sizes[i] == 0) continue;
+      const size_t b = (size_t)sizes[i] * (dtypes[i] == E2F_BF16 ? 2 : 4);
+      const char* o = (const char*)outs[i];
+      r.push_back({o, o + b, i, true});
+      const char* t = (const char*)tensors[i];
+      if (t != o) r.push_back({t, t + b, i, false});
+    }
+    auto less = [](const Range& a, const Range& b) { return a.lo < b.lo; };
+    if (!std::is_sorted(r.begin(), r.end(), less)) std::sort(r.begin(), r.end(), less);
+    const char *any = nullptr, *written = nullptr;  // ends of what came before, and of what of it is written
+    for (const Range& x : r) {
+      if (x.lo < written || (x.out && x.lo < any)) return fail(E2F_EINVAL, "an output overlaps another tensor");
+      any = std::max(any, x.hi);
+      if (x.out) written = std::max(written, x.hi);
+    }
+  } catch (const std::exception&) {
+    return fail(E2F_ENOMEM, "host memory for %d tensors", count);
+  }
+  if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
+  hipStream_t s = (hipStream_t)stream;
+  DeviceGuard g(ctx->device);
+  E2F_TIMED("grad_clip", launch_grad_clip(count, tensors, outs, sizes, dtypes, total, sumsq, max_norm, s));
   return E2F_OK;
 }
 

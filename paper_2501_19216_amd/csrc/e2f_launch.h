@@ -1,5 +1,5 @@
-// Kernel launchers of libe2f (implemented in neighbor.hip, plan.hip, conv.hip
-// and attention.hip).
+// Kernel launchers of libe2f (implemented in neighbor.hip, plan.hip, conv.hip,
+// attention.hip, graph_attention.hip, block_norm.hip and grad_clip.hip).
 // All sizes are checked by the callers in abi.cpp before these run.
 #pragma once
 
@@ -189,6 +189,73 @@ constexpr int kAttnMaxRbf = 32;
 hipError_t launch_attention(const float* pos, const float* q, const float* k, int n, int H, int dk,
                             const float* rbf_w, int R, float rc, const int64_t* row_ptr, const int32_t* col_idx,
                             float* alpha, hipStream_t s);
+
+// ---- capped attention of a graph's edges and its gradients (graph_attention.hip)
+struct AttnArgs {
+  const float* pos;
+  const int32_t* gid;  // or NULL: one graph
+  const void *q, *k;   // atom i's features of head h from q + i ldq + h dk on (float, or bfloat16)
+  const float* w;      // [H][R]
+  const int64_t* row_ptr;
+  const int32_t* col;
+  int64_t E, ldq, ldk;
+  int n, H, Hk, dk, R;
+  float rc, scale, cap;
+  bool bf16;
+};
+// gradients (NULL: not wanted) and what they are made of
+struct AttnGrad {
+  const float *alpha, *lse, *galpha;
+  const int64_t* rowT;
+  const int32_t *colT, *perm;
+  float *ds, *edge, *part;  // scratch [E][H], [E][4], [kAttnParts][H][R]
+  void *gq, *gk;
+  float *gw, *gpos;
+};
+constexpr int kAttnParts = 1024;
+constexpr int kAttnMaxDk = 256;
+hipError_t launch_att_forward(const AttnArgs& a, float* alpha, float* lse, hipStream_t s);
+hipError_t launch_att_backward(const AttnArgs& a, const AttnGrad& g, hipStream_t s);
+// The transposed graph: scratch cnt [n], sums [transpose_scan_blocks(n)], rank and list [E]
+int transpose_scan_blocks(int n);
+hipError_t launch_transpose(const int64_t* row_ptr, const int32_t* col, int n, int64_t E, int32_t* cnt, int64_t* sums,
+                            int32_t* rank, int32_t* list, int64_t* rowT, int32_t* colT, int32_t* perm, hipStream_t s);
+
+// ---- norms around a block, its gate and residual sum (block_norm.hip)
+struct NormArgs {
+  const void *x, *block, *gate;  // block and gate or NULL
+  const float *post_w, *scale, *pre_w;
+  int n, C, G;  // G: gates per channel (0, 1 or L + 1)
+  float eps;
+};
+struct NormGrad {
+  const float* rstd;
+  const void *gout, *gnormed;
+  void *gx, *gblock, *ggate;
+  float* part;  // [norm_parts][2][L + 1][C]
+  float *gpost_w, *gscale, *gpre_w;
+};
+int norm_parts(int L, int C, bool bf16, int n);
+hipError_t launch_norm_forward(int L, bool bf16, const NormArgs& a, void* out, void* normed, float* rstd,
+                               hipStream_t s);
+hipError_t launch_norm_backward(int L, bool bf16, const NormArgs& a, const NormGrad& g, hipStream_t s);
+
+// ---- the norm over many tensors and their clipping (grad_clip.hip)
+constexpr int kTableMax = 128;  // tensors of one launch: its arguments stay below 4 KB
+struct TensorTable {
+  const void* in[kTableMax];
+  void* out[kTableMax];
+  int64_t n[kTableMax];
+  int first[kTableMax];  // first workgroup
+  unsigned bf16[kTableMax / 32];
+  int count;
+};
+int64_t grad_chunk(int64_t total);  // values of a workgroup
+// part: a double for every workgroup (the chunks of every tensor)
+hipError_t launch_grad_norm(int count, const void* const* in, const int64_t* n, const int32_t* dtype, int64_t total,
+                            double* part, double* sumsq, float* norm, hipStream_t s);
+hipError_t launch_grad_clip(int count, const void* const* in, void* const* out, const int64_t* n,
+                            const int32_t* dtype, int64_t total, const double* sumsq, float max_norm, hipStream_t s);
 
 // ---- backward
 // Both per-edge backward products of the edges lo .. hi - 1 (either output may

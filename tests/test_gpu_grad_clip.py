@@ -1,0 +1,154 @@
+"""The norm over many tensors and their clipping against float64.  Run with
+-m gpu."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def e2f():
+    import paper_2501_19216_amd as m
+    return m
+
+
+@pytest.fixture(scope="module")
+def ctx(e2f):
+    c = e2f.e2f_create(0, 0)
+    yield c
+    c.close()
+
+
+def tensors(sizes, seed, mixed=True, gap=0, scale=1.0):
+    """Pieces of one buffer for each type, `gap` values apart; and the buffers."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    low = [mixed and i % 2 == 1 for i in range(len(sizes))]
+    buf = {}
+    out = []
+    at = {True: 0, False: 0}
+    for want, t in ((False, torch.float32), (True, torch.bfloat16)):
+        total = sum(s + gap for s, b in zip(sizes, low) if b == want)
+        buf[want] = (scale * torch.randn(total, device=DEV, generator=g)).to(t)
+    for s, b in zip(sizes, low):
+        out.append(buf[b][at[b]:at[b] + s])
+        at[b] += s + gap
+    return out, buf
+
+
+def check(ts, outs, norm, max_norm):
+    total = sum(float(t.double().square().sum()) for t in ts)
+    want = math.sqrt(total)
+    # float64 sums, one rounding
+    assert abs(float(norm) - want) <= 1.01 * U * want + 1e-45
+    coef = min(1.0, max_norm / (want + 1e-6))
+    for t, o in zip(ts, outs):
+        # the factor's rounding and the product's, and the type's own; the last digits of the smallest values
+        room = t.double().abs() * coef * (2.01 * U + (2.0 ** -8 if t.dtype == torch.bfloat16 else 0.0))
+        least = 2.0 ** -133 if t.dtype == torch.bfloat16 else 2.0 ** -149
+        assert torch.all((o.double() - t.double() * coef).abs() <= room + least)
+        if coef == 1.0:
+            assert torch.equal(o, t)
+
+
+@pytest.mark.parametrize("sizes", [[1], [5], [0, 3, 0], [4096], [4097, 4095], [1, 2, 3, 4, 5, 6, 7, 8, 9], [100000],
+                                   [7] * 127, [7] * 128, [9] * 129, [33] * 300, [3000001, 17, 250000, 1],
+                                   [0] * 200 + [5] + [0] * 200])
+@pytest.mark.parametrize("gap", [0, 1, 3])
+@pytest.mark.parametrize("max_norm", [0.5, 1e9])
+def test_sizes_and_alignments(e2f, ctx, sizes, gap, max_norm):
+    ts, buf = tensors(sizes, len(sizes) + gap, gap=gap)
+    before = {k: v.clone() for k, v in buf.items()}
+    outs, obuf = tensors(sizes, 99, gap=gap)
+    kept = {k: v.clone() for k, v in obuf.items()}
+    norm = e2f.e2f_clip_grad_norm(ctx, ts, max_norm, outs=outs)
+    check(ts, outs, norm, max_norm)
+    assert all(torch.equal(buf[k], before[k]) for k in buf)
+    # in place the same bits, and the gaps as they were, in both
+    mine = [o.clone() for o in outs]
+    sumsq, norm2 = e2f.e2f_grad_norm(ctx, ts)
+    e2f.e2f_grad_clip(ctx, ts, sumsq, max_norm)
+    assert torch.equal(norm, norm2) and all(torch.equal(a, b) for a, b in zip(ts, mine))
+    for b, was in ((buf, before), (obuf, kept)):
+        for low in b:
+            inside = torch.zeros(b[low].numel(), dtype=torch.bool, device=DEV)
+            at = 0
+            for i, s in enumerate(sizes):
+                if (i % 2 == 1) == low:
+                    inside[at:at + s] = True
+                    at += s + gap
+            assert torch.equal(b[low][~inside], was[low][~inside])
+
+
+def test_ranges_of_values(e2f, ctx):
+    # squares that overflow float32, and values below its normal range
+    for scale in (1e30, 1e-30, 1e-41):
+        ts, _ = tensors([5000, 3000, 77], 3, mixed=False, scale=scale)
+        outs = [torch.empty_like(t) for t in ts]
+        norm = e2f.e2f_clip_grad_norm(ctx, ts, 1.0, outs=outs)
+        check(ts, outs, norm, 1.0)
+
+
+def test_no_tensors_and_norms_not_finite(e2f, ctx):
+    assert float(e2f.e2f_clip_grad_norm(ctx, [], 1.0)) == 0.0
+    assert float(e2f.e2f_grad_norm(ctx, [torch.empty(0, device=DEV)])[1]) == 0.0
+    t = torch.ones(1000, device=DEV)
+    t[3] = math.inf
+    norm = e2f.e2f_clip_grad_norm(ctx, [t], 1.0)
+    assert float(norm) == math.inf and int((t == 0).sum()) == 999 and bool(t[3].isnan())
+    t = torch.ones(1000, device=DEV)
+    t[3] = math.nan
+    norm = e2f.e2f_clip_grad_norm(ctx, [t], 1.0)
+    assert math.isnan(float(norm)) and bool(t.isnan().all())
+
+
+def test_parts_of_several_ranks(e2f, ctx):
+    # the sums of two ranks' parts added before clipping: the whole's norm
+    ts, _ = tensors([1000, 70000, 33, 512], 7)
+    whole, _ = e2f.e2f_grad_norm(ctx, ts)
+    parts = sum(e2f.e2f_grad_norm(ctx, p)[0] for p in (ts[:2], ts[2:]))
+    assert abs(float(parts) - float(whole)) <= 1e-12 * float(whole)
+    was = [t.clone() for t in ts]
+    for p in (ts[:2], ts[2:]):
+        e2f.e2f_grad_clip(ctx, p, parts, 2.0)
+    check(was, ts, torch.tensor(math.sqrt(float(parts))), 2.0)
+
+
+def test_deterministic_captured_and_on_another_stream(e2f, ctx):
+    ts, _ = tensors([50000, 3, 1000, 200001] * 40, 5)
+    outs = [torch.empty_like(t) for t in ts]
+    space = torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+    step = lambda: e2f.e2f_clip_grad_norm(ctx, ts, 1.0, outs=outs, workspace=space)  # noqa: E731
+    norm = step()
+    first = [o.clone() for o in outs]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        norm2 = step()
+    torch.cuda.synchronize()
+    assert torch.equal(norm, norm2) and all(torch.equal(a, b) for a, b in zip(first, outs))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    for r in range(3):
+        ts[0].mul_(1.0 if r == 0 else 1.5)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [captured.clone()] + [o.clone() for o in outs]
+        space.fill_(255)
+        want = step()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want) and all(torch.equal(a, b) for a, b in zip(got[1:], outs)), r
+
+
+def test_more_than_2_to_the_31_values(e2f, ctx):
+    n = 2 ** 31 + 12345
+    t = torch.zeros(n, dtype=torch.bfloat16, device=DEV)
+    t[-1], t[0], t[2 ** 31] = 3.0, 4.0, 12.0
+    norm = e2f.e2f_clip_grad_norm(ctx, [t], 6.5)
+    assert float(norm) == 13.0
+    assert [float(t[i]) for i in (0, 2 ** 31, n - 1)] == [2.0, 6.0, 1.5]

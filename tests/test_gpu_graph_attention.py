@@ -1,0 +1,299 @@
+"""Capped attention under a mask by graph, its gradients and the transposed
+graph against float64, elementwise within bounds on float32 arithmetic.  Run
+with -m gpu."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import block_reference as ref
+import oracle as o
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def e2f():
+    import paper_2501_19216_amd as m
+    return m
+
+
+@pytest.fixture(scope="module")
+def ctx(e2f):
+    c = e2f.e2f_create(0, 0)
+    yield c
+    c.close()
+
+
+DEGREES = (0, 1, 2, 3, 15, 16, 17, 31, 33, 63, 64, 65, 128, 130, 200)
+
+
+def graph(n, degrees, seed, rc=6.0):
+    g = torch.Generator().manual_seed(seed)
+    pos = torch.rand(n, 3, generator=g) * (1.2 * rc)
+    deg = torch.tensor([min(degrees[i % len(degrees)], n - 1) for i in range(n)])
+    rows = [torch.sort(torch.randperm(n - 1, generator=g)[:d]).values for d in deg]
+    rows = [r + (r >= i) for i, r in enumerate(rows)]
+    rp = torch.zeros(n + 1, dtype=torch.long)
+    rp[1:] = deg.cumsum(0)
+    return pos, rp, torch.cat(rows).int() if n else torch.zeros(0, dtype=torch.int32), g
+
+
+def inputs(n, H, Hk, dk, R, dtype, g, spread=1.5):
+    q = k = w = None
+    if dk:
+        qk = (spread * torch.randn(n, (H + Hk) * dk, generator=g)).to(dtype)
+        q, k = qk[:, :H * dk].view(n, H, dk), qk[:, H * dk:].view(n, Hk, dk)
+    if R:
+        w = torch.randn(H, R, generator=g)
+    return q, k, w
+
+
+def dev(t):
+    if t is None or t.dim() < 3 or t.is_contiguous():
+        return None if t is None else t.to(DEV)
+    out = torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=DEV)  # (keeps the strides)
+    return out.copy_(t)
+
+
+def run(e2f, ctx, pos, rp, ci, rc, q, k, w, H, scale, cap, gid, ga, out=None):
+    d = [dev(t) for t in (pos, rp, ci, q, k, w, gid, ga)]
+    kw = dict(q=d[3], k=d[4], rbf_w=d[5], heads=H, scale=scale, cap=cap, graph_id=d[6])
+    alpha, lse = e2f.e2f_attention_forward(ctx, d[0], d[1], d[2], rc, **kw)
+    got = {"alpha": alpha, "lse": lse}
+    if ga is not None:
+        t = e2f.e2f_transpose_graph(ctx, pos.shape[0], d[1], d[2])
+        got.update(zip(("grad_q", "grad_k", "grad_w", "grad_pos"),
+                       e2f.e2f_attention_backward(ctx, d[0], d[1], d[2], rc, alpha, lse, d[7], *t, **kw)))
+    return got
+
+
+def compare(got, want, dtype):
+    for name, r in want.items():
+        ref.check(got[name], r, dtype if name in ("grad_q", "grad_k") else torch.float32, name)
+
+
+@pytest.mark.parametrize("H,Hk,dk,R,cap,dtype", [
+    (1, 1, 4, 8, 0.0, torch.float32), (1, 1, 3, 0, 2.0, torch.float32), (1, 1, 1, 2, 0.5, torch.bfloat16),
+    (2, 1, 8, 5, 20.0, torch.float32), (4, 4, 16, 16, 5.0, torch.bfloat16), (6, 2, 20, 10, 20.0, torch.float32),
+    (8, 8, 16, 32, 20.0, torch.float32), (8, 8, 8, 8, 0.0, torch.float32), (8, 1, 64, 31, 50.0, torch.bfloat16),
+    (8, 4, 16, 16, 5.0, torch.float32), (12, 3, 5, 17, 3.0, torch.float32), (16, 16, 32, 32, 30.0, torch.bfloat16),
+    (16, 8, 8, 16, 0.0, torch.float32), (32, 4, 4, 3, 1.0, torch.float32), (64, 64, 2, 32, 10.0, torch.float32),
+    (64, 16, 12, 0, 10.0, torch.bfloat16), (8, 8, 0, 16, 5.0, torch.float32), (5, 5, 256, 4, 8.0, torch.float32),
+    (3, 3, 128, 0, 0.0, torch.bfloat16), (4, 4, 0, 0, 0.0, torch.float32)])
+@pytest.mark.parametrize("masked", [False, True])
+def test_shapes_and_masks(e2f, ctx, H, Hk, dk, R, cap, dtype, masked):
+    n = 230
+    pos, rp, ci, g = graph(n, DEGREES, 100 * H + dk + R)
+    q, k, w = inputs(n, H, Hk, dk, R, dtype, g)
+    gid = None
+    if masked:  # graphs in any order of atoms, ids of any size, some atoms alone
+        gid = torch.randint(0, 3, (n,), generator=g).int() * 1000003 - 5
+        gid[::9] = torch.arange(len(gid[::9])).int() + 7
+    ga = torch.randn(ci.numel(), H, generator=g)
+    scale = dk ** -0.5 if dk else 1.0
+    got = run(e2f, ctx, pos, rp, ci, 6.0, q, k, w, H, scale, cap, gid, ga)
+    compare(got, ref.attention(pos, rp, ci, 6.0, q, k, w, H, scale, cap, gid, ga), dtype)
+
+
+@pytest.mark.parametrize("n,degrees", [(1, (0,)), (2, (1,)), (2, (0, 1)), (65, (64,)), (1030, (1029, 1029, 0, 700)),
+                                       (700, (512, 513, 255, 256, 257)), (5000, (1, 2)), (4097, (3,))])
+def test_row_lengths(e2f, ctx, n, degrees):
+    pos, rp, ci, g = graph(n, degrees, n)
+    if n == 1030:  # two rows of every other atom, two empty ones, and short rows
+        keep = torch.arange(n) % 200 < 4
+        deg = torch.where(keep, rp.diff(), rp.diff().clamp(max=3))
+        ci = torch.cat([ci[int(rp[i]):int(rp[i]) + int(deg[i])] for i in range(n)])
+        rp = torch.cat([rp[:1], deg.cumsum(0)])
+    q, k, w = inputs(n, 4, 2, 8, 8, torch.float32, g)
+    ga = torch.randn(ci.numel(), 4, generator=g)
+    got = run(e2f, ctx, pos, rp, ci, 6.0, q, k, w, 4, 8 ** -0.5, 4.0, None, ga)
+    compare(got, ref.attention(pos, rp, ci, 6.0, q, k, w, 4, 8 ** -0.5, 4.0, None, ga), torch.float32)
+
+
+def test_long_row_few_atoms(e2f, ctx):
+    # one receiver of 20,000 edges (the same senders many times over), and its senders' rows empty
+    n, E = 50, 20000
+    g = torch.Generator().manual_seed(1)
+    pos = torch.rand(n, 3, generator=g) * 5
+    ci = torch.sort(torch.randint(1, n, (E,), generator=g)).values.int()
+    rp = torch.full((n + 1,), E, dtype=torch.long)
+    rp[0] = 0
+    q, k, w = inputs(n, 2, 2, 16, 16, torch.float32, g)
+    ga = torch.randn(E, 2, generator=g)
+    got = run(e2f, ctx, pos, rp, ci, 6.0, q, k, w, 2, 0.25, 10.0, None, ga)
+    compare(got, ref.attention(pos, rp, ci, 6.0, q, k, w, 2, 0.25, 10.0, None, ga), torch.float32)
+
+
+def test_no_edges_and_no_atoms(e2f, ctx):
+    for n in (0, 3):
+        pos, w = torch.rand(n, 3), torch.randn(2, 4)
+        rp, ci = torch.zeros(n + 1, dtype=torch.long), torch.zeros(0, dtype=torch.int32)
+        q, k = torch.randn(n, 2, 4), torch.randn(n, 2, 4)
+        got = run(e2f, ctx, pos, rp, ci, 5.0, q, k, w, 2, 1.0, 1.0, None, torch.zeros(0, 2))
+        assert got["alpha"].shape == (0, 2) and torch.all(got["lse"] == -math.inf)
+        for name in ("grad_q", "grad_k", "grad_w", "grad_pos"):
+            assert torch.all(got[name] == 0), name
+    t = e2f.e2f_transpose_graph(ctx, 3, rp.to(DEV), ci.to(DEV))
+    assert torch.all(t[0] == 0) and t[1].numel() == 0
+
+
+def test_coincident_atoms_and_edges_beyond_the_cutoff(e2f, ctx):
+    n = 60
+    pos, rp, ci, g = graph(n, (20, 7, 40), 3, rc=9.0)
+    pos[10:20] = pos[0]  # distances of 0: no gradient of the position
+    q, k, w = inputs(n, 4, 4, 8, 12, torch.float32, g)
+    ga = torch.randn(ci.numel(), 4, generator=g)
+    got = run(e2f, ctx, pos, rp, ci, 4.0, q, k, w, 4, 0.3, 6.0, None, ga)
+    want = ref.attention(pos, rp, ci, 4.0, q, k, w, 4, 0.3, 6.0, None, ga)
+    assert int((want["alpha"][0] == 0).sum()) > 100
+    assert torch.all(got["alpha"].cpu()[want["alpha"][0] == 0] == 0)
+    compare(got, want, torch.float32)
+
+
+def test_what_masked_atoms_hold_does_not_matter(e2f, ctx):
+    # infinities, NaN and the type's lowest values in another graph's atoms
+    n = 90
+    pos, rp, ci, g = graph(n, (30, 12, 50), 5)
+    gid = (torch.arange(n) % 3).int()
+    for dtype in (torch.float32, torch.bfloat16):
+        q, k, w = inputs(n, 4, 2, 8, 8, dtype, g)
+        ga = torch.randn(ci.numel(), 4, generator=g)
+        want = ref.attention(pos, rp, ci, 6.0, q, k, w, 4, 0.3, 6.0, gid, ga)
+        recv = torch.arange(n).repeat_interleave(rp.diff())
+        cross = gid[recv] != gid[ci.long()]
+        bad, ga2 = gid == 2, ga.clone()
+        ga2[cross] = math.nan
+        pos2, q2, k2 = pos.clone(), q.clone(), k.clone()
+        pos2[bad], q2[bad] = math.inf, math.nan
+        for value in (math.inf, math.nan, torch.finfo(dtype).min):
+            k2[bad] = value
+            got = run(e2f, ctx, pos2, rp, ci, 6.0, q2, k2, w, 4, 0.3, 6.0, gid, ga2)
+            fine_e, fine_n = ~bad[recv], ~bad
+            for name, (v, b) in want.items():
+                if name == "grad_w":
+                    continue  # (sums over every graph)
+                rows = fine_e if name == "alpha" else fine_n
+                ref.check(got[name].cpu()[rows], (v[rows], b[rows]), dtype if name in ("grad_q", "grad_k") else torch.float32, name)
+            assert torch.all(got["alpha"].cpu()[cross] == 0)
+
+
+def test_scores_far_apart(e2f, ctx):
+    # scores of +-10^4 without a cap: weights of 0 and 1, no overflow; capped, every weight counts
+    n = 40
+    pos, rp, ci, g = graph(n, (20, 39), 8)
+    q, k, _ = inputs(n, 2, 2, 4, 0, torch.float32, g, spread=100.0)
+    ga = torch.randn(ci.numel(), 2, generator=g)
+    for cap in (0.0, 3.0):
+        got = run(e2f, ctx, pos, rp, ci, 6.0, q, k, None, 2, 1.0, cap, None, ga)
+        compare({x: got[x] for x in ("alpha", "lse")}, {x: v for x, v in ref.attention(
+            pos, rp, ci, 6.0, q, k, None, 2, 1.0, cap, None, ga).items() if x in ("alpha", "lse")}, torch.float32)
+        assert all(torch.isfinite(v).all() for v in got.values() if v is not None)
+
+
+def test_without_cap_the_framework_s_weights(e2f, ctx):
+    # the same numbers as e2f_attention_weights, and as the oracle
+    rng = np.random.default_rng(4)
+    pos = rng.uniform(0, 12, size=(400, 3)).astype(np.float32)
+    rp, ci = o.neighbor_list(pos, 5.0)
+    q, k, w = (rng.standard_normal(s).astype(np.float32) for s in ((400, 8, 8), (400, 8, 8), (8, 16)))
+    want = o.attention_weights(pos, 0.25 * q, k, w, 5.0, rp, ci)
+    t = [torch.from_numpy(a).to(DEV) for a in (pos, rp, ci, q, k, w)]
+    old = e2f.e2f_attention_weights(ctx, t[0], t[1], t[2], 5.0, 0.25 * t[3], t[4], t[5])
+    new, _ = e2f.e2f_attention_forward(ctx, t[0], t[1], t[2], 5.0, t[3], t[4], t[5], scale=0.25)
+    err = lambda a: float(np.max(np.abs(a.cpu().numpy() - want).max(0) / np.abs(want).max(0)))  # noqa: E731
+    print("%.2e, e2f_attention_weights %.2e" % (err(new), err(old)))
+    assert err(new) <= 1e-5 and err(old) <= 1e-5
+
+
+def test_transposed_graph(e2f, ctx):
+    for n, degrees, seed in ((1, (0,), 1), (300, DEGREES, 2), (5000, (0, 3, 30), 3), (20000, (1,), 4)):
+        _, rp, ci, _ = graph(n, degrees, seed)
+        row_t, col_t, perm = (t.cpu() for t in e2f.e2f_transpose_graph(ctx, n, rp.to(DEV), ci.to(DEV)))
+        want = torch.sort(ci.long(), stable=True).indices
+        recv = torch.arange(n).repeat_interleave(rp.diff())
+        assert torch.equal(perm.long(), want) and torch.equal(col_t.long(), recv[want])
+        assert torch.equal(row_t[1:], torch.bincount(ci.long(), minlength=n).cumsum(0)) and int(row_t[0]) == 0
+    # one sender for every edge: a list as long as the graph
+    n = 3000
+    rp, ci = torch.arange(n + 1), torch.full((n,), 7, dtype=torch.int32)
+    row_t, col_t, perm = (t.cpu() for t in e2f.e2f_transpose_graph(ctx, n, rp.to(DEV), ci.to(DEV)))
+    assert torch.equal(perm.long(), torch.arange(n)) and torch.equal(col_t.long(), torch.arange(n))
+
+
+def test_gradients_against_differences(e2f, ctx):
+    # the float64 reference's own gradients against central differences, and the kernel's directional derivative
+    n, H = 30, 2
+    pos, rp, ci, g = graph(n, (8, 12, 5), 21)
+    q, k, w = inputs(n, H, 1, 4, 6, torch.float32, g)
+    ga = torch.randn(ci.numel(), H, generator=g)
+    got = run(e2f, ctx, pos, rp, ci, 6.0, q, k, w, H, 0.5, 4.0, None, ga)
+    f = lambda p, a, b, c: float((ref.attention(p, rp, ci, 6.0, a, b, c, H, 0.5, 4.0)["alpha"][0] * ga.double()).sum())  # noqa: E731
+    base = [t.double().contiguous() for t in (pos, q, k, w)]
+    h = 1e-5
+    for x, name in enumerate(("grad_pos", "grad_q", "grad_k", "grad_w")):
+        d = torch.randn(base[x].shape, generator=g, dtype=torch.float64)
+        up, down = list(base), list(base)
+        up[x], down[x] = base[x] + h * d, base[x] - h * d
+        num = (f(*up) - f(*down)) / (2 * h)
+        mine = got[name].cpu().double()
+        size = float((mine.abs() * d.abs()).sum())
+        # differences: h^2 times a third derivative, and 2^-53 / h of the sum; float32: some 10^2 half steps
+        assert abs(num - float((mine * d).sum())) <= size * (1e-6 + 1e-4), name
+
+
+def test_deterministic_captured_and_on_another_stream(e2f, ctx):
+    n, H = 900, 8
+    pos, rp, ci, g = graph(n, DEGREES, 31)
+    q, k, w = inputs(n, H, 8, 16, 16, torch.float32, g)
+    ga = torch.randn(ci.numel(), H, generator=g)
+    d = [dev(t) for t in (pos, rp, ci, q, k, w, ga)]
+    kw = dict(q=d[3], k=d[4], rbf_w=d[5], scale=0.25, cap=5.0)
+    space = torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
+
+    def step():
+        alpha, lse = e2f.e2f_attention_forward(ctx, d[0], d[1], d[2], 6.0, **kw)
+        t = e2f.e2f_transpose_graph(ctx, n, d[1], d[2], workspace=space)
+        return [alpha, lse, *t, *e2f.e2f_attention_backward(ctx, d[0], d[1], d[2], 6.0, alpha, lse, d[6], *t,
+                                                            workspace=space, **kw)]
+
+    first = step()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+    graph_ = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph_):
+        out = step()
+    for r in range(3):
+        d[3].mul_(1.0 if r == 0 else 0.9)
+        graph_.replay()
+        torch.cuda.synchronize()
+        space.fill_(255)
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), r
+
+
+def test_outputs_alone(e2f, ctx):
+    # each gradient by itself is the same as all together
+    n, H = 200, 4
+    pos, rp, ci, g = graph(n, DEGREES, 41)
+    q, k, w = inputs(n, H, 4, 8, 8, torch.float32, g)
+    ga = torch.randn(ci.numel(), H, generator=g)
+    d = [dev(t) for t in (pos, rp, ci, q, k, w, ga)]
+    kw = dict(q=d[3], k=d[4], rbf_w=d[5], scale=0.3, cap=5.0)
+    alpha, lse = e2f.e2f_attention_forward(ctx, d[0], d[1], d[2], 6.0, **kw)
+    t = e2f.e2f_transpose_graph(ctx, n, d[1], d[2])
+    back = lambda *tt, **w2: e2f.e2f_attention_backward(ctx, d[0], d[1], d[2], 6.0, alpha, lse, d[6], *tt, **kw, **w2)  # noqa: E731
+    gq, gk, gw, gp = back(*t)
+    a = back(*t, want_rbf=False, want_pos=False)
+    b = back(want_qk=False, want_pos=False)  # no transposed graph
+    c = back(*t, want_qk=False, want_rbf=False)
+    assert torch.equal(a[0], gq) and torch.equal(a[1], gk) and a[2] is None and a[3] is None
+    assert torch.equal(b[2], gw) and torch.equal(c[3], gp)
