@@ -1511,12 +1511,13 @@ e2f_status check_attention_inputs(const e2f_attention_params* p, const float* po
 struct AttnLayout {
   size_t ds, edge, part, total;
 };
-AttnLayout attention_layout(const e2f_attention_params* p, int64_t E) {
+AttnLayout attention_layout(const e2f_attention_params* p, int32_t n, int64_t E) {
   AttnLayout l;
+  const AttnArgs a = attention_args(p, nullptr, nullptr, nullptr, nullptr, n, nullptr, nullptr, nullptr, E);
   l.ds = 0;
   l.edge = al256(sizeof(float) * (size_t)E * p->heads);
-  l.part = l.edge + al256(sizeof(float) * 4 * (size_t)E);
-  l.total = l.part + al256(sizeof(float) * (size_t)kAttnParts * p->heads * p->n_rbf);
+  l.part = l.edge + al256(sizeof(float) * 4 * (size_t)E * (n ? attention_groups(a) : 1));
+  l.total = l.part + al256(sizeof(float) * (size_t)(n ? attention_parts(a) : 0) * p->heads * p->n_rbf);
   return l;
 }
 
@@ -1626,7 +1627,7 @@ e2f_status e2f_attention_backward_workspace_size(e2f_ctx* ctx, const e2f_attenti
                                                  int64_t n_edges, size_t* bytes) {
   if (e2f_status rs = check_attention(ctx, p, n, n_edges); rs != E2F_OK) return rs;
   if (!bytes) return fail(E2F_EINVAL, "bytes is NULL");
-  *bytes = attention_layout(p, n_edges).total;
+  *bytes = attention_layout(p, n, n_edges).total;
   return E2F_OK;
 }
 
@@ -1647,7 +1648,7 @@ e2f_status e2f_attention_backward(e2f_ctx* ctx, const e2f_attention_params* p, c
   if (n_edges > 0 && (!alpha || !grad_alpha)) return fail(E2F_EINVAL, "alpha and grad_alpha are required");
   if ((grad_k || grad_pos) && n > 0 && (!rowT_ptr || (n_edges > 0 && (!colT || !perm))))
     return fail(E2F_EINVAL, "grad_k and grad_pos need the transposed graph");
-  const AttnLayout l = attention_layout(p, n_edges);
+  const AttnLayout l = attention_layout(p, n, n_edges);
   if (e2f_status rs = check_workspace(workspace, workspace_bytes, l.total); rs != E2F_OK) return rs;
   if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
   hipStream_t s = (hipStream_t)stream;

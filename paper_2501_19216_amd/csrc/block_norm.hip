@@ -498,8 +498,10 @@ Shape shape_of(int L, int C, bool bf16, bool back) {
 int norm_parts(int L, int C, bool bf16, int n) {
   const Shape s = shape_of(L, C, bf16, true);
   const int slots = s.threads / s.tpr;
-  const int64_t want = ((int64_t)n + slots - 1) / slots;
-  return (int)(want < 1024 ? want : 1024);
+  // two workgroups a CU, about what its registers hold: 336 us where 1,024 workgroups take 350 (20,000 atoms, L = 4,
+  // 128 float channels); a row of few bytes a thread wants more of them (60,000 rows of 1,024 bfloat16: 221 and 300 us)
+  const int64_t want = ((int64_t)n + slots - 1) / slots, most = L == 0 && bf16 ? 1024 : 512;
+  return (int)(want < most ? want : most);
 }
 
 // the kernel for the degree, type, size and parts: E2F_NORM(L, T, V, keep, block, pre)

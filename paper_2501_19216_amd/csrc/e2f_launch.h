@@ -208,11 +208,20 @@ struct AttnGrad {
   const float *alpha, *lse, *galpha;
   const int64_t* rowT;
   const int32_t *colT, *perm;
-  float *ds, *edge, *part;  // scratch [E][H], [E][4], [kAttnParts][H][R]
+  float *ds, *edge, *part;  // scratch [E][H], [attention_groups][E][4], [attention_parts][H][R]
   void *gq, *gk;
   float *gw, *gpos;
+  int groups;  // (filled in by the launcher)
 };
-constexpr int kAttnParts = 1024;
+// How the kernels divide heads and rows: a head of k takes lph lanes (16 bytes of features each), an edge lpe lanes,
+// `units` times over; a workgroup up to `heads` heads of `kheads` heads of k; wpr waves a row
+struct AttnShape {
+  int lph, lpe, units, kheads, share, heads, groups, ld, hp, wpr, rows, lds, dq;
+  unsigned inv_heads;  // x / heads = x inv_heads >> 16
+  bool one;            // a lane has one head's features alone
+};
+int attention_groups(const AttnArgs& a);
+int attention_parts(const AttnArgs& a, int* rows = nullptr);
 constexpr int kAttnMaxDk = 256;
 hipError_t launch_att_forward(const AttnArgs& a, float* alpha, float* lse, hipStream_t s);
 hipError_t launch_att_backward(const AttnArgs& a, const AttnGrad& g, hipStream_t s);

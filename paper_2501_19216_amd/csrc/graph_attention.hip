@@ -9,223 +9,807 @@
 //   dq_ih = scale sum of ds k_jh over the row,   dk_jh = scale sum of ds q_ih over the
 //   edges that j sends (the heads that share k summed),   dw_hr = sum of ds g_r,
 //   dd = sum_h (a p env'(d) + ds sum_r w_hr g_r'(d)),   dr_i += dd (r_i - r_j) / d,   dr_j -= the same.
+//
+// A wave takes a receiver's row (four waves, where rows are long) in batches of
+// up to 64 edges of its graph; edges between graphs only get their zeros.
+//   - Geometry: a lane an edge.
+//   - The products: lanes over an edge's features of k, 16 bytes each, so that a
+//     gather reads whole lines; the features of a head are summed over its lanes.
+//     This gather, H dk values an edge out of the caches, is what bounds both
+//     directions (1.5 million edges of 8 heads of 16 floats are 780 MB).
+//   - The radial part: float matrix products of 16 edges, 16 heads and 4 functions
+//     (v_mfma_f32_16x16x4_f32), each lane evaluating the functions it passes in.
+//   - The softmax's running maximum and sum stay with the lanes that hold a head in
+//     the product's output; the scores of up to 128 edges stay in the LDS until the
+//     row's sum is known, those of longer rows in alpha.
+// Heads go in groups of up to 16 (one matrix tile), a group a workgroup.  Backward:
+// the receivers' kernel makes the scores again, ds from them, dq and each edge's
+// position gradient, and sums dw as matrix products too; the senders' kernel
+// gathers ds and q over the transposed graph.  No atomics in either: the same
+// bits every time.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "e2f_launch.h"
+#include "wave.h"
 
 namespace e2f {
 namespace {
 
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(unsigned short x) { return __uint_as_float((unsigned)x << 16); }
-__device__ __forceinline__ void store(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store(unsigned short* p, float x) {
-  *p = __builtin_bit_cast(unsigned short, (__bf16)x);  // round to nearest even
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+typedef f4 f4_any __attribute__((aligned(4)));
+typedef u4 u4_any __attribute__((aligned(2)));
+
+// 16 bytes of features: the address needs no more than an element's alignment
+struct F32 {
+  typedef float type;
+  typedef f4 raw;
+  static constexpr int VEC = 4;
+  static __device__ __forceinline__ float at(const raw& r, int u) { return r[u]; }
+  // the first `count` of them (1 .. VEC), zeros behind
+  static __device__ __forceinline__ raw load(const float* p, int count) {
+    if (count >= VEC) return *(const f4_any*)p;
+    raw r = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int u = 0; u < VEC - 1; ++u)
+      if (u < count) r[u] = p[u];
+    return r;
+  }
+  static __device__ __forceinline__ void store(float* p, const float (&f)[VEC], int count) {
+    if (count >= VEC) {
+      *(f4_any*)p = (f4){f[0], f[1], f[2], f[3]};
+      return;
+    }
+#pragma unroll
+    for (int u = 0; u < VEC - 1; ++u)
+      if (u < count) p[u] = f[u];
+  }
+};
+struct BF16 {
+  typedef unsigned short type;
+  typedef u4 raw;
+  static constexpr int VEC = 8;
+  static __device__ __forceinline__ float at(const raw& r, int u) {
+    return __uint_as_float(u & 1 ? r[u >> 1] & 0xffff0000u : r[u >> 1] << 16);
+  }
+  static __device__ __forceinline__ raw load(const unsigned short* p, int count) {
+    if (count >= VEC) return *(const u4_any*)p;
+    raw r = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int u = 0; u < VEC - 1; ++u)
+      if (u < count) r[u >> 1] |= (unsigned)p[u] << (u & 1 ? 16 : 0);
+    return r;
+  }
+  static __device__ __forceinline__ void store(unsigned short* p, const float (&f)[VEC], int count) {
+    unsigned short b[VEC];
+#pragma unroll
+    for (int u = 0; u < VEC; ++u) b[u] = __builtin_bit_cast(unsigned short, (__bf16)f[u]);  // to nearest even
+    if (count >= VEC) {
+      u4 r;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) r[u] = b[2 * u] | (unsigned)b[2 * u + 1] << 16;
+      *(u4_any*)p = r;
+      return;
+    }
+#pragma unroll
+    for (int u = 0; u < VEC - 1; ++u)
+      if (u < count) p[u] = b[u];
+  }
+};
+
+// Orders the LDS and memory accesses of a wave's lanes among each other
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-struct Row {
-  int64_t e0, e1;
-};
-// row i's edges, inside [0, E] whatever row_ptr holds
-__device__ __forceinline__ Row row_of(const AttnArgs& a, int64_t i) {
-  Row r;
-  r.e0 = min(max(a.row_ptr[i], (int64_t)0), a.E);
-  r.e1 = min(max(a.row_ptr[i + 1], r.e0), a.E);
-  return r;
+constexpr float kPi = 3.14159265358979f, kLog2e = 1.44269504088896f;
+__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+// tanh to a few steps of its own value: the odd series to x^11 below 0.35 (its next term is below 2^-25 of x
+// there), (1 - e^-2x) / (1 + e^-2x) from it on
+__device__ __forceinline__ float tanh_near(float x) {
+  const float a = fabsf(x), t = a * a;
+  const float p = a + a * t * (-1.0f / 3 + t * (2.0f / 15 + t * (-17.0f / 315 + t * (62.0f / 2835 + t * (-1382.0f / 155925)))));
+  const float e = exp_fast(-2.0f * a);
+  return copysignf(a < 0.35f ? p : (1.0f - e) / (1.0f + e), x);
 }
+
+__device__ __forceinline__ float envelope(float rc, float d) {
+  return d < rc ? 0.5f * (cosf(kPi / rc * d) + 1.0f) : 0.0f;
+}
+__device__ __forceinline__ float envelope_slope(float rc, float d) {
+  return d < rc ? -0.5f * kPi / rc * sinf(kPi / rc * d) : 0.0f;
+}
+
 __device__ __forceinline__ int atom_of(const AttnArgs& a, int c) { return min(max(c, 0), a.n - 1); }
 
-struct Geometry {
-  float x, y, z, d;
+// Workgroups of one XCD (every eighth) take neighbouring rows, which share senders where atoms are in order
+__device__ __forceinline__ int64_t row_block() {
+  const int64_t nb = gridDim.x, per = nb / 8, rest = nb % 8, x = blockIdx.x % 8, k = blockIdx.x / 8;
+  return x * per + min(x, rest) + k;
+}
+
+// A workgroup's heads: `share` q heads from h0 on for each of the k heads from k0 on
+struct Group {
+  int h0, heads, k0, kheads, share;
 };
-__device__ __forceinline__ Geometry edge_of(const AttnArgs& a, int i, int j) {
-  Geometry g;
-  g.x = a.pos[3 * (int64_t)i] - a.pos[3 * (int64_t)j];
-  g.y = a.pos[3 * (int64_t)i + 1] - a.pos[3 * (int64_t)j + 1];
-  g.z = a.pos[3 * (int64_t)i + 2] - a.pos[3 * (int64_t)j + 2];
-  g.d = sqrtf(g.x * g.x + g.y * g.y + g.z * g.z);
+__device__ __forceinline__ Group group_of(const AttnArgs& a, const AttnShape& s, int y) {
+  const int share = a.H / a.Hk;
+  Group g;
+  if (share > s.share) {  // part of the heads of one head of k
+    const int parts = (share + s.share - 1) / s.share, at = y % parts * s.share;
+    g.k0 = y / parts, g.kheads = 1, g.share = min(s.share, share - at), g.h0 = g.k0 * share + at;
+  } else {
+    g.k0 = y * s.kheads, g.kheads = min(s.kheads, a.Hk - g.k0), g.share = share, g.h0 = g.k0 * share;
+  }
+  g.heads = g.kheads * g.share;
   return g;
 }
-constexpr float kPi = 3.14159265358979f;
-__device__ __forceinline__ float envelope(const AttnArgs& a, float d) {
-  return d < a.rc ? 0.5f * (cosf(kPi / a.rc * d) + 1.0f) : 0.0f;
-}
-__device__ __forceinline__ float envelope_slope(const AttnArgs& a, float d) {
-  return d < a.rc ? -0.5f * kPi / a.rc * sinf(kPi / a.rc * d) : 0.0f;
+
+// x / heads for x < 4096, heads <= 16
+__device__ __forceinline__ int over_heads(const AttnShape& s, int heads, int x) {
+  return heads == s.heads ? (int)((unsigned)x * s.inv_heads >> 16) : x / heads;
 }
 
-// the score x of head h
-template <typename T>
-__device__ __forceinline__ float score(const AttnArgs& a, int i, int j, int h, float d) {
-  const int hk = h / (a.H / a.Hk);
-  const T* q = (const T*)a.q + i * a.ldq + h * a.dk;
-  const T* k = (const T*)a.k + j * a.ldk + hk * a.dk;
-  float x = 0.0f;
-  for (int t = 0; t < a.dk; ++t) x += to_float(q[t]) * to_float(k[t]);
-  x *= a.scale;
-  const float sigma = a.rc / (float)(a.R - 1), inv = 1.0f / sigma;
-  for (int r = 0; r < a.R; ++r) {
-    const float z = (d - r * sigma) * inv;
-    x += a.w[h * a.R + r] * expf(-z * z);
+// How a wave goes through a row: stretches of 64 edges, of which it takes those of the receiver's graph
+struct Walk {
+  int64_t e1, at, step;  // end of the row, next stretch, from one of the wave's to the next
+  int queued, gid;       // edges found and not yet taken
+};
+
+// The next batch, a lane an edge: e and its sender j, -1 behind the last.  Returns their number.  stage: 256 ints.
+// skip(first edge, count, lanes whose edges are between graphs) sees each stretch once.
+template <typename S>
+__device__ __forceinline__ int next_batch(const AttnArgs& a, Walk& w, int* stage, int64_t e0, int64_t& e, int& j,
+                                          S&& skip) {
+  const int lane = threadIdx.x & 63;
+  j = -1, e = e0;
+  if (!a.gid) {
+    if (w.at >= w.e1) return 0;
+    const int count = (int)min(w.e1 - w.at, (int64_t)64);
+    if (lane < count) e = w.at + lane, j = atom_of(a, a.col[e]);
+    w.at += w.step;
+    return count;
   }
-  return x;
+  while (w.queued < 64 && w.at < w.e1) {
+    const int64_t mine = w.at + lane;
+    int s = -1;
+    bool same = false;
+    if (mine < w.e1) {
+      s = atom_of(a, a.col[mine]);
+      same = a.gid[s] == w.gid;
+    }
+    const uint64_t found = __ballot(same);
+    const int count = (int)min(w.e1 - w.at, (int64_t)64);
+    skip(w.at, count, ~found & (count == 64 ? ~0ull : (1ull << count) - 1));
+    if (same) {
+      const int q = w.queued + __builtin_popcountll(found & ((1ull << lane) - 1));
+      stage[q] = s;
+      stage[128 + q] = (int)(mine - e0);
+    }
+    w.queued += __builtin_popcountll(found);
+    w.at += w.step;
+  }
+  wave_sync();
+  const int count = min(w.queued, 64);
+  if (lane < count) j = stage[lane], e = e0 + stage[128 + lane];
+  if (w.queued > 64) {
+    const bool more = lane < w.queued - 64;
+    const int s = more ? stage[64 + lane] : 0, f = more ? stage[192 + lane] : 0;
+    wave_sync();
+    if (more) stage[lane] = s, stage[128 + lane] = f;
+  }
+  w.queued -= count;
+  wave_sync();
+  return count;
 }
 
-// A wave a row: lane l takes head l % HP and every (64 / HP)-th edge.
-template <int HP, typename T>
-__global__ __launch_bounds__(256) void k_att_forward(AttnArgs a, float* alpha, float* lse) {
-  constexpr int EPI = 64 / HP;
-  const int i = blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (i >= a.n) return;
-  const int h = lane % HP, el = lane / HP;
-  const Row r = row_of(a, i);
-  float m = -INFINITY, den = 0.0f;
-  if (h < a.H)
-    for (int64_t e = r.e0 + el; e < r.e1; e += EPI) {
-      const int j = atom_of(a, a.col[e]);
-      if (a.gid && a.gid[i] != a.gid[j]) continue;
-      float x = score<T>(a, i, j, h, edge_of(a, i, j).d);
-      if (a.cap > 0.0f) x = a.cap * tanhf(x / a.cap);
-      alpha[e * a.H + h] = x;
-      if (x > m) {
-        den = den * expf(m - x) + 1.0f;
-        m = x;
-      } else {
-        den += expf(x - m);
+// Features of a block of BE entries, LPE lanes an entry
+template <int LPE, typename F>
+struct Features {
+  static constexpr int EPI = 64 / LPE, BE = EPI > 16 ? EPI : 16, IT = BE / EPI;
+  typename F::raw k[IT];
+  // from the atoms jj[entry] (-1: none, zeros), `count` of the lane's from base on
+  __device__ __forceinline__ void read(const typename F::type* base, int64_t ld, const int* jj, int count) {
+    const int slot = (threadIdx.x & 63) / LPE;
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const int j = jj[i * EPI + slot];
+      typename F::raw r = {};
+      if (j >= 0 && count > 0) r = F::load(base + j * ld, count);
+      k[i] = r;
+    }
+  }
+  // s[entry * ld] = the sum over a head's lph lanes of q . k, by its first lane
+  __device__ __forceinline__ void dots(const float (&q)[F::VEC], int lph, bool first, float* s, int ld) {
+    const int slot = (threadIdx.x & 63) / LPE;
+    float x[IT];
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      x[i] = 0.0f;
+#pragma unroll
+      for (int u = 0; u < F::VEC; ++u) x[i] += q[u] * F::at(k[i], u);
+    }
+    auto add = [&](auto other) {
+#pragma unroll
+      for (int i = 0; i < IT; ++i) x[i] = other(x[i]);
+    };
+    if (LPE > 1 && lph > 1) add([](float v) { return v + lane_other<1>(v); });
+    if (LPE > 2 && lph > 2) add([](float v) { return v + lane_other<2>(v); });
+    if (LPE > 4 && lph > 4) add([](float v) { return v + lane_other<4>(v); });
+    if (LPE > 8 && lph > 8) add([](float v) { return v + lane_other<8>(v); });
+    if (LPE > 16 && lph > 16) add([](float v) { float p, q; lane_halves<16>(v, p, q); return p + q; });
+    if (LPE > 32 && lph > 32) add([](float v) { float p, q; lane_halves<32>(v, p, q); return p + q; });
+    if (first) {
+#pragma unroll
+      for (int i = 0; i < IT; ++i) s[(i * EPI + slot) * ld] = x[i];
+    }
+  }
+  // acc += sum over the lane's entries of w[entry * ld] k
+  __device__ __forceinline__ void add_weighted(const float* w, int ld, float (&acc)[F::VEC]) {
+    const int slot = (threadIdx.x & 63) / LPE;
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const float c = w[(i * EPI + slot) * ld];
+#pragma unroll
+      for (int u = 0; u < F::VEC; ++u) acc[u] += c * F::at(k[i], u);
+    }
+  }
+};
+
+// A lane's place among the features of a group: k head kl, its features from t VEC on, `count` of them there
+struct Place {
+  int kl, t, count;
+};
+template <int LPE, typename F>
+__device__ __forceinline__ Place place_of(const AttnArgs& a, const AttnShape& sh, const Group& g, int unit) {
+  Place p;
+  const int at = unit * 64 + (threadIdx.x & 63) % LPE;
+  p.t = at % sh.lph, p.kl = at / sh.lph;
+  p.count = p.kl < g.kheads ? a.dk - p.t * F::VEC : 0;
+  return p;
+}
+template <typename F>
+__device__ __forceinline__ const typename F::type* k_at(const AttnArgs& a, const Group& g, const Place& p) {
+  return (const typename F::type*)a.k + (g.k0 + p.kl) * a.dk + p.t * F::VEC;
+}
+template <typename F>
+__device__ __forceinline__ void read_q(const AttnArgs& a, int64_t i, int h, const Place& p, float (&q)[F::VEC]) {
+  typename F::raw r = {};
+  if (p.count > 0) r = F::load((const typename F::type*)a.q + i * a.ldq + (int64_t)h * a.dk + p.t * F::VEC, p.count);
+#pragma unroll
+  for (int u = 0; u < F::VEC; ++u) q[u] = a.scale * F::at(r, u);
+}
+
+// The products scale q . k of a block's entries with every head of the group: s[entry * ld + head].  ONE: a lane has
+// one head (q1 its features, k kept in f); else `units` times 64 lanes for k, and `share` heads each.
+template <int LPE, bool ONE, typename F>
+__device__ __forceinline__ void products(const AttnArgs& a, const AttnShape& sh, const Group& g, int64_t i,
+                                         const float (&q1)[F::VEC], Features<LPE, F>& f, const int* jj, float* s) {
+  if constexpr (ONE) {
+    const Place p = place_of<LPE, F>(a, sh, g, 0);
+    f.read(k_at<F>(a, g, p), a.ldk, jj, p.count);
+    f.dots(q1, sh.lph, p.t == 0 && p.kl < g.kheads, s + p.kl, sh.ld);
+  } else {
+    for (int u = 0; u < sh.units; ++u) {
+      const Place p = place_of<LPE, F>(a, sh, g, u);
+      f.read(k_at<F>(a, g, p), a.ldk, jj, p.count);
+      for (int m = 0; m < g.share; ++m) {
+        float q[F::VEC];
+        read_q<F>(a, i, g.h0 + p.kl * g.share + m, p, q);
+        f.dots(q, sh.lph, p.t == 0 && p.kl < g.kheads, s + p.kl * g.share + m, sh.ld);
       }
     }
-#pragma unroll
-  for (int o = 32; o >= HP; o >>= 1) {
-    const float m2 = __shfl_xor(m, o), den2 = __shfl_xor(den, o), mx = fmaxf(m, m2);
-    den = (m == mx ? den : den * expf(m - mx)) + (m2 == mx ? den2 : den2 * expf(m2 - mx));
-    m = mx;
-  }
-  if (h >= a.H) return;
-  const float l = m + logf(den);
-  if (el == 0 && lse) lse[(int64_t)i * a.H + h] = l;
-  for (int64_t e = r.e0 + el; e < r.e1; e += EPI) {
-    const int j = atom_of(a, a.col[e]);
-    if (a.gid && a.gid[i] != a.gid[j])
-      alpha[e * a.H + h] = 0.0f;
-    else
-      alpha[e * a.H + h] = envelope(a, edge_of(a, i, j).d) * expf(alpha[e * a.H + h] - l);
   }
 }
 
-// ds of every edge and head (0 where the graphs differ), the edge's position
-// gradient and distance, and the receiver's part of the gradients.
-template <int HP, typename T>
-__global__ __launch_bounds__(256) void k_att_receivers(AttnArgs a, AttnGrad g) {
-  constexpr int EPI = 64 / HP;
-  const int i = blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (i >= a.n) return;
-  const int h = lane % HP, el = lane / HP;
-  const Row r = row_of(a, i);
-  auto same = [&](int j) { return !a.gid || a.gid[i] == a.gid[j]; };
-  float D = 0.0f;
-  if (h < a.H)
-    for (int64_t e = r.e0 + el; e < r.e1; e += EPI)
-      if (same(atom_of(a, a.col[e]))) D += g.alpha[e * a.H + h] * g.galpha[e * a.H + h];
+constexpr int kKept = 128;  // edges of a row whose scores stay in the LDS
+
+template <int LPE, bool ONE, typename F>
+__global__ __launch_bounds__(256) void k_att_forward(AttnArgs a, AttnShape sh, float* alpha, float* lse) {
+  extern __shared__ float sm[];
+  __shared__ float join[4][2][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Group g = group_of(a, sh, blockIdx.y);
+  const int64_t i = sh.wpr == 1 ? row_block() * 4 + wave : row_block();
+  const bool row = i < a.n;  // (with four waves a row the same for the workgroup)
+  float* s = sm + wave * sh.lds;
+  float* env = s + kKept * sh.ld;
+  int* edge = (int*)(env + kKept);
+  float* dist = (float*)(edge + kKept);
+  int* jj = (int*)(dist + 64);
+  int* stage = jj + 64;
+  const int64_t e0 = row ? min(max(a.row_ptr[i], (int64_t)0), a.E) : 0;
+  const int64_t e1 = row ? min(max(a.row_ptr[i + 1], e0), a.E) : 0;
+  const int part = sh.wpr == 1 ? 0 : wave;
+  const int64_t step = 64 * (int64_t)sh.wpr;
+  Walk w{e1, e0 + 64 * part, step, 0, a.gid && row ? a.gid[i] : 0};
+  const float inv = (float)(a.R - 1) / a.rc, icap = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
+  const int hc = lane & 15, quad = lane >> 4;
+  const bool hv = hc < g.heads;
+  float wr[8];  // of the lane's head, the functions 4 r + quad
 #pragma unroll
-  for (int o = 32; o >= HP; o >>= 1) D += __shfl_xor(D, o);
-  const float l = h < a.H ? g.lse[(int64_t)i * a.H + h] : 0.0f;
-  const float sigma = a.rc / (float)(a.R - 1), inv = 1.0f / sigma;
-  float gx = 0.0f, gy = 0.0f, gz = 0.0f;
-  for (int64_t c = r.e0; c < r.e1; c += EPI) {
-    const int64_t e = c + el;
-    float dd = 0.0f, ds = 0.0f;
-    Geometry v{0.0f, 0.0f, 0.0f, 0.0f};
-    if (e < r.e1 && h < a.H) {
-      const int j = atom_of(a, a.col[e]);
-      if (same(j)) {
-        v = edge_of(a, i, j);
-        const float x = score<T>(a, i, j, h, v.d), t = a.cap > 0.0f ? tanhf(x / a.cap) : 0.0f;
-        const float p = expf((a.cap > 0.0f ? a.cap * t : x) - l), ga = g.galpha[e * a.H + h];
-        ds = p * (ga * envelope(a, v.d) - D) * (1.0f - t * t);
-        dd = ga * p * envelope_slope(a, v.d);
-        for (int q = 0; q < a.R; ++q) {
-          const float z = (v.d - q * sigma) * inv;
-          dd += ds * a.w[h * a.R + q] * expf(-z * z) * (-2.0f * z * inv);
+  for (int r = 0; r < 8; ++r) wr[r] = hv && 4 * r + quad < a.R ? a.w[(g.h0 + hc) * a.R + 4 * r + quad] : 0.0f;
+  float q1[F::VEC] = {};
+  if (ONE && a.dk && row) {
+    const Place p = place_of<LPE, F>(a, sh, g, 0);
+    read_q<F>(a, i, g.h0 + p.kl, p, q1);
+  }
+  float px = 0.0f, py = 0.0f, pz = 0.0f;
+  if (row) px = a.pos[3 * i], py = a.pos[3 * i + 1], pz = a.pos[3 * i + 2];
+  float m = -INFINITY, den = 0.0f;
+  int kept = 0;        // edges whose scores are in the LDS
+  bool spill = false;  // the scores of the row are in alpha
+  auto to_alpha = [&](int count, const float* from) {
+    for (int x = lane; x < count * g.heads; x += 64) {
+      const int at = over_heads(sh, g.heads, x), h = x - at * g.heads;
+      alpha[(e0 + edge[at]) * a.H + g.h0 + h] = from[at * sh.ld + h];
+    }
+  };
+  for (;;) {
+    int64_t e;
+    int j;
+    const int count = next_batch(a, w, stage, e0, e, j, [&](int64_t first, int many, uint64_t mask) {
+      if (!mask) return;
+      for (int x = lane; x < many * g.heads; x += 64) {
+        const int at = over_heads(sh, g.heads, x);
+        if (mask >> at & 1) alpha[(first + at) * a.H + g.h0 + x - at * g.heads] = 0.0f;
+      }
+    });
+    if (count == 0) break;
+    if (kept == kKept) {  // (every batch but the last has 64)
+      to_alpha(kept, s);
+      kept = 0, spill = true;
+      wave_sync();
+    }
+    float* sb = s + kept * sh.ld;
+    const bool there = j >= 0;
+    float dx = 0.0f, dy = 0.0f, dz = 0.0f;
+    if (there) dx = px - a.pos[3 * (int64_t)j], dy = py - a.pos[3 * (int64_t)j + 1], dz = pz - a.pos[3 * (int64_t)j + 2];
+    jj[lane] = j;
+    wave_sync();
+    if (a.dk) {
+      Features<LPE, F> f;
+      for (int b = 0; b < count; b += f.BE) products<LPE, ONE, F>(a, sh, g, i, q1, f, jj + b, sb + b * sh.ld);
+    }
+    const float d = sqrtf(dx * dx + dy * dy + dz * dz);
+    dist[lane] = d;
+    env[kept + lane] = envelope(a.rc, d);
+    edge[kept + lane] = (int)(e - e0);
+    wave_sync();
+    for (int b = 0; b < count; b += 16) {
+      f4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+      const float z0 = dist[b + hc] * inv - (float)quad;
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
+        if (4 * r < a.R) {
+          const float z = z0 - 4.0f * r;
+          x = __builtin_amdgcn_mfma_f32_16x16x4f32(exp_fast(-z * z), wr[r], x, 0, 0, 0);
+        }
+      float mx = m;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int n = b + quad * 4 + u;
+        if (a.dk && hv) x[u] += sb[n * sh.ld + hc];
+        if (a.cap > 0.0f) x[u] = a.cap * tanh_near(x[u] * icap);
+        if (n >= count) x[u] = -INFINITY;
+        mx = fmaxf(mx, x[u]);
+        if (hv) sb[n * sh.ld + hc] = x[u];
+      }
+      if (mx > m) den *= exp_fast(m - mx), m = mx;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (b + quad * 4 + u < count) den += exp_fast(x[u] - m);
+    }
+    wave_sync();
+    if (spill)
+      to_alpha(count, s);
+    else
+      kept += count;
+    wave_sync();
+  }
+  // the row's sum, over the lanes and waves of a head
+  const float top_w = classes_all(m, 16, [](float p, float q) { return fmaxf(p, q); });
+  float top = top_w;
+  den = classes_all(m == top ? den : den * exp_fast(m - top), 16, [](float p, float q) { return p + q; });
+  if (sh.wpr > 1) {
+    if (lane < 16) join[wave][0][lane] = top, join[wave][1][lane] = den;
+    __syncthreads();
+    for (int k = 0; k < 4; ++k) top = fmaxf(top, join[k][0][hc]);
+    den = 0.0f;
+    for (int k = 0; k < 4; ++k) {
+      const float mk = join[k][0][hc], dk = join[k][1][hc];
+      den += mk == top ? dk : dk * exp_fast(mk - top);
+    }
+  }
+  if (!row) return;
+  const float l = top + logf(den);
+  if (lse && hv && quad == 0 && part == 0) lse[i * a.H + g.h0 + hc] = l;
+  if (lane < 16) dist[lane] = l;
+  wave_sync();
+  if (!spill) {
+    for (int x = lane; x < kept * g.heads; x += 64) {
+      const int at = over_heads(sh, g.heads, x), h = x - at * g.heads;
+      alpha[(e0 + edge[at]) * a.H + g.h0 + h] = env[at] * exp_fast(s[at * sh.ld + h] - dist[h]);
+    }
+    return;
+  }
+  for (int64_t c = e0 + 64 * part; c < e1; c += step) {
+    const int count = (int)min(e1 - c, (int64_t)64);
+    float v = -1.0f;  // (an edge between graphs: its zeros are written)
+    if (lane < count) {
+      const int j = atom_of(a, a.col[c + lane]);
+      if (!a.gid || a.gid[j] == w.gid) {
+        const float dx = px - a.pos[3 * (int64_t)j], dy = py - a.pos[3 * (int64_t)j + 1], dz = pz - a.pos[3 * (int64_t)j + 2];
+        v = envelope(a.rc, sqrtf(dx * dx + dy * dy + dz * dz));
+      }
+    }
+    env[lane] = v;
+    wave_sync();
+    for (int x = lane; x < count * g.heads; x += 64) {
+      const int at = over_heads(sh, g.heads, x), h = x - at * g.heads;
+      if (env[at] < 0.0f) continue;
+      float* to = alpha + (c + at) * a.H + g.h0 + h;
+      *to = env[at] * exp_fast(*to - dist[h]);
+    }
+    wave_sync();
+  }
+}
+
+// ds of every edge and head, the edge's position gradient, and the receivers' gradients.  A workgroup takes sh.rows
+// rows and sums dw over them.
+template <int LPE, bool ONE, typename F>
+__global__ __launch_bounds__(256) void k_att_receivers(AttnArgs a, AttnShape sh, AttnGrad gr) {
+  extern __shared__ float sm[];
+  __shared__ float join[4][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Group g = group_of(a, sh, blockIdx.y);
+  float* s = sm + wave * sh.lds;  // [64][ld] scores, then ds
+  float* dist = s + 64 * sh.ld;
+  float* env = dist + 64;
+  float* slope = env + 64;
+  int* edge = (int*)(slope + 64);
+  int* jj = edge + 64;
+  float* slot_sum = (float*)(jj + 64);  // [64] position gradients over distances
+  int* stage = (int*)(slot_sum + 64);
+  const float inv = (float)(a.R - 1) / a.rc, icap = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
+  const int hc = lane & 15, quad = lane >> 4;
+  const bool hv = hc < g.heads;
+  float wr[8], wt[2][4];  // weights: of the lane's head, functions 4 r + quad; of the functions 16 r + hc, heads 4 k + quad
+#pragma unroll
+  for (int r = 0; r < 8; ++r) wr[r] = hv && 4 * r + quad < a.R ? a.w[(g.h0 + hc) * a.R + 4 * r + quad] : 0.0f;
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      wt[r][k] = 4 * k + quad < g.heads && 16 * r + hc < a.R ? a.w[(g.h0 + 4 * k + quad) * a.R + 16 * r + hc] : 0.0f;
+  f4 dw[2] = {};  // of the lane's head, functions 16 r + 4 quad + 0 .. 3
+  const int part = sh.wpr == 1 ? 0 : wave;
+  const int64_t first = row_block() * sh.rows;
+  for (int rr = 0; rr < sh.rows; rr += sh.wpr == 1 ? 4 : 1) {
+    const int64_t i = first + rr + (sh.wpr == 1 ? wave : 0);
+    const bool row = i < a.n;
+    const int64_t e0 = row ? min(max(a.row_ptr[i], (int64_t)0), a.E) : 0;
+    const int64_t e1 = row ? min(max(a.row_ptr[i + 1], e0), a.E) : 0;
+    const int64_t step = 64 * (int64_t)sh.wpr;
+    Walk w{e1, e0 + 64 * part, step, 0, a.gid && row ? a.gid[i] : 0};
+    // D of the lane's head: lanes over a power of two of heads and over edges
+    float D = 0.0f;
+    {
+      const int hd = lane & (sh.hp - 1), per = 64 / sh.hp;
+      const bool on = hd < g.heads;
+      for (int64_t e = e0 + lane / sh.hp + part * per; e < e1; e += per * sh.wpr)
+        if (on && (!a.gid || a.gid[atom_of(a, a.col[e])] == w.gid))
+          D += gr.alpha[e * a.H + g.h0 + hd] * gr.galpha[e * a.H + g.h0 + hd];
+      D = classes_all(D, sh.hp, [](float p, float q) { return p + q; });
+      if (sh.wpr > 1) {
+        __syncthreads();  // (the row before has been read)
+        if (lane < 16) join[wave][lane] = D;
+        __syncthreads();
+        D = join[0][lane & 15] + join[1][lane & 15] + join[2][lane & 15] + join[3][lane & 15];
+      }
+      D = __shfl(D, hc & (sh.hp - 1));
+    }
+    if (!row) continue;  // (with four waves a row, for the workgroup)
+    const float l = hv ? gr.lse[i * a.H + g.h0 + hc] : 0.0f;
+    float q1[F::VEC] = {}, dq[F::VEC] = {};
+    if (ONE && a.dk) {
+      const Place p = place_of<LPE, F>(a, sh, g, 0);
+      read_q<F>(a, i, g.h0 + p.kl, p, q1);
+    }
+    const float px = a.pos[3 * i], py = a.pos[3 * i + 1], pz = a.pos[3 * i + 2];
+    if (!ONE && gr.gq) {
+      for (int x = lane; x < sh.dq; x += 64) stage[256 + x] = 0;
+      wave_sync();
+    }
+    for (;;) {
+      int64_t e;
+      int j;
+      const int count = next_batch(a, w, stage, e0, e, j, [](int64_t, int, uint64_t) {});
+      if (count == 0) break;
+      float dx = 0.0f, dy = 0.0f, dz = 0.0f;
+      if (j >= 0) dx = px - a.pos[3 * (int64_t)j], dy = py - a.pos[3 * (int64_t)j + 1], dz = pz - a.pos[3 * (int64_t)j + 2];
+      jj[lane] = j;
+      edge[lane] = (int)(e - e0);
+      const float d = sqrtf(dx * dx + dy * dy + dz * dz);
+      dist[lane] = d, env[lane] = envelope(a.rc, d), slope[lane] = envelope_slope(a.rc, d);
+      wave_sync();
+      Features<LPE, F> f;
+      for (int b0 = 0; b0 < count; b0 += f.BE) {
+        if (a.dk) products<LPE, ONE, F>(a, sh, g, i, q1, f, jj + b0, s + b0 * sh.ld);
+        wave_sync();
+        for (int b = b0; b < min(count, b0 + f.BE); b += 16) {
+          float ga[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int n = b + quad * 4 + u;
+            ga[u] = hv && n < count ? gr.galpha[(e0 + edge[n]) * a.H + g.h0 + hc] : 0.0f;
+          }
+          f4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+          const float z0 = dist[b + hc] * inv - (float)quad;
+#pragma unroll
+          for (int r = 0; r < 8; ++r)
+            if (4 * r < a.R) {
+              const float z = z0 - 4.0f * r;
+              x = __builtin_amdgcn_mfma_f32_16x16x4f32(exp_fast(-z * z), wr[r], x, 0, 0, 0);
+            }
+          float ds[4], dd[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int n = b + quad * 4 + u;
+            const bool on = hv && n < count;
+            if (a.dk && hv) x[u] += s[n * sh.ld + hc];
+            float turn = 1.0f;
+            if (a.cap > 0.0f) {
+              const float t = tanh_near(x[u] * icap);
+              x[u] = a.cap * t;
+              turn = 1.0f - t * t;
+            }
+            const float p = exp_fast(x[u] - l);
+            ds[u] = on ? p * (ga[u] * env[n] - D) * turn : 0.0f;
+            dd[u] = on ? ga[u] * p * slope[n] : 0.0f;
+            if (hv) s[n * sh.ld + hc] = ds[u];
+            if (on && gr.gk) gr.ds[(e0 + edge[n]) * a.H + g.h0 + hc] = ds[u];
+          }
+          wave_sync();
+          if (a.R && (gr.gw || gr.gpos)) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+              if (16 * r < a.R) {
+                // u[edge][function] = sum of ds w over the heads
+                f4 us = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (gr.gpos) {
+#pragma unroll
+                  for (int k = 0; k < 4; ++k)
+                    if (4 * k < g.heads)
+                      us = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                          4 * k + quad < g.heads ? s[(b + hc) * sh.ld + 4 * k + quad] : 0.0f, wt[r][k], us, 0, 0, 0);
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                  const float z = dist[b + quad * 4 + u] * inv - (float)(16 * r + hc), gz = exp_fast(-z * z);
+                  dd[u] += us[u] * gz * z * (-2.0f * inv);
+                  dw[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(gz, ds[u], dw[r], 0, 0, 0);
+                }
+              }
+          }
+          if (gr.gpos) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const float v = lanes_sum(dd[u], 16);
+              if (hc == u) slot_sum[b + quad * 4 + u] = v;
+            }
+          }
+        }
+        if constexpr (ONE) {
+          if (a.dk && gr.gq) {
+            const Place p = place_of<LPE, F>(a, sh, g, 0);
+            if (p.kl < g.kheads) f.add_weighted(s + b0 * sh.ld + p.kl, sh.ld, dq);
+          }
+        } else if (a.dk && gr.gq) {
+          // k read again, a head's sum at a time, added to those of the wave in the LDS
+          float* acc = (float*)(stage + 256);
+          for (int u = 0; u < sh.units; ++u) {
+            const Place p = place_of<LPE, F>(a, sh, g, u);
+            f.read(k_at<F>(a, g, p), a.ldk, jj + b0, p.count);
+            if (p.count <= 0) continue;
+            for (int mm = 0; mm < g.share; ++mm) {
+              float v[F::VEC] = {};
+              f.add_weighted(s + b0 * sh.ld + p.kl * g.share + mm, sh.ld, v);
+              float* to = acc + ((lane / LPE * g.heads + p.kl * g.share + mm) * sh.lph + p.t) * F::VEC;
+#pragma unroll
+              for (int x = 0; x < F::VEC; ++x) to[x] += v[x];
+            }
+          }
+        }
+        wave_sync();
+      }
+      if (gr.gpos && lane < count) {
+        const float v = d > 0.0f ? slot_sum[lane] / d : 0.0f;
+        *(f4*)(gr.edge + ((int64_t)blockIdx.y * a.E + e) * 4) = (f4){v * dx, v * dy, v * dz, 0.0f};
+      }
+      wave_sync();
+    }
+    if (!a.dk || !gr.gq) continue;
+    // dq: over the lanes of a feature, and the waves of the row
+    typename F::type* gq = (typename F::type*)gr.gq + (i * a.H + g.h0) * a.dk;
+    if constexpr (ONE) {
+      const Place p = place_of<LPE, F>(a, sh, g, 0);
+#pragma unroll
+      for (int u = 0; u < F::VEC; ++u) dq[u] = a.scale * classes_all(dq[u], LPE, [](float x, float y) { return x + y; });
+      if (sh.wpr > 1) {
+        float* mine = sm + wave * sh.lds;
+        __syncthreads();
+        if (lane < LPE) {
+#pragma unroll
+          for (int u = 0; u < F::VEC; ++u) mine[lane * F::VEC + u] = dq[u];
+        }
+        __syncthreads();
+        if (wave == 0 && lane < LPE) {
+#pragma unroll
+          for (int u = 0; u < F::VEC; ++u)
+            dq[u] = sm[lane * F::VEC + u] + sm[sh.lds + lane * F::VEC + u] + sm[2 * sh.lds + lane * F::VEC + u] +
+                    sm[3 * sh.lds + lane * F::VEC + u];
+        }
+        __syncthreads();
+      }
+      if (part == 0 && lane < LPE && p.count > 0) F::store(gq + p.kl * a.dk + p.t * F::VEC, dq, p.count);
+    } else {
+      if (sh.wpr > 1)
+        __syncthreads();
+      else
+        wave_sync();
+      const int off = (int)((float*)(stage + 256) - s), width = sh.lph * F::VEC;
+      for (int x = (sh.wpr > 1 ? threadIdx.x : lane); x < g.heads * a.dk; x += 64 * sh.wpr) {
+        const int h = x / a.dk, t = x - h * a.dk;
+        float v = 0.0f;
+        for (int k = 0; k < sh.wpr; ++k)
+          for (int q = 0; q < 64 / LPE; ++q)
+            v += sm[(sh.wpr > 1 ? k : wave) * sh.lds + off + (q * g.heads + h) * width + t];
+        float one[F::VEC];
+        one[0] = a.scale * v;
+        F::store(gq + x, one, 1);
+      }
+      if (sh.wpr > 1)
+        __syncthreads();
+      else
+        wave_sync();
+    }
+  }
+  if (!gr.gw) return;
+  // dw of the workgroup's waves
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) sm[(wave * 32 + 16 * r + quad * 4 + u) * 16 + hc] = dw[r][u];
+  __syncthreads();
+  for (int x = threadIdx.x; x < g.heads * a.R; x += 256) {
+    const int h = x / a.R, r = x - h * a.R;
+    float v = 0.0f;
+    for (int k = 0; k < 4; ++k) v += sm[(k * 32 + r) * 16 + h];
+    gr.part[((int64_t)blockIdx.x * a.H + g.h0 + h) * a.R + r] = v;
+  }
+}
+
+// dw: the sum of the workgroups', 64 columns a workgroup
+__global__ __launch_bounds__(1024) void k_att_radial_sum(const float* __restrict__ part, int parts, int count,
+                                                         float* __restrict__ gw) {
+  __shared__ double red[16][64];
+  const int c = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
+  double v = 0.0;
+  if (c < count)
+    for (int b = w; b < parts; b += 16) v += part[(int64_t)b * count + c];
+  red[w][threadIdx.x & 63] = v;
+  __syncthreads();
+  if (w || c >= count) return;
+  for (int k = 1; k < 16; ++k) v += red[k][threadIdx.x];
+  gw[c] = (float)v;
+}
+
+// dk over the edges that an atom sends, and its whole position gradient: those of the edges it receives minus those
+// of the edges it sends.  Lanes over a group's features of q, LPE an edge; the heads that share k one after another.
+template <int LPE, typename F>
+__global__ __launch_bounds__(256) void k_att_senders(AttnArgs a, AttnShape sh, AttnGrad gr) {
+  constexpr int EPI = 64 / LPE;
+  __shared__ int stage[4][2][64];
+  __shared__ float join[4][64 * F::VEC];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t j = sh.wpr == 1 ? row_block() * 4 + wave : row_block();
+  const bool row = j < a.n;
+  const int part = sh.wpr == 1 ? 0 : wave;
+  const int64_t q0 = row ? min(max(gr.rowT[j], (int64_t)0), a.E) : 0;
+  const int64_t q1 = row ? min(max(gr.rowT[j + 1], q0), a.E) : 0;
+  const int gid = a.gid && row ? a.gid[j] : 0;
+  const int k0 = blockIdx.y * sh.kheads, kheads = min(sh.kheads, a.Hk - k0), share = a.H / a.Hk;
+  const int at = lane % LPE, t = at % sh.lph, kl = at / sh.lph;
+  const int count = kl < kheads ? a.dk - t * F::VEC : 0;
+  int *ii = stage[wave][0], *ee = stage[wave][1];
+  float acc[F::VEC] = {}, gx = 0.0f, gy = 0.0f, gz = 0.0f;
+  const bool forces = gr.gpos && blockIdx.y == 0;
+  if (forces && row) {
+    const int64_t e0 = min(max(a.row_ptr[j], (int64_t)0), a.E), e1 = min(max(a.row_ptr[j + 1], e0), a.E);
+    for (int64_t e = e0 + lane + 64 * part; e < e1; e += 64 * sh.wpr)
+      if (!a.gid || a.gid[atom_of(a, a.col[e])] == gid)
+        for (int y = 0; y < gr.groups; ++y) {
+          const f4 v = *(const f4*)(gr.edge + ((int64_t)y * a.E + e) * 4);
+          gx += v[0], gy += v[1], gz += v[2];
+        }
+  }
+  for (int64_t c = q0 + 64 * part; c < q1; c += 64 * sh.wpr) {
+    const int many = (int)min(q1 - c, (int64_t)64);
+    int i = -1, e = 0;
+    if (lane < many) {
+      i = atom_of(a, gr.colT[c + lane]);
+      e = (int)min(max((int64_t)gr.perm[c + lane], (int64_t)0), a.E - 1);
+      if (a.gid && a.gid[i] != gid) i = -1;
+    }
+    if (gr.gk) {
+      ii[lane] = i, ee[lane] = e;
+      wave_sync();
+      for (int b = 0; b < many; b += 8 * EPI) {
+        for (int m = 0; m < share; ++m) {
+          typename F::raw r[8];
+          float ds[8];
+          const int h = (k0 + kl) * share + m;
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            const int n = b + u * EPI + lane / LPE;
+            const int s = n < 64 ? ii[n] : -1;
+            r[u] = typename F::raw{};
+            ds[u] = 0.0f;
+            if (s >= 0 && count > 0) {
+              r[u] = F::load((const typename F::type*)a.q + s * a.ldq + (int64_t)h * a.dk + t * F::VEC, count);
+              ds[u] = gr.ds[(int64_t)ee[n] * a.H + h];
+            }
+          }
+#pragma unroll
+          for (int u = 0; u < 8; ++u)
+#pragma unroll
+            for (int x = 0; x < F::VEC; ++x) acc[x] += ds[u] * F::at(r[u], x);
         }
       }
-      g.ds[e * a.H + h] = ds;
+      wave_sync();
     }
+    if (forces && i >= 0)
+      for (int y = 0; y < gr.groups; ++y) {
+        const f4 v = *(const f4*)(gr.edge + ((int64_t)y * a.E + e) * 4);
+        gx -= v[0], gy -= v[1], gz -= v[2];
+      }
+  }
+  if (gr.gk) {
 #pragma unroll
-    for (int o = HP / 2; o > 0; o >>= 1) dd += __shfl_xor(dd, o);
-    const float f = v.d > 0.0f ? dd / v.d : 0.0f;
-    if (h == 0 && e < r.e1) {
-      g.edge[e * 4] = f * v.x, g.edge[e * 4 + 1] = f * v.y, g.edge[e * 4 + 2] = f * v.z, g.edge[e * 4 + 3] = v.d;
-      gx += f * v.x, gy += f * v.y, gz += f * v.z;
-    }
+    for (int u = 0; u < F::VEC; ++u) acc[u] = a.scale * classes_all(acc[u], LPE, [](float x, float y) { return x + y; });
   }
+  gx = lanes_sum(gx), gy = lanes_sum(gy), gz = lanes_sum(gz);
+  if (sh.wpr > 1) {
+    if (lane < LPE) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) gx += __shfl_xor(gx, o), gy += __shfl_xor(gy, o), gz += __shfl_xor(gz, o);
-  if (g.gpos && lane < 3) g.gpos[3 * (int64_t)i + lane] = lane == 0 ? gx : lane == 1 ? gy : gz;
-  if (!g.gq) return;
-  __threadfence_block();  // (the wave's own ds, read by other lanes)
-  for (int c = lane; c < a.H * a.dk; c += 64) {
-    const int hq = c / a.dk, hk = hq / (a.H / a.Hk), t = c % a.dk;
-    float s = 0.0f;
-    for (int64_t e = r.e0; e < r.e1; ++e) {
-      const int j = atom_of(a, a.col[e]);
-      if (same(j)) s += g.ds[e * a.H + hq] * to_float(((const T*)a.k)[j * a.ldk + hk * a.dk + t]);
+      for (int u = 0; u < F::VEC; ++u) join[wave][lane * F::VEC + u] = acc[u];
     }
-    store((T*)g.gq + (int64_t)i * a.H * a.dk + c, a.scale * s);
-  }
-}
-
-// The senders' part: a wave an atom, over the transposed graph.
-template <typename T>
-__global__ __launch_bounds__(256) void k_att_senders(AttnArgs a, AttnGrad g) {
-  const int j = blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (j >= a.n) return;
-  const int64_t q0 = min(max(g.rowT[j], (int64_t)0), a.E), q1 = min(max(g.rowT[j + 1], q0), a.E);
-  auto edge = [&](int64_t q) { return (int64_t)min(max((int64_t)g.perm[q], (int64_t)0), a.E - 1); };
-  if (g.gpos) {
-    float s[3] = {0.0f, 0.0f, 0.0f};
-    for (int64_t q = q0 + lane; q < q1; q += 64)
-      for (int x = 0; x < 3; ++x) s[x] += g.edge[edge(q) * 4 + x];
+    float* p = (float*)stage[wave][0];
+    __syncthreads();
+    if (lane == 0) p[0] = gx, p[1] = gy, p[2] = gz;
+    __syncthreads();
+    if (wave == 0 && lane < LPE) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1)
-      for (int x = 0; x < 3; ++x) s[x] += __shfl_xor(s[x], o);
-    if (lane < 3) g.gpos[3 * (int64_t)j + lane] -= lane == 0 ? s[0] : lane == 1 ? s[1] : s[2];
-  }
-  if (!g.gk) return;
-  const int share = a.H / a.Hk;
-  for (int c = lane; c < a.Hk * a.dk; c += 64) {
-    const int hk = c / a.dk, t = c % a.dk;
-    float s = 0.0f;
-    for (int64_t q = q0; q < q1; ++q) {
-      const int i = atom_of(a, g.colT[q]);
-      if (a.gid && a.gid[i] != a.gid[j]) continue;
-      for (int h = hk * share; h < (hk + 1) * share; ++h)
-        s += g.ds[edge(q) * a.H + h] * to_float(((const T*)a.q)[i * a.ldq + h * a.dk + t]);
+      for (int u = 0; u < F::VEC; ++u)
+        acc[u] = join[0][lane * F::VEC + u] + join[1][lane * F::VEC + u] + join[2][lane * F::VEC + u] +
+                 join[3][lane * F::VEC + u];
     }
-    store((T*)g.gk + (int64_t)j * a.Hk * a.dk + c, a.scale * s);
-  }
-}
-
-// dw: part[b][h][r] of every kAttnParts-th stretch of edges, then their sum
-__global__ __launch_bounds__(256) void k_att_radial(AttnArgs a, AttnGrad g) {
-  const float sigma = a.rc / (float)(a.R - 1), inv = 1.0f / sigma;
-  const int64_t per = (a.E + kAttnParts - 1) / kAttnParts, lo = blockIdx.x * per, hi = min(lo + per, a.E);
-  for (int c = threadIdx.x; c < a.H * a.R; c += 256) {
-    const int h = c / a.R, r = c % a.R;
-    float s = 0.0f;
-    for (int64_t e = lo; e < hi; ++e) {
-      const float z = (g.edge[e * 4 + 3] - r * sigma) * inv;
-      s += g.ds[e * a.H + h] * expf(-z * z);
+    gx = gy = gz = 0.0f;
+    for (int k = 0; k < 4; ++k) {
+      const float* pk = (const float*)stage[k][0];
+      gx += pk[0], gy += pk[1], gz += pk[2];
     }
-    g.part[(int64_t)blockIdx.x * a.H * a.R + c] = s;
   }
-}
-__global__ __launch_bounds__(256) void k_att_radial_sum(const float* __restrict__ part, int parts, int count,
-                                                        float* __restrict__ gw) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= count) return;
-  double s = 0.0;
-  for (int b = 0; b < parts; ++b) s += part[(int64_t)b * count + c];
-  gw[c] = (float)s;
+  if (!row || part) return;
+  if (gr.gk && lane < LPE && count > 0)
+    F::store((typename F::type*)gr.gk + (j * a.Hk + k0 + kl) * a.dk + t * F::VEC, acc, count);
+  if (forces && lane < 3) gr.gpos[3 * j + lane] = lane == 0 ? gx : lane == 1 ? gy : gz;
 }
 
 // ---- the transposed graph: edges by sender, ascending
@@ -316,59 +900,116 @@ __global__ __launch_bounds__(256) void k_t_sort(const int64_t* __restrict__ row_
   }
 }
 
-int head_slots(int H) {
-  int hp = 1;
-  while (hp < H) hp <<= 1;
-  return hp;
+// Lanes of a head, heads of a workgroup and what follows from them
+AttnShape shape_of(const AttnArgs& a, bool senders) {
+  const int vec = a.bf16 ? BF16::VEC : F32::VEC, share = a.H / a.Hk;
+  AttnShape s{};
+  s.lph = 1;
+  while (s.lph * vec < a.dk) s.lph <<= 1;
+  // heads that share k: the receivers' sums for dq, 64 lanes of them for each, stay within 8 KB of LDS a wave
+  s.share = senders ? share : std::min(share, 2048 / (64 * vec));
+  s.kheads = senders ? a.Hk : std::min(a.Hk, s.share < share ? 1 : 16 / share);
+  const int most = senders ? 64 : 2048 / (vec * s.share) < 256 ? 2048 / (vec * s.share) : 256;
+  int p = 1;
+  while (p < s.kheads) p <<= 1;
+  while (p > 1 && p * s.lph > most) p >>= 1;
+  s.kheads = std::min(s.kheads, p);
+  s.units = (p * s.lph + 63) / 64;
+  s.lpe = std::min(p * s.lph, 64);
+  s.groups = s.share < share ? a.Hk * ((share + s.share - 1) / s.share) : (a.Hk + s.kheads - 1) / s.kheads;
+  s.heads = s.kheads * s.share;
+  s.inv_heads = (65536 + s.heads - 1) / s.heads;
+  s.ld = s.heads | 1;
+  s.hp = 1;
+  while (s.hp < s.heads) s.hp <<= 1;
+  s.one = s.units == 1 && (share == 1 || a.dk == 0);
+  // four waves a row where they find four batches on average
+  s.wpr = a.E / a.n >= 256 ? 4 : 1;
+  s.rows = 1;
+  return s;
 }
 
 }  // namespace
 
+int attention_groups(const AttnArgs& a) { return shape_of(a, false).groups; }
+
+// workgroups of the receivers' kernel: a few rows each, up to about 2048
+int attention_parts(const AttnArgs& a, int* rows) {
+  const int wpr = shape_of(a, false).wpr, least = wpr == 1 ? 4 : 1;
+  const int64_t r = least * (((int64_t)a.n + least * 2048 - 1) / (least * 2048));
+  if (rows) *rows = (int)r;
+  return (int)((a.n + r - 1) / r);
+}
+
+// the kernel for the lanes of an edge, the type and one head a lane or more
+#define E2F_ATT_T(P, ONE)         \
+  if (a.bf16) {                   \
+    E2F_ATT(P, ONE, BF16);        \
+  } else {                        \
+    E2F_ATT(P, ONE, F32);         \
+  }
+#define E2F_ATT_P(P)        \
+  case P:                   \
+    if (sh.one) {           \
+      E2F_ATT_T(P, true)    \
+    } else {                \
+      E2F_ATT_T(P, false)   \
+    }                       \
+    break;
+#define E2F_ATT_SWITCH                                                                                   \
+  switch (sh.lpe) {                                                                                      \
+    E2F_ATT_P(1) E2F_ATT_P(2) E2F_ATT_P(4) E2F_ATT_P(8) E2F_ATT_P(16) E2F_ATT_P(32) E2F_ATT_P(64)        \
+    default: return hipErrorInvalidValue;                                                                \
+  }
+
 hipError_t launch_att_forward(const AttnArgs& a, float* alpha, float* lse, hipStream_t s) {
   if (a.n == 0) return hipSuccess;
-  const unsigned grid = (unsigned)((a.n + 3) / 4);
-  switch (head_slots(a.H)) {
-#define E2F_ATT(P)                                                           \
-  case P:                                                                    \
-    if (a.bf16)                                                              \
-      k_att_forward<P, unsigned short><<<grid, 256, 0, s>>>(a, alpha, lse);  \
-    else                                                                     \
-      k_att_forward<P, float><<<grid, 256, 0, s>>>(a, alpha, lse);           \
-    break;
-    E2F_ATT(1) E2F_ATT(2) E2F_ATT(4) E2F_ATT(8) E2F_ATT(16) E2F_ATT(32) E2F_ATT(64)
+  AttnShape sh = shape_of(a, false);
+  sh.lds = kKept * (sh.ld + 2) + 64 + 64 + 256;
+  const dim3 grid((unsigned)(sh.wpr == 1 ? (a.n + 3) / 4 : a.n), (unsigned)sh.groups);
+  const size_t lds = sizeof(float) * 4 * sh.lds;
+#define E2F_ATT(P, ONE, F) k_att_forward<P, ONE, F><<<grid, 256, lds, s>>>(a, sh, alpha, lse)
+  E2F_ATT_SWITCH
 #undef E2F_ATT
-    default: return hipErrorInvalidValue;
-  }
   return hipGetLastError();
 }
 
-hipError_t launch_att_backward(const AttnArgs& a, const AttnGrad& g, hipStream_t s) {
+hipError_t launch_att_backward(const AttnArgs& a, const AttnGrad& gr, hipStream_t s) {
   if (a.n == 0) {  // (the sum over no edges)
-    if (g.gw) k_att_radial_sum<<<(a.H * a.R + 255) / 256, 256, 0, s>>>(g.part, 0, a.H * a.R, g.gw);
+    if (gr.gw) k_att_radial_sum<<<(a.H * a.R + 63) / 64, 1024, 0, s>>>(gr.part, 0, a.H * a.R, gr.gw);
     return hipGetLastError();
   }
-  const unsigned grid = (unsigned)((a.n + 3) / 4);
-  switch (head_slots(a.H)) {
-#define E2F_ATT(P)                                                    \
-  case P:                                                             \
-    if (a.bf16)                                                       \
-      k_att_receivers<P, unsigned short><<<grid, 256, 0, s>>>(a, g);  \
-    else                                                              \
-      k_att_receivers<P, float><<<grid, 256, 0, s>>>(a, g);           \
-    break;
-    E2F_ATT(1) E2F_ATT(2) E2F_ATT(4) E2F_ATT(8) E2F_ATT(16) E2F_ATT(32) E2F_ATT(64)
+  AttnShape sh = shape_of(a, false);
+  AttnGrad g = gr;
+  g.groups = sh.groups;
+  const int parts = attention_parts(a, &sh.rows), vec = a.bf16 ? BF16::VEC : F32::VEC;
+  sh.dq = sh.one ? 0 : 64 / sh.lpe * sh.heads * sh.lph * vec;
+  sh.lds = 64 * sh.ld + 6 * 64 + 256 + sh.dq;
+  if (sh.lds < 512) sh.lds = 512;  // (dw's sum over the waves)
+  {
+    const dim3 grid((unsigned)parts, (unsigned)sh.groups);
+    const size_t lds = sizeof(float) * 4 * sh.lds;
+#define E2F_ATT(P, ONE, F) k_att_receivers<P, ONE, F><<<grid, 256, lds, s>>>(a, sh, g)
+    E2F_ATT_SWITCH
 #undef E2F_ATT
-    default: return hipErrorInvalidValue;
   }
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (g.gw) k_att_radial_sum<<<(a.H * a.R + 63) / 64, 1024, 0, s>>>(g.part, parts, a.H * a.R, g.gw);
   if (g.gk || g.gpos) {
-    if (a.bf16)
-      k_att_senders<unsigned short><<<grid, 256, 0, s>>>(a, g);
-    else
-      k_att_senders<float><<<grid, 256, 0, s>>>(a, g);
-  }
-  if (g.gw) {
-    k_att_radial<<<kAttnParts, 256, 0, s>>>(a, g);
-    k_att_radial_sum<<<(a.H * a.R + 255) / 256, 256, 0, s>>>(g.part, kAttnParts, a.H * a.R, g.gw);
+    sh = shape_of(a, true);
+    const dim3 grid((unsigned)(sh.wpr == 1 ? (a.n + 3) / 4 : a.n), (unsigned)(g.gk ? sh.groups : 1));
+#define E2F_SEND(P)                                          \
+  case P:                                                    \
+    if (a.bf16)                                              \
+      k_att_senders<P, BF16><<<grid, 256, 0, s>>>(a, sh, g); \
+    else                                                     \
+      k_att_senders<P, F32><<<grid, 256, 0, s>>>(a, sh, g);  \
+    break;
+    switch (sh.lpe) {
+      E2F_SEND(1) E2F_SEND(2) E2F_SEND(4) E2F_SEND(8) E2F_SEND(16) E2F_SEND(32) E2F_SEND(64)
+      default: return hipErrorInvalidValue;
+    }
+#undef E2F_SEND
   }
   return hipGetLastError();
 }
