@@ -216,9 +216,8 @@ struct AttnGrad {
 // How the kernels divide heads and rows: a head of k takes lph lanes (16 bytes of features each), an edge lpe lanes,
 // `units` times over; a workgroup up to `heads` heads of `kheads` heads of k; wpr waves a row
 struct AttnShape {
-  int lph, lpe, units, kheads, share, heads, groups, ld, hp, wpr, rows, lds, dq;
-  unsigned inv_heads;  // x / heads = x inv_heads >> 16
-  bool one;            // a lane has one head's features alone
+  int lph, lpe, units, kheads, share, heads, groups, hp, wpr, rows, lds, dq;
+  bool one;            // a lane has one head's features alone, 16 whole bytes of them
 };
 int attention_groups(const AttnArgs& a);
 int attention_parts(const AttnArgs& a, int* rows = nullptr);

@@ -114,14 +114,19 @@ __device__ __forceinline__ float tanh_near(float x) {
   const float a = fabsf(x), t = a * a;
   const float p = a + a * t * (-1.0f / 3 + t * (2.0f / 15 + t * (-17.0f / 315 + t * (62.0f / 2835 + t * (-1382.0f / 155925)))));
   const float e = exp_fast(-2.0f * a);
-  return copysignf(a < 0.35f ? p : (1.0f - e) / (1.0f + e), x);
+  return copysignf(a < 0.35f ? p : (1.0f - e) * __builtin_amdgcn_rcpf(1.0f + e), x);
 }
 
-__device__ __forceinline__ float envelope(float rc, float d) {
-  return d < rc ? 0.5f * (cosf(kPi / rc * d) + 1.0f) : 0.0f;
-}
-__device__ __forceinline__ float envelope_slope(float rc, float d) {
-  return d < rc ? -0.5f * kPi / rc * sinf(kPi / rc * d) : 0.0f;
+// (cos(pi x) + 1) / 2 = c^2 and its slope -pi s c for x = d / cutoff below 1, with c, s the cosine and sine of pi x / 2
+// by their series (the next terms are below 2^-26 there); 0 from 1 on
+__device__ __forceinline__ float envelope(float rc, float d, float* slope = nullptr) {
+  const float h = 0.5f * kPi * (d / rc), t = h * h;
+  const float c = 1.0f + t * (-0.5f + t * (1.0f / 24 + t * (-1.0f / 720 + t * (1.0f / 40320 + t * (-1.0f / 3628800 + t * (1.0f / 479001600))))));
+  if (slope) {
+    const float s = h * (1.0f + t * (-1.0f / 6 + t * (1.0f / 120 + t * (-1.0f / 5040 + t * (1.0f / 362880 + t * (-1.0f / 39916800))))));
+    *slope = d < rc ? -kPi / rc * s * c : 0.0f;
+  }
+  return d < rc ? c * c : 0.0f;
 }
 
 __device__ __forceinline__ int atom_of(const AttnArgs& a, int c) { return min(max(c, 0), a.n - 1); }
@@ -149,9 +154,19 @@ __device__ __forceinline__ Group group_of(const AttnArgs& a, const AttnShape& s,
   return g;
 }
 
-// x / heads for x < 4096, heads <= 16
-__device__ __forceinline__ int over_heads(const AttnShape& s, int heads, int x) {
-  return heads == s.heads ? (int)((unsigned)x * s.inv_heads >> 16) : x / heads;
+constexpr int kLd = 17;  // floats of an entry's scores in the LDS (up to 16 heads; odd: other banks)
+
+// Lanes over a group's heads (hp, their number's next power of two) and over 64 / hp entries: a head belongs to a lane
+struct Lanes {
+  int head, entry, per;
+  bool on;
+};
+__device__ __forceinline__ Lanes lanes_of(const AttnShape& s, const Group& g) {
+  const int lane = threadIdx.x & 63;
+  Lanes l;
+  l.head = lane & (s.hp - 1), l.entry = lane / s.hp, l.per = 64 / s.hp;
+  l.on = l.head < g.heads;
+  return l;
 }
 
 // How a wave goes through a row: stretches of 64 edges, of which it takes those of the receiver's graph
@@ -207,25 +222,34 @@ __device__ __forceinline__ int next_batch(const AttnArgs& a, Walk& w, int* stage
   return count;
 }
 
-// Features of a block of BE entries, LPE lanes an entry
+// Features of a block of BE entries, LPE lanes an entry, up to eight loads of a lane at a time (`part` of PARTS)
 template <int LPE, typename F>
 struct Features {
-  static constexpr int EPI = 64 / LPE, BE = EPI > 16 ? EPI : 16, IT = BE / EPI;
+  static constexpr int EPI = 64 / LPE, BE = EPI > 16 ? EPI : 16, ALL = BE / EPI, IT = ALL > 8 ? 8 : ALL, PARTS = ALL / IT;
   typename F::raw k[IT];
-  // from the atoms jj[entry] (-1: none, zeros), `count` of the lane's from base on
-  __device__ __forceinline__ void read(const typename F::type* base, int64_t ld, const int* jj, int count) {
-    const int slot = (threadIdx.x & 63) / LPE;
+  static __device__ __forceinline__ int entry(int part, int i) {
+    return (part * IT + i) * EPI + (threadIdx.x & 63) / LPE;
+  }
+  // of the atoms jj[entry], `count` of the lane's from base on; WHOLE: all or none of them
+  template <bool WHOLE>
+  __device__ __forceinline__ void read(const typename F::type* base, int64_t ld, const int* jj, int part, int count) {
+    if constexpr (WHOLE) {
 #pragma unroll
-    for (int i = 0; i < IT; ++i) {
-      const int j = jj[i * EPI + slot];
-      typename F::raw r = {};
-      if (j >= 0 && count > 0) r = F::load(base + j * ld, count);
-      k[i] = r;
+      for (int i = 0; i < IT; ++i) k[i] = F::load(base + jj[entry(part, i)] * ld, F::VEC);
+      if (count <= 0) {
+#pragma unroll
+        for (int i = 0; i < IT; ++i) k[i] = typename F::raw{};
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < IT; ++i) {
+        k[i] = typename F::raw{};
+        if (count > 0) k[i] = F::load(base + jj[entry(part, i)] * ld, count);
+      }
     }
   }
-  // s[entry * ld] = the sum over a head's lph lanes of q . k, by its first lane
-  __device__ __forceinline__ void dots(const float (&q)[F::VEC], int lph, bool first, float* s, int ld) {
-    const int slot = (threadIdx.x & 63) / LPE;
+  // s[entry * kLd] = the sum over a head's lph lanes of q . k, by its first lane
+  __device__ __forceinline__ void dots(const float (&q)[F::VEC], int lph, bool first, float* s, int part) {
     float x[IT];
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
@@ -245,15 +269,14 @@ struct Features {
     if (LPE > 32 && lph > 32) add([](float v) { float p, q; lane_halves<32>(v, p, q); return p + q; });
     if (first) {
 #pragma unroll
-      for (int i = 0; i < IT; ++i) s[(i * EPI + slot) * ld] = x[i];
+      for (int i = 0; i < IT; ++i) s[entry(part, i) * kLd] = x[i];
     }
   }
-  // acc += sum over the lane's entries of w[entry * ld] k
-  __device__ __forceinline__ void add_weighted(const float* w, int ld, float (&acc)[F::VEC]) {
-    const int slot = (threadIdx.x & 63) / LPE;
+  // acc += sum over the lane's entries of w[entry * kLd] k
+  __device__ __forceinline__ void add_weighted(const float* w, int part, float (&acc)[F::VEC]) {
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      const float c = w[(i * EPI + slot) * ld];
+      const float c = w[entry(part, i) * kLd];
 #pragma unroll
       for (int u = 0; u < F::VEC; ++u) acc[u] += c * F::at(k[i], u);
     }
@@ -274,7 +297,8 @@ __device__ __forceinline__ Place place_of(const AttnArgs& a, const AttnShape& sh
 }
 template <typename F>
 __device__ __forceinline__ const typename F::type* k_at(const AttnArgs& a, const Group& g, const Place& p) {
-  return (const typename F::type*)a.k + (g.k0 + p.kl) * a.dk + p.t * F::VEC;
+  // (lanes without features read the group's first ones, where they read)
+  return (const typename F::type*)a.k + (p.count > 0 ? (g.k0 + p.kl) * a.dk + p.t * F::VEC : g.k0 * a.dk);
 }
 template <typename F>
 __device__ __forceinline__ void read_q(const AttnArgs& a, int64_t i, int h, const Place& p, float (&q)[F::VEC]) {
@@ -284,24 +308,49 @@ __device__ __forceinline__ void read_q(const AttnArgs& a, int64_t i, int h, cons
   for (int u = 0; u < F::VEC; ++u) q[u] = a.scale * F::at(r, u);
 }
 
-// The products scale q . k of a block's entries with every head of the group: s[entry * ld + head].  ONE: a lane has
-// one head (q1 its features, k kept in f); else `units` times 64 lanes for k, and `share` heads each.
+// The products scale q . k of a block's entries with every head of the group: s[entry * kLd + head].  ONE: a lane has
+// one head (q1 its features), all or none of a load's features; else `units` times 64 lanes for k, and `share` heads each.  k is left in f where f
+// holds all of it.
 template <int LPE, bool ONE, typename F>
 __device__ __forceinline__ void products(const AttnArgs& a, const AttnShape& sh, const Group& g, int64_t i,
                                          const float (&q1)[F::VEC], Features<LPE, F>& f, const int* jj, float* s) {
-  if constexpr (ONE) {
-    const Place p = place_of<LPE, F>(a, sh, g, 0);
-    f.read(k_at<F>(a, g, p), a.ldk, jj, p.count);
-    f.dots(q1, sh.lph, p.t == 0 && p.kl < g.kheads, s + p.kl, sh.ld);
-  } else {
-    for (int u = 0; u < sh.units; ++u) {
-      const Place p = place_of<LPE, F>(a, sh, g, u);
-      f.read(k_at<F>(a, g, p), a.ldk, jj, p.count);
-      for (int m = 0; m < g.share; ++m) {
-        float q[F::VEC];
-        read_q<F>(a, i, g.h0 + p.kl * g.share + m, p, q);
-        f.dots(q, sh.lph, p.t == 0 && p.kl < g.kheads, s + p.kl * g.share + m, sh.ld);
+  for (int u = 0; u < (ONE ? 1 : sh.units); ++u) {
+    const Place p = place_of<LPE, F>(a, sh, g, u);
+    const auto* k = k_at<F>(a, g, p);
+#pragma unroll
+    for (int part = 0; part < f.PARTS; ++part) {
+      f.template read<ONE>(k, a.ldk, jj, part, p.count);
+      if constexpr (ONE) {
+        f.dots(q1, sh.lph, p.t == 0 && p.kl < g.kheads, s + p.kl, part);
+      } else {
+        for (int m = 0; m < g.share; ++m) {
+          float q[F::VEC];
+          read_q<F>(a, i, g.h0 + p.kl * g.share + m, p, q);
+          f.dots(q, sh.lph, p.t == 0 && p.kl < g.kheads, s + p.kl * g.share + m, part);
+        }
       }
+    }
+  }
+}
+
+// s[entry * kLd + head] of 16 entries gets its radial part (is set to it without products): the functions' values times
+// the weights wr of the lane's head (the functions 4 r + quad)
+__device__ __forceinline__ void add_radial(const AttnArgs& a, const AttnShape& sh, const Group& g, const float* dist,
+                                           const float (&wr)[8], float inv, float* s) {
+  const int lane = threadIdx.x & 63, hc = lane & 15, quad = lane >> 4;
+  f4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+  const float z0 = dist[hc] * inv - (float)quad;
+#pragma unroll
+  for (int r = 0; r < 8; ++r)
+    if (4 * r < a.R) {
+      const float z = z0 - 4.0f * r;
+      x = __builtin_amdgcn_mfma_f32_16x16x4f32(exp_fast(-z * z), wr[r], x, 0, 0, 0);
+    }
+  if (hc < g.heads) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      float* to = s + (quad * 4 + u) * kLd + hc;
+      *to = a.dk ? *to + x[u] : x[u];
     }
   }
 }
@@ -309,15 +358,16 @@ __device__ __forceinline__ void products(const AttnArgs& a, const AttnShape& sh,
 constexpr int kKept = 128;  // edges of a row whose scores stay in the LDS
 
 template <int LPE, bool ONE, typename F>
-__global__ __launch_bounds__(256) void k_att_forward(AttnArgs a, AttnShape sh, float* alpha, float* lse) {
+__global__ __launch_bounds__(256, 4) void k_att_forward(AttnArgs a, AttnShape sh, float* alpha, float* lse) {
   extern __shared__ float sm[];
   __shared__ float join[4][2][16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // (a scalar)
   const Group g = group_of(a, sh, blockIdx.y);
+  const Lanes ln = lanes_of(sh, g);
   const int64_t i = sh.wpr == 1 ? row_block() * 4 + wave : row_block();
   const bool row = i < a.n;  // (with four waves a row the same for the workgroup)
   float* s = sm + wave * sh.lds;
-  float* env = s + kKept * sh.ld;
+  float* env = s + kKept * kLd;
   int* edge = (int*)(env + kKept);
   float* dist = (float*)(edge + kKept);
   int* jj = (int*)(dist + 64);
@@ -328,11 +378,12 @@ __global__ __launch_bounds__(256) void k_att_forward(AttnArgs a, AttnShape sh, f
   const int64_t step = 64 * (int64_t)sh.wpr;
   Walk w{e1, e0 + 64 * part, step, 0, a.gid && row ? a.gid[i] : 0};
   const float inv = (float)(a.R - 1) / a.rc, icap = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
-  const int hc = lane & 15, quad = lane >> 4;
-  const bool hv = hc < g.heads;
-  float wr[8];  // of the lane's head, the functions 4 r + quad
+  float wr[8];
 #pragma unroll
-  for (int r = 0; r < 8; ++r) wr[r] = hv && 4 * r + quad < a.R ? a.w[(g.h0 + hc) * a.R + 4 * r + quad] : 0.0f;
+  for (int r = 0; r < 8; ++r) {
+    const int f = 4 * r + (lane >> 4), h = lane & 15;
+    wr[r] = h < g.heads && f < a.R ? a.w[(g.h0 + h) * a.R + f] : 0.0f;
+  }
   float q1[F::VEC] = {};
   if (ONE && a.dk && row) {
     const Place p = place_of<LPE, F>(a, sh, g, 0);
@@ -344,20 +395,17 @@ __global__ __launch_bounds__(256) void k_att_forward(AttnArgs a, AttnShape sh, f
   int kept = 0;        // edges whose scores are in the LDS
   bool spill = false;  // the scores of the row are in alpha
   auto to_alpha = [&](int count, const float* from) {
-    for (int x = lane; x < count * g.heads; x += 64) {
-      const int at = over_heads(sh, g.heads, x), h = x - at * g.heads;
-      alpha[(e0 + edge[at]) * a.H + g.h0 + h] = from[at * sh.ld + h];
-    }
+    if (ln.on)
+      for (int n = ln.entry; n < count; n += ln.per)
+        alpha[(e0 + edge[n]) * a.H + g.h0 + ln.head] = from[n * kLd + ln.head];
   };
   for (;;) {
     int64_t e;
     int j;
     const int count = next_batch(a, w, stage, e0, e, j, [&](int64_t first, int many, uint64_t mask) {
-      if (!mask) return;
-      for (int x = lane; x < many * g.heads; x += 64) {
-        const int at = over_heads(sh, g.heads, x);
-        if (mask >> at & 1) alpha[(first + at) * a.H + g.h0 + x - at * g.heads] = 0.0f;
-      }
+      if (!mask || !ln.on) return;
+      for (int n = ln.entry; n < many; n += ln.per)
+        if (mask >> n & 1) alpha[(first + n) * a.H + g.h0 + ln.head] = 0.0f;
     });
     if (count == 0) break;
     if (kept == kKept) {  // (every batch but the last has 64)
@@ -365,45 +413,45 @@ __global__ __launch_bounds__(256) void k_att_forward(AttnArgs a, AttnShape sh, f
       kept = 0, spill = true;
       wave_sync();
     }
-    float* sb = s + kept * sh.ld;
+    float* sb = s + kept * kLd;
     const bool there = j >= 0;
     float dx = 0.0f, dy = 0.0f, dz = 0.0f;
     if (there) dx = px - a.pos[3 * (int64_t)j], dy = py - a.pos[3 * (int64_t)j + 1], dz = pz - a.pos[3 * (int64_t)j + 2];
-    jj[lane] = j;
+    const int j0 = __builtin_amdgcn_readfirstlane(j);  // (by every lane: lane 0 has the batch's first edge)
+    jj[lane] = there ? j : j0;                          // the first sender once more behind the last
     wave_sync();
     if (a.dk) {
       Features<LPE, F> f;
-      for (int b = 0; b < count; b += f.BE) products<LPE, ONE, F>(a, sh, g, i, q1, f, jj + b, sb + b * sh.ld);
+      for (int b = 0; b < count; b += f.BE) products<LPE, ONE, F>(a, sh, g, i, q1, f, jj + b, sb + b * kLd);
     }
     const float d = sqrtf(dx * dx + dy * dy + dz * dz);
     dist[lane] = d;
     env[kept + lane] = envelope(a.rc, d);
     edge[kept + lane] = (int)(e - e0);
     wave_sync();
-    for (int b = 0; b < count; b += 16) {
-      f4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-      const float z0 = dist[b + hc] * inv - (float)quad;
+    if (a.R)
+      for (int b = 0; b < count; b += 16) add_radial(a, sh, g, dist + b, wr, inv, sb + b * kLd);
+    wave_sync();
+    // the scores, and the running maximum and sum, four entries at a time
+    if (ln.on)
+      for (int n0 = ln.entry; n0 < count; n0 += 4 * ln.per) {
+        float x[4], mx = m;
 #pragma unroll
-      for (int r = 0; r < 8; ++r)
-        if (4 * r < a.R) {
-          const float z = z0 - 4.0f * r;
-          x = __builtin_amdgcn_mfma_f32_16x16x4f32(exp_fast(-z * z), wr[r], x, 0, 0, 0);
+        for (int u = 0; u < 4; ++u) {
+          const int n = n0 + u * ln.per;
+          x[u] = -INFINITY;
+          if (n < count) {
+            x[u] = a.dk || a.R ? sb[n * kLd + ln.head] : 0.0f;
+            if (a.cap > 0.0f) x[u] = a.cap * tanh_near(x[u] * icap);
+            sb[n * kLd + ln.head] = x[u];
+          }
+          mx = fmaxf(mx, x[u]);
         }
-      float mx = m;
+        if (mx > m) den *= exp_fast(m - mx), m = mx;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int n = b + quad * 4 + u;
-        if (a.dk && hv) x[u] += sb[n * sh.ld + hc];
-        if (a.cap > 0.0f) x[u] = a.cap * tanh_near(x[u] * icap);
-        if (n >= count) x[u] = -INFINITY;
-        mx = fmaxf(mx, x[u]);
-        if (hv) sb[n * sh.ld + hc] = x[u];
+        for (int u = 0; u < 4; ++u)
+          if (n0 + u * ln.per < count) den += exp_fast(x[u] - m);
       }
-      if (mx > m) den *= exp_fast(m - mx), m = mx;
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (b + quad * 4 + u < count) den += exp_fast(x[u] - m);
-    }
     wave_sync();
     if (spill)
       to_alpha(count, s);
@@ -412,29 +460,25 @@ __global__ __launch_bounds__(256) void k_att_forward(AttnArgs a, AttnShape sh, f
     wave_sync();
   }
   // the row's sum, over the lanes and waves of a head
-  const float top_w = classes_all(m, 16, [](float p, float q) { return fmaxf(p, q); });
-  float top = top_w;
-  den = classes_all(m == top ? den : den * exp_fast(m - top), 16, [](float p, float q) { return p + q; });
+  float top = classes_all(m, sh.hp, [](float p, float q) { return fmaxf(p, q); });
+  den = classes_all(m == top ? den : den * exp_fast(m - top), sh.hp, [](float p, float q) { return p + q; });
   if (sh.wpr > 1) {
-    if (lane < 16) join[wave][0][lane] = top, join[wave][1][lane] = den;
+    if (lane < sh.hp) join[wave][0][lane] = top, join[wave][1][lane] = den;
     __syncthreads();
-    for (int k = 0; k < 4; ++k) top = fmaxf(top, join[k][0][hc]);
+    for (int k = 0; k < 4; ++k) top = fmaxf(top, join[k][0][ln.head]);
     den = 0.0f;
     for (int k = 0; k < 4; ++k) {
-      const float mk = join[k][0][hc], dk = join[k][1][hc];
+      const float mk = join[k][0][ln.head], dk = join[k][1][ln.head];
       den += mk == top ? dk : dk * exp_fast(mk - top);
     }
   }
   if (!row) return;
   const float l = top + logf(den);
-  if (lse && hv && quad == 0 && part == 0) lse[i * a.H + g.h0 + hc] = l;
-  if (lane < 16) dist[lane] = l;
-  wave_sync();
+  if (lse && ln.on && ln.entry == 0 && part == 0) lse[i * a.H + g.h0 + ln.head] = l;
   if (!spill) {
-    for (int x = lane; x < kept * g.heads; x += 64) {
-      const int at = over_heads(sh, g.heads, x), h = x - at * g.heads;
-      alpha[(e0 + edge[at]) * a.H + g.h0 + h] = env[at] * exp_fast(s[at * sh.ld + h] - dist[h]);
-    }
+    if (ln.on)
+      for (int n = ln.entry; n < kept; n += ln.per)
+        alpha[(e0 + edge[n]) * a.H + g.h0 + ln.head] = env[n] * exp_fast(s[n * kLd + ln.head] - l);
     return;
   }
   for (int64_t c = e0 + 64 * part; c < e1; c += step) {
@@ -449,12 +493,12 @@ __global__ __launch_bounds__(256) void k_att_forward(AttnArgs a, AttnShape sh, f
     }
     env[lane] = v;
     wave_sync();
-    for (int x = lane; x < count * g.heads; x += 64) {
-      const int at = over_heads(sh, g.heads, x), h = x - at * g.heads;
-      if (env[at] < 0.0f) continue;
-      float* to = alpha + (c + at) * a.H + g.h0 + h;
-      *to = env[at] * exp_fast(*to - dist[h]);
-    }
+    if (ln.on)
+      for (int n = ln.entry; n < count; n += ln.per) {
+        if (env[n] < 0.0f) continue;
+        float* to = alpha + (c + n) * a.H + g.h0 + ln.head;
+        *to = env[n] * exp_fast(*to - l);
+      }
     wave_sync();
   }
 }
@@ -462,25 +506,25 @@ __global__ __launch_bounds__(256) void k_att_forward(AttnArgs a, AttnShape sh, f
 // ds of every edge and head, the edge's position gradient, and the receivers' gradients.  A workgroup takes sh.rows
 // rows and sums dw over them.
 template <int LPE, bool ONE, typename F>
-__global__ __launch_bounds__(256) void k_att_receivers(AttnArgs a, AttnShape sh, AttnGrad gr) {
+__global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape sh, AttnGrad gr) {
   extern __shared__ float sm[];
   __shared__ float join[4][16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // (a scalar)
   const Group g = group_of(a, sh, blockIdx.y);
-  float* s = sm + wave * sh.lds;  // [64][ld] scores, then ds
-  float* dist = s + 64 * sh.ld;
+  const Lanes ln = lanes_of(sh, g);
+  float* s = sm + wave * sh.lds;  // [64][kLd] scores, then ds
+  float* dist = s + 64 * kLd;
   float* env = dist + 64;
   float* slope = env + 64;
   int* edge = (int*)(slope + 64);
   int* jj = edge + 64;
-  float* slot_sum = (float*)(jj + 64);  // [64] position gradients over distances
-  int* stage = (int*)(slot_sum + 64);
+  float* force = (float*)(jj + 64);  // [64] d loss / d distance
+  int* stage = (int*)(force + 64);
   const float inv = (float)(a.R - 1) / a.rc, icap = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
   const int hc = lane & 15, quad = lane >> 4;
-  const bool hv = hc < g.heads;
   float wr[8], wt[2][4];  // weights: of the lane's head, functions 4 r + quad; of the functions 16 r + hc, heads 4 k + quad
 #pragma unroll
-  for (int r = 0; r < 8; ++r) wr[r] = hv && 4 * r + quad < a.R ? a.w[(g.h0 + hc) * a.R + 4 * r + quad] : 0.0f;
+  for (int r = 0; r < 8; ++r) wr[r] = hc < g.heads && 4 * r + quad < a.R ? a.w[(g.h0 + hc) * a.R + 4 * r + quad] : 0.0f;
 #pragma unroll
   for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -496,25 +540,31 @@ __global__ __launch_bounds__(256) void k_att_receivers(AttnArgs a, AttnShape sh,
     const int64_t e1 = row ? min(max(a.row_ptr[i + 1], e0), a.E) : 0;
     const int64_t step = 64 * (int64_t)sh.wpr;
     Walk w{e1, e0 + 64 * part, step, 0, a.gid && row ? a.gid[i] : 0};
-    // D of the lane's head: lanes over a power of two of heads and over edges
     float D = 0.0f;
     {
-      const int hd = lane & (sh.hp - 1), per = 64 / sh.hp;
-      const bool on = hd < g.heads;
-      for (int64_t e = e0 + lane / sh.hp + part * per; e < e1; e += per * sh.wpr)
-        if (on && (!a.gid || a.gid[atom_of(a, a.col[e])] == w.gid))
-          D += gr.alpha[e * a.H + g.h0 + hd] * gr.galpha[e * a.H + g.h0 + hd];
+      const int64_t stride = ln.per * sh.wpr;
+      const float *al = gr.alpha + g.h0 + ln.head, *ga = gr.galpha + g.h0 + ln.head;
+      for (int64_t e = e0 + ln.entry + part * ln.per; ln.on && e < e1; e += 4 * stride) {
+        float x[4], y[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int64_t at = min(e + u * stride, e1 - 1);
+          x[u] = al[at * a.H], y[u] = ga[at * a.H];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (e + u * stride < e1 && (!a.gid || a.gid[atom_of(a, a.col[e + u * stride])] == w.gid)) D += x[u] * y[u];
+      }
       D = classes_all(D, sh.hp, [](float p, float q) { return p + q; });
       if (sh.wpr > 1) {
         __syncthreads();  // (the row before has been read)
-        if (lane < 16) join[wave][lane] = D;
+        if (lane < sh.hp) join[wave][lane] = D;
         __syncthreads();
-        D = join[0][lane & 15] + join[1][lane & 15] + join[2][lane & 15] + join[3][lane & 15];
+        D = join[0][ln.head] + join[1][ln.head] + join[2][ln.head] + join[3][ln.head];
       }
-      D = __shfl(D, hc & (sh.hp - 1));
     }
     if (!row) continue;  // (with four waves a row, for the workgroup)
-    const float l = hv ? gr.lse[i * a.H + g.h0 + hc] : 0.0f;
+    const float l = ln.on ? gr.lse[i * a.H + g.h0 + ln.head] : 0.0f;
     float q1[F::VEC] = {}, dq[F::VEC] = {};
     if (ONE && a.dk) {
       const Place p = place_of<LPE, F>(a, sh, g, 0);
@@ -532,103 +582,122 @@ __global__ __launch_bounds__(256) void k_att_receivers(AttnArgs a, AttnShape sh,
       if (count == 0) break;
       float dx = 0.0f, dy = 0.0f, dz = 0.0f;
       if (j >= 0) dx = px - a.pos[3 * (int64_t)j], dy = py - a.pos[3 * (int64_t)j + 1], dz = pz - a.pos[3 * (int64_t)j + 2];
-      jj[lane] = j;
+      const int j0 = __builtin_amdgcn_readfirstlane(j);  // (by every lane: lane 0 has the batch's first edge)
+      jj[lane] = j >= 0 ? j : j0;                         // the first sender once more behind the last
       edge[lane] = (int)(e - e0);
       const float d = sqrtf(dx * dx + dy * dy + dz * dz);
-      dist[lane] = d, env[lane] = envelope(a.rc, d), slope[lane] = envelope_slope(a.rc, d);
+      float sl;
+      env[lane] = envelope(a.rc, d, &sl);
+      dist[lane] = d, slope[lane] = sl;
       wave_sync();
       Features<LPE, F> f;
       for (int b0 = 0; b0 < count; b0 += f.BE) {
-        if (a.dk) products<LPE, ONE, F>(a, sh, g, i, q1, f, jj + b0, s + b0 * sh.ld);
+        float* sb = s + b0 * kLd;
+        const int many = min(count - b0, f.BE);  // of the block's entries
+        float ga[4];
+        auto read_ga = [&](int c) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int n = c + ln.entry + u * ln.per;
+            ga[u] = ln.on && n < many ? gr.galpha[(e0 + edge[b0 + n]) * a.H + g.h0 + ln.head] : 0.0f;
+          }
+        };
+        read_ga(0);
+        if (a.dk) products<LPE, ONE, F>(a, sh, g, i, q1, f, jj + b0, sb);
         wave_sync();
-        for (int b = b0; b < min(count, b0 + f.BE); b += 16) {
-          float ga[4];
+        if (a.R)
+          for (int b = 0; b < many; b += 16) add_radial(a, sh, g, dist + b0 + b, wr, inv, sb + b * kLd);
+        wave_sync();
+        // ds, and the envelope's part of the distances' gradients, four entries at a time
+        for (int c = 0; c < f.BE; c += 4 * ln.per) {
+          if (c > 0) read_ga(c);
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
-            const int n = b + quad * 4 + u;
-            ga[u] = hv && n < count ? gr.galpha[(e0 + edge[n]) * a.H + g.h0 + hc] : 0.0f;
-          }
-          f4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-          const float z0 = dist[b + hc] * inv - (float)quad;
-#pragma unroll
-          for (int r = 0; r < 8; ++r)
-            if (4 * r < a.R) {
-              const float z = z0 - 4.0f * r;
-              x = __builtin_amdgcn_mfma_f32_16x16x4f32(exp_fast(-z * z), wr[r], x, 0, 0, 0);
+            const int n = c + ln.entry + u * ln.per;
+            if (c + u * ln.per >= f.BE) break;  // (the same for the wave)
+            float x = 0.0f, turn = 1.0f, ds = 0.0f, dd = 0.0f;
+            if (ln.on && n < f.BE) {
+              if (n < many) {
+                if (a.dk || a.R) x = sb[n * kLd + ln.head];
+                if (a.cap > 0.0f) {
+                  const float t = tanh_near(x * icap);
+                  x = a.cap * t;
+                  turn = 1.0f - t * t;
+                }
+                const float p = exp_fast(x - l);
+                ds = p * (ga[u] * env[b0 + n] - D) * turn;
+                dd = ga[u] * p * slope[b0 + n];
+                if (gr.gk) gr.ds[(e0 + edge[b0 + n]) * a.H + g.h0 + ln.head] = ds;
+              }
+              sb[n * kLd + ln.head] = ds;
             }
-          float ds[4], dd[4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int n = b + quad * 4 + u;
-            const bool on = hv && n < count;
-            if (a.dk && hv) x[u] += s[n * sh.ld + hc];
-            float turn = 1.0f;
-            if (a.cap > 0.0f) {
-              const float t = tanh_near(x[u] * icap);
-              x[u] = a.cap * t;
-              turn = 1.0f - t * t;
+            if (gr.gpos) {
+              dd = lanes_sum(dd, sh.hp);
+              if (ln.head == 0 && n < f.BE) force[b0 + n] = dd;
             }
-            const float p = exp_fast(x[u] - l);
-            ds[u] = on ? p * (ga[u] * env[n] - D) * turn : 0.0f;
-            dd[u] = on ? ga[u] * p * slope[n] : 0.0f;
-            if (hv) s[n * sh.ld + hc] = ds[u];
-            if (on && gr.gk) gr.ds[(e0 + edge[n]) * a.H + g.h0 + hc] = ds[u];
           }
-          wave_sync();
-          if (a.R && (gr.gw || gr.gpos)) {
+        }
+        wave_sync();
+        if (a.R && (gr.gw || gr.gpos))
+          for (int b = 0; b < many; b += 16) {
+            float dd[4] = {};
 #pragma unroll
             for (int r = 0; r < 2; ++r)
               if (16 * r < a.R) {
-                // u[edge][function] = sum of ds w over the heads
+                // us[edge][function] = the sum of ds w over the heads
                 f4 us = {0.0f, 0.0f, 0.0f, 0.0f};
                 if (gr.gpos) {
 #pragma unroll
                   for (int k = 0; k < 4; ++k)
                     if (4 * k < g.heads)
                       us = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                          4 * k + quad < g.heads ? s[(b + hc) * sh.ld + 4 * k + quad] : 0.0f, wt[r][k], us, 0, 0, 0);
+                          4 * k + quad < g.heads ? sb[(b + hc) * kLd + 4 * k + quad] : 0.0f, wt[r][k], us, 0, 0, 0);
                 }
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                  const float z = dist[b + quad * 4 + u] * inv - (float)(16 * r + hc), gz = exp_fast(-z * z);
-                  dd[u] += us[u] * gz * z * (-2.0f * inv);
-                  dw[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(gz, ds[u], dw[r], 0, 0, 0);
+                  const int n = b + quad * 4 + u;
+                  const float z = dist[b0 + n] * inv - (float)(16 * r + hc), gz = exp_fast(-z * z);
+                  dd[u] += us[u] * gz * z;
+                  dw[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(gz, hc < g.heads ? sb[n * kLd + hc] : 0.0f, dw[r], 0, 0, 0);
                 }
               }
-          }
-          if (gr.gpos) {
+            if (gr.gpos) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const float v = lanes_sum(dd[u], 16);
-              if (hc == u) slot_sum[b + quad * 4 + u] = v;
+              for (int u = 0; u < 4; ++u) {
+                const float v = lanes_sum(dd[u], 16);
+                if (hc == u) force[b0 + b + quad * 4 + u] -= 2.0f * inv * v;
+              }
             }
           }
-        }
-        if constexpr (ONE) {
-          if (a.dk && gr.gq) {
-            const Place p = place_of<LPE, F>(a, sh, g, 0);
-            if (p.kl < g.kheads) f.add_weighted(s + b0 * sh.ld + p.kl, sh.ld, dq);
-          }
-        } else if (a.dk && gr.gq) {
-          // k read again, a head's sum at a time, added to those of the wave in the LDS
-          float* acc = (float*)(stage + 256);
-          for (int u = 0; u < sh.units; ++u) {
+        if (a.dk && gr.gq) {
+          // k is read again where f does not hold all of it, a head's sum at a time, added to those of the wave in
+          // the LDS where a lane has several
+          [[maybe_unused]] float* acc = (float*)(stage + 256);
+          for (int u = 0; u < (ONE ? 1 : sh.units); ++u) {
             const Place p = place_of<LPE, F>(a, sh, g, u);
-            f.read(k_at<F>(a, g, p), a.ldk, jj + b0, p.count);
-            if (p.count <= 0) continue;
-            for (int mm = 0; mm < g.share; ++mm) {
-              float v[F::VEC] = {};
-              f.add_weighted(s + b0 * sh.ld + p.kl * g.share + mm, sh.ld, v);
-              float* to = acc + ((lane / LPE * g.heads + p.kl * g.share + mm) * sh.lph + p.t) * F::VEC;
+            const auto* k = k_at<F>(a, g, p);
 #pragma unroll
-              for (int x = 0; x < F::VEC; ++x) to[x] += v[x];
+            for (int y = 0; y < f.PARTS; ++y) {
+              if (!ONE || f.PARTS > 1) f.template read<ONE>(k, a.ldk, jj + b0, y, p.count);
+              if (p.kl >= g.kheads) continue;
+              if constexpr (ONE) {
+                f.add_weighted(sb + p.kl, y, dq);
+              } else {
+                for (int mm = 0; mm < g.share; ++mm) {
+                  float v[F::VEC] = {};
+                  f.add_weighted(sb + p.kl * g.share + mm, y, v);
+                  float* to = acc + ((lane / LPE * g.heads + p.kl * g.share + mm) * sh.lph + p.t) * F::VEC;
+#pragma unroll
+                  for (int x = 0; x < F::VEC; ++x) to[x] += v[x];
+                }
+              }
             }
           }
         }
         wave_sync();
       }
       if (gr.gpos && lane < count) {
-        const float v = d > 0.0f ? slot_sum[lane] / d : 0.0f;
+        const float v = d > 0.0f ? force[lane] / d : 0.0f;
         *(f4*)(gr.edge + ((int64_t)blockIdx.y * a.E + e) * 4) = (f4){v * dx, v * dy, v * dz, 0.0f};
       }
       wave_sync();
@@ -695,18 +764,20 @@ __global__ __launch_bounds__(256) void k_att_receivers(AttnArgs a, AttnShape sh,
   }
 }
 
-// dw: the sum of the workgroups', 64 columns a workgroup
+// dw: the sum of the workgroups', 16 columns a workgroup
 __global__ __launch_bounds__(1024) void k_att_radial_sum(const float* __restrict__ part, int parts, int count,
                                                          float* __restrict__ gw) {
-  __shared__ double red[16][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
+  __shared__ double red[64][16];
+  const int x = threadIdx.x & 15, c = blockIdx.x * 16 + x, w = threadIdx.x >> 4;
   double v = 0.0;
-  if (c < count)
-    for (int b = w; b < parts; b += 16) v += part[(int64_t)b * count + c];
-  red[w][threadIdx.x & 63] = v;
+  if (c < count) {
+#pragma unroll 8
+    for (int b = w; b < parts; b += 64) v += part[(int64_t)b * count + c];
+  }
+  red[w][x] = v;
   __syncthreads();
   if (w || c >= count) return;
-  for (int k = 1; k < 16; ++k) v += red[k][threadIdx.x];
+  for (int k = 1; k < 64; ++k) v += red[k][x];
   gw[c] = (float)v;
 }
 
@@ -717,7 +788,7 @@ __global__ __launch_bounds__(256) void k_att_senders(AttnArgs a, AttnShape sh, A
   constexpr int EPI = 64 / LPE;
   __shared__ int stage[4][2][64];
   __shared__ float join[4][64 * F::VEC];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // (a scalar)
   const int64_t j = sh.wpr == 1 ? row_block() * 4 + wave : row_block();
   const bool row = j < a.n;
   const int part = sh.wpr == 1 ? 0 : wave;
@@ -828,7 +899,7 @@ constexpr int kScanSpan = 4096;
 __global__ __launch_bounds__(1024) void k_t_scan(const int32_t* __restrict__ cnt, int n, int64_t* __restrict__ rowT,
                                                  int64_t* __restrict__ sums) {
   const int64_t at = (int64_t)blockIdx.x * kScanSpan + threadIdx.x * 4;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // (a scalar)
   int v[4];
   for (int u = 0; u < 4; ++u) v[u] = at + u < n ? cnt[at + u] : 0;
   const int own = v[0] + v[1] + v[2] + v[3];
@@ -918,11 +989,9 @@ AttnShape shape_of(const AttnArgs& a, bool senders) {
   s.lpe = std::min(p * s.lph, 64);
   s.groups = s.share < share ? a.Hk * ((share + s.share - 1) / s.share) : (a.Hk + s.kheads - 1) / s.kheads;
   s.heads = s.kheads * s.share;
-  s.inv_heads = (65536 + s.heads - 1) / s.heads;
-  s.ld = s.heads | 1;
   s.hp = 1;
   while (s.hp < s.heads) s.hp <<= 1;
-  s.one = s.units == 1 && (share == 1 || a.dk == 0);
+  s.one = s.units == 1 && (share == 1 || a.dk == 0) && a.dk % vec == 0;
   // four waves a row where they find four batches on average
   s.wpr = a.E / a.n >= 256 ? 4 : 1;
   s.rows = 1;
@@ -965,7 +1034,7 @@ int attention_parts(const AttnArgs& a, int* rows) {
 hipError_t launch_att_forward(const AttnArgs& a, float* alpha, float* lse, hipStream_t s) {
   if (a.n == 0) return hipSuccess;
   AttnShape sh = shape_of(a, false);
-  sh.lds = kKept * (sh.ld + 2) + 64 + 64 + 256;
+  sh.lds = kKept * (kLd + 2) + 64 + 64 + 256;
   const dim3 grid((unsigned)(sh.wpr == 1 ? (a.n + 3) / 4 : a.n), (unsigned)sh.groups);
   const size_t lds = sizeof(float) * 4 * sh.lds;
 #define E2F_ATT(P, ONE, F) k_att_forward<P, ONE, F><<<grid, 256, lds, s>>>(a, sh, alpha, lse)
@@ -976,7 +1045,7 @@ hipError_t launch_att_forward(const AttnArgs& a, float* alpha, float* lse, hipSt
 
 hipError_t launch_att_backward(const AttnArgs& a, const AttnGrad& gr, hipStream_t s) {
   if (a.n == 0) {  // (the sum over no edges)
-    if (gr.gw) k_att_radial_sum<<<(a.H * a.R + 63) / 64, 1024, 0, s>>>(gr.part, 0, a.H * a.R, gr.gw);
+    if (gr.gw) k_att_radial_sum<<<(a.H * a.R + 15) / 16, 1024, 0, s>>>(gr.part, 0, a.H * a.R, gr.gw);
     return hipGetLastError();
   }
   AttnShape sh = shape_of(a, false);
@@ -984,7 +1053,7 @@ hipError_t launch_att_backward(const AttnArgs& a, const AttnGrad& gr, hipStream_
   g.groups = sh.groups;
   const int parts = attention_parts(a, &sh.rows), vec = a.bf16 ? BF16::VEC : F32::VEC;
   sh.dq = sh.one ? 0 : 64 / sh.lpe * sh.heads * sh.lph * vec;
-  sh.lds = 64 * sh.ld + 6 * 64 + 256 + sh.dq;
+  sh.lds = 64 * kLd + 6 * 64 + 256 + sh.dq;
   if (sh.lds < 512) sh.lds = 512;  // (dw's sum over the waves)
   {
     const dim3 grid((unsigned)parts, (unsigned)sh.groups);
@@ -994,7 +1063,7 @@ hipError_t launch_att_backward(const AttnArgs& a, const AttnGrad& gr, hipStream_
 #undef E2F_ATT
   }
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  if (g.gw) k_att_radial_sum<<<(a.H * a.R + 63) / 64, 1024, 0, s>>>(g.part, parts, a.H * a.R, g.gw);
+  if (g.gw) k_att_radial_sum<<<(a.H * a.R + 15) / 16, 1024, 0, s>>>(g.part, parts, a.H * a.R, g.gw);
   if (g.gk || g.gpos) {
     sh = shape_of(a, true);
     const dim3 grid((unsigned)(sh.wpr == 1 ? (a.n + 3) / 4 : a.n), (unsigned)(g.gk ? sh.groups : 1));
