@@ -1443,15 +1443,14 @@ e2f_status check_workspace(const void* ws, size_t have, size_t need) {
 }
 
 struct TransposeLayout {
-  size_t cnt, sums, rank, list, total;
+  size_t cnt, sums, pos, total;
 };
 TransposeLayout transpose_layout(int32_t n, int64_t E) {
   TransposeLayout t;
   t.cnt = 0;
-  t.sums = al256(sizeof(int32_t) * (size_t)n);
-  t.rank = t.sums + al256(sizeof(int64_t) * (size_t)transpose_scan_blocks(n));
-  t.list = t.rank + al256(sizeof(int32_t) * (size_t)E);
-  t.total = t.list + al256(sizeof(int32_t) * (size_t)E);
+  t.sums = al256(sizeof(int32_t) * (3 * (size_t)n + 1));
+  t.pos = t.sums + al256(sizeof(int64_t) * (size_t)transpose_scan_blocks(n));
+  t.total = t.pos + al256(3 * sizeof(int32_t) * (size_t)E);
   return t;
 }
 
@@ -1509,15 +1508,14 @@ e2f_status check_attention_inputs(const e2f_attention_params* p, const float* po
 }
 
 struct AttnLayout {
-  size_t ds, edge, part, total;
+  size_t edge, part, total;
 };
 AttnLayout attention_layout(const e2f_attention_params* p, int32_t n, int64_t E) {
-  AttnLayout l;
+  AttnLayout l{};
+  if (n == 0) return l;
   const AttnArgs a = attention_args(p, nullptr, nullptr, nullptr, nullptr, n, nullptr, nullptr, nullptr, E);
-  l.ds = 0;
-  l.edge = al256(sizeof(float) * (size_t)E * p->heads);
-  l.part = l.edge + al256(sizeof(float) * 4 * (size_t)E * (n ? attention_groups(a) : 1));
-  l.total = l.part + al256(sizeof(float) * (size_t)(n ? attention_parts(a) : 0) * p->heads * p->n_rbf);
+  l.part = al256(sizeof(float) * (size_t)E * attention_record(a));
+  l.total = l.part + al256(sizeof(float) * (size_t)attention_parts(a) * p->heads * p->n_rbf);
   return l;
 }
 
@@ -1601,8 +1599,7 @@ e2f_status e2f_transpose_graph(e2f_ctx* ctx, int32_t n, const int64_t* row_ptr, 
   DeviceGuard g(ctx->device);
   char* ws = (char*)workspace;
   E2F_TIMED("transpose", launch_transpose(row_ptr, col_idx, n, n_edges, (int32_t*)(ws + t.cnt),
-                                          (int64_t*)(ws + t.sums), (int32_t*)(ws + t.rank), (int32_t*)(ws + t.list),
-                                          rowT_ptr, colT, perm, s));
+                                          (int64_t*)(ws + t.sums), (int32_t*)(ws + t.pos), rowT_ptr, colT, perm, s));
   return E2F_OK;
 }
 
@@ -1656,7 +1653,7 @@ e2f_status e2f_attention_backward(e2f_ctx* ctx, const e2f_attention_params* p, c
   char* ws = (char*)workspace;
   AttnGrad d{};
   d.alpha = alpha, d.lse = lse, d.galpha = grad_alpha, d.rowT = rowT_ptr, d.colT = colT, d.perm = perm;
-  d.ds = (float*)(ws + l.ds), d.edge = (float*)(ws + l.edge), d.part = (float*)(ws + l.part);
+  d.edge = (float*)(ws + l.edge), d.part = (float*)(ws + l.part);
   d.gq = grad_q, d.gk = grad_k, d.gw = grad_rbf_w, d.gpos = grad_pos;
   E2F_TIMED("attention_grad", launch_att_backward(attention_args(p, pos, graph_id, q, k, n, rbf_w, row_ptr, col_idx,
                                                                  n_edges), d, s));

@@ -208,26 +208,27 @@ struct AttnGrad {
   const float *alpha, *lse, *galpha;
   const int64_t* rowT;
   const int32_t *colT, *perm;
-  float *ds, *edge, *part;  // scratch [E][H], [attention_groups][E][4], [attention_parts][H][R]
+  float *edge, *part;  // scratch [E][attention_record], [attention_parts][H][R]
   void *gq, *gk;
   float *gw, *gpos;
-  int groups;  // (filled in by the launcher)
+  int groups, stride, force;  // (filled in by the launcher)
 };
 // How the kernels divide heads and rows: a head of k takes lph lanes (16 bytes of features each), an edge lpe lanes,
-// `units` times over; a workgroup up to `heads` heads of `kheads` heads of k; wpr waves a row
+// `units` times over; a workgroup up to `heads` heads of `kheads` heads of k, `share` of the
+// `sharing` heads that share one; hp their number's next power of two; wpr waves a row
 struct AttnShape {
-  int lph, lpe, units, kheads, share, heads, groups, hp, wpr, rows, lds, dq;
+  int lph, lph_log, lpe, units, kheads, share, sharing, heads, groups, hp, hp_log, wpr, rows, lds, dq;
   bool one;            // a lane has one head's features alone, 16 whole bytes of them
 };
-int attention_groups(const AttnArgs& a);
-int attention_parts(const AttnArgs& a, int* rows = nullptr);
+int attention_record(const AttnArgs& a, int* force = nullptr);
+int attention_parts(const AttnArgs& a);
 constexpr int kAttnMaxDk = 256;
 hipError_t launch_att_forward(const AttnArgs& a, float* alpha, float* lse, hipStream_t s);
 hipError_t launch_att_backward(const AttnArgs& a, const AttnGrad& g, hipStream_t s);
-// The transposed graph: scratch cnt [n], sums [transpose_scan_blocks(n)], rank and list [E]
+// The transposed graph: scratch cnt [3 n + 1], sums [transpose_scan_blocks(n)], pos [3 E]
 int transpose_scan_blocks(int n);
 hipError_t launch_transpose(const int64_t* row_ptr, const int32_t* col, int n, int64_t E, int32_t* cnt, int64_t* sums,
-                            int32_t* rank, int32_t* list, int64_t* rowT, int32_t* colT, int32_t* perm, hipStream_t s);
+                            int32_t* pos, int64_t* rowT, int32_t* colT, int32_t* perm, hipStream_t s);
 
 // ---- norms around a block, its gate and residual sum (block_norm.hip)
 struct NormArgs {

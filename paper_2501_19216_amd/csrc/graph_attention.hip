@@ -142,13 +142,12 @@ struct Group {
   int h0, heads, k0, kheads, share;
 };
 __device__ __forceinline__ Group group_of(const AttnArgs& a, const AttnShape& s, int y) {
-  const int share = a.H / a.Hk;
   Group g;
-  if (share > s.share) {  // part of the heads of one head of k
-    const int parts = (share + s.share - 1) / s.share, at = y % parts * s.share;
-    g.k0 = y / parts, g.kheads = 1, g.share = min(s.share, share - at), g.h0 = g.k0 * share + at;
+  if (s.share < s.sharing) {  // part of the heads of one head of k
+    const int parts = (s.sharing + s.share - 1) / s.share, at = y % parts * s.share;
+    g.k0 = y / parts, g.kheads = 1, g.share = min(s.share, s.sharing - at), g.h0 = g.k0 * s.sharing + at;
   } else {
-    g.k0 = y * s.kheads, g.kheads = min(s.kheads, a.Hk - g.k0), g.share = share, g.h0 = g.k0 * share;
+    g.k0 = y * s.kheads, g.kheads = min(s.kheads, a.Hk - g.k0), g.share = s.share, g.h0 = g.k0 * s.share;
   }
   g.heads = g.kheads * g.share;
   return g;
@@ -164,53 +163,54 @@ struct Lanes {
 __device__ __forceinline__ Lanes lanes_of(const AttnShape& s, const Group& g) {
   const int lane = threadIdx.x & 63;
   Lanes l;
-  l.head = lane & (s.hp - 1), l.entry = lane / s.hp, l.per = 64 / s.hp;
+  l.head = lane & (s.hp - 1), l.entry = lane >> s.hp_log, l.per = 64 >> s.hp_log;
   l.on = l.head < g.heads;
   return l;
 }
 
 // How a wave goes through a row: stretches of 64 edges, of which it takes those of the receiver's graph
 struct Walk {
-  int64_t e1, at, step;  // end of the row, next stretch, from one of the wave's to the next
-  int queued, gid;       // edges found and not yet taken
+  int64_t e0;              // first edge of the row; the others count from it
+  unsigned len, at, step;  // edges of the row, next stretch, from one of the wave's to the next
+  int queued, gid;         // edges found and not yet taken
 };
 
-// The next batch, a lane an edge: e and its sender j, -1 behind the last.  Returns their number.  stage: 256 ints.
-// skip(first edge, count, lanes whose edges are between graphs) sees each stretch once.
+// The next batch, a lane an edge: its place e in the row and its sender j, -1 behind the last.  Returns their number.
+// stage: 256 ints.  skip(first edge, count, lanes whose edges are between graphs) sees each stretch once.
 template <typename S>
-__device__ __forceinline__ int next_batch(const AttnArgs& a, Walk& w, int* stage, int64_t e0, int64_t& e, int& j,
-                                          S&& skip) {
+__device__ __forceinline__ int next_batch(const AttnArgs& a, Walk& w, int* stage, unsigned& e, int& j, S&& skip) {
   const int lane = threadIdx.x & 63;
-  j = -1, e = e0;
+  const int32_t* col = a.col + w.e0;
+  j = -1, e = 0;
   if (!a.gid) {
-    if (w.at >= w.e1) return 0;
-    const int count = (int)min(w.e1 - w.at, (int64_t)64);
-    if (lane < count) e = w.at + lane, j = atom_of(a, a.col[e]);
+    if (w.at >= w.len) return 0;
+    const int count = (int)min(w.len - w.at, 64u);
+    if (lane < count) e = w.at + lane, j = atom_of(a, col[e]);
     w.at += w.step;
     return count;
   }
-  while (w.queued < 64 && w.at < w.e1) {
-    const int64_t mine = w.at + lane;
+  while (w.queued < 64 && w.at < w.len) {
+    const unsigned mine = w.at + lane;
     int s = -1;
     bool same = false;
-    if (mine < w.e1) {
-      s = atom_of(a, a.col[mine]);
+    if (mine < w.len) {
+      s = atom_of(a, col[mine]);
       same = a.gid[s] == w.gid;
     }
     const uint64_t found = __ballot(same);
-    const int count = (int)min(w.e1 - w.at, (int64_t)64);
+    const int count = (int)min(w.len - w.at, 64u);
     skip(w.at, count, ~found & (count == 64 ? ~0ull : (1ull << count) - 1));
     if (same) {
       const int q = w.queued + __builtin_popcountll(found & ((1ull << lane) - 1));
       stage[q] = s;
-      stage[128 + q] = (int)(mine - e0);
+      stage[128 + q] = (int)mine;
     }
     w.queued += __builtin_popcountll(found);
     w.at += w.step;
   }
   wave_sync();
   const int count = min(w.queued, 64);
-  if (lane < count) j = stage[lane], e = e0 + stage[128 + lane];
+  if (lane < count) j = stage[lane], e = stage[128 + lane];
   if (w.queued > 64) {
     const bool more = lane < w.queued - 64;
     const int s = more ? stage[64 + lane] : 0, f = more ? stage[192 + lane] : 0;
@@ -220,6 +220,12 @@ __device__ __forceinline__ int next_batch(const AttnArgs& a, Walk& w, int* stage
   w.queued -= count;
   wave_sync();
   return count;
+}
+
+// row i's edges, inside [0, E] whatever row_ptr holds; the wave `part` of `wpr` takes every wpr-th stretch
+__device__ __forceinline__ Walk walk_of(const AttnArgs& a, int64_t i, int part, int wpr) {
+  const int64_t E = a.E, e0 = min(max(a.row_ptr[i], (int64_t)0), E), e1 = min(max(a.row_ptr[i + 1], e0), E);
+  return Walk{e0, (unsigned)(e1 - e0), 64u * part, 64u * wpr, 0, a.gid ? a.gid[i] : 0};
 }
 
 // Features of a block of BE entries, LPE lanes an entry, up to eight loads of a lane at a time (`part` of PARTS)
@@ -291,7 +297,7 @@ template <int LPE, typename F>
 __device__ __forceinline__ Place place_of(const AttnArgs& a, const AttnShape& sh, const Group& g, int unit) {
   Place p;
   const int at = unit * 64 + (threadIdx.x & 63) % LPE;
-  p.t = at % sh.lph, p.kl = at / sh.lph;
+  p.t = at & (sh.lph - 1), p.kl = at >> sh.lph_log;
   p.count = p.kl < g.kheads ? a.dk - p.t * F::VEC : 0;
   return p;
 }
@@ -364,19 +370,12 @@ __global__ __launch_bounds__(256, 4) void k_att_forward(AttnArgs a, AttnShape sh
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // (a scalar)
   const Group g = group_of(a, sh, blockIdx.y);
   const Lanes ln = lanes_of(sh, g);
-  const int64_t i = sh.wpr == 1 ? row_block() * 4 + wave : row_block();
-  const bool row = i < a.n;  // (with four waves a row the same for the workgroup)
   float* s = sm + wave * sh.lds;
   float* env = s + kKept * kLd;
   int* edge = (int*)(env + kKept);
   float* dist = (float*)(edge + kKept);
   int* jj = (int*)(dist + 64);
   int* stage = jj + 64;
-  const int64_t e0 = row ? min(max(a.row_ptr[i], (int64_t)0), a.E) : 0;
-  const int64_t e1 = row ? min(max(a.row_ptr[i + 1], e0), a.E) : 0;
-  const int part = sh.wpr == 1 ? 0 : wave;
-  const int64_t step = 64 * (int64_t)sh.wpr;
-  Walk w{e1, e0 + 64 * part, step, 0, a.gid && row ? a.gid[i] : 0};
   const float inv = (float)(a.R - 1) / a.rc, icap = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
   float wr[8];
 #pragma unroll
@@ -384,122 +383,130 @@ __global__ __launch_bounds__(256, 4) void k_att_forward(AttnArgs a, AttnShape sh
     const int f = 4 * r + (lane >> 4), h = lane & 15;
     wr[r] = h < g.heads && f < a.R ? a.w[(g.h0 + h) * a.R + f] : 0.0f;
   }
-  float q1[F::VEC] = {};
-  if (ONE && a.dk && row) {
-    const Place p = place_of<LPE, F>(a, sh, g, 0);
-    read_q<F>(a, i, g.h0 + p.kl, p, q1);
-  }
-  float px = 0.0f, py = 0.0f, pz = 0.0f;
-  if (row) px = a.pos[3 * i], py = a.pos[3 * i + 1], pz = a.pos[3 * i + 2];
-  float m = -INFINITY, den = 0.0f;
-  int kept = 0;        // edges whose scores are in the LDS
-  bool spill = false;  // the scores of the row are in alpha
-  auto to_alpha = [&](int count, const float* from) {
-    if (ln.on)
-      for (int n = ln.entry; n < count; n += ln.per)
-        alpha[(e0 + edge[n]) * a.H + g.h0 + ln.head] = from[n * kLd + ln.head];
-  };
-  for (;;) {
-    int64_t e;
-    int j;
-    const int count = next_batch(a, w, stage, e0, e, j, [&](int64_t first, int many, uint64_t mask) {
-      if (!mask || !ln.on) return;
-      for (int n = ln.entry; n < many; n += ln.per)
-        if (mask >> n & 1) alpha[(first + n) * a.H + g.h0 + ln.head] = 0.0f;
-    });
-    if (count == 0) break;
-    if (kept == kKept) {  // (every batch but the last has 64)
-      to_alpha(kept, s);
-      kept = 0, spill = true;
+  const int64_t first = row_block() * sh.rows;
+  for (int rr = 0; rr < sh.rows; rr += sh.wpr == 1 ? 4 : 1) {
+    const int64_t i = first + rr + (sh.wpr == 1 ? wave : 0);
+    if (i >= a.n) break;  // (with four waves a row the same for the workgroup)
+    const int part = sh.wpr == 1 ? 0 : wave;
+    Walk w = walk_of(a, i, part, sh.wpr);
+    float* out = alpha + w.e0 * a.H + g.h0;  // the row's weights of the group's heads
+    float q1[F::VEC] = {};
+    if (ONE && a.dk) {
+      const Place p = place_of<LPE, F>(a, sh, g, 0);
+      read_q<F>(a, i, g.h0 + p.kl, p, q1);
+    }
+    const float px = a.pos[3 * i], py = a.pos[3 * i + 1], pz = a.pos[3 * i + 2];
+    float m = -INFINITY, den = 0.0f;
+    int kept = 0;        // edges whose scores are in the LDS
+    bool spill = false;  // the scores of the row are in alpha
+    auto to_alpha = [&](int count, const float* from) {
+      if (ln.on)
+        for (int n = ln.entry; n < count; n += ln.per)
+          out[(uint64_t)(unsigned)edge[n] * a.H + ln.head] = from[n * kLd + ln.head];
+    };
+    for (;;) {
+      unsigned e;
+      int j;
+      const int count = next_batch(a, w, stage, e, j, [&](unsigned first, int many, uint64_t mask) {
+        if (!mask || !ln.on) return;
+        for (int n = ln.entry; n < many; n += ln.per)
+          if (mask >> n & 1) out[(uint64_t)(first + n) * a.H + ln.head] = 0.0f;
+      });
+      if (count == 0) break;
+      if (kept == kKept) {  // (every batch but the last has 64)
+        to_alpha(kept, s);
+        kept = 0, spill = true;
+        wave_sync();
+      }
+      float* sb = s + kept * kLd;
+      const bool there = j >= 0;
+      float dx = 0.0f, dy = 0.0f, dz = 0.0f;
+      if (there) dx = px - a.pos[3 * (int64_t)j], dy = py - a.pos[3 * (int64_t)j + 1], dz = pz - a.pos[3 * (int64_t)j + 2];
+      const int j0 = __builtin_amdgcn_readfirstlane(j);  // (by every lane: lane 0 has the batch's first edge)
+      jj[lane] = there ? j : j0;                          // the first sender once more behind the last
+      wave_sync();
+      if (a.dk) {
+        Features<LPE, F> f;
+        for (int b = 0; b < count; b += f.BE) products<LPE, ONE, F>(a, sh, g, i, q1, f, jj + b, sb + b * kLd);
+      }
+      const float d = sqrtf(dx * dx + dy * dy + dz * dz);
+      dist[lane] = d;
+      env[kept + lane] = envelope(a.rc, d);
+      edge[kept + lane] = (int)e;
+      wave_sync();
+      if (a.R)
+        for (int b = 0; b < count; b += 16) add_radial(a, sh, g, dist + b, wr, inv, sb + b * kLd);
+      wave_sync();
+      // the scores, and the running maximum and sum, four entries at a time
+      if (ln.on)
+        for (int n0 = ln.entry; n0 < count; n0 += 4 * ln.per) {
+          float x[4], mx = m;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int n = n0 + u * ln.per;
+            x[u] = -INFINITY;
+            if (n < count) {
+              x[u] = a.dk || a.R ? sb[n * kLd + ln.head] : 0.0f;
+              if (a.cap > 0.0f) x[u] = a.cap * tanh_near(x[u] * icap);
+              sb[n * kLd + ln.head] = x[u];
+            }
+            mx = fmaxf(mx, x[u]);
+          }
+          if (mx > m) den *= exp_fast(m - mx), m = mx;
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            if (n0 + u * ln.per < count) den += exp_fast(x[u] - m);
+        }
+      wave_sync();
+      if (spill)
+        to_alpha(count, s);
+      else
+        kept += count;
       wave_sync();
     }
-    float* sb = s + kept * kLd;
-    const bool there = j >= 0;
-    float dx = 0.0f, dy = 0.0f, dz = 0.0f;
-    if (there) dx = px - a.pos[3 * (int64_t)j], dy = py - a.pos[3 * (int64_t)j + 1], dz = pz - a.pos[3 * (int64_t)j + 2];
-    const int j0 = __builtin_amdgcn_readfirstlane(j);  // (by every lane: lane 0 has the batch's first edge)
-    jj[lane] = there ? j : j0;                          // the first sender once more behind the last
-    wave_sync();
-    if (a.dk) {
-      Features<LPE, F> f;
-      for (int b = 0; b < count; b += f.BE) products<LPE, ONE, F>(a, sh, g, i, q1, f, jj + b, sb + b * kLd);
+    // the row's sum, over the lanes and waves of a head
+    float top = classes_all(m, sh.hp, [](float p, float q) { return fmaxf(p, q); });
+    den = classes_all(m == top ? den : den * exp_fast(m - top), sh.hp, [](float p, float q) { return p + q; });
+    if (sh.wpr > 1) {
+      __syncthreads();  // (the row before has been read)
+      if (lane < sh.hp) join[wave][0][lane] = top, join[wave][1][lane] = den;
+      __syncthreads();
+      for (int k = 0; k < 4; ++k) top = fmaxf(top, join[k][0][ln.head]);
+      den = 0.0f;
+      for (int k = 0; k < 4; ++k) {
+        const float mk = join[k][0][ln.head], dk = join[k][1][ln.head];
+        den += mk == top ? dk : dk * exp_fast(mk - top);
+      }
     }
-    const float d = sqrtf(dx * dx + dy * dy + dz * dz);
-    dist[lane] = d;
-    env[kept + lane] = envelope(a.rc, d);
-    edge[kept + lane] = (int)(e - e0);
-    wave_sync();
-    if (a.R)
-      for (int b = 0; b < count; b += 16) add_radial(a, sh, g, dist + b, wr, inv, sb + b * kLd);
-    wave_sync();
-    // the scores, and the running maximum and sum, four entries at a time
-    if (ln.on)
-      for (int n0 = ln.entry; n0 < count; n0 += 4 * ln.per) {
-        float x[4], mx = m;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int n = n0 + u * ln.per;
-          x[u] = -INFINITY;
-          if (n < count) {
-            x[u] = a.dk || a.R ? sb[n * kLd + ln.head] : 0.0f;
-            if (a.cap > 0.0f) x[u] = a.cap * tanh_near(x[u] * icap);
-            sb[n * kLd + ln.head] = x[u];
-          }
-          mx = fmaxf(mx, x[u]);
+    const float l = top + logf(den);
+    if (lse && ln.on && ln.entry == 0 && part == 0) lse[i * a.H + g.h0 + ln.head] = l;
+    if (!spill) {
+      if (ln.on)
+        for (int n = ln.entry; n < kept; n += ln.per)
+          out[(uint64_t)(unsigned)edge[n] * a.H + ln.head] = env[n] * exp_fast(s[n * kLd + ln.head] - l);
+      wave_sync();  // (before the next row's scores)
+      continue;
+    }
+    for (unsigned c = 64u * part; c < w.len; c += w.step) {
+      const int count = (int)min(w.len - c, 64u);
+      float v = -1.0f;  // (an edge between graphs: its zeros are written)
+      if (lane < count) {
+        const int j = atom_of(a, a.col[w.e0 + c + lane]);
+        if (!a.gid || a.gid[j] == w.gid) {
+          const float dx = px - a.pos[3 * (int64_t)j], dy = py - a.pos[3 * (int64_t)j + 1], dz = pz - a.pos[3 * (int64_t)j + 2];
+          v = envelope(a.rc, sqrtf(dx * dx + dy * dy + dz * dz));
         }
-        if (mx > m) den *= exp_fast(m - mx), m = mx;
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (n0 + u * ln.per < count) den += exp_fast(x[u] - m);
       }
-    wave_sync();
-    if (spill)
-      to_alpha(count, s);
-    else
-      kept += count;
-    wave_sync();
-  }
-  // the row's sum, over the lanes and waves of a head
-  float top = classes_all(m, sh.hp, [](float p, float q) { return fmaxf(p, q); });
-  den = classes_all(m == top ? den : den * exp_fast(m - top), sh.hp, [](float p, float q) { return p + q; });
-  if (sh.wpr > 1) {
-    if (lane < sh.hp) join[wave][0][lane] = top, join[wave][1][lane] = den;
-    __syncthreads();
-    for (int k = 0; k < 4; ++k) top = fmaxf(top, join[k][0][ln.head]);
-    den = 0.0f;
-    for (int k = 0; k < 4; ++k) {
-      const float mk = join[k][0][ln.head], dk = join[k][1][ln.head];
-      den += mk == top ? dk : dk * exp_fast(mk - top);
+      env[lane] = v;
+      wave_sync();
+      if (ln.on)
+        for (int n = ln.entry; n < count; n += ln.per) {
+          if (env[n] < 0.0f) continue;
+          float* to = out + (uint64_t)(c + n) * a.H + ln.head;
+          *to = env[n] * exp_fast(*to - l);
+        }
+      wave_sync();
     }
-  }
-  if (!row) return;
-  const float l = top + logf(den);
-  if (lse && ln.on && ln.entry == 0 && part == 0) lse[i * a.H + g.h0 + ln.head] = l;
-  if (!spill) {
-    if (ln.on)
-      for (int n = ln.entry; n < kept; n += ln.per)
-        alpha[(e0 + edge[n]) * a.H + g.h0 + ln.head] = env[n] * exp_fast(s[n * kLd + ln.head] - l);
-    return;
-  }
-  for (int64_t c = e0 + 64 * part; c < e1; c += step) {
-    const int count = (int)min(e1 - c, (int64_t)64);
-    float v = -1.0f;  // (an edge between graphs: its zeros are written)
-    if (lane < count) {
-      const int j = atom_of(a, a.col[c + lane]);
-      if (!a.gid || a.gid[j] == w.gid) {
-        const float dx = px - a.pos[3 * (int64_t)j], dy = py - a.pos[3 * (int64_t)j + 1], dz = pz - a.pos[3 * (int64_t)j + 2];
-        v = envelope(a.rc, sqrtf(dx * dx + dy * dy + dz * dz));
-      }
-    }
-    env[lane] = v;
-    wave_sync();
-    if (ln.on)
-      for (int n = ln.entry; n < count; n += ln.per) {
-        if (env[n] < 0.0f) continue;
-        float* to = alpha + (c + n) * a.H + g.h0 + ln.head;
-        *to = env[n] * exp_fast(*to - l);
-      }
-    wave_sync();
   }
 }
 
@@ -536,24 +543,24 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
   for (int rr = 0; rr < sh.rows; rr += sh.wpr == 1 ? 4 : 1) {
     const int64_t i = first + rr + (sh.wpr == 1 ? wave : 0);
     const bool row = i < a.n;
-    const int64_t e0 = row ? min(max(a.row_ptr[i], (int64_t)0), a.E) : 0;
-    const int64_t e1 = row ? min(max(a.row_ptr[i + 1], e0), a.E) : 0;
-    const int64_t step = 64 * (int64_t)sh.wpr;
-    Walk w{e1, e0 + 64 * part, step, 0, a.gid && row ? a.gid[i] : 0};
+    Walk w = {};
+    if (row) w = walk_of(a, i, part, sh.wpr);
+    const float* gal = gr.galpha + w.e0 * a.H + g.h0;  // the row's gradients of the group's heads
     float D = 0.0f;
     {
-      const int64_t stride = ln.per * sh.wpr;
-      const float *al = gr.alpha + g.h0 + ln.head, *ga = gr.galpha + g.h0 + ln.head;
-      for (int64_t e = e0 + ln.entry + part * ln.per; ln.on && e < e1; e += 4 * stride) {
+      const unsigned stride = ln.per * sh.wpr;
+      const float* al = gr.alpha + w.e0 * a.H + g.h0;
+      for (unsigned e = ln.entry + part * ln.per; ln.on && e < w.len; e += 4 * stride) {
         float x[4], y[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const int64_t at = min(e + u * stride, e1 - 1);
-          x[u] = al[at * a.H], y[u] = ga[at * a.H];
+          const uint64_t at = (uint64_t)min(e + u * stride, w.len - 1) * a.H + ln.head;
+          x[u] = al[at], y[u] = gal[at];
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-          if (e + u * stride < e1 && (!a.gid || a.gid[atom_of(a, a.col[e + u * stride])] == w.gid)) D += x[u] * y[u];
+          if (e + u * stride < w.len && (!a.gid || a.gid[atom_of(a, a.col[w.e0 + e + u * stride])] == w.gid))
+            D += x[u] * y[u];
       }
       D = classes_all(D, sh.hp, [](float p, float q) { return p + q; });
       if (sh.wpr > 1) {
@@ -564,6 +571,7 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
       }
     }
     if (!row) continue;  // (with four waves a row, for the workgroup)
+    float* rec = gr.edge + w.e0 * gr.stride;
     const float l = ln.on ? gr.lse[i * a.H + g.h0 + ln.head] : 0.0f;
     float q1[F::VEC] = {}, dq[F::VEC] = {};
     if (ONE && a.dk) {
@@ -576,15 +584,15 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
       wave_sync();
     }
     for (;;) {
-      int64_t e;
+      unsigned e;
       int j;
-      const int count = next_batch(a, w, stage, e0, e, j, [](int64_t, int, uint64_t) {});
+      const int count = next_batch(a, w, stage, e, j, [](unsigned, int, uint64_t) {});
       if (count == 0) break;
       float dx = 0.0f, dy = 0.0f, dz = 0.0f;
       if (j >= 0) dx = px - a.pos[3 * (int64_t)j], dy = py - a.pos[3 * (int64_t)j + 1], dz = pz - a.pos[3 * (int64_t)j + 2];
       const int j0 = __builtin_amdgcn_readfirstlane(j);  // (by every lane: lane 0 has the batch's first edge)
       jj[lane] = j >= 0 ? j : j0;                         // the first sender once more behind the last
-      edge[lane] = (int)(e - e0);
+      edge[lane] = (int)e;
       const float d = sqrtf(dx * dx + dy * dy + dz * dz);
       float sl;
       env[lane] = envelope(a.rc, d, &sl);
@@ -599,7 +607,7 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             const int n = c + ln.entry + u * ln.per;
-            ga[u] = ln.on && n < many ? gr.galpha[(e0 + edge[b0 + n]) * a.H + g.h0 + ln.head] : 0.0f;
+            ga[u] = ln.on && n < many ? gal[(uint64_t)(unsigned)edge[b0 + n] * a.H + ln.head] : 0.0f;
           }
         };
         read_ga(0);
@@ -627,7 +635,7 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
                 const float p = exp_fast(x - l);
                 ds = p * (ga[u] * env[b0 + n] - D) * turn;
                 dd = ga[u] * p * slope[b0 + n];
-                if (gr.gk) gr.ds[(e0 + edge[b0 + n]) * a.H + g.h0 + ln.head] = ds;
+                if (gr.gk) rec[(uint64_t)(unsigned)edge[b0 + n] * gr.stride + g.h0 + ln.head] = ds;
               }
               sb[n * kLd + ln.head] = ds;
             }
@@ -698,7 +706,7 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
       }
       if (gr.gpos && lane < count) {
         const float v = d > 0.0f ? force[lane] / d : 0.0f;
-        *(f4*)(gr.edge + ((int64_t)blockIdx.y * a.E + e) * 4) = (f4){v * dx, v * dy, v * dz, 0.0f};
+        *(f4*)(rec + (uint64_t)e * gr.stride + gr.force + 4 * blockIdx.y) = (f4){v * dx, v * dy, v * dz, 0.0f};
       }
       wave_sync();
     }
@@ -795,8 +803,8 @@ __global__ __launch_bounds__(256) void k_att_senders(AttnArgs a, AttnShape sh, A
   const int64_t q0 = row ? min(max(gr.rowT[j], (int64_t)0), a.E) : 0;
   const int64_t q1 = row ? min(max(gr.rowT[j + 1], q0), a.E) : 0;
   const int gid = a.gid && row ? a.gid[j] : 0;
-  const int k0 = blockIdx.y * sh.kheads, kheads = min(sh.kheads, a.Hk - k0), share = a.H / a.Hk;
-  const int at = lane % LPE, t = at % sh.lph, kl = at / sh.lph;
+  const int k0 = blockIdx.y * sh.kheads, kheads = min(sh.kheads, a.Hk - k0), share = sh.sharing;
+  const int at = lane % LPE, t = at & (sh.lph - 1), kl = at >> sh.lph_log;
   const int count = kl < kheads ? a.dk - t * F::VEC : 0;
   int *ii = stage[wave][0], *ee = stage[wave][1];
   float acc[F::VEC] = {}, gx = 0.0f, gy = 0.0f, gz = 0.0f;
@@ -806,7 +814,7 @@ __global__ __launch_bounds__(256) void k_att_senders(AttnArgs a, AttnShape sh, A
     for (int64_t e = e0 + lane + 64 * part; e < e1; e += 64 * sh.wpr)
       if (!a.gid || a.gid[atom_of(a, a.col[e])] == gid)
         for (int y = 0; y < gr.groups; ++y) {
-          const f4 v = *(const f4*)(gr.edge + ((int64_t)y * a.E + e) * 4);
+          const f4 v = *(const f4*)(gr.edge + e * gr.stride + gr.force + 4 * y);
           gx += v[0], gy += v[1], gz += v[2];
         }
   }
@@ -834,7 +842,7 @@ __global__ __launch_bounds__(256) void k_att_senders(AttnArgs a, AttnShape sh, A
             ds[u] = 0.0f;
             if (s >= 0 && count > 0) {
               r[u] = F::load((const typename F::type*)a.q + s * a.ldq + (int64_t)h * a.dk + t * F::VEC, count);
-              ds[u] = gr.ds[(int64_t)ee[n] * a.H + h];
+              ds[u] = gr.edge[(int64_t)ee[n] * gr.stride + h];
             }
           }
 #pragma unroll
@@ -847,7 +855,7 @@ __global__ __launch_bounds__(256) void k_att_senders(AttnArgs a, AttnShape sh, A
     }
     if (forces && i >= 0)
       for (int y = 0; y < gr.groups; ++y) {
-        const f4 v = *(const f4*)(gr.edge + ((int64_t)y * a.E + e) * 4);
+        const f4 v = *(const f4*)(gr.edge + (int64_t)e * gr.stride + gr.force + 4 * y);
         gx -= v[0], gy -= v[1], gz -= v[2];
       }
   }
@@ -883,25 +891,89 @@ __global__ __launch_bounds__(256) void k_att_senders(AttnArgs a, AttnShape sh, A
   if (forces && lane < 3) gr.gpos[3 * j + lane] = lane == 0 ? gx : lane == 1 ? gy : gz;
 }
 
-// ---- the transposed graph: edges by sender, ascending
-__global__ __launch_bounds__(256) void k_t_zero(int32_t* __restrict__ cnt, int n) {
+// ---- the transposed graph: edges by sender, ascending.  Where the rows ascend, an edge (j, i) of row j finds by a
+// search of j in row i whether its reverse (i, j) is there, which is one of the edges that j sends: j's list is the
+// reverses of its own row, in order, and those of its edges that have none are counted, placed behind and sorted in.
+// So a graph with every edge both ways (a radius graph) takes no atomics and no sort.  Graphs whose rows do not
+// ascend count and sort every edge.
+struct Transposed {
+  const int64_t* row_ptr;
+  const int32_t* col;
+  int n;
+  int64_t E;
+  int32_t *cnt, *found, *extra, *pos, *list, *from;  // cnt[n]: not 0 if a row does not ascend
+  int64_t *sums, *rowT;
+  int32_t *colT, *perm;
+};
+__global__ __launch_bounds__(256) void k_t_zero(Transposed t) {
   const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i < n) cnt[i] = 0;
+  if (i <= t.n) t.cnt[i] = 0;
+  if (i < t.n) t.extra[i] = 0;
 }
-// rank[e]: some place of e among its sender's edges (no two alike)
-__global__ __launch_bounds__(256) void k_t_count(const int32_t* __restrict__ col, int64_t E, int n,
-                                                 int32_t* __restrict__ cnt, int32_t* __restrict__ rank) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (e < E) rank[e] = atomicAdd(&cnt[min(max(col[e], 0), n - 1)], 1);
+// the place of x among the n ascending values at p, or -1 (one read a step and none after it: scattered reads are what
+// this costs; three at once in half the steps took 68 us where single ones took 39, 1.5 million edges)
+__device__ __forceinline__ int place_among(const int32_t* p, int n, int x) {
+  int lo = 0;
+  while (n > 0) {
+    const int half = n >> 1, v = p[lo + half];
+    if (v == x) return lo + half;
+    if (v < x)
+      lo += half + 1, n -= half + 1;
+    else
+      n = half;
+  }
+  return -1;
 }
-// rowT[i] = sum of cnt before i within i's stretch of kScanSpan, and the stretches' sums
+struct RowEnds {
+  int64_t e0, e1;
+};
+// pos[e] of the edge e = (j, i): the edge (i, j), or -1 - (some place among the edges that i sends without a
+// reverse); found[j]: the reverses of row j, extra[i]: the edges that i sends without one
+__global__ __launch_bounds__(256) void k_t_reverse(Transposed t) {
+  const int lane = threadIdx.x & 63, j = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (j >= t.n || __hip_atomic_load(t.cnt + t.n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) return;
+  const int64_t e0 = t.row_ptr[j], e1 = t.row_ptr[j + 1];
+  bool good = e0 >= 0 && e0 <= e1 && e1 <= t.E && (j > 0 || e0 == 0) && (j + 1 < t.n || e1 == t.E);
+  int found = 0, last = -1;  // last sender of the stretch before
+  if (good)
+    for (int64_t c = e0; c < e1; c += 64) {
+      const int64_t e = c + lane;
+      const int i = e < e1 ? t.col[e] : t.n;
+      const int up = __shfl_up(i, 1), before = lane ? up : last;
+      last = __shfl(i, 63);
+      bool has = false;
+      if (e < e1) {
+        const bool fine = i < t.n && before < i;
+        RowEnds r = {0, 0};
+        if (fine) __builtin_memcpy(&r, t.row_ptr + i, sizeof(r));
+        const int64_t lo = min(max(r.e0, (int64_t)0), t.E), hi = min(max(r.e1, lo), t.E);
+        const int at = place_among(t.col + lo, (int)(hi - lo), j);
+        has = at >= 0;
+        if (has)
+          t.pos[e] = (int32_t)lo + at;
+        else if (fine)
+          t.pos[e] = -1 - atomicAdd(t.extra + i, 1);
+        good = good && fine;
+      }
+      found += __builtin_popcountll(__ballot(has));
+    }
+  if (lane == 0) t.found[j] = found;
+  if (__any(!good) && lane == 0) __hip_atomic_store(t.cnt + t.n, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// (rows that do not ascend) pos[e]: some place of e among its sender's edges (no two alike)
+__global__ __launch_bounds__(256) void k_t_count(Transposed t) {
+  if (!t.cnt[t.n]) return;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < t.E; e += (int64_t)gridDim.x * 256)
+    t.pos[e] = atomicAdd(&t.cnt[min(max(t.col[e], 0), t.n - 1)], 1);
+}
+// rowT[i] = sum of the counts before i within i's stretch of kScanSpan, and the stretches' sums
 constexpr int kScanSpan = 4096;
-__global__ __launch_bounds__(1024) void k_t_scan(const int32_t* __restrict__ cnt, int n, int64_t* __restrict__ rowT,
-                                                 int64_t* __restrict__ sums) {
+__global__ __launch_bounds__(1024) void k_t_scan(Transposed t) {
+  const bool any = t.cnt[t.n];
   const int64_t at = (int64_t)blockIdx.x * kScanSpan + threadIdx.x * 4;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // (a scalar)
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int v[4];
-  for (int u = 0; u < 4; ++u) v[u] = at + u < n ? cnt[at + u] : 0;
+  for (int u = 0; u < 4; ++u) v[u] = at + u >= t.n ? 0 : any ? t.cnt[at + u] : t.found[at + u] + t.extra[at + u];
   const int own = v[0] + v[1] + v[2] + v[3];
   int inc = own;
   for (int o = 1; o < 64; o <<= 1) {
@@ -914,16 +986,16 @@ __global__ __launch_bounds__(1024) void k_t_scan(const int32_t* __restrict__ cnt
   int before = inc - own;
   for (int k = 0; k < wave; ++k) before += w[k];
   for (int u = 0; u < 4; ++u) {
-    if (at + u < n) rowT[at + u] = before;
+    if (at + u < t.n) t.rowT[at + u] = before;
     before += v[u];
   }
-  if (threadIdx.x == 1023) sums[blockIdx.x] = before;
+  if (threadIdx.x == 1023) t.sums[blockIdx.x] = before;
+  if (gridDim.x == 1 && threadIdx.x == 0) t.rowT[t.n] = t.E;
 }
-__global__ __launch_bounds__(1024) void k_t_offset(int n, int64_t E, int64_t* __restrict__ rowT,
-                                                   const int64_t* __restrict__ sums) {
+__global__ __launch_bounds__(1024) void k_t_offset(Transposed t) {
   __shared__ int64_t w[16];
   int64_t s = 0;
-  for (int b = threadIdx.x; b < (int)blockIdx.x; b += 1024) s += sums[b];
+  for (int b = threadIdx.x; b < (int)blockIdx.x; b += 1024) s += t.sums[b];
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
   if ((threadIdx.x & 63) == 0) w[threadIdx.x >> 6] = s;
   __syncthreads();
@@ -931,43 +1003,67 @@ __global__ __launch_bounds__(1024) void k_t_offset(int n, int64_t E, int64_t* __
   for (int k = 0; k < 16; ++k) s += w[k];
   for (int u = 0; u < 4; ++u) {
     const int64_t at = (int64_t)blockIdx.x * kScanSpan + threadIdx.x + 1024 * u;
-    if (at < n) rowT[at] += s;
+    if (at < t.n) t.rowT[at] += s;
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) rowT[n] = E;
+  if (blockIdx.x == 0 && threadIdx.x == 0) t.rowT[t.n] = t.E;
 }
-// the edges to their senders' lists, in any order there
-__global__ __launch_bounds__(256) void k_t_place(const int32_t* __restrict__ col, int n, int64_t E,
-                                                 const int64_t* __restrict__ rowT, const int32_t* __restrict__ rank,
-                                                 int32_t* __restrict__ perm) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (e < E) perm[rowT[min(max(col[e], 0), n - 1)] + rank[e]] = (int32_t)e;
+// a wave a row: the reverses of its edges are its atom's list; what has none, and the lists that wait for such an
+// edge, go to `list`
+__global__ __launch_bounds__(256) void k_t_place(Transposed t) {
+  if (t.cnt[t.n]) {
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < t.E; e += (int64_t)gridDim.x * 256)
+      t.list[t.rowT[min(max(t.col[e], 0), t.n - 1)] + t.pos[e]] = (int32_t)e;
+    return;
+  }
+  const int lane = threadIdx.x & 63;
+  for (int64_t j = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); j < t.n; j += (int64_t)gridDim.x * 4) {
+    const int64_t e1 = t.row_ptr[j + 1];
+    int64_t to = t.rowT[j];
+    const bool whole = t.extra[j] == 0;
+    for (int64_t c = t.row_ptr[j]; c < e1; c += 64) {
+      const int64_t e = c + lane;
+      const int i = e < e1 ? t.col[e] : 0, p = e < e1 ? t.pos[e] : -1;
+      const uint64_t m = __ballot(p >= 0);
+      const int64_t at = to + __builtin_popcountll(m & ((1ull << lane) - 1));
+      if (p >= 0 && whole)
+        t.perm[at] = p, t.colT[at] = i;
+      else if (e < e1) {
+        const int64_t slot = p >= 0 ? at : t.rowT[i] + t.found[i] - 1 - p;
+        t.list[slot] = p >= 0 ? p : (int32_t)e;
+        t.from[slot] = p >= 0 ? i : (int32_t)j;
+      }
+      to += __builtin_popcountll(m);
+    }
+  }
 }
-// a wave a sender: its list in ascending order, an edge's place the number of
-// smaller ones, and the receivers by bisection of row_ptr
-__global__ __launch_bounds__(256) void k_t_sort(const int64_t* __restrict__ row_ptr, int n, int64_t E,
-                                                const int64_t* __restrict__ rowT, const int32_t* __restrict__ in,
-                                                int32_t* __restrict__ perm, int32_t* __restrict__ colT) {
-  const int j = blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (j >= n) return;
-  const int64_t q0 = rowT[j], q1 = rowT[j + 1];
-  for (int64_t c = q0; c < q1; c += 64) {
-    const int e = c + lane < q1 ? in[c + lane] : 0;
-    int place = 0;
-    for (int64_t b = q0; b < q1; b += 64) {
-      const int f = b + lane < q1 ? in[b + lane] : 0x7fffffff;
-      for (int u = 0; u < 64; ++u) place += __builtin_amdgcn_readlane(f, u) < e;
+// a wave a sender whose list is not in order yet: an edge's place is the number of smaller ones (where rows do
+// not ascend its receiver is found by bisection of row_ptr)
+__global__ __launch_bounds__(256) void k_t_sort(Transposed t) {
+  const bool any = t.cnt[t.n];
+  const int lane = threadIdx.x & 63;
+  for (int64_t j = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); j < t.n; j += (int64_t)gridDim.x * 4) {
+    if (!any && t.extra[j] == 0) continue;
+    const int64_t q0 = t.rowT[j], q1 = t.rowT[j + 1];
+    for (int64_t c = q0; c < q1; c += 64) {
+      const int e = c + lane < q1 ? t.list[c + lane] : 0;
+      int place = 0;
+      for (int64_t b = q0; b < q1; b += 64) {
+        const int f = b + lane < q1 ? t.list[b + lane] : 0x7fffffff;
+        const int many = (int)min(q1 - b, (int64_t)64);
+        for (int u = 0; u < many; ++u) place += __builtin_amdgcn_readlane(f, u) < e;
+      }
+      if (c + lane >= q1) continue;
+      t.perm[q0 + place] = e;
+      int lo = any ? 0 : t.from[c + lane], hi = any ? t.n - 1 : lo;  // the last row that begins at or before e
+      while (lo < hi) {
+        const int mid = (int)(((int64_t)lo + hi + 1) >> 1);
+        if (t.row_ptr[mid] <= e)
+          lo = mid;
+        else
+          hi = mid - 1;
+      }
+      t.colT[q0 + place] = lo;
     }
-    if (c + lane >= q1) continue;
-    perm[q0 + place] = e;
-    int lo = 0, hi = n - 1;  // the last row that begins at or before e
-    while (lo < hi) {
-      const int mid = (int)(((int64_t)lo + hi + 1) >> 1);
-      if (row_ptr[mid] <= e)
-        lo = mid;
-      else
-        hi = mid - 1;
-    }
-    colT[q0 + place] = lo;
   }
 }
 
@@ -976,7 +1072,8 @@ AttnShape shape_of(const AttnArgs& a, bool senders) {
   const int vec = a.bf16 ? BF16::VEC : F32::VEC, share = a.H / a.Hk;
   AttnShape s{};
   s.lph = 1;
-  while (s.lph * vec < a.dk) s.lph <<= 1;
+  while (s.lph * vec < a.dk) s.lph <<= 1, ++s.lph_log;
+  s.sharing = share;
   // heads that share k: the receivers' sums for dq, 64 lanes of them for each, stay within 8 KB of LDS a wave
   s.share = senders ? share : std::min(share, 2048 / (64 * vec));
   s.kheads = senders ? a.Hk : std::min(a.Hk, s.share < share ? 1 : 16 / share);
@@ -990,7 +1087,7 @@ AttnShape shape_of(const AttnArgs& a, bool senders) {
   s.groups = s.share < share ? a.Hk * ((share + s.share - 1) / s.share) : (a.Hk + s.kheads - 1) / s.kheads;
   s.heads = s.kheads * s.share;
   s.hp = 1;
-  while (s.hp < s.heads) s.hp <<= 1;
+  while (s.hp < s.heads) s.hp <<= 1, ++s.hp_log;
   s.one = s.units == 1 && (share == 1 || a.dk == 0) && a.dk % vec == 0;
   // four waves a row where they find four batches on average
   s.wpr = a.E / a.n >= 256 ? 4 : 1;
@@ -1000,14 +1097,22 @@ AttnShape shape_of(const AttnArgs& a, bool senders) {
 
 }  // namespace
 
-int attention_groups(const AttnArgs& a) { return shape_of(a, false).groups; }
+// Rows of a workgroup: one round of workgroups over the card, `per_cu` a CU
+static int rows_of(const AttnArgs& a, int wpr, int per_cu) {
+  const int least = wpr == 1 ? 4 : 1;
+  return least * (int)(((int64_t)a.n + least * 256 * per_cu - 1) / (least * 256 * per_cu));
+}
 
-// workgroups of the receivers' kernel: a few rows each, up to about 2048
-int attention_parts(const AttnArgs& a, int* rows) {
-  const int wpr = shape_of(a, false).wpr, least = wpr == 1 ? 4 : 1;
-  const int64_t r = least * (((int64_t)a.n + least * 2048 - 1) / (least * 2048));
-  if (rows) *rows = (int)r;
-  return (int)((a.n + r - 1) / r);
+int attention_parts(const AttnArgs& a) {
+  const int rows = rows_of(a, shape_of(a, false).wpr, 3);
+  return (a.n + rows - 1) / rows;
+}
+
+// floats of an edge's record: ds of every head, and the position gradient of every head group from *force on
+int attention_record(const AttnArgs& a, int* force) {
+  const int f = (a.H + 3) / 4 * 4;
+  if (force) *force = f;
+  return f + 4 * shape_of(a, false).groups;
 }
 
 // the kernel for the lanes of an edge, the type and one head a lane or more
@@ -1035,7 +1140,8 @@ hipError_t launch_att_forward(const AttnArgs& a, float* alpha, float* lse, hipSt
   if (a.n == 0) return hipSuccess;
   AttnShape sh = shape_of(a, false);
   sh.lds = kKept * (kLd + 2) + 64 + 64 + 256;
-  const dim3 grid((unsigned)(sh.wpr == 1 ? (a.n + 3) / 4 : a.n), (unsigned)sh.groups);
+  sh.rows = sh.wpr == 1 ? 4 : 1;
+  const dim3 grid((unsigned)((a.n + sh.rows - 1) / sh.rows), (unsigned)sh.groups);
   const size_t lds = sizeof(float) * 4 * sh.lds;
 #define E2F_ATT(P, ONE, F) k_att_forward<P, ONE, F><<<grid, 256, lds, s>>>(a, sh, alpha, lse)
   E2F_ATT_SWITCH
@@ -1051,7 +1157,9 @@ hipError_t launch_att_backward(const AttnArgs& a, const AttnGrad& gr, hipStream_
   AttnShape sh = shape_of(a, false);
   AttnGrad g = gr;
   g.groups = sh.groups;
-  const int parts = attention_parts(a, &sh.rows), vec = a.bf16 ? BF16::VEC : F32::VEC;
+  g.stride = attention_record(a, &g.force);
+  sh.rows = rows_of(a, sh.wpr, 3);
+  const int parts = attention_parts(a), vec = a.bf16 ? BF16::VEC : F32::VEC;
   sh.dq = sh.one ? 0 : 64 / sh.lpe * sh.heads * sh.lph * vec;
   sh.lds = 64 * kLd + 6 * 64 + 256 + sh.dq;
   if (sh.lds < 512) sh.lds = 512;  // (dw's sum over the waves)
@@ -1086,20 +1194,22 @@ hipError_t launch_att_backward(const AttnArgs& a, const AttnGrad& gr, hipStream_
 int transpose_scan_blocks(int n) { return (n + kScanSpan - 1) / kScanSpan; }
 
 hipError_t launch_transpose(const int64_t* row_ptr, const int32_t* col, int n, int64_t E, int32_t* cnt, int64_t* sums,
-                            int32_t* rank, int32_t* list, int64_t* rowT, int32_t* colT, int32_t* perm,
-                            hipStream_t s) {
+                            int32_t* pos, int64_t* rowT, int32_t* colT, int32_t* perm, hipStream_t s) {
+  const Transposed t{row_ptr, col,     n,           E,    cnt,  cnt + n + 1, cnt + 2 * (int64_t)n + 1,
+                     pos,     pos + E, pos + 2 * E, sums, rowT, colT,        perm};
   if (n == 0) {
-    k_t_offset<<<1, 1024, 0, s>>>(0, 0, rowT, nullptr);
+    k_t_offset<<<1, 1024, 0, s>>>(t);
     return hipGetLastError();
   }
-  const unsigned blocks = (unsigned)transpose_scan_blocks(n), eb = (unsigned)((E + 255) / 256);
-  k_t_zero<<<(n + 255) / 256, 256, 0, s>>>(cnt, n);
-  if (E > 0) k_t_count<<<eb, 256, 0, s>>>(col, E, n, cnt, rank);
-  k_t_scan<<<blocks, 1024, 0, s>>>(cnt, n, rowT, sums);
-  k_t_offset<<<blocks, 1024, 0, s>>>(n, E, rowT, sums);
+  const unsigned blocks = (unsigned)transpose_scan_blocks(n), nb = (unsigned)(((int64_t)n + 3) / 4);
+  k_t_zero<<<n / 256 + 1, 256, 0, s>>>(t);
+  k_t_reverse<<<nb, 256, 0, s>>>(t);
+  if (E > 0) k_t_count<<<(unsigned)std::min<int64_t>((E + 255) / 256, 1024), 256, 0, s>>>(t);
+  k_t_scan<<<blocks, 1024, 0, s>>>(t);
+  if (blocks > 1) k_t_offset<<<blocks, 1024, 0, s>>>(t);
   if (E > 0) {
-    k_t_place<<<eb, 256, 0, s>>>(col, n, E, rowT, rank, list);
-    k_t_sort<<<(n + 3) / 4, 256, 0, s>>>(row_ptr, n, E, rowT, list, perm, colT);
+    k_t_place<<<std::min(nb, 8192u), 256, 0, s>>>(t);
+    k_t_sort<<<std::min(nb, 8192u), 256, 0, s>>>(t);
   }
   return hipGetLastError();
 }

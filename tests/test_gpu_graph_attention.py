@@ -297,3 +297,62 @@ def test_outputs_alone(e2f, ctx):
     c = back(*t, want_qk=False, want_rbf=False)
     assert torch.equal(a[0], gq) and torch.equal(a[1], gk) and a[2] is None and a[3] is None
     assert torch.equal(b[2], gw) and torch.equal(c[3], gp)
+
+
+def transposed(n, rp, ci):
+    want = torch.sort(ci.long(), stable=True).indices
+    recv = torch.arange(n).repeat_interleave(rp.diff())
+    row_t = torch.cat([torch.zeros(1, dtype=torch.long), torch.bincount(ci.long(), minlength=n).cumsum(0)])
+    return row_t, recv[want].int(), want.int()
+
+
+@pytest.mark.parametrize("change", ["none", "one edge less", "one edge more", "rows not ascending", "an edge twice"])
+def test_transposed_graph_with_and_without_reverses(e2f, ctx, change):
+    # every edge with its reverse, and graphs that miss it by one edge or by their order
+    n = 700
+    pos = np.random.default_rng(2).uniform(0, 14, size=(n, 3)).astype(np.float32)
+    rp, ci = (torch.from_numpy(a) for a in o.neighbor_list(pos, 4.0))
+    rows = [ci[int(rp[i]):int(rp[i + 1])].tolist() for i in range(n)]
+    if change == "one edge less":
+        rows[333].pop(2)
+    elif change == "one edge more":
+        rows[600] = sorted(rows[600] + [next(j for j in range(n) if j not in rows[600] and j != 600)])
+    elif change == "rows not ascending":
+        rows[5].reverse()
+    elif change == "an edge twice":
+        a, b = 100, rows[100][0]
+        rows[a], rows[b] = sorted(rows[a] + [b]), sorted(rows[b] + [a])
+    rp = torch.tensor([0] + [len(r) for r in rows]).cumsum(0)
+    ci = torch.tensor(sum(rows, []), dtype=torch.int32)
+    for _ in range(2):
+        got = e2f.e2f_transpose_graph(ctx, n, rp.to(DEV), ci.to(DEV))
+        for a, b in zip(got, transposed(n, rp, ci)):
+            assert torch.equal(a.cpu(), b)
+
+
+def test_malformed_graphs_stay_inside(e2f, ctx):
+    # senders outside the atoms, rows that decrease or begin and end elsewhere: read with clamped indices, outputs
+    # unspecified, and what lies behind the arrays as it was
+    n, E, H = 40, 200, 2
+    g = torch.Generator().manual_seed(3)
+    pos, q, k, w = torch.rand(n, 3, generator=g), torch.randn(n, H, 4, generator=g), torch.randn(n, H, 4, generator=g), torch.randn(H, 4, generator=g)
+    ga = torch.randn(E, H, generator=g)
+    good_rp, good_ci = torch.arange(n + 1) * (E // n), torch.randint(0, n, (E,), generator=g).int()
+    for bad in ("senders", "rows"):
+        rp, ci = good_rp.clone(), good_ci.clone()
+        if bad == "senders":
+            ci[::7], ci[::11] = 2 ** 31 - 1, -5
+        else:
+            rp[3], rp[10], rp[20], rp[-1] = -100, 10 ** 12, 3, 10 ** 9
+        d = [t.to(DEV) for t in (pos, rp, ci, q, k, w, ga)]
+        kw = dict(q=d[3], k=d[4], rbf_w=d[5], cap=3.0)
+        alpha, lse = torch.full((E + 64, H), 7.0, device=DEV), torch.full((n + 64, H), 7.0, device=DEV)
+        e2f.e2f_attention_forward(ctx, d[0], d[1], d[2], 2.0, alpha=alpha[:E], lse=lse[:n], **kw)
+        t = e2f.e2f_transpose_graph(ctx, n, d[1], d[2])
+        e2f.e2f_attention_backward(ctx, d[0], d[1], d[2], 2.0, alpha[:E].contiguous(), lse[:n].contiguous(), d[6], *t, **kw)
+        torch.cuda.synchronize()
+        assert torch.all(alpha[E:] == 7.0) and torch.all(lse[n:] == 7.0)
+        # a transposed graph that is not one
+        t = (t[0].flip(0) * 1000 - 5, t[1] * 1000003, t[2] - 2 ** 30)
+        e2f.e2f_attention_backward(ctx, d[0], d[1], d[2], 2.0, alpha[:E].contiguous(), lse[:n].contiguous(), d[6], *t, **kw)
+        torch.cuda.synchronize()
