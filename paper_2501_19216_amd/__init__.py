@@ -9,6 +9,7 @@ package raises: there is no fallback.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 
@@ -285,18 +286,24 @@ def e2f_attention_weights(ctx: Context, pos, row_ptr, col_idx, cutoff: float, q=
     return out
 
 
+def _arg(ctx, t, dtype, shape, name):
+    """The address of a contiguous tensor of this type and shape on the context's device (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.get_device() != ctx.device or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor on the context's device" % (name, dtype))
+    if t.shape != shape:
+        raise ValueError("%s must have shape %s" % (name, tuple(shape)))
+    return t.data_ptr()
+
+
 def _workspace(ctx, workspace, nbytes, device):
     """The caller's workspace, or the context's own grown to nbytes."""
     if workspace is None:
         return ctx.workspace_for(nbytes, device)
-    if not workspace.is_cuda or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous uint8 device tensor")
+    if workspace.get_device() != ctx.device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on the context's device")
     return workspace
-
-
-def _shape(t, shape, name):
-    if t is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError("%s must have shape %s" % (name, tuple(shape)))
 
 
 _DTYPES = {torch.float32: E2F_F32, torch.bfloat16: E2F_BF16}
@@ -304,51 +311,44 @@ _DTYPES = {torch.float32: E2F_F32, torch.bfloat16: E2F_BF16}
 
 def e2f_transpose_graph(ctx, n, row_ptr, col_idx, workspace=None):
     """The graph by senders: (rowT_ptr int64 [n+1], colT int32 [E], the
-    receivers, perm int32 [E], the edges in the graph's own order)."""
-    _dev(row_ptr, torch.int64, "row_ptr")
-    _dev(col_idx, torch.int32, "col_idx")
-    _shape(row_ptr, (n + 1,), "row_ptr")
+    receivers, perm int32 [E], the edges in the graph's own order).  Here and
+    below, workspace: a uint8 device tensor, or None: the context's own, which
+    grows on demand (code under graph capture gives one of its own)."""
     E, dev = col_idx.numel(), col_idx.device
+    rp, ci = _arg(ctx, row_ptr, torch.int64, (n + 1,), "row_ptr"), _arg(ctx, col_idx, torch.int32, (E,), "col_idx")
     b = ctypes.c_size_t(0)
     _check(lib.e2f_transpose_graph_workspace_size(ctx.handle, n, E, ctypes.byref(b)),
            "e2f_transpose_graph_workspace_size")
     workspace = _workspace(ctx, workspace, b.value, dev)
     row_t = torch.empty(n + 1, dtype=torch.int64, device=dev)
     col_t, perm = (torch.empty(E, dtype=torch.int32, device=dev) for _ in range(2))
-    _check(lib.e2f_transpose_graph(ctx.handle, n, _ptr(row_ptr), _ptr(col_idx), E, _ptr(row_t), _ptr(col_t),
-                                   _ptr(perm), _ptr(workspace), workspace.numel(), _stream(dev)),
-           "e2f_transpose_graph")
+    _check(lib.e2f_transpose_graph(ctx.handle, n, rp, ci, E, row_t.data_ptr(), col_t.data_ptr(), perm.data_ptr(),
+                                   workspace.data_ptr(), workspace.numel(), _stream(dev)), "e2f_transpose_graph")
     return row_t, col_t, perm
 
 
-def _features(t, n, name):
+def _features(ctx, t, n, name):
     """dtype, heads, features and elements between atoms of q or k [n, heads, dk] (heads and features packed)."""
-    if not t.is_cuda or t.dtype not in _DTYPES:
-        raise ValueError("%s must be a float32 or bfloat16 device tensor" % name)
+    if t.get_device() != ctx.device or t.dtype not in _DTYPES:
+        raise ValueError("%s must be a float32 or bfloat16 tensor on the context's device" % name)
     if t.dim() != 3 or t.shape[0] != n:
         raise ValueError("%s must be [n, heads, dk]" % name)
     _, h, d = t.shape
-    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d) or (n > 1 and t.stride(0) < h * d):
+    s0, s1, s2 = t.stride()
+    if (d > 1 and s2 != 1) or (h > 1 and s1 != d) or (n > 1 and s0 < h * d):
         raise ValueError("%s must be packed within an atom, with at least heads * dk elements between atoms" % name)
-    return _DTYPES[t.dtype], h, d, t.stride(0) if n > 1 else 0
+    return _DTYPES[t.dtype], h, d, s0 if n > 1 else 0
 
 
-def _attention_params(pos, row_ptr, col_idx, cutoff, q, k, rbf_w, heads, scale, cap, graph_id):
-    for t, name in ((pos, "pos"), (rbf_w, "rbf_w")):
-        _dev(t, torch.float32, name)
-    _dev(row_ptr, torch.int64, "row_ptr")
-    _dev(col_idx, torch.int32, "col_idx")
-    _dev(graph_id, torch.int32, "graph_id")
-    n = pos.shape[0]
-    _shape(pos, (n, 3), "pos")
-    _shape(row_ptr, (n + 1,), "row_ptr")
-    _shape(graph_id, (n,), "graph_id")
+def _attention_args(ctx, pos, row_ptr, col_idx, cutoff, q, k, rbf_w, heads, scale, cap, graph_id):
+    """The parameters, and the addresses of what both directions read."""
+    n, E = pos.shape[0], col_idx.numel()
     if (q is None) != (k is None):
         raise ValueError("q and k go together")
     dt, H, dk, ldq, Hk, ldk = E2F_F32, heads, 0, 0, heads, 0
     if q is not None:
-        dt, H, dk, ldq = _features(q, n, "q")
-        dt2, Hk, dk2, ldk = _features(k, n, "k")
+        dt, H, dk, ldq = _features(ctx, q, n, "q")
+        dt2, Hk, dk2, ldk = _features(ctx, k, n, "k")
         if dt2 != dt or dk2 != dk:
             raise ValueError("q and k must agree in type and features")
         if heads is not None and heads != H:
@@ -357,10 +357,13 @@ def _attention_params(pos, row_ptr, col_idx, cutoff, q, k, rbf_w, heads, scale, 
         H = rbf_w.shape[0] if H is None else H
     if H is None:
         raise ValueError("heads must be given without q and rbf_w")
-    if rbf_w is not None and (rbf_w.dim() != 2 or rbf_w.shape[0] != H):
-        raise ValueError("rbf_w must be [heads, n_rbf]")
-    return AttentionParams(H, H if Hk is None else Hk, dk, 0 if rbf_w is None else rbf_w.shape[1], float(cutoff),
-                           float(scale), float(cap), dt, ldq, ldk)
+    R = 0 if rbf_w is None else rbf_w.shape[-1]
+    prm = AttentionParams(H, H if Hk is None else Hk, dk, R, cutoff, scale, cap, dt, ldq, ldk)
+    return prm, (_arg(ctx, pos, torch.float32, (n, 3), "pos"), _arg(ctx, graph_id, torch.int32, (n,), "graph_id"),
+                 None if q is None else q.data_ptr(), None if k is None else k.data_ptr(), n,
+                 _arg(ctx, rbf_w, torch.float32, (H, R), "rbf_w"),
+                 _arg(ctx, row_ptr, torch.int64, (n + 1,), "row_ptr"),
+                 _arg(ctx, col_idx, torch.int32, (E,), "col_idx"), E)
 
 
 def e2f_attention_forward(ctx, pos, row_ptr, col_idx, cutoff, q=None, k=None, rbf_w=None, heads=None, scale=1.0,
@@ -369,19 +372,16 @@ def e2f_attention_forward(ctx, pos, row_ptr, col_idx, cutoff, q=None, k=None, rb
     [E, heads], lse [n, heads]) float32.  q [n, heads, dk], k [n, k_heads, dk]
     float32 or bfloat16, packed within an atom (columns of one projection are
     fine); rbf_w [heads, R] or None; cap 0: none."""
-    prm = _attention_params(pos, row_ptr, col_idx, cutoff, q, k, rbf_w, heads, scale, cap, graph_id)
-    n, E, H = pos.shape[0], col_idx.numel(), prm.heads
+    prm, args = _attention_args(ctx, pos, row_ptr, col_idx, cutoff, q, k, rbf_w, heads, scale, cap, graph_id)
+    n, E, H, dev = pos.shape[0], col_idx.numel(), prm.heads, pos.device
     if alpha is None:
-        alpha = torch.empty(E, H, dtype=torch.float32, device=pos.device)
+        alpha = torch.empty(E, H, dtype=torch.float32, device=dev)
     if lse is None:
-        lse = torch.empty(n, H, dtype=torch.float32, device=pos.device)
-    _dev(alpha, torch.float32, "alpha")
-    _dev(lse, torch.float32, "lse")
-    _shape(alpha, (E, H), "alpha")
-    _shape(lse, (n, H), "lse")
-    _check(lib.e2f_attention_forward(ctx.handle, ctypes.byref(prm), _ptr(pos), _ptr(graph_id), _ptr(q), _ptr(k), n,
-                                     _ptr(rbf_w), _ptr(row_ptr), _ptr(col_idx), E, _ptr(alpha), _ptr(lse),
-                                     _stream(pos.device)), "e2f_attention_forward")
+        lse = torch.empty(n, H, dtype=torch.float32, device=dev)
+    _check(lib.e2f_attention_forward(ctx.handle, ctypes.byref(prm), *args,
+                                     _arg(ctx, alpha, torch.float32, (E, H), "alpha"),
+                                     _arg(ctx, lse, torch.float32, (n, H), "lse"), _stream(dev)),
+           "e2f_attention_forward")
     return alpha, lse
 
 
@@ -392,56 +392,42 @@ def e2f_attention_backward(ctx, pos, row_ptr, col_idx, cutoff, alpha, lse, grad_
     dk], grad_k [n, k_heads, dk], grad_rbf_w [heads, R], grad_pos [n, 3]), each
     None unless requested and there.  row_t, col_t, perm: e2f_transpose_graph's
     (not needed for grad_rbf_w alone)."""
-    prm = _attention_params(pos, row_ptr, col_idx, cutoff, q, k, rbf_w, heads, scale, cap, graph_id)
-    n, E, H = pos.shape[0], col_idx.numel(), prm.heads
-    for t, shape, name in ((alpha, (E, H), "alpha"), (lse, (n, H), "lse"), (grad_alpha, (E, H), "grad_alpha")):
-        _dev(t, torch.float32, name)
-        _shape(t, shape, name)
-    _dev(row_t, torch.int64, "row_t")
-    _dev(col_t, torch.int32, "col_t")
-    _dev(perm, torch.int32, "perm")
-    for t, shape, name in ((row_t, (n + 1,), "row_t"), (col_t, (E,), "col_t"), (perm, (E,), "perm")):
-        _shape(t, shape, name)
-    gq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if want_qk and prm.dk else None
-    gk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if want_qk and prm.dk else None
+    prm, args = _attention_args(ctx, pos, row_ptr, col_idx, cutoff, q, k, rbf_w, heads, scale, cap, graph_id)
+    n, E, H, dev = pos.shape[0], col_idx.numel(), prm.heads, pos.device
+    read = (_arg(ctx, row_t, torch.int64, (n + 1,), "row_t"), _arg(ctx, col_t, torch.int32, (E,), "col_t"),
+            _arg(ctx, perm, torch.int32, (E,), "perm"), _arg(ctx, alpha, torch.float32, (E, H), "alpha"),
+            _arg(ctx, lse, torch.float32, (n, H), "lse"), _arg(ctx, grad_alpha, torch.float32, (E, H), "grad_alpha"))
+    gq = torch.empty(q.shape, dtype=q.dtype, device=dev) if want_qk and prm.dk else None
+    gk = torch.empty(k.shape, dtype=k.dtype, device=dev) if want_qk and prm.dk else None
     gw = torch.empty_like(rbf_w) if want_rbf and prm.n_rbf else None
     gp = torch.empty_like(pos) if want_pos else None
     b = ctypes.c_size_t(0)
     _check(lib.e2f_attention_backward_workspace_size(ctx.handle, ctypes.byref(prm), n, E, ctypes.byref(b)),
            "e2f_attention_backward_workspace_size")
-    workspace = _workspace(ctx, workspace, b.value, pos.device)
-    _check(lib.e2f_attention_backward(ctx.handle, ctypes.byref(prm), _ptr(pos), _ptr(graph_id), _ptr(q), _ptr(k), n,
-                                      _ptr(rbf_w), _ptr(row_ptr), _ptr(col_idx), E, _ptr(row_t), _ptr(col_t),
-                                      _ptr(perm), _ptr(alpha), _ptr(lse), _ptr(grad_alpha), _ptr(gq), _ptr(gk),
-                                      _ptr(gw), _ptr(gp), _ptr(workspace), workspace.numel(), _stream(pos.device)),
+    workspace = _workspace(ctx, workspace, b.value, dev)
+    _check(lib.e2f_attention_backward(ctx.handle, ctypes.byref(prm), *args, *read,
+                                      *(None if t is None else t.data_ptr() for t in (gq, gk, gw, gp)),
+                                      workspace.data_ptr(), workspace.numel(), _stream(dev)),
            "e2f_attention_backward")
     return gq, gk, gw, gp
 
 
-def _norm_params(x, lmax, block, gate, post_w, res_scale, pre_w, eps):
-    if not x.is_cuda or x.dtype not in _DTYPES or not x.is_contiguous():
-        raise ValueError("x must be a contiguous float32 or bfloat16 device tensor")
-    if x.dim() == 2 and lmax == 0:
-        n, C = x.shape
-    else:
-        n, K, C = x.shape
-        if K != (lmax + 1) ** 2:
-            raise ValueError("x must be [n, (lmax+1)^2, C]")
-    _dev(block, x.dtype, "block")
-    _dev(gate, x.dtype, "gate")
-    if block is not None and block.shape != x.shape:
-        raise ValueError("block must have x's shape")
+def _norm_args(ctx, x, lmax, block, gate, post_w, res_scale, pre_w, eps):
+    """The parameters, and the addresses of what both directions read."""
+    dt, shape = x.dtype, x.shape
+    if dt not in _DTYPES:
+        raise ValueError("x must be float32 or bfloat16")
+    n, C = shape[0], shape[-1]
+    if shape != (n, (lmax + 1) ** 2, C) and (lmax or shape != (n, C)):
+        raise ValueError("x must be [n, (lmax+1)^2, C]")
     G = 0
     if gate is not None:
         G = 1 if gate.dim() == 2 else gate.shape[1]
-        if gate.shape[0] != n or gate.shape[-1] != C or gate.numel() != n * G * C:
-            raise ValueError("gate must be [n, gates, C]")
-    for t, name in ((post_w, "post_w"), (res_scale, "res_scale"), (pre_w, "pre_w")):
-        _dev(t, torch.float32, name)
-        if t is not None and (t.numel() != (lmax + 1) * C or t.shape[-1] != C):
-            raise ValueError("%s must be [lmax+1, C]" % name)
-    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    return NormParams(lmax, C, G, float(eps), _DTYPES[x.dtype], ptr(post_w), ptr(res_scale), ptr(pre_w)), n
+    w = [_arg(ctx, t, torch.float32, (lmax + 1, C), name)
+         for t, name in ((post_w, "post_w"), (res_scale, "res_scale"), (pre_w, "pre_w"))]
+    return NormParams(lmax, C, G, eps, _DTYPES[dt], *w), (
+        _arg(ctx, x, dt, shape, "x"), _arg(ctx, block, dt, shape, "block"),
+        _arg(ctx, gate, dt, (n, C) if gate is not None and gate.dim() == 2 else (n, G, C), "gate"))
 
 
 def e2f_block_norm_forward(ctx, x, lmax, block=None, gate=None, post_w=None, res_scale=None, pre_w=None, eps=1e-5,
@@ -451,18 +437,17 @@ def e2f_block_norm_forward(ctx, x, lmax, block=None, gate=None, post_w=None, res
     normed like x, or None without pre_w; rstd [n, 2] float32 for the backward).
     x, block [n, (lmax+1)^2, C] (lmax = 0: also [n, C]) float32 or bfloat16; gate
     [n, 1 or lmax+1, C] of x's type; post_w, res_scale, pre_w [lmax+1, C] float32."""
-    prm, n = _norm_params(x, lmax, block, gate, post_w, res_scale, pre_w, eps)
+    prm, args = _norm_args(ctx, x, lmax, block, gate, post_w, res_scale, pre_w, eps)
+    n = x.shape[0]
     if block is not None and out is None:
         out = torch.empty_like(x)
     if pre_w is not None and normed is None:
         normed = torch.empty_like(x)
-    for t, name in ((out, "out"), (normed, "normed")):
-        _dev(t, x.dtype, name)
-        if t is not None and t.shape != x.shape:
-            raise ValueError("%s must have x's shape" % name)
     rstd = torch.empty(n, 2, dtype=torch.float32, device=x.device)
-    _check(lib.e2f_block_norm_forward(ctx.handle, ctypes.byref(prm), _ptr(x), _ptr(block), _ptr(gate), n, _ptr(out),
-                                      _ptr(normed), _ptr(rstd), _stream(x.device)), "e2f_block_norm_forward")
+    _check(lib.e2f_block_norm_forward(ctx.handle, ctypes.byref(prm), *args, n,
+                                      _arg(ctx, out, x.dtype, x.shape, "out"),
+                                      _arg(ctx, normed, x.dtype, x.shape, "normed"), rstd.data_ptr(),
+                                      _stream(x.device)), "e2f_block_norm_forward")
     return x if block is None else out, normed, rstd
 
 
@@ -471,94 +456,79 @@ def e2f_block_norm_backward(ctx, x, rstd, lmax, block=None, gate=None, post_w=No
     """Vector-Jacobian products of e2f_block_norm_forward: (grad_x, grad_block,
     grad_gate, grad_post_w, grad_res_scale, grad_pre_w), each None where the
     input is; the last three also without want_weights."""
-    prm, n = _norm_params(x, lmax, block, gate, post_w, res_scale, pre_w, eps)
-    _dev(rstd, torch.float32, "rstd")
-    _shape(rstd, (n, 2), "rstd")
-    for t, name in ((grad_out, "grad_out"), (grad_normed, "grad_normed")):
-        _dev(t, x.dtype, name)
-        if t is not None and t.shape != x.shape:
-            raise ValueError("%s must have x's shape" % name)
-    like = lambda t: None if t is None else torch.empty_like(t)  # noqa: E731
-    gx, gb, gg = like(x), like(block), like(gate)
-    gw = [like(t) if want_weights else None for t in (post_w, res_scale, pre_w)]
-    nbytes = 0
-    if any(t is not None for t in gw):
+    prm, args = _norm_args(ctx, x, lmax, block, gate, post_w, res_scale, pre_w, eps)
+    n = x.shape[0]
+    read = (_arg(ctx, rstd, torch.float32, (n, 2), "rstd"), n, _arg(ctx, grad_out, x.dtype, x.shape, "grad_out"),
+            _arg(ctx, grad_normed, x.dtype, x.shape, "grad_normed"))
+    grads = [None if t is None else torch.empty_like(t) for t in (x, block, gate)]
+    grads += [None if t is None or not want_weights else torch.empty_like(t) for t in (post_w, res_scale, pre_w)]
+    space = (None, 0)
+    if any(t is not None for t in grads[3:]):
         b = ctypes.c_size_t(0)
         _check(lib.e2f_block_norm_workspace_size(ctx.handle, ctypes.byref(prm), n, ctypes.byref(b)),
                "e2f_block_norm_workspace_size")
-        nbytes = b.value
-    workspace = _workspace(ctx, workspace, nbytes, x.device)
-    _check(lib.e2f_block_norm_backward(ctx.handle, ctypes.byref(prm), _ptr(x), _ptr(block), _ptr(gate), _ptr(rstd), n,
-                                       _ptr(grad_out), _ptr(grad_normed), _ptr(gx), _ptr(gb), _ptr(gg), _ptr(gw[0]),
-                                       _ptr(gw[1]), _ptr(gw[2]), _ptr(workspace), workspace.numel(),
+        workspace = _workspace(ctx, workspace, b.value, x.device)
+        space = (workspace.data_ptr(), workspace.numel())
+    _check(lib.e2f_block_norm_backward(ctx.handle, ctypes.byref(prm), *args, *read,
+                                       *(None if t is None else t.data_ptr() for t in grads), *space,
                                        _stream(x.device)), "e2f_block_norm_backward")
-    return (gx, gb, gg, *gw)
+    return tuple(grads)
 
 
-def _tensor_list(tensors, name):
-    """Host arrays of the addresses, sizes and types of device tensors (contiguous, on one device)."""
-    count = len(tensors)
-    for t in tensors:
-        if t.dtype not in _DTYPES or not t.is_contiguous() or not t.is_cuda:
-            raise ValueError("%s must be contiguous float32 or bfloat16 device tensors" % name)
-    return ((ctypes.c_void_p * count)(*[t.data_ptr() for t in tensors]),
-            (ctypes.c_int64 * count)(*[t.numel() for t in tensors]),
-            (ctypes.c_int32 * count)(*[_DTYPES[t.dtype] for t in tensors]))
+class _TensorList:
+    """Host arrays of the addresses, sizes and types of device tensors (contiguous, on the context's device)."""
+
+    def __init__(self, ctx, tensors, name):
+        dtypes = array.array("i", [_DTYPES.get(t.dtype, -1) for t in tensors])
+        if (-1 in dtypes or not all(map(torch.Tensor.is_contiguous, tensors)) or
+                not {ctx.device}.issuperset(map(torch.Tensor.get_device, tensors))):
+            raise ValueError("%s must be contiguous float32 or bfloat16 tensors on the context's device" % name)
+        self.count = len(tensors)
+        self.keep = (array.array("Q", map(torch.Tensor.data_ptr, tensors)),
+                     array.array("q", map(torch.Tensor.numel, tensors)), dtypes)
+        self.ptrs, self.sizes, self.dtypes = (a.buffer_info()[0] for a in self.keep)
 
 
-def _grad_norm(ctx, count, ptrs, sizes, dtypes, device, sumsq, norm, workspace):
+def _grad_norm(ctx, t, device, workspace):
     b = ctypes.c_size_t(0)
-    _check(lib.e2f_grad_norm_workspace_size(ctx.handle, count, sizes, ctypes.byref(b)),
+    _check(lib.e2f_grad_norm_workspace_size(ctx.handle, t.count, t.sizes, ctypes.byref(b)),
            "e2f_grad_norm_workspace_size")
     workspace = _workspace(ctx, workspace, b.value, device)
-    _check(lib.e2f_grad_norm(ctx.handle, count, ptrs, sizes, dtypes, _ptr(sumsq), _ptr(norm), _ptr(workspace),
-                             workspace.numel(), _stream(device)), "e2f_grad_norm")
+    sumsq, norm = (torch.empty((), dtype=d, device=device) for d in (torch.float64, torch.float32))
+    _check(lib.e2f_grad_norm(ctx.handle, t.count, t.ptrs, t.sizes, t.dtypes, _ptr(sumsq), _ptr(norm),
+                             _ptr(workspace), workspace.numel(), _stream(device)), "e2f_grad_norm")
+    return sumsq, norm
 
 
-def _device_of(ctx, tensors):
-    return tensors[0].device if tensors else torch.device("cuda", max(ctx.device, 0))
+def _grad_clip(ctx, t, outs, sumsq, max_norm, device):
+    to = t if outs is None else _TensorList(ctx, outs, "outs")
+    if to.keep[1:] != t.keep[1:]:
+        raise ValueError("outs must have the tensors' sizes and types")
+    _check(lib.e2f_grad_clip(ctx.handle, t.count, t.ptrs, to.ptrs, t.sizes, t.dtypes, _ptr(sumsq), float(max_norm),
+                             _stream(device)), "e2f_grad_clip")
 
 
 def e2f_grad_norm(ctx, tensors, workspace=None):
     """The norm over all values of the tensors: (sumsq float64, norm float32),
     device tensors without dimensions.  Ranks that hold parts add sumsq."""
-    dev = _device_of(ctx, tensors)
-    ptrs, sizes, dtypes = _tensor_list(tensors, "tensors")
-    sumsq, norm = (torch.empty((), dtype=t, device=dev) for t in (torch.float64, torch.float32))
-    _grad_norm(ctx, len(tensors), ptrs, sizes, dtypes, dev, sumsq, norm, workspace)
-    return sumsq, norm
-
-
-def _outs(tensors, outs, ptrs, sizes, dtypes):
-    if outs is None:
-        return ptrs
-    to, to_sizes, to_dtypes = _tensor_list(outs, "outs")
-    if bytes(to_sizes) != bytes(sizes) or bytes(to_dtypes) != bytes(dtypes):
-        raise ValueError("outs must have the tensors' sizes and types")
-    return to
+    return _grad_norm(ctx, _TensorList(ctx, tensors, "tensors"), torch.device("cuda", ctx.device), workspace)
 
 
 def e2f_grad_clip(ctx, tensors, sumsq, max_norm, outs=None):
     """outs[t] = tensors[t] * min(1, max_norm / (sqrt(sumsq) + 1e-6)), in place
     without outs; sumsq: e2f_grad_norm's (or the sum of several ranks')."""
-    _dev(sumsq, torch.float64, "sumsq")
-    ptrs, sizes, dtypes = _tensor_list(tensors, "tensors")
-    to = _outs(tensors, outs, ptrs, sizes, dtypes)
-    _check(lib.e2f_grad_clip(ctx.handle, len(tensors), ptrs, to, sizes, dtypes, _ptr(sumsq), float(max_norm),
-                             _stream(_device_of(ctx, tensors))), "e2f_grad_clip")
+    _arg(ctx, sumsq, torch.float64, (), "sumsq")
+    _grad_clip(ctx, _TensorList(ctx, tensors, "tensors"), outs, sumsq, max_norm, torch.device("cuda", ctx.device))
     return tensors if outs is None else outs
 
 
 def e2f_clip_grad_norm(ctx, tensors, max_norm, outs=None, workspace=None):
     """e2f_grad_norm and e2f_grad_clip of the same tensors; returns the norm
     before clipping (float32, a device tensor without dimensions)."""
-    dev = _device_of(ctx, tensors)
-    ptrs, sizes, dtypes = _tensor_list(tensors, "tensors")
-    to = _outs(tensors, outs, ptrs, sizes, dtypes)
-    sumsq, norm = (torch.empty((), dtype=t, device=dev) for t in (torch.float64, torch.float32))
-    _grad_norm(ctx, len(tensors), ptrs, sizes, dtypes, dev, sumsq, norm, workspace)
-    _check(lib.e2f_grad_clip(ctx.handle, len(tensors), ptrs, to, sizes, dtypes, _ptr(sumsq), float(max_norm),
-                             _stream(dev)), "e2f_grad_clip")
+    device = torch.device("cuda", ctx.device)
+    t = _TensorList(ctx, tensors, "tensors")
+    sumsq, norm = _grad_norm(ctx, t, device, workspace)
+    _grad_clip(ctx, t, outs, sumsq, max_norm, device)
     return norm
 
 

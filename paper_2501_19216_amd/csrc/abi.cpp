@@ -1777,32 +1777,27 @@ e2f_status e2f_grad_clip(e2f_ctx* ctx, int32_t count, const void* const* tensors
     return rs;
   if (!sumsq) return fail(E2F_EINVAL, "sumsq is required");
   if (!finite_pos(max_norm)) return fail(E2F_EINVAL, "max_norm must be finite and positive");
-  // no output overlaps another tensor: sorted by address, each range ends before the next begins, unless
-  // both are only read or they are one tensor's, in place
+  // no output overlaps another tensor: the outputs, sorted by address, each end before the next begins, and an input
+  // that is not its own output lies between two of them
   struct Range {
     const char* lo;
     const char* hi;
-    int tensor;
-    bool out;
   };
   try {
     std::vector<Range> r;
-    r.reserve(2 * (size_t)count);
-    for (int i = 0; i < count; ++i) {
-      if (sizes[i] == 0) continue;
-      const size_t b = (size_t)sizes[i] * (dtypes[i] == E2F_BF16 ? 2 : 4);
-      const char* o = (const char*)outs[i];
-      r.push_back({o, o + b, i, true});
-      const char* t = (const char*)tensors[i];
-      if (t != o) r.push_back({t, t + b, i, false});
-    }
+    r.reserve((size_t)count);
+    for (int i = 0; i < count; ++i)
+      if (sizes[i]) r.push_back({(const char*)outs[i], (const char*)outs[i] + sizes[i] * (dtypes[i] == E2F_BF16 ? 2 : 4)});
     auto less = [](const Range& a, const Range& b) { return a.lo < b.lo; };
     if (!std::is_sorted(r.begin(), r.end(), less)) std::sort(r.begin(), r.end(), less);
-    const char *any = nullptr, *written = nullptr;  // ends of what came before, and of what of it is written
-    for (const Range& x : r) {
-      if (x.lo < written || (x.out && x.lo < any)) return fail(E2F_EINVAL, "an output overlaps another tensor");
-      any = std::max(any, x.hi);
-      if (x.out) written = std::max(written, x.hi);
+    for (size_t i = 1; i < r.size(); ++i)
+      if (r[i].lo < r[i - 1].hi) return fail(E2F_EINVAL, "two outputs overlap");
+    for (int i = 0; i < count; ++i) {
+      const char* lo = (const char*)tensors[i];
+      const char* hi = lo + sizes[i] * (dtypes[i] == E2F_BF16 ? 2 : 4);
+      if (!sizes[i] || tensors[i] == outs[i] || hi <= r.front().lo || lo >= r.back().hi) continue;
+      const auto next = std::lower_bound(r.begin(), r.end(), Range{hi, hi}, less);  // the first that begins behind it
+      if (next != r.begin() && lo < (next - 1)->hi) return fail(E2F_EINVAL, "an output overlaps another tensor");
     }
   } catch (const std::exception&) {
     return fail(E2F_ENOMEM, "host memory for %d tensors", count);

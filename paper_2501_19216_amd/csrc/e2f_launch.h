@@ -250,15 +250,6 @@ hipError_t launch_norm_forward(int L, bool bf16, const NormArgs& a, void* out, v
 hipError_t launch_norm_backward(int L, bool bf16, const NormArgs& a, const NormGrad& g, hipStream_t s);
 
 // ---- the norm over many tensors and their clipping (grad_clip.hip)
-constexpr int kTableMax = 128;  // tensors of one launch: its arguments stay below 4 KB
-struct TensorTable {
-  const void* in[kTableMax];
-  void* out[kTableMax];
-  int64_t n[kTableMax];
-  int first[kTableMax];  // first workgroup
-  unsigned bf16[kTableMax / 32];
-  int count;
-};
 int64_t grad_chunk(int64_t total);  // values of a workgroup
 // part: a double for every workgroup (the chunks of every tensor)
 hipError_t launch_grad_norm(int count, const void* const* in, const int64_t* n, const int32_t* dtype, int64_t total,
