@@ -153,7 +153,9 @@ __device__ __forceinline__ Group group_of(const AttnArgs& a, const AttnShape& s,
   return g;
 }
 
-constexpr int kLd = 17;  // floats of an entry's scores in the LDS (up to 16 heads; odd: other banks)
+// floats of an entry's scores in the LDS: 9 (up to 8 heads, in the forward, where the LDS bounds the waves of a CU: five
+// instead of four a SIMD, 109 us instead of 126 for 1.5 million edges of 8 heads) or 17 (up to 16); odd: other banks
+constexpr int kLd = 17;
 
 // Lanes over a group's heads (hp, their number's next power of two) and over 64 / hp entries: a head belongs to a lane
 struct Lanes {
@@ -254,7 +256,8 @@ struct Features {
       }
     }
   }
-  // s[entry * kLd] = the sum over a head's lph lanes of q . k, by its first lane
+  // s[entry * LD] = the sum over a head's lph lanes of q . k, by its first lane
+  template <int LD>
   __device__ __forceinline__ void dots(const float (&q)[F::VEC], int lph, bool first, float* s, int part) {
     float x[IT];
 #pragma unroll
@@ -275,7 +278,7 @@ struct Features {
     if (LPE > 32 && lph > 32) add([](float v) { float p, q; lane_halves<32>(v, p, q); return p + q; });
     if (first) {
 #pragma unroll
-      for (int i = 0; i < IT; ++i) s[entry(part, i) * kLd] = x[i];
+      for (int i = 0; i < IT; ++i) s[entry(part, i) * LD] = x[i];
     }
   }
   // acc += sum over the lane's entries of w[entry * kLd] k
@@ -314,10 +317,10 @@ __device__ __forceinline__ void read_q(const AttnArgs& a, int64_t i, int h, cons
   for (int u = 0; u < F::VEC; ++u) q[u] = a.scale * F::at(r, u);
 }
 
-// The products scale q . k of a block's entries with every head of the group: s[entry * kLd + head].  ONE: a lane has
+// The products scale q . k of a block's entries with every head of the group: s[entry * LD + head].  ONE: a lane has
 // one head (q1 its features), all or none of a load's features; else `units` times 64 lanes for k, and `share` heads each.  k is left in f where f
 // holds all of it.
-template <int LPE, bool ONE, typename F>
+template <int LPE, bool ONE, int LD, typename F>
 __device__ __forceinline__ void products(const AttnArgs& a, const AttnShape& sh, const Group& g, int64_t i,
                                          const float (&q1)[F::VEC], Features<LPE, F>& f, const int* jj, float* s) {
   for (int u = 0; u < (ONE ? 1 : sh.units); ++u) {
@@ -327,21 +330,23 @@ __device__ __forceinline__ void products(const AttnArgs& a, const AttnShape& sh,
     for (int part = 0; part < f.PARTS; ++part) {
       f.template read<ONE>(k, a.ldk, jj, part, p.count);
       if constexpr (ONE) {
-        f.dots(q1, sh.lph, p.t == 0 && p.kl < g.kheads, s + p.kl, part);
+        f.template dots<LD>(q1, sh.lph, p.t == 0 && p.kl < g.kheads, s + p.kl, part);
       } else {
         for (int m = 0; m < g.share; ++m) {
           float q[F::VEC];
           read_q<F>(a, i, g.h0 + p.kl * g.share + m, p, q);
-          f.dots(q, sh.lph, p.t == 0 && p.kl < g.kheads, s + p.kl * g.share + m, part);
+          f.template dots<LD>(q, sh.lph, p.t == 0 && p.kl < g.kheads, s + p.kl * g.share + m, part);
         }
       }
     }
   }
 }
 
-// s[entry * kLd + head] of 16 entries gets its radial part (is set to it without products): the functions' values times
-// the weights wr of the lane's head (the functions 4 r + quad)
-__device__ __forceinline__ void add_radial(const AttnArgs& a, const AttnShape& sh, const Group& g, const float* dist,
+// s[entry * LD + head] of 16 entries gets its radial part (is set to it without products): the functions' values times
+// the weights wr of the lane's head (the functions 4 r + quad; zeros of a head that is not there, whose scores stay
+// what they are where there is room for them)
+template <int LD>
+__device__ __forceinline__ void add_radial(const AttnArgs& a, const float* dist,
                                            const float (&wr)[8], float inv, float* s) {
   const int lane = threadIdx.x & 63, hc = lane & 15, quad = lane >> 4;
   f4 x = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -352,10 +357,10 @@ __device__ __forceinline__ void add_radial(const AttnArgs& a, const AttnShape& s
       const float z = z0 - 4.0f * r;
       x = __builtin_amdgcn_mfma_f32_16x16x4f32(exp_fast(-z * z), wr[r], x, 0, 0, 0);
     }
-  if (hc < g.heads) {
+  if (hc < LD - 1) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      float* to = s + (quad * 4 + u) * kLd + hc;
+      float* to = s + (quad * 4 + u) * LD + hc;
       *to = a.dk ? *to + x[u] : x[u];
     }
   }
@@ -363,7 +368,7 @@ __device__ __forceinline__ void add_radial(const AttnArgs& a, const AttnShape& s
 
 constexpr int kKept = 128;  // edges of a row whose scores stay in the LDS
 
-template <int LPE, bool ONE, typename F>
+template <int LPE, bool ONE, int LD, typename F>
 __global__ __launch_bounds__(256, 4) void k_att_forward(AttnArgs a, AttnShape sh, float* alpha, float* lse) {
   extern __shared__ float sm[];
   __shared__ float join[4][2][16];
@@ -371,7 +376,7 @@ __global__ __launch_bounds__(256, 4) void k_att_forward(AttnArgs a, AttnShape sh
   const Group g = group_of(a, sh, blockIdx.y);
   const Lanes ln = lanes_of(sh, g);
   float* s = sm + wave * sh.lds;
-  float* env = s + kKept * kLd;
+  float* env = s + kKept * LD;
   int* edge = (int*)(env + kKept);
   float* dist = (float*)(edge + kKept);
   int* jj = (int*)(dist + 64);
@@ -402,7 +407,7 @@ __global__ __launch_bounds__(256, 4) void k_att_forward(AttnArgs a, AttnShape sh
     auto to_alpha = [&](int count, const float* from) {
       if (ln.on)
         for (int n = ln.entry; n < count; n += ln.per)
-          out[(uint64_t)(unsigned)edge[n] * a.H + ln.head] = from[n * kLd + ln.head];
+          out[(uint64_t)(unsigned)edge[n] * a.H + ln.head] = from[n * LD + ln.head];
     };
     for (;;) {
       unsigned e;
@@ -418,7 +423,7 @@ __global__ __launch_bounds__(256, 4) void k_att_forward(AttnArgs a, AttnShape sh
         kept = 0, spill = true;
         wave_sync();
       }
-      float* sb = s + kept * kLd;
+      float* sb = s + kept * LD;
       const bool there = j >= 0;
       float dx = 0.0f, dy = 0.0f, dz = 0.0f;
       if (there) dx = px - a.pos[3 * (int64_t)j], dy = py - a.pos[3 * (int64_t)j + 1], dz = pz - a.pos[3 * (int64_t)j + 2];
@@ -427,7 +432,7 @@ __global__ __launch_bounds__(256, 4) void k_att_forward(AttnArgs a, AttnShape sh
       wave_sync();
       if (a.dk) {
         Features<LPE, F> f;
-        for (int b = 0; b < count; b += f.BE) products<LPE, ONE, F>(a, sh, g, i, q1, f, jj + b, sb + b * kLd);
+        for (int b = 0; b < count; b += f.BE) products<LPE, ONE, LD, F>(a, sh, g, i, q1, f, jj + b, sb + b * LD);
       }
       const float d = sqrtf(dx * dx + dy * dy + dz * dz);
       dist[lane] = d;
@@ -435,7 +440,7 @@ __global__ __launch_bounds__(256, 4) void k_att_forward(AttnArgs a, AttnShape sh
       edge[kept + lane] = (int)e;
       wave_sync();
       if (a.R)
-        for (int b = 0; b < count; b += 16) add_radial(a, sh, g, dist + b, wr, inv, sb + b * kLd);
+        for (int b = 0; b < count; b += 16) add_radial<LD>(a, dist + b, wr, inv, sb + b * LD);
       wave_sync();
       // the scores, and the running maximum and sum, four entries at a time
       if (ln.on)
@@ -446,9 +451,9 @@ __global__ __launch_bounds__(256, 4) void k_att_forward(AttnArgs a, AttnShape sh
             const int n = n0 + u * ln.per;
             x[u] = -INFINITY;
             if (n < count) {
-              x[u] = a.dk || a.R ? sb[n * kLd + ln.head] : 0.0f;
+              x[u] = a.dk || a.R ? sb[n * LD + ln.head] : 0.0f;
               if (a.cap > 0.0f) x[u] = a.cap * tanh_near(x[u] * icap);
-              sb[n * kLd + ln.head] = x[u];
+              sb[n * LD + ln.head] = x[u];
             }
             mx = fmaxf(mx, x[u]);
           }
@@ -483,7 +488,7 @@ __global__ __launch_bounds__(256, 4) void k_att_forward(AttnArgs a, AttnShape sh
     if (!spill) {
       if (ln.on)
         for (int n = ln.entry; n < kept; n += ln.per)
-          out[(uint64_t)(unsigned)edge[n] * a.H + ln.head] = env[n] * exp_fast(s[n * kLd + ln.head] - l);
+          out[(uint64_t)(unsigned)edge[n] * a.H + ln.head] = env[n] * exp_fast(s[n * LD + ln.head] - l);
       wave_sync();  // (before the next row's scores)
       continue;
     }
@@ -519,7 +524,8 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // (a scalar)
   const Group g = group_of(a, sh, blockIdx.y);
   const Lanes ln = lanes_of(sh, g);
-  float* s = sm + wave * sh.lds;  // [64][kLd] scores, then ds
+  float* s = sm + wave * sh.lds;  // [64][kLd] scores, then ds; heads that are not there stay 0
+  for (int x = lane; x < 64 * kLd; x += 64) s[x] = 0.0f;
   float* dist = s + 64 * kLd;
   float* env = dist + 64;
   float* slope = env + 64;
@@ -611,10 +617,10 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
           }
         };
         read_ga(0);
-        if (a.dk) products<LPE, ONE, F>(a, sh, g, i, q1, f, jj + b0, sb);
+        if (a.dk) products<LPE, ONE, kLd, F>(a, sh, g, i, q1, f, jj + b0, sb);
         wave_sync();
         if (a.R)
-          for (int b = 0; b < many; b += 16) add_radial(a, sh, g, dist + b0 + b, wr, inv, sb + b * kLd);
+          for (int b = 0; b < many; b += 16) add_radial<kLd>(a, dist + b0 + b, wr, inv, sb + b * kLd);
         wave_sync();
         // ds, and the envelope's part of the distances' gradients, four entries at a time
         for (int c = 0; c < f.BE; c += 4 * ln.per) {
@@ -659,14 +665,14 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
                   for (int k = 0; k < 4; ++k)
                     if (4 * k < g.heads)
                       us = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                          4 * k + quad < g.heads ? sb[(b + hc) * kLd + 4 * k + quad] : 0.0f, wt[r][k], us, 0, 0, 0);
+                          sb[(b + hc) * kLd + 4 * k + quad], wt[r][k], us, 0, 0, 0);
                 }
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                   const int n = b + quad * 4 + u;
                   const float z = dist[b0 + n] * inv - (float)(16 * r + hc), gz = exp_fast(-z * z);
                   dd[u] += us[u] * gz * z;
-                  dw[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(gz, hc < g.heads ? sb[n * kLd + hc] : 0.0f, dw[r], 0, 0, 0);
+                  dw[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(gz, sb[n * kLd + hc], dw[r], 0, 0, 0);
                 }
               }
             if (gr.gpos) {
@@ -718,7 +724,7 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
 #pragma unroll
       for (int u = 0; u < F::VEC; ++u) dq[u] = a.scale * classes_all(dq[u], LPE, [](float x, float y) { return x + y; });
       if (sh.wpr > 1) {
-        float* mine = sm + wave * sh.lds;
+        float* mine = dist;  // (what follows s: 640 floats that the row has done with)
         __syncthreads();
         if (lane < LPE) {
 #pragma unroll
@@ -728,8 +734,8 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
         if (wave == 0 && lane < LPE) {
 #pragma unroll
           for (int u = 0; u < F::VEC; ++u)
-            dq[u] = sm[lane * F::VEC + u] + sm[sh.lds + lane * F::VEC + u] + sm[2 * sh.lds + lane * F::VEC + u] +
-                    sm[3 * sh.lds + lane * F::VEC + u];
+            dq[u] = dist[lane * F::VEC + u] + dist[sh.lds + lane * F::VEC + u] + dist[2 * sh.lds + lane * F::VEC + u] +
+                    dist[3 * sh.lds + lane * F::VEC + u];
         }
         __syncthreads();
       }
@@ -1139,11 +1145,16 @@ int attention_record(const AttnArgs& a, int* force) {
 hipError_t launch_att_forward(const AttnArgs& a, float* alpha, float* lse, hipStream_t s) {
   if (a.n == 0) return hipSuccess;
   AttnShape sh = shape_of(a, false);
-  sh.lds = kKept * (kLd + 2) + 64 + 64 + 256;
+  const bool few = sh.heads <= 8;
+  sh.lds = kKept * ((few ? 9 : kLd) + 2) + 64 + 64 + 256;
   sh.rows = sh.wpr == 1 ? 4 : 1;
   const dim3 grid((unsigned)((a.n + sh.rows - 1) / sh.rows), (unsigned)sh.groups);
   const size_t lds = sizeof(float) * 4 * sh.lds;
-#define E2F_ATT(P, ONE, F) k_att_forward<P, ONE, F><<<grid, 256, lds, s>>>(a, sh, alpha, lse)
+#define E2F_ATT(P, ONE, F)                                              \
+  if (few)                                                              \
+    k_att_forward<P, ONE, 9, F><<<grid, 256, lds, s>>>(a, sh, alpha, lse); \
+  else                                                                  \
+    k_att_forward<P, ONE, kLd, F><<<grid, 256, lds, s>>>(a, sh, alpha, lse)
   E2F_ATT_SWITCH
 #undef E2F_ATT
   return hipGetLastError();
