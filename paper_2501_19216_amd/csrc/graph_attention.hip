@@ -369,7 +369,7 @@ __device__ __forceinline__ void add_radial(const AttnArgs& a, const float* dist,
 constexpr int kKept = 128;  // edges of a row whose scores stay in the LDS
 
 template <int LPE, bool ONE, int LD, typename F>
-__global__ __launch_bounds__(256, 4) void k_att_forward(AttnArgs a, AttnShape sh, float* alpha, float* lse) {
+__global__ __launch_bounds__(256, ONE && LD == 9 ? 5 : 4) void k_att_forward(AttnArgs a, AttnShape sh, float* alpha, float* lse) {
   extern __shared__ float sm[];
   __shared__ float join[4][2][16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // (a scalar)
