@@ -163,9 +163,11 @@ typedef struct {
  * (unused if dk = 0); rbf_w float32 [H][n_rbf]; alpha float32 [n_edges][H];
  * lse float32 [n][H], kept for the backward.  Sums and statistics are float32.
  * Without a cap, for float32 features and one graph the weights are those of
- * e2f_attention_weights with q scaled.  The CSR is trusted for values but read
- * with clamped indices.  Asynchronous, no allocation, can be captured in a HIP
- * graph; deterministic. */
+ * e2f_attention_weights with q scaled (up to rounding).  The CSR is trusted for
+ * values but read with clamped indices.  Rows are gathered from k in index order
+ * of the atoms: where atoms that are near have near indices the gathers hit the
+ * caches.  Outputs must not overlap inputs.  Asynchronous, no allocation, can be
+ * captured in a HIP graph; deterministic. */
 e2f_status e2f_attention_forward(e2f_ctx* ctx, const e2f_attention_params* params, const float* pos,
                                  const int32_t* graph_id, const void* q, const void* k, int32_t n,
                                  const float* rbf_w, const int64_t* row_ptr, const int32_t* col_idx, int64_t n_edges,
@@ -495,7 +497,9 @@ e2f_status e2f_last_slices(const e2f_ctx* ctx, int64_t* slices /* host */);
 /* Kernel timing.  e2f_profile(ctx, 1) waits for the device, clears the
  * records and starts bracketing every launch group of this context with HIP
  * events on its stream (bbox, nl_count, nl_fill, tile_plan, sh, node_tp,
- * aggregate, recouple, mix, edge_tp); e2f_profile(ctx, 0) stops.  (sync) */
+ * aggregate, recouple, mix, edge_tp, attention, attention_grad, transpose,
+ * block_norm, block_norm_grad, grad_norm, grad_clip and others);
+ * e2f_profile(ctx, 0) stops.  (sync) */
 e2f_status e2f_profile(e2f_ctx* ctx, int enable);
 /* Text "name launches total_ms" per line for the records so far, into buf
  * (host, `bytes` long, NUL-terminated); E2F_ECAPACITY if too small.  (sync) */

@@ -1435,6 +1435,9 @@ e2f_status e2f_wigner6j_conv_forward_global(e2f_ctx* ctx, const e2f_conv_params*
 // ---- the operators around the convolution: capped attention, norms, clipping
 namespace {
 
+// atoms whose numbers, rounded up to whole workgroups, stay in 32 bits
+constexpr int32_t kMaxAtoms = std::numeric_limits<int32_t>::max() - 4096;
+
 e2f_status check_workspace(const void* ws, size_t have, size_t need) {
   if (need == 0) return E2F_OK;
   if (!ws || have < need) return fail(E2F_ECAPACITY, "workspace of %zu bytes is required", need);
@@ -1458,6 +1461,7 @@ e2f_status check_edges(e2f_ctx* ctx, int32_t n, int64_t n_edges) {
   if (!ctx) return fail(E2F_EINVAL, "ctx is NULL");
   if (n < 0 || n_edges < 0) return fail(E2F_EINVAL, "n or n_edges < 0");
   if (n == 0 && n_edges > 0) return fail(E2F_EINVAL, "edges without atoms");
+  if (n > kMaxAtoms) return fail(E2F_EUNSUPPORTED, "n = %d > %d", n, kMaxAtoms);
   if (n_edges > std::numeric_limits<int32_t>::max()) return fail(E2F_EUNSUPPORTED, "more than 2^31-1 edges");
   return E2F_OK;
 }
@@ -1523,6 +1527,7 @@ e2f_status check_norm(e2f_ctx* ctx, const e2f_norm_params* p, int32_t n) {
   if (!ctx) return fail(E2F_EINVAL, "ctx is NULL");
   if (!p) return fail(E2F_EINVAL, "params is NULL");
   if (n < 0) return fail(E2F_EINVAL, "n < 0");
+  if (n > kMaxAtoms) return fail(E2F_EUNSUPPORTED, "n = %d > %d", n, kMaxAtoms);
   if (p->lmax < 0) return fail(E2F_EINVAL, "lmax = %d < 0", p->lmax);
   if (p->lmax > kMaxL) return fail(E2F_EUNSUPPORTED, "lmax = %d > %d", p->lmax, kMaxL);
   if (p->channels < 4 || p->channels % 4 || p->channels > 1024)

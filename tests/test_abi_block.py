@@ -54,7 +54,7 @@ def test_attention_refusals(e2f, ctx):
                    dict(ldk=15), dict(ldq=-32), dict(n=-1), dict(edges=-1), dict(n=0), dict(pos=None), dict(q=None),
                    dict(k=None), dict(w=None), dict(rp=None), dict(ci=None), dict(alpha=None)):
             assert call(**kw) == EINVAL, kw
-        for kw in (dict(heads=65, k_heads=65), dict(dk=257), dict(n_rbf=33), dict(edges=2 ** 31)):
+        for kw in (dict(heads=65, k_heads=65), dict(dk=257), dict(n_rbf=33), dict(edges=2 ** 31), dict(n=2 ** 31 - 1)):
             assert call(**kw) == EUNS, kw
         for kw in (dict(ldq=32, ldk=16), dict(ldq=4096), dict(cap=0.0), dict(dtype=1), dict(n_rbf=0, w=None, **(dict(gw=None) if call is bwd else {})),
                    dict(dk=0, q=None, k=None, **(dict(gq=None, gk=None) if call is bwd else {}))):
@@ -87,7 +87,7 @@ def test_transpose_refusals(e2f, ctx):
     for kw in (dict(n=-1), dict(edges=-1), dict(n=0), dict(rp=None), dict(ci=None), dict(rt=None), dict(ct=None),
                dict(pm=None), dict(handle=None), dict(ws=at((1 << 20) + 8))):
         assert call(**kw) == EINVAL, kw
-    assert call(edges=2 ** 31) == EUNS
+    assert call(edges=2 ** 31) == EUNS and call(n=2 ** 31 - 1) == EUNS
     assert call(edges=0, ci=None, ct=None, pm=None) == EDEV
     b = ctypes.c_size_t(0)
     assert lib.e2f_transpose_graph_workspace_size(ctx.handle, 10, 30, ctypes.byref(b)) == e2f.E2F_OK
@@ -121,7 +121,7 @@ def test_norm_refusals(e2f, ctx):
         for kw in (dict(n=-1), dict(lmax=-1), dict(gates=2), dict(gates=-1), dict(eps=-1.0), dict(eps=float("nan")),
                    dict(dtype=2), dict(x=None), dict(gate=None), dict(gates=0), dict(block=None)):
             assert call(**kw) == EINVAL, kw
-        for kw in (dict(lmax=7), dict(channels=0), dict(channels=18), dict(channels=1028)):
+        for kw in (dict(lmax=7), dict(channels=0), dict(channels=18), dict(channels=1028), dict(n=2 ** 31 - 1)):
             assert call(**kw) == EUNS, kw
         assert call(gates=3) == EDEV and call(dtype=1) == EDEV and call(eps=0.0) == EDEV
     assert fwd(handle=None) == EINVAL and fwd(none=True) == EINVAL

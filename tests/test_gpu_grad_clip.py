@@ -152,3 +152,24 @@ def test_more_than_2_to_the_31_values(e2f, ctx):
     norm = e2f.e2f_clip_grad_norm(ctx, [t], 6.5)
     assert float(norm) == 13.0
     assert [float(t[i]) for i in (0, 2 ** 31, n - 1)] == [2.0, 6.0, 1.5]
+
+
+@pytest.mark.parametrize("skew", [1, 2, 3, 5])
+def test_outputs_of_another_alignment(e2f, ctx, skew):
+    sizes = [40000, 5, 9000, 1031, 16384, 16385]
+    ts, _ = tensors(sizes, 4, gap=1)
+    outs = [torch.empty(s + skew + 1, dtype=t.dtype, device=DEV).fill_(7.0)[skew:-1] for s, t in zip(sizes, ts)]
+    norm = e2f.e2f_clip_grad_norm(ctx, ts, 0.5, outs=outs)
+    check(ts, outs, norm, 0.5)
+
+
+def test_lists_that_do_not_fit(e2f, ctx):
+    a, b = torch.ones(4, device=DEV), torch.ones(5, device=DEV)
+    for bad in ([torch.ones(4)], [torch.ones(4, device=DEV, dtype=torch.float64)], [torch.ones(4, 4, device=DEV).t()]):
+        with pytest.raises(ValueError):
+            e2f.e2f_grad_norm(ctx, bad)
+    for outs in ([b], [a, b], [a.bfloat16()]):
+        with pytest.raises(ValueError):
+            e2f.e2f_clip_grad_norm(ctx, [a], 1.0, outs=outs)
+    with pytest.raises(e2f.E2FError):  # the same tensor twice, in place
+        e2f.e2f_clip_grad_norm(ctx, [a, a], 1.0)

@@ -356,3 +356,40 @@ def test_malformed_graphs_stay_inside(e2f, ctx):
         t = (t[0].flip(0) * 1000 - 5, t[1] * 1000003, t[2] - 2 ** 30)
         e2f.e2f_attention_backward(ctx, d[0], d[1], d[2], 2.0, alpha[:E].contiguous(), lse[:n].contiguous(), d[6], *t, **kw)
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("H,Hk,dk,R,dtype", [(12, 12, 8, 8, torch.float32), (4, 4, 12, 16, torch.float32),
+                                             (7, 7, 24, 5, torch.float32), (3, 3, 40, 9, torch.bfloat16),
+                                             (16, 2, 16, 32, torch.float32), (24, 24, 32, 20, torch.float32),
+                                             (9, 9, 8, 4, torch.float32), (2, 1, 100, 2, torch.float32)])
+@pytest.mark.parametrize("masked", [False, True])
+def test_long_rows(e2f, ctx, H, Hk, dk, R, dtype, masked):
+    # rows of some hundred edges of one graph, by one wave and by four, lanes without a head or features
+    for n, degrees in ((620, (600, 3, 0, 1, 2, 5)), (620, (619, 400, 300))):
+        pos, rp, ci, g = graph(n, degrees, H + dk)
+        q, k, w = inputs(n, H, Hk, dk, R, dtype, g)
+        gid = (torch.arange(n) % 2).int() if masked else None
+        ga = torch.randn(ci.numel(), H, generator=g)
+        got = run(e2f, ctx, pos, rp, ci, 6.0, q, k, w, H, dk ** -0.5, 8.0, gid, ga)
+        compare(got, ref.attention(pos, rp, ci, 6.0, q, k, w, H, dk ** -0.5, 8.0, gid, ga), dtype)
+
+
+def test_arguments_that_do_not_fit(e2f, ctx):
+    n = 10
+    pos, rp, ci, g = graph(n, (3,), 1)
+    d = [dev(t) for t in (pos, rp, ci)]
+    q = torch.randn(n, 2, 4, device=DEV)
+    w = torch.randn(2, 8, device=DEV)
+    fwd = lambda **kw: e2f.e2f_attention_forward(ctx, *d, 5.0, **{**dict(q=q, k=q, rbf_w=w), **kw})  # noqa: E731
+    fwd()
+    for kw in (dict(k=None), dict(k=q.bfloat16()), dict(k=q[:5]), dict(q=q.double(), k=q.double()), dict(heads=3),
+               dict(q=q.transpose(1, 2).contiguous().transpose(1, 2)), dict(q=q[:1].expand(n, 2, 4)), dict(q=q.cpu()),
+               dict(rbf_w=w[:1]), dict(rbf_w=w.double()), dict(graph_id=torch.zeros(n, device=DEV)),
+               dict(graph_id=torch.zeros(n - 1, dtype=torch.int32, device=DEV)),
+               dict(alpha=torch.empty(3, 2, device=DEV))):
+        with pytest.raises(ValueError):
+            fwd(**kw)
+    with pytest.raises(ValueError):
+        e2f.e2f_attention_forward(ctx, d[0], d[1][:-1], d[2], 5.0, q=q, k=q)
+    with pytest.raises(e2f.E2FError):
+        fwd(cap=-1.0)
