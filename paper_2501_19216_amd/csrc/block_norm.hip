@@ -470,8 +470,8 @@ __global__ __launch_bounds__(1024) void k_norm_weights(NormArgs a, NormGrad g, i
 }
 
 // Channels of a thread: as many as keep a row's arrays in its registers (two in the forward, four in the
-// backward), in loads of up to 16 bytes.  In registers 20,000 atoms at L = 4, 128 float channels take 194 us forward
-// and 350 us backward; read again for each use from the caches, 358 and 904 us.
+// backward), in loads of up to 16 bytes.  In registers 20,000 atoms at L = 4, 128 float channels take 190 us forward
+// and 336 us backward; read again for each use from the caches, 358 and 904 us.
 int channels_per_thread(int L, int C, bool bf16, bool back) {
   if (L == 0 && bf16 && C % 8 == 0 && !back) return 8;
   if (L <= 1) return 4;

@@ -393,3 +393,21 @@ def test_arguments_that_do_not_fit(e2f, ctx):
         e2f.e2f_attention_forward(ctx, d[0], d[1][:-1], d[2], 5.0, q=q, k=q)
     with pytest.raises(e2f.E2FError):
         fwd(cap=-1.0)
+
+
+@pytest.mark.parametrize("ascending", [True, False])
+@pytest.mark.parametrize("n", [129, 130, 513, 1500, 70001])
+def test_transposed_graph_of_atoms_that_send_to_all(e2f, ctx, n, ascending):
+    # two atoms in every other row (the second's own row lists the first: one of the first's edges has a reverse), and
+    # one more sender a row; lists of 127, 128 and more, which one wave or a workgroup puts in order
+    hub, other = n // 3, n // 2
+    rows = [[] if i == hub else sorted({hub, (7 * i) % n} | ({other} if i != other else set())) for i in range(n)]
+    rows[hub] = [other]
+    if not ascending:
+        rows = [r[::-1] for r in rows]
+    rp = torch.tensor([0] + [len(r) for r in rows]).cumsum(0)
+    ci = torch.tensor([j for r in rows for j in r], dtype=torch.int32)
+    for _ in range(2):
+        got = e2f.e2f_transpose_graph(ctx, n, rp.to(DEV), ci.to(DEV))
+        for a, b in zip(got, transposed(n, rp, ci)):
+            assert torch.equal(a.cpu(), b)
