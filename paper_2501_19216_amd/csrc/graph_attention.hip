@@ -16,7 +16,9 @@
 //   - The products: lanes over an edge's features of k, 16 bytes each, so that a
 //     gather reads whole lines; the features of a head are summed over its lanes.
 //     This gather, H dk values an edge out of the caches, is what bounds both
-//     directions (1.5 million edges of 8 heads of 16 floats are 780 MB).
+//     directions (1.5 million edges of 8 heads of 16 floats are 780 MB; with 32 radial
+//     functions and 20,000 atoms forward 101 us, backward 238 for the receivers and 124
+//     for the senders, the transposed graph 86).
 //   - The radial part: float matrix products of 16 edges, 16 heads and 4 functions
 //     (v_mfma_f32_16x16x4_f32), each lane evaluating the functions it passes in.
 //   - The softmax's running maximum and sum stay with the lanes that hold a head in
