@@ -178,6 +178,7 @@ class Context:
         self.device = dev
         self.lmax_max = lmax_max
         self.workspace = None
+        self.stream_workspaces = {}
 
     def workspace_for(self, nbytes: int, device) -> torch.Tensor:
         """A device buffer of at least nbytes, kept for later calls."""
@@ -189,6 +190,7 @@ class Context:
     def close(self):
         if self.handle:
             self.workspace = None
+            self.stream_workspaces = {}
             lib.e2f_destroy(self.handle)
             self.handle = None
 
@@ -297,10 +299,16 @@ def _arg(ctx, t, dtype, shape, name):
     return t.data_ptr()
 
 
-def _workspace(ctx, workspace, nbytes, device):
-    """The caller's workspace, or the context's own grown to nbytes."""
+def _workspace(ctx, workspace, nbytes, device, stream):
+    """The caller's workspace, or the context's own for the (current) stream, grown to nbytes."""
     if workspace is None:
-        return ctx.workspace_for(nbytes, device)
+        if torch.cuda.is_current_stream_capturing():
+            raise ValueError("under graph capture the workspace must be given")
+        kept = ctx.stream_workspaces.get(stream.value)
+        if kept is None or kept.numel() < nbytes:
+            ctx.stream_workspaces[stream.value] = kept = None  # (its memory may become the larger one's)
+            ctx.stream_workspaces[stream.value] = kept = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+        return kept
     if workspace.get_device() != ctx.device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous uint8 tensor on the context's device")
     return workspace
@@ -312,18 +320,20 @@ _DTYPES = {torch.float32: E2F_F32, torch.bfloat16: E2F_BF16}
 def e2f_transpose_graph(ctx, n, row_ptr, col_idx, workspace=None):
     """The graph by senders: (rowT_ptr int64 [n+1], colT int32 [E], the
     receivers, perm int32 [E], the edges in the graph's own order).  Here and
-    below, workspace: a uint8 device tensor, or None: the context's own, which
-    grows on demand (code under graph capture gives one of its own)."""
+    below, workspace: a uint8 device tensor, or None: the context's own for the
+    current stream, which grows on demand (code under graph capture gives one
+    of its own)."""
     E, dev = col_idx.numel(), col_idx.device
     rp, ci = _arg(ctx, row_ptr, torch.int64, (n + 1,), "row_ptr"), _arg(ctx, col_idx, torch.int32, (E,), "col_idx")
     b = ctypes.c_size_t(0)
     _check(lib.e2f_transpose_graph_workspace_size(ctx.handle, n, E, ctypes.byref(b)),
            "e2f_transpose_graph_workspace_size")
-    workspace = _workspace(ctx, workspace, b.value, dev)
+    stream = _stream(dev)
+    workspace = _workspace(ctx, workspace, b.value, dev, stream)
     row_t = torch.empty(n + 1, dtype=torch.int64, device=dev)
     col_t, perm = (torch.empty(E, dtype=torch.int32, device=dev) for _ in range(2))
     _check(lib.e2f_transpose_graph(ctx.handle, n, rp, ci, E, row_t.data_ptr(), col_t.data_ptr(), perm.data_ptr(),
-                                   workspace.data_ptr(), workspace.numel(), _stream(dev)), "e2f_transpose_graph")
+                                   workspace.data_ptr(), workspace.numel(), stream), "e2f_transpose_graph")
     return row_t, col_t, perm
 
 
@@ -404,10 +414,11 @@ def e2f_attention_backward(ctx, pos, row_ptr, col_idx, cutoff, alpha, lse, grad_
     b = ctypes.c_size_t(0)
     _check(lib.e2f_attention_backward_workspace_size(ctx.handle, ctypes.byref(prm), n, E, ctypes.byref(b)),
            "e2f_attention_backward_workspace_size")
-    workspace = _workspace(ctx, workspace, b.value, dev)
+    stream = _stream(dev)
+    workspace = _workspace(ctx, workspace, b.value, dev, stream)
     _check(lib.e2f_attention_backward(ctx.handle, ctypes.byref(prm), *args, *read,
                                       *(None if t is None else t.data_ptr() for t in (gq, gk, gw, gp)),
-                                      workspace.data_ptr(), workspace.numel(), _stream(dev)),
+                                      workspace.data_ptr(), workspace.numel(), stream),
            "e2f_attention_backward")
     return gq, gk, gw, gp
 
@@ -462,16 +473,16 @@ def e2f_block_norm_backward(ctx, x, rstd, lmax, block=None, gate=None, post_w=No
             _arg(ctx, grad_normed, x.dtype, x.shape, "grad_normed"))
     grads = [None if t is None else torch.empty_like(t) for t in (x, block, gate)]
     grads += [None if t is None or not want_weights else torch.empty_like(t) for t in (post_w, res_scale, pre_w)]
-    space = (None, 0)
+    space, stream = (None, 0), _stream(x.device)
     if any(t is not None for t in grads[3:]):
         b = ctypes.c_size_t(0)
         _check(lib.e2f_block_norm_workspace_size(ctx.handle, ctypes.byref(prm), n, ctypes.byref(b)),
                "e2f_block_norm_workspace_size")
-        workspace = _workspace(ctx, workspace, b.value, x.device)
+        workspace = _workspace(ctx, workspace, b.value, x.device, stream)
         space = (workspace.data_ptr(), workspace.numel())
     _check(lib.e2f_block_norm_backward(ctx.handle, ctypes.byref(prm), *args, *read,
                                        *(None if t is None else t.data_ptr() for t in grads), *space,
-                                       _stream(x.device)), "e2f_block_norm_backward")
+                                       stream), "e2f_block_norm_backward")
     return tuple(grads)
 
 
@@ -489,36 +500,37 @@ class _TensorList:
         self.ptrs, self.sizes, self.dtypes = (a.buffer_info()[0] for a in self.keep)
 
 
-def _grad_norm(ctx, t, device, workspace):
+def _grad_norm(ctx, t, device, workspace, stream):
     b = ctypes.c_size_t(0)
     _check(lib.e2f_grad_norm_workspace_size(ctx.handle, t.count, t.sizes, ctypes.byref(b)),
            "e2f_grad_norm_workspace_size")
-    workspace = _workspace(ctx, workspace, b.value, device)
+    workspace = _workspace(ctx, workspace, b.value, device, stream)
     sumsq, norm = (torch.empty((), dtype=d, device=device) for d in (torch.float64, torch.float32))
     _check(lib.e2f_grad_norm(ctx.handle, t.count, t.ptrs, t.sizes, t.dtypes, _ptr(sumsq), _ptr(norm),
-                             _ptr(workspace), workspace.numel(), _stream(device)), "e2f_grad_norm")
+                             _ptr(workspace), workspace.numel(), stream), "e2f_grad_norm")
     return sumsq, norm
 
 
-def _grad_clip(ctx, t, outs, sumsq, max_norm, device):
+def _grad_clip(ctx, t, outs, sumsq, max_norm, stream):
     to = t if outs is None else _TensorList(ctx, outs, "outs")
     if to.keep[1:] != t.keep[1:]:
         raise ValueError("outs must have the tensors' sizes and types")
     _check(lib.e2f_grad_clip(ctx.handle, t.count, t.ptrs, to.ptrs, t.sizes, t.dtypes, _ptr(sumsq), float(max_norm),
-                             _stream(device)), "e2f_grad_clip")
+                             stream), "e2f_grad_clip")
 
 
 def e2f_grad_norm(ctx, tensors, workspace=None):
     """The norm over all values of the tensors: (sumsq float64, norm float32),
     device tensors without dimensions.  Ranks that hold parts add sumsq."""
-    return _grad_norm(ctx, _TensorList(ctx, tensors, "tensors"), torch.device("cuda", ctx.device), workspace)
+    device = torch.device("cuda", ctx.device)
+    return _grad_norm(ctx, _TensorList(ctx, tensors, "tensors"), device, workspace, _stream(device))
 
 
 def e2f_grad_clip(ctx, tensors, sumsq, max_norm, outs=None):
     """outs[t] = tensors[t] * min(1, max_norm / (sqrt(sumsq) + 1e-6)), in place
     without outs; sumsq: e2f_grad_norm's (or the sum of several ranks')."""
     _arg(ctx, sumsq, torch.float64, (), "sumsq")
-    _grad_clip(ctx, _TensorList(ctx, tensors, "tensors"), outs, sumsq, max_norm, torch.device("cuda", ctx.device))
+    _grad_clip(ctx, _TensorList(ctx, tensors, "tensors"), outs, sumsq, max_norm, _stream(sumsq.device))
     return tensors if outs is None else outs
 
 
@@ -527,8 +539,9 @@ def e2f_clip_grad_norm(ctx, tensors, max_norm, outs=None, workspace=None):
     before clipping (float32, a device tensor without dimensions)."""
     device = torch.device("cuda", ctx.device)
     t = _TensorList(ctx, tensors, "tensors")
-    sumsq, norm = _grad_norm(ctx, t, device, workspace)
-    _grad_clip(ctx, t, outs, sumsq, max_norm, device)
+    stream = _stream(device)
+    sumsq, norm = _grad_norm(ctx, t, device, workspace, stream)
+    _grad_clip(ctx, t, outs, sumsq, max_norm, stream)
     return norm
 
 

@@ -173,3 +173,32 @@ def test_lists_that_do_not_fit(e2f, ctx):
             e2f.e2f_clip_grad_norm(ctx, [a], 1.0, outs=outs)
     with pytest.raises(e2f.E2FError):  # the same tensor twice, in place
         e2f.e2f_clip_grad_norm(ctx, [a, a], 1.0)
+
+
+def test_two_streams_at_once_without_a_workspace(e2f, ctx):
+    # each stream has its own partial sums; the second list needs more of them than the first
+    lists = [tensors([60001] * 50, 11)[0], tensors([90001] * 70, 12)[0]]
+    want = [[t.clone() for t in e2f.e2f_grad_norm(ctx, ts)] for ts in lists]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in lists]
+    got = []
+    for _ in range(10):
+        for ts, side in zip(lists, streams):
+            with torch.cuda.stream(side):
+                got.append(e2f.e2f_grad_norm(ctx, ts))
+    torch.cuda.synchronize()
+    for i, (sumsq, norm) in enumerate(got):
+        assert torch.equal(sumsq, want[i % 2][0]) and torch.equal(norm, want[i % 2][1]), i
+
+
+def test_capture_needs_a_workspace(e2f, ctx):
+    ts = tensors([100], 13)[0]
+    e2f.e2f_grad_norm(ctx, ts)  # (not the context's own either, once there is one)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = torch.zeros(1, device=DEV)
+        with pytest.raises(ValueError, match="capture"):
+            e2f.e2f_grad_norm(ctx, ts)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert out.item() == 0.0
