@@ -159,7 +159,8 @@ typedef struct {
  *   lse[i][h] = log(sum over row i of exp(s)).
  * graph_id [n] or NULL: an edge between atoms of different ids has alpha = 0,
  * takes no part in the sums, and what its sender holds is not looked at; a row
- * left without an edge has lse = -infinity.  q [n][H][dk], k [n][k_heads][dk]
+ * left without an edge has lse = -infinity.  A score of -infinity beside others has
+ * alpha = 0; where all of a row's are, lse = -infinity and alpha is NaN (0 / 0).  q [n][H][dk], k [n][k_heads][dk]
  * (unused if dk = 0); rbf_w float32 [H][n_rbf]; alpha float32 [n_edges][H];
  * lse float32 [n][H], kept for the backward.  Sums and statistics are float32.
  * Without a cap, for float32 features and one graph the weights are those of

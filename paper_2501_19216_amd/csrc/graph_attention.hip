@@ -460,9 +460,10 @@ __global__ __launch_bounds__(256, ONE && LD == 9 ? 5 : 4) void k_att_forward(Att
             mx = fmaxf(mx, x[u]);
           }
           if (mx > m) den *= exp_fast(m - mx), m = mx;
+          const float from = m == -INFINITY ? 0.0f : m;  // (scores of -infinity alone: terms of 0)
 #pragma unroll
           for (int u = 0; u < 4; ++u)
-            if (n0 + u * ln.per < count) den += exp_fast(x[u] - m);
+            if (n0 + u * ln.per < count) den += exp_fast(x[u] - from);
         }
       wave_sync();
       if (spill)

@@ -1,0 +1,95 @@
+"""Capped attention where scores are infinite, large, far apart or saturated, against float64.  Atoms at one point have
+an envelope of 1 and, without radial functions, scores that are exact by their construction: what is left are the
+roundings of the softmax itself, counted at each bound.  Run with -m gpu."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def e2f():
+    import paper_2501_19216_amd as m
+    return m
+
+
+@pytest.fixture(scope="module")
+def ctx(e2f):
+    c = e2f.e2f_create(0, 0)
+    yield c
+    c.close()
+
+
+def stars(receivers, degree):
+    """Rows of `degree` edges from senders of their own, which come behind the receivers: edge e is sent by receivers + e."""
+    E = receivers * degree
+    rp = torch.cat([torch.arange(receivers + 1) * degree, torch.full((E,), E)])
+    return receivers + E, rp.to(DEV), (receivers + torch.arange(E)).int().to(DEV)
+
+
+def from_scores(x, receivers):
+    """q [n, H, 1] of ones and k [n, H, 1] of the edges' scores x [E, H]."""
+    H = x.shape[1]
+    q = torch.ones(receivers + x.shape[0], H, 1, device=DEV)
+    return q, torch.cat([torch.zeros(receivers, H), x]).view(-1, H, 1).to(DEV)
+
+
+# a lane of eight heads takes every eighth edge, of four waves a row every 32nd: the first and last edges are single
+# ones of their lanes, and 300 edges pass the 128 whose scores stay in the LDS
+@pytest.mark.parametrize("receivers,degree", [(40, 1), (40, 5), (40, 8), (40, 64), (9, 200), (3, 300), (1, 3000)])
+@pytest.mark.parametrize("H", [1, 8, 12])
+def test_scores_of_minus_infinity(e2f, ctx, receivers, degree, H):
+    g = torch.Generator().manual_seed(degree + H)
+    n, rp, ci = stars(receivers, degree)
+    x = torch.randn(receivers * degree, H, generator=g).view(receivers, degree, H)
+    r = torch.arange(receivers)
+    x[r % 5 == 0, 0] = -math.inf
+    x[r % 5 == 1, -1] = -math.inf
+    x[r % 5 == 2, degree // 2:] = -math.inf
+    x[r % 5 == 3, :, 0] = -math.inf  # all of one head's, which leave the others alone
+    x = x.reshape(-1, H)
+    q, k = from_scores(x, receivers)
+    pos = torch.zeros(n, 3, device=DEV)
+    alpha, lse = e2f.e2f_attention_forward(ctx, pos, rp, ci, 5.0, q=q, k=k)
+    s = x.double().view(receivers, degree, H)
+    want, total = torch.softmax(s, 1), torch.logsumexp(s, 1)  # (NaN and -infinity where all are -infinity)
+    got = alpha.cpu().double().view(receivers, degree, H)
+    assert torch.equal(got.isnan(), want.isnan())
+    assert torch.equal(lse.cpu().double()[:receivers] == -math.inf, total == -math.inf)
+    fine = ~want.isnan()
+    # exponentials of up to 10 and their sum, at most degree / 8 terms and eight more in a chain; lse's own rounding
+    room = U * (degree / 4 + 80)
+    assert torch.all((got - want)[fine].abs() <= room * want[fine] + 1e-37)
+    assert torch.all(got[fine & (s == -math.inf)] == 0)
+    some = total != -math.inf
+    assert torch.all((lse.cpu().double()[:receivers] - total)[some].abs() <= room * (1 + total[some].abs()))
+
+
+@pytest.mark.parametrize("receivers,degree", [(40, 5), (9, 200), (1, 3000)])
+def test_gradients_beside_scores_of_minus_infinity(e2f, ctx, receivers, degree):
+    # products that overflow: q and k are finite, so every gradient is, and that of such a score is 0
+    g = torch.Generator().manual_seed(degree)
+    n, rp, ci = stars(receivers, degree)
+    E, H = receivers * degree, 4
+    x = torch.randn(E, H, generator=g)
+    x[::3] = -3e38
+    q, k = from_scores(x, receivers)
+    ga = torch.randn(E, H, generator=g).to(DEV)
+    pos = torch.zeros(n, 3, device=DEV)
+    alpha, lse = e2f.e2f_attention_forward(ctx, pos, rp, ci, 5.0, q=q, k=k, scale=16.0)
+    t = e2f.e2f_transpose_graph(ctx, n, rp, ci)
+    gq, gk, _, gp = e2f.e2f_attention_backward(ctx, pos, rp, ci, 5.0, alpha, lse, ga, *t, q=q, k=k, scale=16.0)
+    assert torch.isfinite(alpha).all() and torch.all(alpha[::3] == 0)
+    assert torch.isfinite(gk).all() and torch.all(gk[receivers::3] == 0) and torch.all(gp == 0)
+    p = torch.softmax((16.0 * x.double()).masked_fill(x.double() < -1e38, -math.inf).view(receivers, degree, H), 1)
+    a = ga.cpu().double().view(receivers, degree, H)
+    D = (p * a).sum(1, keepdim=True)
+    want = 16.0 * p * (a - D)
+    # scores of up to 16 * 4, once rounded, in the weights and in lse; the sums of a row
+    room = U * (degree / 4 + 80 + 4 * 64) * 16.0 * p * (a.abs() + (p * a.abs()).sum(1, keepdim=True)) + 1e-36
+    got = gk[receivers:].cpu().double().view(receivers, degree, H)
+    assert torch.all((got - want).abs() <= room)
