@@ -345,10 +345,10 @@ __device__ __forceinline__ void products(const AttnArgs& a, const AttnShape& sh,
 }
 
 // s[entry * LD + head] of 16 entries gets its radial part (is set to it without products): the functions' values times
-// the weights wr of the lane's head (the functions 4 r + quad; zeros of a head that is not there, whose scores stay
-// what they are where there is room for them)
+// the weights wr of the lane's head (the functions 4 r + quad; zeros of a head that is not there, and what a distance
+// that is not finite makes of them is not kept)
 template <int LD>
-__device__ __forceinline__ void add_radial(const AttnArgs& a, const float* dist,
+__device__ __forceinline__ void add_radial(const AttnArgs& a, int heads, const float* dist,
                                            const float (&wr)[8], float inv, float* s) {
   const int lane = threadIdx.x & 63, hc = lane & 15, quad = lane >> 4;
   f4 x = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -359,7 +359,7 @@ __device__ __forceinline__ void add_radial(const AttnArgs& a, const float* dist,
       const float z = z0 - 4.0f * r;
       x = __builtin_amdgcn_mfma_f32_16x16x4f32(exp_fast(-z * z), wr[r], x, 0, 0, 0);
     }
-  if (hc < LD - 1) {
+  if (hc < heads) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       float* to = s + (quad * 4 + u) * LD + hc;
@@ -442,7 +442,7 @@ __global__ __launch_bounds__(256, ONE && LD == 9 ? 5 : 4) void k_att_forward(Att
       edge[kept + lane] = (int)e;
       wave_sync();
       if (a.R)
-        for (int b = 0; b < count; b += 16) add_radial<LD>(a, dist + b, wr, inv, sb + b * LD);
+        for (int b = 0; b < count; b += 16) add_radial<LD>(a, g.heads, dist + b, wr, inv, sb + b * LD);
       wave_sync();
       // the scores, and the running maximum and sum, four entries at a time
       if (ln.on)
@@ -623,7 +623,7 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
         if (a.dk) products<LPE, ONE, kLd, F>(a, sh, g, i, q1, f, jj + b0, sb);
         wave_sync();
         if (a.R)
-          for (int b = 0; b < many; b += 16) add_radial<kLd>(a, dist + b0 + b, wr, inv, sb + b * kLd);
+          for (int b = 0; b < many; b += 16) add_radial<kLd>(a, g.heads, dist + b0 + b, wr, inv, sb + b * kLd);
         wave_sync();
         // ds, and the envelope's part of the distances' gradients, four entries at a time
         for (int c = 0; c < f.BE; c += 4 * ln.per) {
