@@ -486,12 +486,14 @@ __global__ __launch_bounds__(256, ONE && LD == 9 ? 5 : 4) void k_att_forward(Att
         den += mk == top ? dk : dk * exp_fast(mk - top);
       }
     }
-    const float l = top + logf(den);
-    if (lse && ln.on && ln.entry == 0 && part == 0) lse[i * a.H + g.h0 + ln.head] = l;
+    // (the weights from the maximum and the sum: exp(s - lse) would carry lse's rounding, half a step of the scores,
+    // into all of a row's)
+    const float rden = 1.0f / den;
+    if (lse && ln.on && ln.entry == 0 && part == 0) lse[i * a.H + g.h0 + ln.head] = top + logf(den);
     if (!spill) {
       if (ln.on)
         for (int n = ln.entry; n < kept; n += ln.per)
-          out[(uint64_t)(unsigned)edge[n] * a.H + ln.head] = env[n] * exp_fast(s[n * LD + ln.head] - l);
+          out[(uint64_t)(unsigned)edge[n] * a.H + ln.head] = env[n] * (exp_fast(s[n * LD + ln.head] - top) * rden);
       wave_sync();  // (before the next row's scores)
       continue;
     }
@@ -511,7 +513,7 @@ __global__ __launch_bounds__(256, ONE && LD == 9 ? 5 : 4) void k_att_forward(Att
         for (int n = ln.entry; n < count; n += ln.per) {
           if (env[n] < 0.0f) continue;
           float* to = out + (uint64_t)(c + n) * a.H + ln.head;
-          *to = env[n] * exp_fast(*to - l);
+          *to = env[n] * (exp_fast(*to - top) * rden);
         }
       wave_sync();
     }

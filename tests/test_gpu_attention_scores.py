@@ -93,3 +93,27 @@ def test_gradients_beside_scores_of_minus_infinity(e2f, ctx, receivers, degree):
     room = U * (degree / 4 + 80 + 4 * 64) * 16.0 * p * (a.abs() + (p * a.abs()).sum(1, keepdim=True)) + 1e-36
     got = gk[receivers:].cpu().double().view(receivers, degree, H)
     assert torch.all((got - want).abs() <= room)
+
+
+# Roundings of a weight of few edges, in steps U of itself: the exponential 3 (the instruction's last place is two), a
+# lane's sum of four 3, its rescaling to the row's maximum 4, sums over lanes and waves 8, the quotient's two
+# factors 2, the exponential in front 3: 23, and the envelope of 1
+FEW = 24
+
+
+@pytest.mark.parametrize("offset", [0.0, 100.0, 1000.0, 10000.0, -10000.0])
+@pytest.mark.parametrize("H,degree", [(1, 200), (8, 20), (8, 32), (12, 7), (3, 129)])
+def test_one_offset_of_a_row_s_scores_does_not_change_its_weights(e2f, ctx, offset, H, degree):
+    # scores offset + m / 64: exact, as are their differences, which are below 1/2 (the exponential's argument to
+    # the base of two stays below 1, whose rounding is half a step of the result at most)
+    receivers = 20
+    g = torch.Generator().manual_seed(degree)
+    n, rp, ci = stars(receivers, degree)
+    x = offset + torch.randint(0, 32, (receivers * degree, H), generator=g) / 64
+    q, k = from_scores(x, receivers)
+    alpha, _ = e2f.e2f_attention_forward(ctx, torch.zeros(n, 3, device=DEV), rp, ci, 5.0, q=q, k=k)
+    want = torch.softmax(x.double().view(receivers, degree, H), 1)
+    got = alpha.cpu().double().view(receivers, degree, H)
+    steps = float(((got - want).abs() / want).max()) / U
+    print("%.1f steps" % steps)
+    assert steps <= FEW + degree / 32
