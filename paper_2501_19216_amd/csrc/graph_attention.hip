@@ -109,14 +109,30 @@ __device__ __forceinline__ void wave_sync() {
 }
 
 constexpr float kPi = 3.14159265358979f, kLog2e = 1.44269504088896f;
-__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
-// tanh to a few steps of its own value: the odd series to x^11 below 0.35 (its next term is below 2^-25 of x
+// exp(-z^2) for the radial functions: the rounding of the argument is z^2 steps of the value, and z^2 exp(-z^2) stays
+// below 0.37: less than half a step of 1, which the largest function of a distance is near to
+__device__ __forceinline__ float exp_radial(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+// exp(x) for x <= 0 to three half steps of its value however far x is: 2^t (1 + r) with t log 2 + r = x and t near
+// x log2(e): rounding x log2(e) alone leaves |x| half steps, 64 of them at 80 (1.5 million edges, forward: 98 us with that
+// and a reciprocal in the tangent, 102 with this and the quotient below).  (Below 2^-126: 0.)
+__device__ __forceinline__ float exp_near(float x) {
+  constexpr float ln2 = 0.693147182464599609f, low = -1.90465430e-9f;  // log 2 = ln2 + low
+  const float t = x * kLog2e, r = fmaf(-t, low, fmaf(-t, ln2, x));
+  const float e = __builtin_amdgcn_exp2f(t);
+  return e > 0.0f ? fmaf(e, r, e) : e;  // (r of an infinite x is NaN)
+}
+// n / d for d in 1 .. 2: the reciprocal's quotient and one correction by its remainder
+__device__ __forceinline__ float quotient(float n, float d) {
+  const float r = __builtin_amdgcn_rcpf(d), q = n * r;
+  return fmaf(fmaf(-d, q, n), r, q);
+}
+// tanh to a few half steps of its own value: the odd series to x^11 below 0.35 (its next term is below 2^-25 of x
 // there), (1 - e^-2x) / (1 + e^-2x) from it on
 __device__ __forceinline__ float tanh_near(float x) {
   const float a = fabsf(x), t = a * a;
   const float p = a + a * t * (-1.0f / 3 + t * (2.0f / 15 + t * (-17.0f / 315 + t * (62.0f / 2835 + t * (-1382.0f / 155925)))));
-  const float e = exp_fast(-2.0f * a);
-  return copysignf(a < 0.35f ? p : (1.0f - e) * __builtin_amdgcn_rcpf(1.0f + e), x);
+  const float e = exp_near(-2.0f * a);
+  return copysignf(a < 0.35f ? p : quotient(1.0f - e, 1.0f + e), x);
 }
 
 // (cos(pi x) + 1) / 2 = c^2 and its slope -pi s c for x = d / cutoff below 1, with c, s the cosine and sine of pi x / 2
@@ -357,7 +373,7 @@ __device__ __forceinline__ void add_radial(const AttnArgs& a, int heads, const f
   for (int r = 0; r < 8; ++r)
     if (4 * r < a.R) {
       const float z = z0 - 4.0f * r;
-      x = __builtin_amdgcn_mfma_f32_16x16x4f32(exp_fast(-z * z), wr[r], x, 0, 0, 0);
+      x = __builtin_amdgcn_mfma_f32_16x16x4f32(exp_radial(-z * z), wr[r], x, 0, 0, 0);
     }
   if (hc < heads) {
 #pragma unroll
@@ -459,11 +475,11 @@ __global__ __launch_bounds__(256, ONE && LD == 9 ? 5 : 4) void k_att_forward(Att
             }
             mx = fmaxf(mx, x[u]);
           }
-          if (mx > m) den *= exp_fast(m - mx), m = mx;
+          if (mx > m) den *= exp_near(m - mx), m = mx;
           const float from = m == -INFINITY ? 0.0f : m;  // (scores of -infinity alone: terms of 0)
 #pragma unroll
           for (int u = 0; u < 4; ++u)
-            if (n0 + u * ln.per < count) den += exp_fast(x[u] - from);
+            if (n0 + u * ln.per < count) den += exp_near(x[u] - from);
         }
       wave_sync();
       if (spill)
@@ -474,7 +490,7 @@ __global__ __launch_bounds__(256, ONE && LD == 9 ? 5 : 4) void k_att_forward(Att
     }
     // the row's sum, over the lanes and waves of a head
     float top = classes_all(m, sh.hp, [](float p, float q) { return fmaxf(p, q); });
-    den = classes_all(m == top ? den : den * exp_fast(m - top), sh.hp, [](float p, float q) { return p + q; });
+    den = classes_all(m == top ? den : den * exp_near(m - top), sh.hp, [](float p, float q) { return p + q; });
     if (sh.wpr > 1) {
       __syncthreads();  // (the row before has been read)
       if (lane < sh.hp) join[wave][0][lane] = top, join[wave][1][lane] = den;
@@ -483,7 +499,7 @@ __global__ __launch_bounds__(256, ONE && LD == 9 ? 5 : 4) void k_att_forward(Att
       den = 0.0f;
       for (int k = 0; k < 4; ++k) {
         const float mk = join[k][0][ln.head], dk = join[k][1][ln.head];
-        den += mk == top ? dk : dk * exp_fast(mk - top);
+        den += mk == top ? dk : dk * exp_near(mk - top);
       }
     }
     // (the weights from the maximum and the sum: exp(s - lse) would carry lse's rounding, half a step of the scores,
@@ -493,7 +509,7 @@ __global__ __launch_bounds__(256, ONE && LD == 9 ? 5 : 4) void k_att_forward(Att
     if (!spill) {
       if (ln.on)
         for (int n = ln.entry; n < kept; n += ln.per)
-          out[(uint64_t)(unsigned)edge[n] * a.H + ln.head] = env[n] * (exp_fast(s[n * LD + ln.head] - top) * rden);
+          out[(uint64_t)(unsigned)edge[n] * a.H + ln.head] = env[n] * (exp_near(s[n * LD + ln.head] - top) * rden);
       wave_sync();  // (before the next row's scores)
       continue;
     }
@@ -513,7 +529,7 @@ __global__ __launch_bounds__(256, ONE && LD == 9 ? 5 : 4) void k_att_forward(Att
         for (int n = ln.entry; n < count; n += ln.per) {
           if (env[n] < 0.0f) continue;
           float* to = out + (uint64_t)(c + n) * a.H + ln.head;
-          *to = env[n] * (exp_fast(*to - top) * rden);
+          *to = env[n] * (exp_near(*to - top) * rden);
         }
       wave_sync();
     }
@@ -643,7 +659,7 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
                   x = a.cap * t;
                   turn = 1.0f - t * t;
                 }
-                const float p = exp_fast(x - l);
+                const float p = exp_near(x - l);
                 ds = p * (ga[u] * env[b0 + n] - D) * turn;
                 dd = ga[u] * p * slope[b0 + n];
                 if (gr.gk) rec[(uint64_t)(unsigned)edge[b0 + n] * gr.stride + g.h0 + ln.head] = ds;
@@ -675,7 +691,7 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                   const int n = b + quad * 4 + u;
-                  const float z = dist[b0 + n] * inv - (float)(16 * r + hc), gz = exp_fast(-z * z);
+                  const float z = dist[b0 + n] * inv - (float)(16 * r + hc), gz = exp_radial(-z * z);
                   dd[u] += us[u] * gz * z;
                   dw[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(gz, sb[n * kLd + hc], dw[r], 0, 0, 0);
                 }

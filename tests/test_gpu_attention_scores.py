@@ -117,3 +117,36 @@ def test_one_offset_of_a_row_s_scores_does_not_change_its_weights(e2f, ctx, offs
     steps = float(((got - want).abs() / want).max()) / U
     print("%.1f steps" % steps)
     assert steps <= FEW + degree / 32
+
+
+@pytest.mark.parametrize("H,degree", [(8, 20), (8, 32), (12, 7), (4, 60)])
+def test_scores_far_below_the_largest_keep_their_digits(e2f, ctx, H, degree):
+    # scores m / 64 down to -80: exact; a lane sees four edges at most, in one step. The exponential holds three
+    # half steps however far its argument is
+    receivers = 50
+    g = torch.Generator().manual_seed(degree)
+    n, rp, ci = stars(receivers, degree)
+    x = -torch.randint(0, 80 * 64, (receivers * degree, H), generator=g) / 64
+    q, k = from_scores(x, receivers)
+    alpha, _ = e2f.e2f_attention_forward(ctx, torch.zeros(n, 3, device=DEV), rp, ci, 5.0, q=q, k=k)
+    want = torch.softmax(x.double().view(receivers, degree, H), 1)
+    got = alpha.cpu().double().view(receivers, degree, H)
+    steps = float(((got - want).abs() / want).max()) / U
+    print("%.1f steps" % steps)
+    assert steps <= FEW
+
+
+def test_capped_scores_alone(e2f, ctx):
+    # one edge a row: lse is its score. cap 2^4, so that x / cap is exact; the hyperbolic tangent by exponentials: e to 3
+    # half steps, 2 e / (1 - e^2) < 1.32 times that, a difference, a sum and two for the quotient, and the product
+    # with cap: 9; by its series fewer
+    receivers, H, cap = 4000, 8, 16.0
+    g = torch.Generator().manual_seed(1)
+    n, rp, ci = stars(receivers, 1)
+    x = torch.exp(torch.rand(receivers, H, generator=g) * 14 - 8) * (torch.randint(0, 2, (receivers, H), generator=g) * 2 - 1)
+    q, k = from_scores(x, receivers)
+    alpha, lse = e2f.e2f_attention_forward(ctx, torch.zeros(n, 3, device=DEV), rp, ci, 5.0, q=q, k=k, cap=cap)
+    want = cap * torch.tanh(x.double() / cap)
+    steps = float(((lse[:receivers].cpu().double() - want).abs() / want.abs()).max()) / U
+    print("%.1f steps" % steps)
+    assert steps <= 9 and torch.all(alpha == 1.0)
