@@ -135,13 +135,16 @@ __device__ __forceinline__ float tanh_near(float x) {
   return copysignf(a < 0.35f ? p : quotient(1.0f - e, 1.0f + e), x);
 }
 
+// Distance and envelope have every fused product written out: forward and backward get the same bits, so that the
+// backward finds the softmax's p in alpha = env p.
+__device__ __forceinline__ float length(float x, float y, float z) { return sqrtf(fmaf(z, z, fmaf(y, y, x * x))); }
 // (cos(pi x) + 1) / 2 = c^2 and its slope -pi s c for x = d / cutoff below 1, with c, s the cosine and sine of pi x / 2
 // by their series (the next terms are below 2^-26 there); 0 from 1 on
 __device__ __forceinline__ float envelope(float rc, float d, float* slope = nullptr) {
   const float h = 0.5f * kPi * (d / rc), t = h * h;
-  const float c = 1.0f + t * (-0.5f + t * (1.0f / 24 + t * (-1.0f / 720 + t * (1.0f / 40320 + t * (-1.0f / 3628800 + t * (1.0f / 479001600))))));
+  const float c = fmaf(t, fmaf(t, fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.0f / 479001600, -1.0f / 3628800), 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
   if (slope) {
-    const float s = h * (1.0f + t * (-1.0f / 6 + t * (1.0f / 120 + t * (-1.0f / 5040 + t * (1.0f / 362880 + t * (-1.0f / 39916800))))));
+    const float s = h * fmaf(t, fmaf(t, fmaf(t, fmaf(t, fmaf(t, -1.0f / 39916800, 1.0f / 362880), -1.0f / 5040), 1.0f / 120), -1.0f / 6), 1.0f);
     *slope = d < rc ? -kPi / rc * s * c : 0.0f;
   }
   return d < rc ? c * c : 0.0f;
@@ -452,7 +455,7 @@ __global__ __launch_bounds__(256, ONE && LD == 9 ? 5 : 4) void k_att_forward(Att
         Features<LPE, F> f;
         for (int b = 0; b < count; b += f.BE) products<LPE, ONE, LD, F>(a, sh, g, i, q1, f, jj + b, sb + b * LD);
       }
-      const float d = sqrtf(dx * dx + dy * dy + dz * dz);
+      const float d = length(dx, dy, dz);
       dist[lane] = d;
       env[kept + lane] = envelope(a.rc, d);
       edge[kept + lane] = (int)e;
@@ -520,7 +523,7 @@ __global__ __launch_bounds__(256, ONE && LD == 9 ? 5 : 4) void k_att_forward(Att
         const int j = atom_of(a, a.col[w.e0 + c + lane]);
         if (!a.gid || a.gid[j] == w.gid) {
           const float dx = px - a.pos[3 * (int64_t)j], dy = py - a.pos[3 * (int64_t)j + 1], dz = pz - a.pos[3 * (int64_t)j + 2];
-          v = envelope(a.rc, sqrtf(dx * dx + dy * dy + dz * dz));
+          v = envelope(a.rc, length(dx, dy, dz));
         }
       }
       env[lane] = v;
@@ -549,7 +552,8 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
   for (int x = lane; x < 64 * kLd; x += 64) s[x] = 0.0f;
   float* dist = s + 64 * kLd;
   float* env = dist + 64;
-  float* slope = env + 64;
+  float* renv = env + 64;  // 1 / env
+  float* slope = renv + 64;
   int* edge = (int*)(slope + 64);
   int* jj = edge + 64;
   float* force = (float*)(jj + 64);  // [64] d loss / d distance
@@ -572,11 +576,11 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
     const bool row = i < a.n;
     Walk w = {};
     if (row) w = walk_of(a, i, part, sh.wpr);
-    const float* gal = gr.galpha + w.e0 * a.H + g.h0;  // the row's gradients of the group's heads
+    const float* gal = gr.galpha + w.e0 * a.H + g.h0;  // the row's gradients of the group's heads, and its weights
+    const float* al = gr.alpha + w.e0 * a.H + g.h0;
     float D = 0.0f;
     {
       const unsigned stride = ln.per * sh.wpr;
-      const float* al = gr.alpha + w.e0 * a.H + g.h0;
       for (unsigned e = ln.entry + part * ln.per; ln.on && e < w.len; e += 4 * stride) {
         float x[4], y[4];
 #pragma unroll
@@ -620,24 +624,28 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
       const int j0 = __builtin_amdgcn_readfirstlane(j);  // (by every lane: lane 0 has the batch's first edge)
       jj[lane] = j >= 0 ? j : j0;                         // the first sender once more behind the last
       edge[lane] = (int)e;
-      const float d = sqrtf(dx * dx + dy * dy + dz * dz);
+      const float d = length(dx, dy, dz);
       float sl;
       env[lane] = envelope(a.rc, d, &sl);
-      dist[lane] = d, slope[lane] = sl;
+      dist[lane] = d, slope[lane] = sl, renv[lane] = 1.0f / env[lane];
       wave_sync();
       Features<LPE, F> f;
       for (int b0 = 0; b0 < count; b0 += f.BE) {
         float* sb = s + b0 * kLd;
         const int many = min(count - b0, f.BE);  // of the block's entries
-        float ga[4];
-        auto read_ga = [&](int c) {
+        float ga[4], al4[4];
+        auto read_row = [&](int c) {
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             const int n = c + ln.entry + u * ln.per;
-            ga[u] = ln.on && n < many ? gal[(uint64_t)(unsigned)edge[b0 + n] * a.H + ln.head] : 0.0f;
+            ga[u] = al4[u] = 0.0f;
+            if (ln.on && n < many) {
+              const uint64_t at = (uint64_t)(unsigned)edge[b0 + n] * a.H + ln.head;
+              ga[u] = gal[at], al4[u] = al[at];
+            }
           }
         };
-        read_ga(0);
+        read_row(0);
         if (a.dk) products<LPE, ONE, kLd, F>(a, sh, g, i, q1, f, jj + b0, sb);
         wave_sync();
         if (a.R)
@@ -645,7 +653,7 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
         wave_sync();
         // ds, and the envelope's part of the distances' gradients, four entries at a time
         for (int c = 0; c < f.BE; c += 4 * ln.per) {
-          if (c > 0) read_ga(c);
+          if (c > 0) read_row(c);
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             const int n = c + ln.entry + u * ln.per;
@@ -659,7 +667,9 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
                   x = a.cap * t;
                   turn = 1.0f - t * t;
                 }
-                const float p = exp_near(x - l);
+                // p from the weight; where the envelope leaves nothing of it, at the cutoff and beyond, or it is next to
+                // nothing, from the score, with lse's rounding in it
+                const float p = al4[u] >= 0x1p-100f ? al4[u] * renv[b0 + n] : exp_near(x - l);
                 ds = p * (ga[u] * env[b0 + n] - D) * turn;
                 dd = ga[u] * p * slope[b0 + n];
                 if (gr.gk) rec[(uint64_t)(unsigned)edge[b0 + n] * gr.stride + g.h0 + ln.head] = ds;
@@ -745,7 +755,7 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
 #pragma unroll
       for (int u = 0; u < F::VEC; ++u) dq[u] = a.scale * classes_all(dq[u], LPE, [](float x, float y) { return x + y; });
       if (sh.wpr > 1) {
-        float* mine = dist;  // (what follows s: 640 floats that the row has done with)
+        float* mine = dist;  // (what follows s: 704 floats that the row has done with)
         __syncthreads();
         if (lane < LPE) {
 #pragma unroll
@@ -1263,7 +1273,7 @@ hipError_t launch_att_backward(const AttnArgs& a, const AttnGrad& gr, hipStream_
   sh.rows = rows_of(a, sh.wpr, 3);
   const int parts = attention_parts(a), vec = a.bf16 ? BF16::VEC : F32::VEC;
   sh.dq = sh.one ? 0 : 64 / sh.lpe * sh.heads * sh.lph * vec;
-  sh.lds = 64 * kLd + 6 * 64 + 256 + sh.dq;
+  sh.lds = 64 * kLd + 7 * 64 + 256 + sh.dq;
   if (sh.lds < 512) sh.lds = 512;  // (dw's sum over the waves)
   {
     const dim3 grid((unsigned)parts, (unsigned)sh.groups);

@@ -150,3 +150,50 @@ def test_capped_scores_alone(e2f, ctx):
     steps = float(((lse[:receivers].cpu().double() - want).abs() / want.abs()).max()) / U
     print("%.1f steps" % steps)
     assert steps <= 9 and torch.all(alpha == 1.0)
+
+
+def gradient_of_scores(x, env, ga, receivers, degree):
+    """ds [receivers, degree, H] in float64, and what ten operations after the weights may add to it: those have FEW
+    roundings and the envelope 20 steps of 1 (its argument's, its series' and its square's); the sum over the row
+    degree / 4 more; the core, p and ds two each."""
+    p = torch.softmax(x.double().view(receivers, degree, -1), 1)
+    a = ga.cpu().double().view(receivers, degree, -1)
+    e = env.double().view(receivers, degree, 1)
+    D = (p * e * a).sum(1, keepdim=True)
+    bD = U * ((p * a.abs() * ((FEW + degree / 4 + 12) * e + 20)).sum(1, keepdim=True) + 2 * D.abs())
+    ds = p * (e * a - D)
+    return p, ds, p * (U * (20 * a.abs() + 2 * (e * a - D).abs()) + bD) + U * (FEW + 8) * ds.abs() + 1e-36
+
+
+@pytest.mark.parametrize("offset", [0.0, 100.0, 1000.0, 10000.0, -10000.0])
+@pytest.mark.parametrize("H,degree", [(1, 200), (8, 20), (12, 7), (4, 60)])
+@pytest.mark.parametrize("apart", [False, True])
+def test_gradients_at_one_offset_of_a_row_s_scores(e2f, ctx, offset, H, degree, apart):
+    # the gradient of an edge's k is that of its score; with `apart` the senders lie between the receiver and the
+    # cutoff, some of them next to it, and every seventh beyond it
+    receivers, rc = 20, 5.0
+    g = torch.Generator().manual_seed(degree + H)
+    n, rp, ci = stars(receivers, degree)
+    E = receivers * degree
+    x = offset + torch.randint(0, 32, (E, H), generator=g) / 64
+    q, k = from_scores(x, receivers)
+    pos, env, beyond = torch.zeros(n, 3), torch.ones(E), torch.zeros(E, dtype=torch.bool)
+    if apart:
+        d = (rc * (1 - torch.exp(-16 * torch.rand(E, generator=g)))).float()  # down to 10^-7 from the cutoff
+        beyond = torch.arange(E) % 7 == 3
+        d[beyond] = 5.5
+        pos[receivers:, 0] = d
+        env = torch.where(d < rc, torch.cos(math.pi / 2 * d.double() / rc) ** 2, 0.0)
+    pos = pos.to(DEV)
+    ga = torch.randn(E, H, generator=g).to(DEV)
+    alpha, lse = e2f.e2f_attention_forward(ctx, pos, rp, ci, rc, q=q, k=k)
+    t = e2f.e2f_transpose_graph(ctx, n, rp, ci)
+    _, gk, _, _ = e2f.e2f_attention_backward(ctx, pos, rp, ci, rc, alpha, lse, ga, *t, q=q, k=k)
+    p, want, room = gradient_of_scores(x, env, ga, receivers, degree)
+    # without a weight p is exp(x - lse): half a step of lse and of the difference
+    beyond = beyond.view(receivers, degree, 1)
+    room = room + U * want.abs() * torch.where(beyond, 2 * lse.cpu().double()[:receivers, None].abs(), 0.0)
+    got = gk[receivers:].cpu().double().view(receivers, degree, H)
+    worst = float(((got - want).abs() / room).max())
+    print("%.3f of the bound" % worst)
+    assert worst <= 1.0
