@@ -121,17 +121,19 @@ __device__ __forceinline__ float exp_near(float x) {
   const float e = __builtin_amdgcn_exp2f(t);
   return e > 0.0f ? fmaf(e, r, e) : e;  // (r of an infinite x is NaN)
 }
-// n / d for d in 1 .. 2: the reciprocal's quotient and one correction by its remainder
+// n / d for d in 1 .. 4: the reciprocal's quotient and one correction by its remainder
 __device__ __forceinline__ float quotient(float n, float d) {
   const float r = __builtin_amdgcn_rcpf(d), q = n * r;
   return fmaf(fmaf(-d, q, n), r, q);
 }
 // tanh to a few half steps of its own value: the odd series to x^11 below 0.35 (its next term is below 2^-25 of x
-// there), (1 - e^-2x) / (1 + e^-2x) from it on
-__device__ __forceinline__ float tanh_near(float x) {
+// there), (1 - e^-2x) / (1 + e^-2x) from it on.  turn: 1 - tanh^2, there as 4 e^-2x / (1 + e^-2x)^2, which keeps its
+// digits where the tangent comes near 1
+__device__ __forceinline__ float tanh_near(float x, float* turn = nullptr) {
   const float a = fabsf(x), t = a * a;
   const float p = a + a * t * (-1.0f / 3 + t * (2.0f / 15 + t * (-17.0f / 315 + t * (62.0f / 2835 + t * (-1382.0f / 155925)))));
   const float e = exp_near(-2.0f * a);
+  if (turn) *turn = a < 0.35f ? 1.0f - p * p : quotient(4.0f * e, (1.0f + e) * (1.0f + e));
   return copysignf(a < 0.35f ? p : quotient(1.0f - e, 1.0f + e), x);
 }
 
@@ -663,9 +665,7 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
               if (n < many) {
                 if (a.dk || a.R) x = sb[n * kLd + ln.head];
                 if (a.cap > 0.0f) {
-                  const float t = tanh_near(x * icap);
-                  x = a.cap * t;
-                  turn = 1.0f - t * t;
+                  x = a.cap * tanh_near(x * icap, &turn);
                 }
                 // p from the weight; where the envelope leaves nothing of it, at the cutoff and beyond, or it is next to
                 // nothing, from the score, with lse's rounding in it

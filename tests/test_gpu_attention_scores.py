@@ -197,3 +197,33 @@ def test_gradients_at_one_offset_of_a_row_s_scores(e2f, ctx, offset, H, degree, 
     worst = float(((got - want).abs() / room).max())
     print("%.3f of the bound" % worst)
     assert worst <= 1.0
+
+
+@pytest.mark.parametrize("cap", [1.0, 16.0])
+@pytest.mark.parametrize("largest", [0.3, 2.0, 8.0, 30.0])
+def test_gradients_of_capped_scores(e2f, ctx, cap, largest):
+    # x / cap exact; 1 - tanh^2 as 4 e / (1 + e)^2: e to three half steps, its sum and square two, the quotient three
+    # (by 1 - t^2 below 0.35: less). p holds cap times nine half steps of the score, twice (test_capped_scores_alone)
+    receivers, degree, H = 30, 20, 8
+    g = torch.Generator().manual_seed(int(cap + 10 * largest))
+    n, rp, ci = stars(receivers, degree)
+    E = receivers * degree
+    x = torch.randint(-4096, 4097, (E, H), generator=g) * (cap * largest / 4096)
+    q, k = from_scores(x, receivers)
+    ga = torch.randn(E, H, generator=g).to(DEV)
+    pos = torch.zeros(n, 3, device=DEV)
+    alpha, lse = e2f.e2f_attention_forward(ctx, pos, rp, ci, 5.0, q=q, k=k, cap=cap)
+    t = e2f.e2f_transpose_graph(ctx, n, rp, ci)
+    _, gk, _, _ = e2f.e2f_attention_backward(ctx, pos, rp, ci, 5.0, alpha, lse, ga, *t, q=q, k=k, cap=cap)
+    z = x.double() / cap
+    e = torch.exp(-2 * z.abs())
+    turn = (4 * e / (1 + e) ** 2).view(receivers, degree, H)
+    p, ds, room = gradient_of_scores(cap * torch.tanh(z), torch.ones(E), ga, receivers, degree)
+    a = ga.cpu().double().view(receivers, degree, H)
+    pa = (p * a.abs()).sum(1, keepdim=True)
+    room = room + U * 18 * cap * p * (a.abs() + 2 * pa)
+    want = ds * turn
+    got = gk[receivers:].cpu().double().view(receivers, degree, H)
+    worst = float(((got - want).abs() / (room * turn + U * 12 * want.abs() + 1e-36)).max())
+    print("%.3f of the bound" % worst)
+    assert worst <= 1.0
