@@ -146,7 +146,7 @@ __device__ __forceinline__ float envelope(float rc, float d, float* slope = null
   const float h = 0.5f * kPi * (d / rc), t = h * h;
   const float c = fmaf(t, fmaf(t, fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.0f / 479001600, -1.0f / 3628800), 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
   if (slope) {
-    const float s = h * fmaf(t, fmaf(t, fmaf(t, fmaf(t, fmaf(t, -1.0f / 39916800, 1.0f / 362880), -1.0f / 5040), 1.0f / 120), -1.0f / 6), 1.0f);
+    const float s = h * fmaf(t, fmaf(t, fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.0f / 6227020800, -1.0f / 39916800), 1.0f / 362880), -1.0f / 5040), 1.0f / 120), -1.0f / 6), 1.0f);
     *slope = d < rc ? -kPi / rc * s * c : 0.0f;
   }
   return d < rc ? c * c : 0.0f;
