@@ -214,7 +214,8 @@ __global__ __launch_bounds__(KEEP ? 512 : 1024) void k_norm_forward(NormArgs a, 
   constexpr int K = (L + 1) * (L + 1);
   __shared__ float red[16];
   const int slot = threadIdx.x / tpr, slots = blockDim.x / tpr;
-  const int64_t first = (int64_t)blockIdx.x * slots;
+  const int64_t first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * slots;
+  if (first >= a.n) return;  // (the last round's)
   const bool mine = threadIdx.x % tpr * V < a.C, on = mine && first + slot < a.n;
   const int c = mine ? threadIdx.x % tpr * V : 0, at = (int)min((int64_t)slot, a.n - 1 - first);
   const unsigned own = (unsigned)(at * K * a.C + c) * (unsigned)sizeof(T);
@@ -551,7 +552,8 @@ hipError_t launch_norm_forward(int L, bool bf16, const NormArgs& a, void* out, v
   if (a.n == 0) return hipSuccess;
   const Shape s = shape_of(L, a.C, bf16, false);
   const int slots = s.threads / s.tpr;
-  const unsigned grid = (unsigned)(((int64_t)a.n + slots - 1) / slots);
+  const Rounds r = rounds_of(((int64_t)a.n + slots - 1) / slots, s.threads);
+  const dim3 grid(r.x, r.rounds);
 #define E2F_NORM(LL, T, VV, KEEP, B, P) \
   k_norm_forward<LL, T, VV, KEEP, B, P><<<grid, s.threads, 0, st>>>(a, s.tpr, (T*)out, (T*)normed, rstd)
   E2F_NORM_SWITCH(2)

@@ -190,6 +190,15 @@ hipError_t launch_attention(const float* pos, const float* q, const float* k, in
                             const float* rbf_w, int R, float rc, const int64_t* row_ptr, const int32_t* col_idx,
                             float* alpha, hipStream_t s);
 
+// A launch holds below 2^32 threads in a direction: the workgroups of one in x, rounds of them in another
+struct Rounds {
+  unsigned x, rounds;
+};
+inline Rounds rounds_of(int64_t blocks, unsigned threads) {
+  const int64_t most = 0xffffffff / threads, x = blocks < most ? blocks : most;
+  return {(unsigned)x, (unsigned)(x ? (blocks + x - 1) / x : 0)};
+}
+
 // ---- capped attention of a graph's edges and its gradients (graph_attention.hip)
 struct AttnArgs {
   const float* pos;

@@ -20,6 +20,8 @@
 namespace e2f {
 namespace {
 
+constexpr int64_t kMostBlocks = 0xffffffff / 256;  // of one launch, which holds below 2^32 threads
+
 // the tensors of one launch
 template <int N>
 struct Table {
@@ -182,7 +184,7 @@ hipError_t each_table(int count, const void* const* in, void* const* out, const 
     for (; i < count && t.count < Table::MAX; ++i) {
       if (n[i] == 0) continue;
       const int64_t b = (n[i] + chunk - 1) / chunk;
-      if (t.count && blocks + b > 0x7fffffff) break;
+      if (t.count && blocks + b > kMostBlocks) break;
       const int k = t.count++;
       t.in[k] = in[i];
       if constexpr (std::is_same_v<Table, WriteTable>) t.out[k] = out[i];

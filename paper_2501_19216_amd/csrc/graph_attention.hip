@@ -157,7 +157,7 @@ __device__ __forceinline__ int atom_of(const AttnArgs& a, int c) { return min(ma
 // Workgroups of one XCD (every eighth) take neighbouring rows, which share senders where atoms are in order
 __device__ __forceinline__ int64_t row_block() {
   const int64_t nb = gridDim.x, per = nb / 8, rest = nb % 8, x = blockIdx.x % 8, k = blockIdx.x / 8;
-  return x * per + min(x, rest) + k;
+  return x * per + min(x, rest) + k + blockIdx.z * nb;
 }
 
 // A workgroup's heads: `share` q heads from h0 on for each of the k heads from k0 on
@@ -967,8 +967,10 @@ struct RowEnds {
 // pos[e] of the edge e = (j, i): the edge (i, j), or -1 - (some place among the edges that i sends without a
 // reverse); found[j]: the reverses of row j, extra[i]: the edges that i sends without one
 __global__ __launch_bounds__(256) void k_t_reverse(Transposed t) {
-  const int lane = threadIdx.x & 63, j = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (j >= t.n || __hip_atomic_load(t.cnt + t.n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) return;
+  const int lane = threadIdx.x & 63;
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int j = (int)row;
+  if (row >= t.n || __hip_atomic_load(t.cnt + t.n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) return;
   const int64_t e0 = t.row_ptr[j], e1 = t.row_ptr[j + 1];
   bool good = e0 >= 0 && e0 <= e1 && e1 <= t.E && (j > 0 || e0 == 0) && (j + 1 < t.n || e1 == t.E);
   int found = 0, last = -1;  // last sender of the stretch before
@@ -1212,7 +1214,7 @@ static int rows_of(const AttnArgs& a, int wpr, int per_cu) {
 
 int attention_parts(const AttnArgs& a) {
   const int rows = rows_of(a, shape_of(a, false).wpr, 3);
-  return (a.n + rows - 1) / rows;
+  return (int)(((int64_t)a.n + rows - 1) / rows);
 }
 
 // floats of an edge's record: ds of every head, and the position gradient of every head group from *force on
@@ -1249,7 +1251,8 @@ hipError_t launch_att_forward(const AttnArgs& a, float* alpha, float* lse, hipSt
   const bool few = sh.heads <= 8;
   sh.lds = kKept * ((few ? 9 : kLd) + 2) + 64 + 64 + 256;
   sh.rows = sh.wpr == 1 ? 4 : 1;
-  const dim3 grid((unsigned)((a.n + sh.rows - 1) / sh.rows), (unsigned)sh.groups);
+  const Rounds r = rounds_of(((int64_t)a.n + sh.rows - 1) / sh.rows, 256);
+  const dim3 grid(r.x, (unsigned)sh.groups, r.rounds);
   const size_t lds = sizeof(float) * 4 * sh.lds;
 #define E2F_ATT(P, ONE, F)                                              \
   if (few)                                                              \
@@ -1286,7 +1289,8 @@ hipError_t launch_att_backward(const AttnArgs& a, const AttnGrad& gr, hipStream_
   if (g.gw) k_att_radial_sum<<<(a.H * a.R + 15) / 16, 1024, 0, s>>>(g.part, parts, a.H * a.R, g.gw);
   if (g.gk || g.gpos) {
     sh = shape_of(a, true);
-    const dim3 grid((unsigned)(sh.wpr == 1 ? (a.n + 3) / 4 : a.n), (unsigned)(g.gk ? sh.groups : 1));
+    const Rounds r = rounds_of(sh.wpr == 1 ? ((int64_t)a.n + 3) / 4 : a.n, 256);
+    const dim3 grid(r.x, (unsigned)(g.gk ? sh.groups : 1), r.rounds);
 #define E2F_SEND(P)                                          \
   case P:                                                    \
     if (a.bf16)                                              \
@@ -1303,7 +1307,7 @@ hipError_t launch_att_backward(const AttnArgs& a, const AttnGrad& gr, hipStream_
   return hipGetLastError();
 }
 
-int transpose_scan_blocks(int n) { return (n + kScanSpan - 1) / kScanSpan; }
+int transpose_scan_blocks(int n) { return (int)(((int64_t)n + kScanSpan - 1) / kScanSpan); }
 
 hipError_t launch_transpose(const int64_t* row_ptr, const int32_t* col, int n, int64_t E, int32_t* cnt, int64_t* sums,
                             int32_t* pos, int64_t* rowT, int32_t* colT, int32_t* perm, hipStream_t s) {
@@ -1314,8 +1318,9 @@ hipError_t launch_transpose(const int64_t* row_ptr, const int32_t* col, int n, i
     return hipGetLastError();
   }
   const unsigned blocks = (unsigned)transpose_scan_blocks(n), nb = (unsigned)(((int64_t)n + 3) / 4);
+  const Rounds r = rounds_of(nb, 256);
   k_t_zero<<<n / 256 + 1, 256, 0, s>>>(t);
-  k_t_reverse<<<nb, 256, 0, s>>>(t);
+  k_t_reverse<<<dim3(r.x, r.rounds), 256, 0, s>>>(t);
   if (E > 0) k_t_count<<<(unsigned)std::min<int64_t>((E + 255) / 256, 1024), 256, 0, s>>>(t);
   k_t_scan<<<blocks, 1024, 0, s>>>(t);
   if (blocks > 1) k_t_offset<<<blocks, 1024, 0, s>>>(t);
