@@ -130,8 +130,8 @@ e2f_status e2f_attention_weights(e2f_ctx* ctx, const float* pos, const float* q,
  * Made once for a graph and used by the backward of every layer on it.
  * Senders outside [0, n) are taken as the nearest atom (e2f_validate_graph
  * finds them).  workspace: e2f_transpose_graph_workspace_size bytes, 256-byte
- * aligned (E2F_ECAPACITY below).  Asynchronous, no allocation, can be captured
- * in a HIP graph; deterministic. */
+ * aligned (E2F_ECAPACITY below).  Outputs must not overlap inputs (E2F_EINVAL).
+ * Asynchronous, no allocation, can be captured in a HIP graph; deterministic. */
 e2f_status e2f_transpose_graph_workspace_size(e2f_ctx* ctx, int32_t n, int64_t n_edges, size_t* bytes);
 e2f_status e2f_transpose_graph(e2f_ctx* ctx, int32_t n, const int64_t* row_ptr, const int32_t* col_idx,
                                int64_t n_edges, int64_t* rowT_ptr, int32_t* colT, int32_t* perm, void* workspace,
@@ -167,8 +167,8 @@ typedef struct {
  * e2f_attention_weights with q scaled (up to rounding).  The CSR is trusted for
  * values but read with clamped indices.  Rows are gathered from k in index order
  * of the atoms: where atoms that are near have near indices the gathers hit the
- * caches.  Outputs must not overlap inputs.  Asynchronous, no allocation, can be
- * captured in a HIP graph; deterministic. */
+ * caches.  Outputs must not overlap inputs (E2F_EINVAL).  Asynchronous, no allocation,
+ * can be captured in a HIP graph; deterministic. */
 e2f_status e2f_attention_forward(e2f_ctx* ctx, const e2f_attention_params* params, const float* pos,
                                  const int32_t* graph_id, const void* q, const void* k, int32_t n,
                                  const float* rbf_w, const int64_t* row_ptr, const int32_t* col_idx, int64_t n_edges,
@@ -185,8 +185,8 @@ e2f_status e2f_attention_forward(e2f_ctx* ctx, const e2f_attention_params* param
  * Any of them may be NULL (not all).  rowT_ptr, colT, perm: e2f_transpose_graph's,
  * needed for grad_k and grad_pos (else NULL).  workspace:
  * e2f_attention_backward_workspace_size bytes, 256-byte aligned (E2F_ECAPACITY
- * below).  Outputs must not overlap inputs.  Asynchronous, no allocation, can be
- * captured in a HIP graph; deterministic. */
+ * below).  Outputs must not overlap inputs (E2F_EINVAL).  Asynchronous, no allocation,
+ * can be captured in a HIP graph; deterministic. */
 e2f_status e2f_attention_backward_workspace_size(e2f_ctx* ctx, const e2f_attention_params* params, int32_t n,
                                                  int64_t n_edges, size_t* bytes);
 e2f_status e2f_attention_backward(e2f_ctx* ctx, const e2f_attention_params* params, const float* pos,

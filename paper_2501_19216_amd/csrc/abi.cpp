@@ -10,6 +10,7 @@
 #include <algorithm>
 #include <cstring>
 #include <exception>
+#include <initializer_list>
 #include <limits>
 #include <map>
 #include <string>
@@ -1445,6 +1446,27 @@ e2f_status check_workspace(const void* ws, size_t have, size_t need) {
   return E2F_OK;
 }
 
+struct Span {
+  const void* at;
+  size_t bytes;
+};
+bool overlap(const Span& a, const Span& b) {
+  const char *x = (const char*)a.at, *y = (const char*)b.at;
+  return x && y && a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
+}
+// no output (the workspace among them) over an input or another output
+e2f_status check_overlaps(std::initializer_list<Span> in, std::initializer_list<Span> out) {
+  for (const Span& o : out) {
+    for (const Span& i : in)
+      if (overlap(o, i)) return fail(E2F_EINVAL, "an output overlaps an input");
+    for (const Span& other : out) {
+      if (&other == &o) break;
+      if (overlap(o, other)) return fail(E2F_EINVAL, "two outputs overlap");
+    }
+  }
+  return E2F_OK;
+}
+
 struct TransposeLayout {
   size_t cnt, sums, pos, total;
 };
@@ -1511,6 +1533,21 @@ e2f_status check_attention_inputs(const e2f_attention_params* p, const float* po
   return E2F_OK;
 }
 
+// what both directions read, in bytes of sizes that they checked
+struct AttnSpans {
+  Span pos, gid, q, k, w, row_ptr, col, alpha, lse;
+};
+AttnSpans attention_spans(const AttnArgs& a, const void* alpha, const void* lse) {
+  const size_t n = (size_t)a.n, E = (size_t)a.E, el = a.bf16 ? 2 : 4, f = sizeof(float);
+  // from the first atom's features to the last one's
+  const auto rows = [&](const void* p, int64_t ld, int heads) {
+    return Span{p, a.dk ? el * ((n - 1) * (size_t)ld + (size_t)heads * a.dk) : 0};
+  };
+  return {{a.pos, 3 * f * n}, {a.gid, sizeof(int32_t) * n}, rows(a.q, a.ldq, a.H), rows(a.k, a.ldk, a.Hk),
+          {a.w, f * a.H * a.R}, {a.row_ptr, sizeof(int64_t) * (n + 1)}, {a.col, sizeof(int32_t) * E},
+          {alpha, f * E * a.H}, {lse, f * n * a.H}};
+}
+
 struct AttnLayout {
   size_t edge, part, total;
 };
@@ -1546,14 +1583,6 @@ e2f_status check_norm_inputs(const e2f_norm_params* p, const void* x, const void
   if (!block && (p->gates || p->post_w || p->res_scale) && n > 0)
     return fail(E2F_EINVAL, "gates, post_w and res_scale need a block");
   return E2F_OK;
-}
-
-struct Span {
-  const char* lo;
-  size_t bytes;
-};
-bool overlap(const Span& a, const Span& b) {
-  return a.lo && b.lo && a.bytes && b.bytes && a.lo < b.lo + b.bytes && b.lo < a.lo + a.bytes;
 }
 
 e2f_status check_tensors(e2f_ctx* ctx, int32_t count, const int64_t* sizes, const int32_t* dtypes,
@@ -1599,6 +1628,11 @@ e2f_status e2f_transpose_graph(e2f_ctx* ctx, int32_t n, const int64_t* row_ptr, 
   if (n_edges > 0 && (!col_idx || !colT || !perm)) return fail(E2F_EINVAL, "col_idx, colT and perm are required");
   const TransposeLayout t = transpose_layout(n, n_edges);
   if (e2f_status rs = check_workspace(workspace, workspace_bytes, t.total); rs != E2F_OK) return rs;
+  const size_t rows = sizeof(int64_t) * ((size_t)n + 1), edges = sizeof(int32_t) * (size_t)n_edges;
+  if (e2f_status rs = check_overlaps({{row_ptr, n ? rows : 0}, {col_idx, edges}},
+                                     {{rowT_ptr, rows}, {colT, edges}, {perm, edges}, {workspace, t.total}});
+      rs != E2F_OK)
+    return rs;
   if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
   hipStream_t s = (hipStream_t)stream;
   DeviceGuard g(ctx->device);
@@ -1616,12 +1650,18 @@ e2f_status e2f_attention_forward(e2f_ctx* ctx, const e2f_attention_params* p, co
   if (e2f_status rs = check_attention_inputs(p, pos, q, k, n, rbf_w, row_ptr, col_idx, n_edges); rs != E2F_OK)
     return rs;
   if (n_edges > 0 && !alpha) return fail(E2F_EINVAL, "alpha is required");
+  const AttnArgs a = attention_args(p, pos, graph_id, q, k, n, rbf_w, row_ptr, col_idx, n_edges);
+  if (n > 0) {
+    const AttnSpans m = attention_spans(a, alpha, lse);
+    if (e2f_status rs = check_overlaps({m.pos, m.gid, m.q, m.k, m.w, m.row_ptr, m.col}, {m.alpha, m.lse});
+        rs != E2F_OK)
+      return rs;
+  }
   if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
   if (n == 0) return E2F_OK;
   hipStream_t s = (hipStream_t)stream;
   DeviceGuard g(ctx->device);
-  E2F_TIMED("attention", launch_att_forward(attention_args(p, pos, graph_id, q, k, n, rbf_w, row_ptr, col_idx,
-                                                           n_edges), alpha, lse, s));
+  E2F_TIMED("attention", launch_att_forward(a, alpha, lse, s));
   return E2F_OK;
 }
 
@@ -1653,6 +1693,18 @@ e2f_status e2f_attention_backward(e2f_ctx* ctx, const e2f_attention_params* p, c
   const AttnLayout l = attention_layout(p, n, n_edges);
   if (e2f_status rs = check_workspace(workspace, workspace_bytes, l.total); rs != E2F_OK) return rs;
   if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
+  const AttnArgs a = attention_args(p, pos, graph_id, q, k, n, rbf_w, row_ptr, col_idx, n_edges);
+  if (n > 0) {
+    const AttnSpans m = attention_spans(a, alpha, lse);
+    const size_t el = a.bf16 ? 2 : 4, edges = sizeof(int32_t) * (size_t)n_edges;
+    if (e2f_status rs = check_overlaps(
+            {m.pos, m.gid, m.q, m.k, m.w, m.row_ptr, m.col, m.alpha, m.lse, {grad_alpha, m.alpha.bytes},
+             {rowT_ptr, m.row_ptr.bytes}, {colT, edges}, {perm, edges}},
+            {{grad_q, el * n * a.H * a.dk}, {grad_k, el * n * a.Hk * a.dk}, {grad_rbf_w, m.w.bytes},
+             {grad_pos, m.pos.bytes}, {workspace, l.total}});
+        rs != E2F_OK)
+      return rs;
+  }
   hipStream_t s = (hipStream_t)stream;
   DeviceGuard g(ctx->device);
   char* ws = (char*)workspace;
@@ -1660,8 +1712,7 @@ e2f_status e2f_attention_backward(e2f_ctx* ctx, const e2f_attention_params* p, c
   d.alpha = alpha, d.lse = lse, d.galpha = grad_alpha, d.rowT = rowT_ptr, d.colT = colT, d.perm = perm;
   d.edge = (float*)(ws + l.edge), d.part = (float*)(ws + l.part);
   d.gq = grad_q, d.gk = grad_k, d.gw = grad_rbf_w, d.gpos = grad_pos;
-  E2F_TIMED("attention_grad", launch_att_backward(attention_args(p, pos, graph_id, q, k, n, rbf_w, row_ptr, col_idx,
-                                                                 n_edges), d, s));
+  E2F_TIMED("attention_grad", launch_att_backward(a, d, s));
   return E2F_OK;
 }
 
@@ -1673,16 +1724,10 @@ e2f_status e2f_block_norm_forward(e2f_ctx* ctx, const e2f_norm_params* p, const 
   if (n > 0 && (normed != nullptr) != (p->pre_w != nullptr)) return fail(E2F_EINVAL, "normed goes with pre_w");
   if (n > 0 && !out && !normed) return fail(E2F_EINVAL, "neither a block nor pre_w: nothing to compute");
   const size_t el = p->dtype == E2F_BF16 ? 2 : 4, all = el * (size_t)n * nk_of(p->lmax) * p->channels;
-  const Span in[3] = {{(const char*)x, all}, {(const char*)block, all},
-                      {(const char*)gate, el * (size_t)n * p->gates * p->channels}};
-  const Span to[3] = {{(const char*)out, all}, {(const char*)normed, all},
-                      {(const char*)rstd, sizeof(float) * 2 * (size_t)n}};
-  for (int i = 0; i < 3; ++i) {
-    for (int j = 0; j < 3; ++j)
-      if (overlap(to[i], in[j])) return fail(E2F_EINVAL, "an output overlaps an input");
-    for (int j = 0; j < i; ++j)
-      if (overlap(to[i], to[j])) return fail(E2F_EINVAL, "two outputs overlap");
-  }
+  if (e2f_status rs = check_overlaps({{x, all}, {block, all}, {gate, el * (size_t)n * p->gates * p->channels}},
+                                     {{out, all}, {normed, all}, {rstd, sizeof(float) * 2 * (size_t)n}});
+      rs != E2F_OK)
+    return rs;
   if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
   if (n == 0) return E2F_OK;
   hipStream_t s = (hipStream_t)stream;
@@ -1723,18 +1768,13 @@ e2f_status e2f_block_norm_backward(e2f_ctx* ctx, const e2f_norm_params* p, const
   }
   const size_t el = p->dtype == E2F_BF16 ? 2 : 4, all = el * (size_t)n * nk_of(p->lmax) * p->channels;
   const size_t gates = el * (size_t)n * p->gates * p->channels, w = sizeof(float) * (p->lmax + 1) * p->channels;
-  const Span in[9] = {{(const char*)x, all}, {(const char*)block, all}, {(const char*)gate, gates},
-                      {(const char*)grad_out, all}, {(const char*)grad_normed, all},
-                      {(const char*)rstd, sizeof(float) * 2 * (size_t)n}, {(const char*)p->post_w, w},
-                      {(const char*)p->res_scale, w}, {(const char*)p->pre_w, w}};
-  const Span to[6] = {{(const char*)grad_x, all}, {(const char*)grad_block, all}, {(const char*)grad_gate, gates},
-                      {(const char*)grad_post_w, w}, {(const char*)grad_res_scale, w}, {(const char*)grad_pre_w, w}};
-  for (int i = 0; i < 6; ++i) {
-    for (int j = 0; j < 9; ++j)
-      if (overlap(to[i], in[j])) return fail(E2F_EINVAL, "an output overlaps an input");
-    for (int j = 0; j < i; ++j)
-      if (overlap(to[i], to[j])) return fail(E2F_EINVAL, "two outputs overlap");
-  }
+  if (e2f_status rs = check_overlaps({{x, all}, {block, all}, {gate, gates}, {grad_out, all}, {grad_normed, all},
+                                      {rstd, sizeof(float) * 2 * (size_t)n}, {p->post_w, w}, {p->res_scale, w},
+                                      {p->pre_w, w}},
+                                     {{grad_x, all}, {grad_block, all}, {grad_gate, gates}, {grad_post_w, w},
+                                      {grad_res_scale, w}, {grad_pre_w, w}});
+      rs != E2F_OK)
+    return rs;
   if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
   hipStream_t s = (hipStream_t)stream;
   DeviceGuard g(ctx->device);

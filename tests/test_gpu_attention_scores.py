@@ -227,3 +227,36 @@ def test_gradients_of_capped_scores(e2f, ctx, cap, largest):
     worst = float(((got - want).abs() / (room * turn + U * 12 * want.abs() + 1e-36)).max())
     print("%.3f of the bound" % worst)
     assert worst <= 1.0
+
+
+def test_gradients_over_inputs_are_refused(e2f, ctx):
+    # an array for everything that the backward reads and writes; nothing is launched where an output overlaps
+    import ctypes
+    n, H, dk, R, E = 10, 4, 8, 8, 30
+    prm = e2f.AttentionParams(H, H, dk, R, 5.0, 0.3, 10.0, 0, 0, 0)
+    need = ctypes.c_size_t(0)
+    assert e2f.lib.e2f_attention_backward_workspace_size(ctx.handle, ctypes.byref(prm), n, E, ctypes.byref(need)) == 0
+    size = dict(pos=12 * n, gid=4 * n, q=4 * n * H * dk, k=4 * n * H * dk, w=4 * H * R, rp=8 * (n + 1), ci=4 * E,
+                rt=8 * (n + 1), ct=4 * E, pm=4 * E, alpha=4 * E * H, lse=4 * n * H, ga=4 * E * H)
+    out = dict(gq=4 * n * H * dk, gk=4 * n * H * dk, gw=4 * H * R, gp=12 * n)
+    space = torch.zeros((len(size) + len(out)) * 8192 + need.value, dtype=torch.uint8, device=DEV)
+    base, at = {}, space.data_ptr()
+    for name in (*size, *out):
+        base[name] = at
+        at += 8192
+    base["ws"] = at
+
+    def call(**kw):
+        v = {**base, **kw}
+        p = [v[x] for x in ("pos", "gid", "q", "k")] + [n] + [v[x] for x in ("w", "rp", "ci")] + [E]
+        p += [v[x] for x in ("rt", "ct", "pm", "alpha", "lse", "ga", "gq", "gk", "gw", "gp", "ws")]
+        return e2f.lib.e2f_attention_backward(ctx.handle, ctypes.byref(prm), *p, need.value, None)
+
+    assert call() == e2f.E2F_OK  # (a graph without edges: rp is all 0)
+    torch.cuda.synchronize()
+    for o, mine in out.items():
+        for i, its in size.items():
+            for where in (base[i], base[i] + its - 4, base[i] - mine + 4):
+                assert call(**{o: where}) == e2f.E2F_EINVAL, (o, i)
+    assert call(gq=base["gk"] + 4 * n * H * dk - 4) == e2f.E2F_EINVAL
+    assert call(gp=base["ws"] + 128) == e2f.E2F_EINVAL and call(ws=base["q"] // 256 * 256) == e2f.E2F_EINVAL
