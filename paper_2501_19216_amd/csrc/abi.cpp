@@ -1724,7 +1724,9 @@ e2f_status e2f_block_norm_forward(e2f_ctx* ctx, const e2f_norm_params* p, const 
   if (n > 0 && (normed != nullptr) != (p->pre_w != nullptr)) return fail(E2F_EINVAL, "normed goes with pre_w");
   if (n > 0 && !out && !normed) return fail(E2F_EINVAL, "neither a block nor pre_w: nothing to compute");
   const size_t el = p->dtype == E2F_BF16 ? 2 : 4, all = el * (size_t)n * nk_of(p->lmax) * p->channels;
-  if (e2f_status rs = check_overlaps({{x, all}, {block, all}, {gate, el * (size_t)n * p->gates * p->channels}},
+  const size_t w = n ? sizeof(float) * (p->lmax + 1) * p->channels : 0;
+  if (e2f_status rs = check_overlaps({{x, all}, {block, all}, {gate, el * (size_t)n * p->gates * p->channels},
+                                      {p->post_w, w}, {p->res_scale, w}, {p->pre_w, w}},
                                      {{out, all}, {normed, all}, {rstd, sizeof(float) * 2 * (size_t)n}});
       rs != E2F_OK)
     return rs;
@@ -1772,7 +1774,7 @@ e2f_status e2f_block_norm_backward(e2f_ctx* ctx, const e2f_norm_params* p, const
                                       {rstd, sizeof(float) * 2 * (size_t)n}, {p->post_w, w}, {p->res_scale, w},
                                       {p->pre_w, w}},
                                      {{grad_x, all}, {grad_block, all}, {grad_gate, gates}, {grad_post_w, w},
-                                      {grad_res_scale, w}, {grad_pre_w, w}});
+                                      {grad_res_scale, w}, {grad_pre_w, w}, {workspace, need}});
       rs != E2F_OK)
     return rs;
   if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");

@@ -74,3 +74,30 @@ def test_transposed_graph(e2f, ctx):
         assert call(**kw) == e2f.E2F_EINVAL, kw
     for kw in (dict(ct=at(2, 4 * EDGES)), dict(pm=at(4, 4 * EDGES)), dict(ci=at(1, 8 * (n + 1)))):
         assert call(**kw) == e2f.E2F_EDEVICE, kw
+
+
+def test_norms(e2f, ctx):
+    L, C = 2, 16
+    w = 4 * (L + 1) * C
+    prm = e2f.NormParams(L, C, 1, 1e-5, 0, at(1).value, at(2).value, at(3).value)
+
+    def fwd(out=at(7), normed=at(8), rstd=at(9)):
+        return e2f.lib.e2f_block_norm_forward(ctx.handle, ctypes.byref(prm), at(4), at(5), at(6), n, out, normed, rstd,
+                                              None)
+
+    assert fwd() == e2f.E2F_EDEVICE
+    for slot in (1, 2, 3):  # the weights are inputs too
+        for name in ("out", "normed", "rstd"):
+            assert fwd(**{name: at(slot)}) == e2f.E2F_EINVAL and fwd(**{name: at(slot, w - 4)}) == e2f.E2F_EINVAL
+            assert fwd(**{name: at(slot, w)}) == e2f.E2F_EDEVICE
+    need = ctypes.c_size_t(0)
+    assert e2f.lib.e2f_block_norm_workspace_size(ctx.handle, ctypes.byref(prm), n, ctypes.byref(need)) == e2f.E2F_OK
+
+    def bwd(ws=at(20), gx=at(13), gp=at(16)):
+        return e2f.lib.e2f_block_norm_backward(ctx.handle, ctypes.byref(prm), at(4), at(5), at(6), at(9), n, at(10),
+                                               at(11), gx, at(14), at(15), gp, at(17), at(18), ws, need.value, None)
+
+    assert bwd() == e2f.E2F_EDEVICE
+    for slot in (1, 2, 3, 4, 5, 6, 9, 10, 11, 13, 14, 15, 16, 17, 18):  # the workspace over any of them
+        assert bwd(ws=at(slot)) == e2f.E2F_EINVAL, slot
+    assert bwd(gx=at(20, need.value - 4)) == e2f.E2F_EINVAL and bwd(gx=at(20, need.value)) == e2f.E2F_EDEVICE
