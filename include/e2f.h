@@ -255,7 +255,7 @@ e2f_status e2f_grad_norm(e2f_ctx* ctx, int32_t count, const void* const* tensors
  * factor rounded to float32 (a norm that is infinite gives 0, NaN gives NaN: the caller
  * that wants to skip such a step looks at the norm).  outs[t] may be tensors[t] (nothing
  * is then written where the factor is 1); apart from that no out may overlap another
- * tensor (E2F_EINVAL).  max_norm > 0.  Asynchronous, no allocation, can be captured in
+ * tensor, or hold *sumsq (E2F_EINVAL).  max_norm > 0.  Asynchronous, no allocation, can be captured in
  * a HIP graph. */
 e2f_status e2f_grad_clip(e2f_ctx* ctx, int32_t count, const void* const* tensors /* host */,
                          void* const* outs /* host */, const int64_t* sizes /* host */,

@@ -1850,6 +1850,10 @@ e2f_status e2f_grad_clip(e2f_ctx* ctx, int32_t count, const void* const* tensors
     return fail(E2F_ENOMEM, "host memory for %d tensors", count);
   }
   if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
+  // every workgroup reads *sumsq: those that begin later would find what earlier ones wrote there
+  for (int i = 0; i < count; ++i)
+    if (overlap({sumsq, sizeof(double)}, {outs[i], (size_t)sizes[i] * (dtypes[i] == E2F_BF16 ? 2 : 4)}))
+      return fail(E2F_EINVAL, "sumsq lies in an output");
   hipStream_t s = (hipStream_t)stream;
   DeviceGuard g(ctx->device);
   E2F_TIMED("grad_clip", launch_grad_clip(count, tensors, outs, sizes, dtypes, total, sumsq, max_norm, s));
