@@ -142,9 +142,9 @@ typedef struct {
   int32_t k_heads;  /* heads of k, a divisor of H: head h reads k's head h / (H / k_heads) */
   int32_t dk;       /* features of a head, 0 (no product) .. 256 */
   int32_t n_rbf;    /* radial functions, 0 (none) or 2..32 */
-  float cutoff;     /* of the envelope and the radial functions */
+  float cutoff;     /* of the envelope and the radial functions, at least 2^-100 */
   float scale;      /* of the product, usually dk^-0.5 */
-  float cap;        /* the scores' bound; 0: none */
+  float cap;        /* the scores' bound, at least 2^-100; 0: none */
   e2f_dtype dtype;  /* of q, k and their gradients */
   int64_t ldq, ldk; /* elements from one atom's q (k) to the next's, at least heads dk (k_heads dk):
                        q and k may be columns of one projection; 0: packed */

@@ -1502,6 +1502,10 @@ e2f_status check_attention(e2f_ctx* ctx, const e2f_attention_params* p, int32_t 
   if (!finite_pos(p->cutoff)) return fail(E2F_EINVAL, "cutoff must be finite and positive");
   if (!std::isfinite(p->scale)) return fail(E2F_EINVAL, "scale must be finite");
   if (!std::isfinite(p->cap) || p->cap < 0.0f) return fail(E2F_EINVAL, "cap must be finite and >= 0");
+  // (the kernels multiply by their reciprocals, which 0 times infinity would make NaN)
+  constexpr float least = 0x1p-100f;
+  if (p->cutoff < least || (p->cap > 0.0f && p->cap < least))
+    return fail(E2F_EINVAL, "cutoff and a cap must be at least 2^-100");
   if ((int)p->dtype != E2F_F32 && (int)p->dtype != E2F_BF16) return fail(E2F_EINVAL, "dtype %d", (int)p->dtype);
   if ((p->ldq && p->ldq < (int64_t)p->heads * p->dk) || (p->ldk && p->ldk < (int64_t)p->k_heads * p->dk))
     return fail(E2F_EINVAL, "ldq or ldk is smaller than an atom's features");

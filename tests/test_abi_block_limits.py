@@ -1,0 +1,35 @@
+"""CPU-only checks of the block's operators at the ends of what their arguments can hold."""
+import ctypes
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def e2f():
+    import paper_2501_19216_amd as e
+    return e
+
+
+@pytest.fixture(scope="module")
+def ctx(e2f):
+    c = e2f.e2f_create(0, None)
+    yield c
+    c.close()
+
+
+def test_cutoffs_and_caps_without_a_reciprocal(e2f, ctx):
+    need = ctypes.c_size_t(0)
+
+    def call(cutoff=5.0, cap=10.0):
+        prm = e2f.AttentionParams(4, 4, 8, 32, cutoff, 0.3, cap, 0, 0, 0)
+        size = e2f.lib.e2f_attention_backward_workspace_size(ctx.handle, ctypes.byref(prm), 10, 30, ctypes.byref(need))
+        p = [ctypes.c_void_p((i + 1) << 20) for i in range(9)]
+        forward = e2f.lib.e2f_attention_forward(ctx.handle, ctypes.byref(prm), p[0], None, p[1], p[2], 10, p[3], p[4],
+                                                p[5], 30, p[6], p[7], None)
+        assert forward == (e2f.E2F_EDEVICE if size == e2f.E2F_OK else size)
+        return size
+
+    for tiny in (2.0 ** -149, 2.0 ** -126, 2.0 ** -101):
+        assert call(cap=tiny) == e2f.E2F_EINVAL and call(cutoff=tiny) == e2f.E2F_EINVAL
+    assert call(cap=2.0 ** -100, cutoff=2.0 ** -100) == e2f.E2F_OK and call(cap=0.0) == e2f.E2F_OK
+    assert call(cap=3e38, cutoff=3e38) == e2f.E2F_OK
