@@ -299,6 +299,12 @@ def _arg(ctx, t, dtype, shape, name):
     return t.data_ptr()
 
 
+def _fits(*sizes):
+    """The C interface's sizes are 32-bit: ctypes would take larger ones modulo 2^32."""
+    if max(sizes) > 0x7fffffff:
+        raise ValueError("atoms, heads, features and channels must be below 2^31")
+
+
 def _workspace(ctx, workspace, nbytes, device, stream):
     """The caller's workspace, or the context's own for the (current) stream, grown to nbytes."""
     if workspace is None:
@@ -324,6 +330,7 @@ def e2f_transpose_graph(ctx, n, row_ptr, col_idx, workspace=None):
     current stream, which grows on demand (code under graph capture gives one
     of its own)."""
     E, dev = col_idx.numel(), col_idx.device
+    _fits(n)
     rp, ci = _arg(ctx, row_ptr, torch.int64, (n + 1,), "row_ptr"), _arg(ctx, col_idx, torch.int32, (E,), "col_idx")
     b = ctypes.c_size_t(0)
     _check(lib.e2f_transpose_graph_workspace_size(ctx.handle, n, E, ctypes.byref(b)),
@@ -368,6 +375,7 @@ def _attention_args(ctx, pos, row_ptr, col_idx, cutoff, q, k, rbf_w, heads, scal
     if H is None:
         raise ValueError("heads must be given without q and rbf_w")
     R = 0 if rbf_w is None else rbf_w.shape[-1]
+    _fits(n, H, 0 if Hk is None else Hk, dk, R)
     prm = AttentionParams(H, H if Hk is None else Hk, dk, R, cutoff, scale, cap, dt, ldq, ldk)
     return prm, (_arg(ctx, pos, torch.float32, (n, 3), "pos"), _arg(ctx, graph_id, torch.int32, (n,), "graph_id"),
                  None if q is None else q.data_ptr(), None if k is None else k.data_ptr(), n,
@@ -434,6 +442,7 @@ def _norm_args(ctx, x, lmax, block, gate, post_w, res_scale, pre_w, eps):
     G = 0
     if gate is not None:
         G = 1 if gate.dim() == 2 else gate.shape[1]
+    _fits(n, C, G)
     w = [_arg(ctx, t, torch.float32, (lmax + 1, C), name)
          for t, name in ((post_w, "post_w"), (res_scale, "res_scale"), (pre_w, "pre_w"))]
     return NormParams(lmax, C, G, eps, _DTYPES[dt], *w), (

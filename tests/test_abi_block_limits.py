@@ -33,3 +33,25 @@ def test_cutoffs_and_caps_without_a_reciprocal(e2f, ctx):
         assert call(cap=tiny) == e2f.E2F_EINVAL and call(cutoff=tiny) == e2f.E2F_EINVAL
     assert call(cap=2.0 ** -100, cutoff=2.0 ** -100) == e2f.E2F_OK and call(cap=0.0) == e2f.E2F_OK
     assert call(cap=3e38, cutoff=3e38) == e2f.E2F_OK
+
+
+def test_bindings_do_not_take_sizes_modulo_two_to_the_32(e2f, ctx):
+    # tensors without memory: the call ends before their addresses are taken
+    import torch
+    meta = lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device="meta")  # noqa: E731
+    many = 2 ** 32 + 4
+    edges = dict(row_ptr=meta(many + 1, dtype=torch.int64), col_idx=meta(8, dtype=torch.int32))
+    assert meta(1).get_device() == ctx.device
+    for call in (lambda: e2f.e2f_transpose_graph(ctx, many, **edges),
+                 lambda: e2f.e2f_attention_forward(ctx, meta(many, 3), **edges, cutoff=5.0, heads=4),
+                 lambda: e2f.e2f_attention_forward(ctx, meta(1, 3), meta(2, dtype=torch.int64), edges["col_idx"], 5.0,
+                                                   q=meta(1, many, 2), k=meta(1, many, 2)),
+                 lambda: e2f.e2f_attention_forward(ctx, meta(1, 3), meta(2, dtype=torch.int64), edges["col_idx"], 5.0,
+                                                   rbf_w=meta(4, many)),
+                 lambda: e2f.e2f_attention_backward(ctx, meta(many, 3), **edges, cutoff=5.0, alpha=meta(8, 4),
+                                                    lse=meta(many, 4), grad_alpha=meta(8, 4), heads=4),
+                 lambda: e2f.e2f_block_norm_forward(ctx, meta(many, 4), 0, pre_w=meta(1, 4)),
+                 lambda: e2f.e2f_block_norm_forward(ctx, meta(1, many), 0, pre_w=meta(1, many)),
+                 lambda: e2f.e2f_block_norm_backward(ctx, meta(many, 4), meta(many, 2), 0, pre_w=meta(1, 4))):
+        with pytest.raises(ValueError, match="2\\^31"):
+            call()
