@@ -305,10 +305,18 @@ def _fits(*sizes):
         raise ValueError("atoms, heads, features and channels must be below 2^31")
 
 
+def _capturing(device):
+    """Whether this device's current stream is (torch asks the current device's)."""
+    if torch.cuda.current_device() == device:
+        return torch.cuda.is_current_stream_capturing()
+    with torch.cuda.device(device):
+        return torch.cuda.is_current_stream_capturing()
+
+
 def _workspace(ctx, workspace, nbytes, device, stream):
     """The caller's workspace, or the context's own for the (current) stream, grown to nbytes."""
     if workspace is None:
-        if torch.cuda.is_current_stream_capturing():
+        if _capturing(ctx.device):
             raise ValueError("under graph capture the workspace must be given")
         kept = ctx.stream_workspaces.get(stream.value)
         if kept is None or kept.numel() < nbytes:

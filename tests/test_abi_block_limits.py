@@ -55,3 +55,37 @@ def test_bindings_do_not_take_sizes_modulo_two_to_the_32(e2f, ctx):
                  lambda: e2f.e2f_block_norm_backward(ctx, meta(many, 4), meta(many, 2), 0, pre_w=meta(1, 4))):
         with pytest.raises(ValueError, match="2\\^31"):
             call()
+
+
+def test_capture_is_asked_of_the_context_s_device(e2f, monkeypatch):
+    # two devices, as torch shows them: the current one, and one whose current stream is being captured
+    import types
+
+    import torch
+    state = dict(current=0, capturing=1)
+
+    class Device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            self.before, state["current"] = state["current"], self.index
+
+        def __exit__(self, *a):
+            state["current"] = self.before
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: state["current"])
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: state["current"] == state["capturing"])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    for current in (0, 1):
+        for device in (0, 1):
+            state["current"] = current
+            own = types.SimpleNamespace(device=device, stream_workspaces={})
+            ask = lambda: e2f._workspace(own, None, 10, torch.device("cpu"), types.SimpleNamespace(value=7))  # noqa: E731
+            if device == state["capturing"]:
+                with pytest.raises(ValueError, match="capture"):
+                    ask()
+                assert not own.stream_workspaces
+            else:
+                assert ask().numel() >= 10
+            assert state["current"] == current
