@@ -629,7 +629,8 @@ __global__ __launch_bounds__(256, 3) void k_att_receivers(AttnArgs a, AttnShape 
       const float d = length(dx, dy, dz);
       float sl;
       env[lane] = envelope(a.rc, d, &sl);
-      dist[lane] = d, slope[lane] = sl, renv[lane] = 1.0f / env[lane];
+      // (a radial function's slope holds z exp(-z^2), which is to be 0 where a distance's square is past float32)
+      dist[lane] = d > 1e18f ? 1e18f : d, slope[lane] = sl, renv[lane] = 1.0f / env[lane];
       wave_sync();
       Features<LPE, F> f;
       for (int b0 = 0; b0 < count; b0 += f.BE) {
