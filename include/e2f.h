@@ -164,7 +164,9 @@ typedef struct {
  * (unused if dk = 0); rbf_w float32 [H][n_rbf]; alpha float32 [n_edges][H];
  * lse float32 [n][H], kept for the backward.  Sums and statistics are float32.
  * Without a cap, for float32 features and one graph the weights are those of
- * e2f_attention_weights with q scaled (up to rounding).  The CSR is trusted for
+ * e2f_attention_weights with q scaled (up to rounding): which call is shorter goes by the
+ * size, that one up to some 10^5 edges of a few heads, this one from there on (and
+ * this one alone has a backward).  The CSR is trusted for
  * values but read with clamped indices.  Rows are gathered from k in index order
  * of the atoms: where atoms that are near have near indices the gathers hit the
  * caches.  Outputs must not overlap inputs (E2F_EINVAL).  Asynchronous, no allocation,

@@ -17,16 +17,18 @@
 //     gather reads whole lines; the features of a head are summed over its lanes.
 //     This gather, H dk values an edge out of the caches, is what bounds both
 //     directions (1.5 million edges of 8 heads of 16 floats are 780 MB; with 32 radial
-//     functions and 20,000 atoms forward 101 us, backward 238 for the receivers and 124
-//     for the senders, the transposed graph 86).
+//     functions and 20,000 atoms forward 102 us, backward 261 for the receivers and 125
+//     for the senders, the transposed graph 88).
 //   - The radial part: float matrix products of 16 edges, 16 heads and 4 functions
 //     (v_mfma_f32_16x16x4_f32), each lane evaluating the functions it passes in.
 //   - The softmax's running maximum and sum stay with the lanes that hold a head in
 //     the product's output; the scores of up to 128 edges stay in the LDS until the
 //     row's sum is known, those of longer rows in alpha.
 // Heads go in groups of up to 16 (one matrix tile), a group a workgroup.  Backward:
-// the receivers' kernel makes the scores again, ds from them, dq and each edge's
-// position gradient, and sums dw as matrix products too; the senders' kernel
+// the receivers' kernel makes the scores again (the cap's slope and the edges beyond the
+// cutoff need them) and takes p from alpha, which holds no rounding of lse (forward and backward
+// 553 us; p from the scores and lse 543), ds from both, dq and each edge's position gradient,
+// and sums dw as matrix products too; the senders' kernel
 // gathers ds and q over the transposed graph.  No atomics in either: the same
 // bits every time.
 #include <hip/hip_runtime.h>
@@ -113,8 +115,8 @@ constexpr float kPi = 3.14159265358979f, kLog2e = 1.44269504088896f;
 // below 0.37: less than half a step of 1, which the largest function of a distance is near to
 __device__ __forceinline__ float exp_radial(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 // exp(x) for x <= 0 to three half steps of its value however far x is: 2^t (1 + r) with t log 2 + r = x and t near
-// x log2(e): rounding x log2(e) alone leaves |x| half steps, 64 of them at 80 (1.5 million edges, forward: 98 us with that
-// and a reciprocal in the tangent, 102 with this and the quotient below).  (Below 2^-126: 0.)
+// x log2(e): rounding x log2(e) alone leaves |x| half steps, 64 of them at 80, and saves no time (1.5 million edges,
+// forward: 102 us with that and a reciprocal in the tangent, 97 with this and the quotient below).  (Below 2^-126: 0.)
 __device__ __forceinline__ float exp_near(float x) {
   constexpr float ln2 = 0.693147182464599609f, low = -1.90465430e-9f;  // log 2 = ln2 + low
   const float t = x * kLog2e, r = fmaf(-t, low, fmaf(-t, ln2, x));
@@ -177,7 +179,7 @@ __device__ __forceinline__ Group group_of(const AttnArgs& a, const AttnShape& s,
 }
 
 // floats of an entry's scores in the LDS: 9 (up to 8 heads, in the forward, where the LDS bounds the waves of a CU: five
-// instead of four a SIMD, 109 us instead of 126 for 1.5 million edges of 8 heads) or 17 (up to 16); odd: other banks
+// instead of four a SIMD, 97 us instead of 122 for 1.5 million edges of 8 heads) or 17 (up to 16); odd: other banks
 constexpr int kLd = 17;
 
 // Lanes over a group's heads (hp, their number's next power of two) and over 64 / hp entries: a head belongs to a lane
@@ -949,7 +951,7 @@ __global__ __launch_bounds__(256) void k_t_zero(Transposed t) {
   if (i < t.n) t.extra[i] = 0;
 }
 // the place of x among the n ascending values at p, or -1 (one read a step and none after it: scattered reads are what
-// this costs; three at once in half the steps took 68 us where single ones took 39, 1.5 million edges)
+// this costs; three at once in half the steps took 68 us where single ones take 52, 1.5 million edges)
 __device__ __forceinline__ int place_among(const int32_t* p, int n, int x) {
   int lo = 0;
   while (n > 0) {
@@ -1199,7 +1201,10 @@ AttnShape shape_of(const AttnArgs& a, bool senders) {
   s.hp = 1;
   while (s.hp < s.heads) s.hp <<= 1, ++s.hp_log;
   s.one = s.units == 1 && (share == 1 || a.dk == 0) && a.dk % vec == 0;
-  // four waves a row where they find four batches on average
+  // four waves a row where they find four batches on average (8 heads of 16, forward and backward: 2,000 rows of 128
+  // edges 21 and 74 us by one wave, 27 and 94 by four; of 192 35 and 100, 32 and 105; of 256 45 and 127, 33 and 113;
+  // 20,000 rows of 76 98 and 367, 185 and 708; of 256 344 and 1,137, 278 and 1,202).  By the average: one long row
+  // among short ones is one wave's work (20,000 edges in one of 20,000 rows of 30: 3.1 and 5.3 ms, by four 0.8 and 1.7)
   s.wpr = a.E / a.n >= 256 ? 4 : 1;
   s.rows = 1;
   return s;
@@ -1207,7 +1212,8 @@ AttnShape shape_of(const AttnArgs& a, bool senders) {
 
 }  // namespace
 
-// Rows of a workgroup: one round of workgroups over the card, `per_cu` a CU
+// Rows of a workgroup: one round of workgroups over the card, `per_cu` a CU.  Three are what its registers hold
+// (20,000 atoms, forward and backward: 556 us; two 616, six 577, twelve 568; 256 molecules of 30: 76, 80, 81 and 82)
 static int rows_of(const AttnArgs& a, int wpr, int per_cu) {
   const int least = wpr == 1 ? 4 : 1;
   return least * (int)(((int64_t)a.n + least * 256 * per_cu - 1) / (least * 256 * per_cu));
@@ -1278,7 +1284,7 @@ hipError_t launch_att_backward(const AttnArgs& a, const AttnGrad& gr, hipStream_
   const int parts = attention_parts(a), vec = a.bf16 ? BF16::VEC : F32::VEC;
   sh.dq = sh.one ? 0 : 64 / sh.lpe * sh.heads * sh.lph * vec;
   sh.lds = 64 * kLd + 7 * 64 + 256 + sh.dq;
-  if (sh.lds < 512) sh.lds = 512;  // (dw's sum over the waves)
+  static_assert(64 * kLd + 7 * 64 + 256 >= 512, "room for dw's sum over the waves");
   {
     const dim3 grid((unsigned)parts, (unsigned)sh.groups);
     const size_t lds = sizeof(float) * 4 * sh.lds;
