@@ -263,6 +263,112 @@ e2f_status e2f_grad_clip(e2f_ctx* ctx, int32_t count, const void* const* tensors
                          void* const* outs /* host */, const int64_t* sizes /* host */,
                          const int32_t* dtypes /* host */, const double* sumsq, float max_norm, void* stream);
 
+typedef struct {
+  int32_t vocab;      /* V, rows of the table */
+  int32_t channels;   /* C, 1..65536 */
+  int lmax;           /* L, 0..6; 0: plain rows [n][C] */
+  float scale;        /* finite */
+  e2f_dtype table_dtype; /* of the table and its gradient */
+  e2f_dtype dtype;    /* of out and its gradient */
+  int32_t index_bytes;/* 4 (int32) or 8 (int64) */
+  int64_t ld;         /* elements from one row of out (or of its gradient) to the next, at least (L+1)^2 C; 0: packed */
+} e2f_embedding_params;
+
+/* Rows of a table by the types of atoms (or of edges, of tokens) as the scalars of irrep
+ * features, the first input of a model's blocks:
+ *   out[i][0][c] = scale table[index[i]][c],   out[i][k][c] = 0 for k = 1 .. (L+1)^2 - 1.
+ * An index outside [0, V) (padding) gives a row of zeros.  index [n], table [V][C], out
+ * [n][(L+1)^2][C], rows ld apart (what lies between them is not written).  The product
+ * is float32, rounded once.  Outputs must not overlap inputs (E2F_EINVAL).
+ * Asynchronous, no allocation, can be captured in a HIP graph; deterministic. */
+e2f_status e2f_embedding_forward(e2f_ctx* ctx, const e2f_embedding_params* params, const void* table,
+                                 const void* index, int32_t n, void* out, void* stream);
+/* The table's gradient for grad_out (like out; of its components only the scalars are read):
+ *   grad_table[v][c] = scale sum over the i with index[i] = v of grad_out[i][0][c],
+ * written whole, zeros for types that no row has; rows with an index outside [0, V) add
+ * nothing and are not looked at.  The rows are sorted by type and summed in float32 in a fixed
+ * order (up to 256 neighbours of the sorted rows at a time, then these sums), rounded once.
+ * workspace: e2f_embedding_backward_workspace_size bytes, 256-byte aligned (E2F_ECAPACITY
+ * below).  Outputs must not overlap inputs (E2F_EINVAL).  Asynchronous, no allocation, can be
+ * captured in a HIP graph; deterministic. */
+e2f_status e2f_embedding_backward_workspace_size(e2f_ctx* ctx, const e2f_embedding_params* params, int32_t n,
+                                                 size_t* bytes);
+e2f_status e2f_embedding_backward(e2f_ctx* ctx, const e2f_embedding_params* params, const void* index, int32_t n,
+                                  const void* grad_out, void* grad_table, void* workspace, size_t workspace_bytes,
+                                  void* stream);
+
+typedef struct {
+  int lmax;              /* L, 0..6; 0: plain rows [n][C] */
+  int32_t channels;      /* C: with L = 0 1..8192, else a multiple of 4, <= 1024 */
+  float eps;             /* added to the variance and the mean square, >= 0 */
+  int32_t silu;          /* 1: y sigmoid(y) behind the norm (L = 0 only); 0: none */
+  e2f_dtype dtype;       /* of x, out and their gradients */
+  const float* weight;   /* device [(L+1)][C], or NULL: ones */
+  const float* bias;     /* device [C], or NULL: zeros */
+  int64_t ldx;           /* elements from one row of x to the next, at least (L+1)^2 C; 0: packed */
+} e2f_layer_norm_params;
+
+/* Layer norm of irrep features (equivariant: the scalars by mean and variance, all higher
+ * degrees by one root mean square), and with L = 0 of rows of any length, e.g. in a radial
+ * network, with its activation:
+ *   m = mean_c x[i][0][c],  r0 = (mean_c (x[i][0][c] - m)^2 + eps)^-1/2,
+ *   y = weight[0][c] (x[i][0][c] - m) r0 + bias[c],   out[i][0][c] = y, or y sigmoid(y),
+ *   r1 = (mean over l = 1..L of the mean over (m, c) of x_l^2, plus eps)^-1/2,
+ *   out[i][l,m][c] = weight[l][c] x r1 for l >= 1.
+ * (e2f_block_norm_forward takes one root mean square over all degrees instead, without a mean
+ * or bias.)  x [n][(L+1)^2][C], rows ldx apart (columns of a projection, the scalars of irrep
+ * features); out packed.  Statistics and all between loads and stores are float32, rounded
+ * once.  Outputs must not overlap inputs (E2F_EINVAL).  Asynchronous, no allocation, can be
+ * captured in a HIP graph; deterministic. */
+e2f_status e2f_layer_norm_forward(e2f_ctx* ctx, const e2f_layer_norm_params* params, const void* x, int32_t n,
+                                  void* out, void* stream);
+/* Backward of e2f_layer_norm_forward (same parameters and x; its statistics are taken again):
+ * the vector-Jacobian products for grad_out [n][(L+1)^2][C], packed: grad_x of the same shape,
+ * packed; grad_weight float32 [(L+1)][C] and grad_bias float32 [C], summed over the rows (also
+ * where weight or bias is NULL).  Any of them may be NULL (not all).  workspace:
+ * e2f_layer_norm_workspace_size bytes, 256-byte aligned (E2F_ECAPACITY below); not needed
+ * without grad_weight and grad_bias.  Outputs must not overlap inputs (E2F_EINVAL).
+ * Asynchronous, no allocation, can be captured in a HIP graph; deterministic. */
+e2f_status e2f_layer_norm_workspace_size(e2f_ctx* ctx, const e2f_layer_norm_params* params, int32_t n, size_t* bytes);
+e2f_status e2f_layer_norm_backward(e2f_ctx* ctx, const e2f_layer_norm_params* params, const void* x, int32_t n,
+                                   const void* grad_out, void* grad_x, float* grad_weight, float* grad_bias,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+typedef struct {
+  int32_t rows, cols;    /* of every matrix, row-major and packed; up to 65536, 2^31 - 1 values */
+  int32_t steps;         /* Newton-Schulz steps, 0..64 */
+  const float* coefs;    /* host [steps][3]: a, b, c of each; NULL: 3.4445, -4.7750, 2.0315 */
+  float eps;             /* added to the norm, >= 0 */
+  float momentum;        /* mu */
+  int32_t nesterov;      /* 1: g + mu m' is orthogonalised, 0: m' */
+  float scale;           /* of the orthogonalised matrix */
+  float decay;           /* of the weights; 0: they are not read */
+  e2f_dtype grad_dtype;  /* of the gradients */
+  e2f_dtype dtype;       /* of weights and outs */
+} e2f_orthogonalize_params;
+
+/* Orthogonalised updates of `count` matrices of one size, e.g. of a model's mixing weights
+ * after e2f_grad_clip (the step of the Muon optimiser).  For each:
+ *   m' = momentum m + g,   u = g + momentum m' (nesterov) or m';   without moments u = g;
+ *   X = u / (|u|_F + eps),  then `steps` times  X <- a X + (b P + c P^2) X,  P = X X^T;
+ *   out = decay weight + scale X.
+ * grads, moments, new_moments, weights, outs: host arrays of `count` device addresses (an
+ * element's alignment), read before the call returns.  moments (float32) and new_moments go together and may be NULL;
+ * new_moments[t] may be moments[t].  weights may be NULL with decay = 0; outs[t] may be weights[t].  Apart
+ * from these no output may overlap another tensor (E2F_EINVAL), and with decay = 0 and
+ * momentum = 0 an input is still one.  X and the sums of the products are float32; the products'
+ * operands have 22 bits (two float16 parts, scaled by bounds of the singular values that follow from the
+ * coefficients: those for which they leave [0, 64], or |b t + c t^2| 4096, are refused, E2F_EINVAL).
+ * A matrix with a value that is not finite becomes NaN; one of zeros stays zero (with eps > 0).
+ * workspace: e2f_orthogonalize_workspace_size bytes, 256-byte aligned (E2F_ECAPACITY below).
+ * Asynchronous, no allocation, can be captured in a HIP graph; deterministic. */
+e2f_status e2f_orthogonalize_workspace_size(e2f_ctx* ctx, const e2f_orthogonalize_params* params, int32_t count,
+                                            size_t* bytes);
+e2f_status e2f_orthogonalize(e2f_ctx* ctx, const e2f_orthogonalize_params* params, int32_t count,
+                             const void* const* grads /* host */, const float* const* moments /* host */,
+                             float* const* new_moments /* host */, const void* const* weights /* host */,
+                             void* const* outs /* host */, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Real regular solid harmonics (Def. 2.1) of p_i = pos_i - origins[origin_id[i]]
  * (origin 0 if origin_id is NULL; the zero vector if origins is NULL),
  * evaluated in float64 and rounded: out [N][(lmax+1)^2] float32. */
@@ -501,7 +607,8 @@ e2f_status e2f_last_slices(const e2f_ctx* ctx, int64_t* slices /* host */);
  * records and starts bracketing every launch group of this context with HIP
  * events on its stream (bbox, nl_count, nl_fill, tile_plan, sh, node_tp,
  * aggregate, recouple, mix, edge_tp, attention, attention_grad, transpose,
- * block_norm, block_norm_grad, grad_norm, grad_clip and others);
+ * block_norm, block_norm_grad, grad_norm, grad_clip, embedding, embedding_grad,
+ * layer_norm, layer_norm_grad, orthogonalize and others);
  * e2f_profile(ctx, 0) stops.  (sync) */
 e2f_status e2f_profile(e2f_ctx* ctx, int enable);
 /* Text "name launches total_ms" per line for the records so far, into buf

@@ -33,7 +33,9 @@ EXPORTED = ["e2f_create", "e2f_destroy", "e2f_last_error", "e2f_node_tp_dim", "e
             "e2f_transpose_graph_workspace_size", "e2f_transpose_graph", "e2f_attention_forward",
             "e2f_attention_backward_workspace_size", "e2f_attention_backward", "e2f_block_norm_forward",
             "e2f_block_norm_workspace_size", "e2f_block_norm_backward", "e2f_grad_norm_workspace_size",
-            "e2f_grad_norm", "e2f_grad_clip", "e2f_profile", "e2f_profile_read", "e2f_last_slices"]
+            "e2f_grad_norm", "e2f_grad_clip", "e2f_embedding_forward", "e2f_embedding_backward_workspace_size",
+            "e2f_embedding_backward", "e2f_layer_norm_forward", "e2f_layer_norm_workspace_size",
+            "e2f_layer_norm_backward", "e2f_orthogonalize_workspace_size", "e2f_orthogonalize", "e2f_profile", "e2f_profile_read", "e2f_last_slices"]
 
 
 class E2FError(RuntimeError):
@@ -59,6 +61,25 @@ class NormParams(ctypes.Structure):
     _fields_ = [("lmax", ctypes.c_int), ("channels", ctypes.c_int32), ("gates", ctypes.c_int32),
                 ("eps", ctypes.c_float), ("dtype", ctypes.c_int), ("post_w", ctypes.c_void_p),
                 ("res_scale", ctypes.c_void_p), ("pre_w", ctypes.c_void_p)]
+
+
+class EmbeddingParams(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int32), ("channels", ctypes.c_int32), ("lmax", ctypes.c_int),
+                ("scale", ctypes.c_float), ("table_dtype", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("index_bytes", ctypes.c_int32), ("ld", ctypes.c_int64)]
+
+
+class LayerNormParams(ctypes.Structure):
+    _fields_ = [("lmax", ctypes.c_int), ("channels", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("silu", ctypes.c_int32), ("dtype", ctypes.c_int), ("weight", ctypes.c_void_p),
+                ("bias", ctypes.c_void_p), ("ldx", ctypes.c_int64)]
+
+
+class OrthogonalizeParams(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("steps", ctypes.c_int32),
+                ("coefs", ctypes.c_void_p), ("eps", ctypes.c_float), ("momentum", ctypes.c_float),
+                ("nesterov", ctypes.c_int32), ("scale", ctypes.c_float), ("decay", ctypes.c_float),
+                ("grad_dtype", ctypes.c_int), ("dtype", ctypes.c_int)]
 
 
 def _load():
@@ -123,6 +144,7 @@ def _load():
     L.e2f_wigner6j_conv_backward.restype = i
     sz, psz = ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)
     pa, pn = ctypes.POINTER(AttentionParams), ctypes.POINTER(NormParams)
+    pe, pl, po = (ctypes.POINTER(t) for t in (EmbeddingParams, LayerNormParams, OrthogonalizeParams))
     for name, args in (("e2f_transpose_graph_workspace_size", [p, i32, i64, psz]),
                        ("e2f_transpose_graph", [p, i32, p, p, i64, p, p, p, p, sz, p]),
                        ("e2f_attention_forward", [p, pa, p, p, p, p, i32, p, p, p, i64, p, p, p]),
@@ -133,7 +155,15 @@ def _load():
                        ("e2f_block_norm_backward", [p, pn, p, p, p, p, i32] + [p] * 9 + [sz, p]),
                        ("e2f_grad_norm_workspace_size", [p, i32, p, psz]),
                        ("e2f_grad_norm", [p, i32, p, p, p, p, p, p, sz, p]),
-                       ("e2f_grad_clip", [p, i32, p, p, p, p, p, f, p])):
+                       ("e2f_grad_clip", [p, i32, p, p, p, p, p, f, p]),
+                       ("e2f_embedding_forward", [p, pe, p, p, i32, p, p]),
+                       ("e2f_embedding_backward_workspace_size", [p, pe, i32, psz]),
+                       ("e2f_embedding_backward", [p, pe, p, i32, p, p, p, sz, p]),
+                       ("e2f_layer_norm_forward", [p, pl, p, i32, p, p]),
+                       ("e2f_layer_norm_workspace_size", [p, pl, i32, psz]),
+                       ("e2f_layer_norm_backward", [p, pl, p, i32, p, p, p, p, p, sz, p]),
+                       ("e2f_orthogonalize_workspace_size", [p, po, i32, psz]),
+                       ("e2f_orthogonalize", [p, po, i32, p, p, p, p, p, p, sz, p])):
         getattr(L, name).argtypes = args
         getattr(L, name).restype = i
     return L
@@ -560,6 +590,205 @@ def e2f_clip_grad_norm(ctx, tensors, max_norm, outs=None, workspace=None):
     sumsq, norm = _grad_norm(ctx, t, device, workspace, stream)
     _grad_clip(ctx, t, outs, sumsq, max_norm, stream)
     return norm
+
+
+def _rows(ctx, t, n, lmax, C, dtype, name):
+    """Elements between rows of t [n, (lmax+1)^2, C] (lmax = 0: also [n, C]), packed within a row; 0: packed."""
+    if t.dtype != dtype or t.get_device() != ctx.device:
+        raise ValueError("%s must be a %s tensor on the context's device" % (name, dtype))
+    K = (lmax + 1) ** 2
+    shape, stride = t.shape, t.stride()
+    if shape != (n, K, C) and (lmax or shape != (n, C)):
+        raise ValueError("%s must be [%d, %d, %d]" % (name, n, K, C))
+    if (C > 1 and stride[-1] != 1) or (K > 1 and stride[1] != C) or (n > 1 and stride[0] < K * C):
+        raise ValueError("%s must be packed within a row, with at least (lmax+1)^2 C elements between rows" % name)
+    return stride[0] if n > 1 else 0
+
+
+def _embedding_args(ctx, index, vocab, C, lmax, scale, table_dtype, dtype, ld):
+    """The parameters and the index's address."""
+    if index.dtype not in (torch.int32, torch.int64) or index.dim() != 1:
+        raise ValueError("index must be [n] of int32 or int64")
+    if table_dtype not in _DTYPES or dtype not in _DTYPES:
+        raise ValueError("the table and the rows must be float32 or bfloat16")
+    _fits(index.shape[0], vocab, C)
+    return (EmbeddingParams(vocab, C, lmax, scale, _DTYPES[table_dtype], _DTYPES[dtype],
+                            4 if index.dtype == torch.int32 else 8, ld),
+            _arg(ctx, index, index.dtype, index.shape, "index"))
+
+
+def e2f_embedding_forward(ctx, table, index, lmax=0, scale=1.0, dtype=None, out=None):
+    """Rows of the table [V, C] (float32 or bfloat16) by their types, as the
+    scalars of irrep features: out [n, (lmax+1)^2, C] (lmax = 0: [n, C]) of
+    `dtype` (the table's where None), the other components 0.  index [n] int32 or
+    int64; those outside [0, V) give zeros.  out may have rows further apart."""
+    if table.dim() != 2:
+        raise ValueError("table must be [V, C]")
+    n, (V, C) = index.shape[0], table.shape
+    if out is None:
+        dtype = table.dtype if dtype is None else dtype
+        out = torch.empty((n, (lmax + 1) ** 2, C) if lmax else (n, C), dtype=dtype, device=table.device)
+        ld = 0
+    else:
+        dtype = out.dtype if dtype is None else dtype
+        ld = _rows(ctx, out, n, lmax, C, dtype, "out")
+    prm, at = _embedding_args(ctx, index, V, C, lmax, scale, table.dtype, dtype, ld)
+    _check(lib.e2f_embedding_forward(ctx.handle, ctypes.byref(prm), _arg(ctx, table, table.dtype, (V, C), "table"), at,
+                                     n, out.data_ptr(), _stream(table.device)), "e2f_embedding_forward")
+    return out
+
+
+def e2f_embedding_backward(ctx, index, grad_out, vocab, lmax=0, scale=1.0, dtype=None, grad_table=None,
+                           workspace=None):
+    """The gradient of e2f_embedding_forward's table, [vocab, C] of `dtype`
+    (grad_out's where None), zeros for types without rows.  grad_out [n,
+    (lmax+1)^2, C] (lmax = 0: also [n, C]) may have rows further apart."""
+    n, C, dev = index.shape[0], grad_out.shape[-1], grad_out.device
+    ld = _rows(ctx, grad_out, n, lmax, C, grad_out.dtype, "grad_out")
+    if grad_table is None:
+        grad_table = torch.empty(vocab, C, dtype=grad_out.dtype if dtype is None else dtype, device=dev)
+    elif dtype is not None and grad_table.dtype != dtype:
+        raise ValueError("grad_table must be of `dtype`")
+    prm, at = _embedding_args(ctx, index, vocab, C, lmax, scale, grad_table.dtype, grad_out.dtype, ld)
+    b = ctypes.c_size_t(0)
+    _check(lib.e2f_embedding_backward_workspace_size(ctx.handle, ctypes.byref(prm), n, ctypes.byref(b)),
+           "e2f_embedding_backward_workspace_size")
+    stream = _stream(dev)
+    workspace = _workspace(ctx, workspace, b.value, dev, stream)
+    _check(lib.e2f_embedding_backward(ctx.handle, ctypes.byref(prm), at, n, grad_out.data_ptr(),
+                                      _arg(ctx, grad_table, grad_table.dtype, (vocab, C), "grad_table"),
+                                      workspace.data_ptr(), workspace.numel(), stream), "e2f_embedding_backward")
+    return grad_table
+
+
+def _layer_args(ctx, x, lmax, weight, bias, eps, silu):
+    """The parameters, the rows and a row's channels."""
+    if x.dtype not in _DTYPES:
+        raise ValueError("x must be float32 or bfloat16")
+    n, C = x.shape[0], x.shape[-1]
+    _fits(n, C)
+    if weight is not None and not lmax and weight.dim() == 1:
+        weight = weight[None]
+    return n, C, LayerNormParams(lmax, C, eps, int(bool(silu)), _DTYPES[x.dtype],
+                                 _arg(ctx, weight, torch.float32, (lmax + 1, C), "weight"),
+                                 _arg(ctx, bias, torch.float32, (C,), "bias"),
+                                 _rows(ctx, x, n, lmax, C, x.dtype, "x"))
+
+
+def e2f_layer_norm_forward(ctx, x, lmax=0, weight=None, bias=None, eps=1e-5, silu=False, out=None):
+    """Layer norm of irrep features x [n, (lmax+1)^2, C] (scalars by mean and
+    variance, higher degrees by one root mean square), or of rows [n, C] with lmax
+    = 0, there with silu also its activation: out like x, packed.  x float32 or
+    bfloat16, whose rows may be further apart; weight [lmax+1, C] (lmax = 0: also
+    [C]), bias [C] float32."""
+    n, C, prm = _layer_args(ctx, x, lmax, weight, bias, eps, silu)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _check(lib.e2f_layer_norm_forward(ctx.handle, ctypes.byref(prm), x.data_ptr(), n,
+                                      _arg(ctx, out, x.dtype, x.shape, "out"), _stream(x.device)),
+           "e2f_layer_norm_forward")
+    return out
+
+
+def e2f_layer_norm_backward(ctx, x, grad_out, lmax=0, weight=None, bias=None, eps=1e-5, silu=False, want_x=True,
+                            want_weights=True, workspace=None):
+    """Vector-Jacobian products of e2f_layer_norm_forward: (grad_x like x,
+    packed; grad_weight [lmax+1, C]; grad_bias [C]), None unless wanted."""
+    n, C, prm = _layer_args(ctx, x, lmax, weight, bias, eps, silu)
+    dev = x.device
+    gx = torch.empty(x.shape, dtype=x.dtype, device=dev) if want_x else None
+    gw = gb = None
+    space, stream = (None, 0), _stream(dev)
+    if want_weights:
+        gw = torch.empty(lmax + 1, C, dtype=torch.float32, device=dev)
+        gb = torch.empty(C, dtype=torch.float32, device=dev)
+        if weight is not None and weight.dim() == 1:
+            gw = gw[0]
+        b = ctypes.c_size_t(0)
+        _check(lib.e2f_layer_norm_workspace_size(ctx.handle, ctypes.byref(prm), n, ctypes.byref(b)),
+               "e2f_layer_norm_workspace_size")
+        workspace = _workspace(ctx, workspace, b.value, dev, stream)
+        space = (workspace.data_ptr(), workspace.numel())
+    _check(lib.e2f_layer_norm_backward(ctx.handle, ctypes.byref(prm), x.data_ptr(), n,
+                                       _arg(ctx, grad_out, x.dtype, x.shape, "grad_out"),
+                                       *(None if t is None else t.data_ptr() for t in (gx, gw, gb)), *space, stream),
+           "e2f_layer_norm_backward")
+    return gx, gw, gb
+
+
+def _matrices(ctx, tensors, name, dtype=None, like=None):
+    """Checks a list of matrices [rows, cols] or stacks of them [batch, rows, cols] (contiguous, of one type)."""
+    if like is not None and len(tensors) != len(like):
+        raise ValueError("%s must have a tensor for every gradient" % name)
+    for k, t in enumerate(tensors):
+        if t.get_device() != ctx.device or not t.is_contiguous() or t.dtype != (dtype or t.dtype):
+            raise ValueError("%s must be contiguous tensors of one type on the context's device" % name)
+        if t.dim() not in (2, 3) or (like is not None and t.shape != like[k].shape):
+            raise ValueError("%s must be [rows, cols] or [batch, rows, cols], like the gradients" % name)
+
+
+def e2f_orthogonalize(ctx, grads, outs=None, weights=None, moments=None, new_moments=None, momentum=0.95,
+                      nesterov=True, steps=5, coefs=None, scale=1.0, decay=0.0, eps=1e-7, workspace=None):
+    """Orthogonalised updates of matrices (the step of the Muon optimiser):
+    outs[t] = decay weights[t] + scale X, X from grads[t] through its momentum by
+    `steps` Newton-Schulz steps with coefs (a, b, c), or one such triple for
+    each step (None: 3.4445, -4.7750, 2.0315).  Tensors are matrices [rows, cols]
+    or stacks [batch, rows, cols] of any sizes; grads of one type, weights and outs of one
+    (float32 or bfloat16), moments float32.  Without moments the gradients
+    themselves are orthogonalised.  None: new tensors like weights (or grads) for outs, and
+    moments themselves for new_moments; outs may be weights.  Returns outs."""
+    if not grads:
+        return [] if outs is None else outs
+    gt = grads[0].dtype
+    _matrices(ctx, grads, "grads", gt)
+    if outs is None:
+        outs = [torch.empty_like(t) for t in (grads if weights is None else weights)]
+    wt = outs[0].dtype if outs else None
+    if gt not in _DTYPES or wt not in _DTYPES:
+        raise ValueError("grads and outs must be float32 or bfloat16")
+    _matrices(ctx, outs, "outs", wt, grads)
+    if weights is not None:
+        _matrices(ctx, weights, "weights", wt, grads)
+    if new_moments is None:
+        new_moments = moments
+    elif moments is None:
+        raise ValueError("new_moments without moments")
+    if moments is not None:
+        _matrices(ctx, moments, "moments", torch.float32, grads)
+        _matrices(ctx, new_moments, "new_moments", torch.float32, grads)
+    flat = None
+    if coefs is not None:
+        flat = [float(c) for row in (coefs if len(coefs) and hasattr(coefs[0], "__len__") else [coefs] * steps)
+                for c in row]
+        if len(flat) != 3 * steps:
+            raise ValueError("coefs must be three numbers, or three for each step")
+        flat = array.array("f", flat)
+    by_size = {}
+    for k, t in enumerate(grads):
+        by_size.setdefault(t.shape[-2:], []).append(k)
+    device = grads[0].device
+    stream = _stream(device)
+    for (rows, cols), which in by_size.items():
+        _fits(rows, cols)
+        lists = []
+        for tensors in (grads, moments, new_moments, weights, outs):
+            if tensors is None:
+                lists.append(None)
+                continue
+            step = rows * cols * tensors[which[0]].element_size()
+            lists.append(array.array("Q", [t.data_ptr() + i * step for t in (tensors[k] for k in which)
+                                           for i in range(t.shape[0] if t.dim() == 3 else 1)]))
+        count = len(lists[0])
+        prm = OrthogonalizeParams(rows, cols, steps, None if flat is None else flat.buffer_info()[0], eps, momentum,
+                                  int(bool(nesterov)), scale, decay, _DTYPES[gt], _DTYPES[wt])
+        b = ctypes.c_size_t(0)
+        _check(lib.e2f_orthogonalize_workspace_size(ctx.handle, ctypes.byref(prm), count, ctypes.byref(b)),
+               "e2f_orthogonalize_workspace_size")
+        space = _workspace(ctx, workspace, b.value, device, stream)
+        _check(lib.e2f_orthogonalize(ctx.handle, ctypes.byref(prm), count,
+                                     *(None if a is None else a.buffer_info()[0] for a in lists), space.data_ptr(),
+                                     space.numel(), stream), "e2f_orthogonalize")
+    return outs
 
 
 def e2f_solid_harmonics(ctx: Context, pos: torch.Tensor, lmax: int, origins: torch.Tensor | None = None,

@@ -17,6 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libe2f.so")
 SOURCES = ["neighbor.hip", "plan.hip", "conv.hip", "fused.hip", "edge_grad.hip", "dense.hip", "attention.hip", "graph_attention.hip", "block_norm.hip", "grad_clip.hip",
+           "layer_norm.hip", "embedding.hip", "orthogonalize.hip",
            "abi.cpp", "tables.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1614,6 +1614,147 @@ size_t grad_norm_bytes(int32_t count, const int64_t* sizes, int64_t total) {
   return al256(sizeof(double) * (size_t)std::max<int64_t>(parts, 1));
 }
 
+bool dtype_ok(int d) { return d == E2F_F32 || d == E2F_BF16; }
+size_t bytes_of(int d) { return d == E2F_BF16 ? 2 : 4; }
+bool aligned(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
+constexpr int64_t kMaxLd = (int64_t)1 << 40;
+
+e2f_status check_embedding(e2f_ctx* ctx, const e2f_embedding_params* p, int32_t n) {
+  if (!ctx) return fail(E2F_EINVAL, "ctx is NULL");
+  if (!p) return fail(E2F_EINVAL, "params is NULL");
+  if (n < 0) return fail(E2F_EINVAL, "n < 0");
+  if (n > kMaxAtoms) return fail(E2F_EUNSUPPORTED, "n = %d > %d", n, kMaxAtoms);
+  if (p->vocab < 1) return fail(E2F_EINVAL, "vocab = %d < 1", p->vocab);
+  if (p->vocab > kMaxAtoms) return fail(E2F_EUNSUPPORTED, "vocab = %d > %d", p->vocab, kMaxAtoms);
+  if (p->channels < 1) return fail(E2F_EINVAL, "channels = %d < 1", p->channels);
+  if (p->channels > 65536) return fail(E2F_EUNSUPPORTED, "channels = %d > 65536", p->channels);
+  if (p->lmax < 0) return fail(E2F_EINVAL, "lmax = %d < 0", p->lmax);
+  if (p->lmax > kMaxL) return fail(E2F_EUNSUPPORTED, "lmax = %d > %d", p->lmax, kMaxL);
+  if (!std::isfinite(p->scale)) return fail(E2F_EINVAL, "scale must be finite");
+  if (!dtype_ok((int)p->table_dtype) || !dtype_ok((int)p->dtype)) return fail(E2F_EINVAL, "dtype");
+  if (p->index_bytes != 4 && p->index_bytes != 8) return fail(E2F_EINVAL, "index_bytes must be 4 or 8");
+  if (p->ld && p->ld < (int64_t)nk_of(p->lmax) * p->channels) return fail(E2F_EINVAL, "ld is smaller than a row");
+  if (p->ld > kMaxLd) return fail(E2F_EUNSUPPORTED, "ld > 2^40");
+  return E2F_OK;
+}
+
+EmbedArgs embedding_args(const e2f_embedding_params* p, const void* index, int32_t n) {
+  EmbedArgs a{};
+  a.index = index, a.n = n, a.V = p->vocab, a.C = p->channels, a.K = nk_of(p->lmax);
+  a.ld = p->ld ? p->ld : (int64_t)a.K * a.C;
+  a.scale = p->scale, a.wide = p->index_bytes == 8;
+  a.table_bf16 = p->table_dtype == E2F_BF16, a.bf16 = p->dtype == E2F_BF16;
+  return a;
+}
+
+// from the first row to the end of the last one
+size_t rows_bytes(int32_t n, int64_t ld, int64_t row, size_t el) {
+  return n ? el * ((size_t)(n - 1) * (size_t)ld + (size_t)row) : 0;
+}
+
+e2f_status check_layer(e2f_ctx* ctx, const e2f_layer_norm_params* p, int32_t n) {
+  if (!ctx) return fail(E2F_EINVAL, "ctx is NULL");
+  if (!p) return fail(E2F_EINVAL, "params is NULL");
+  if (n < 0) return fail(E2F_EINVAL, "n < 0");
+  if (n > kMaxAtoms) return fail(E2F_EUNSUPPORTED, "n = %d > %d", n, kMaxAtoms);
+  if (p->lmax < 0) return fail(E2F_EINVAL, "lmax = %d < 0", p->lmax);
+  if (p->lmax > kMaxL) return fail(E2F_EUNSUPPORTED, "lmax = %d > %d", p->lmax, kMaxL);
+  if (p->channels < 1) return fail(E2F_EINVAL, "channels = %d < 1", p->channels);
+  if (p->lmax == 0 && p->channels > kLayerMaxRow)
+    return fail(E2F_EUNSUPPORTED, "channels = %d > %d", p->channels, kLayerMaxRow);
+  if (p->lmax > 0 && (p->channels % 4 || p->channels > 1024))
+    return fail(E2F_EUNSUPPORTED, "channels %d must be a multiple of 4 in 4..1024 with lmax > 0", p->channels);
+  if (!std::isfinite(p->eps) || p->eps < 0.0f) return fail(E2F_EINVAL, "eps must be finite and >= 0");
+  if (p->silu != 0 && p->silu != 1) return fail(E2F_EINVAL, "silu must be 0 or 1");
+  if (p->silu && p->lmax) return fail(E2F_EINVAL, "silu needs lmax = 0");
+  if (!dtype_ok((int)p->dtype)) return fail(E2F_EINVAL, "dtype %d", (int)p->dtype);
+  if (p->ldx && p->ldx < (int64_t)nk_of(p->lmax) * p->channels) return fail(E2F_EINVAL, "ldx is smaller than a row");
+  if (p->ldx > kMaxLd) return fail(E2F_EUNSUPPORTED, "ldx > 2^40");
+  return E2F_OK;
+}
+
+LayerArgs layer_args(const e2f_layer_norm_params* p, const void* x, int32_t n) {
+  const int64_t row = (int64_t)nk_of(p->lmax) * p->channels;
+  return {x, p->weight, p->bias, p->ldx ? p->ldx : row, n, p->channels, p->eps, p->silu != 0};
+}
+
+const float kDefaultCoefs[3] = {3.4445f, -4.7750f, 2.0315f};
+struct Coefs {
+  float v[3 * kOrthoMaxSteps];
+};
+
+e2f_status check_orthogonalize(e2f_ctx* ctx, const e2f_orthogonalize_params* p, int32_t count, Coefs* coefs) {
+  if (!ctx) return fail(E2F_EINVAL, "ctx is NULL");
+  if (!p) return fail(E2F_EINVAL, "params is NULL");
+  if (count < 0) return fail(E2F_EINVAL, "count < 0");
+  if (p->rows < 0 || p->cols < 0) return fail(E2F_EINVAL, "rows or cols < 0");
+  if (p->rows > 65536 || p->cols > 65536 || (int64_t)p->rows * p->cols > std::numeric_limits<int32_t>::max())
+    return fail(E2F_EUNSUPPORTED, "matrices of %d x %d", p->rows, p->cols);
+  if (p->steps < 0) return fail(E2F_EINVAL, "steps = %d < 0", p->steps);
+  if (p->steps > kOrthoMaxSteps) return fail(E2F_EUNSUPPORTED, "steps = %d > %d", p->steps, kOrthoMaxSteps);
+  if (!std::isfinite(p->eps) || p->eps < 0.0f) return fail(E2F_EINVAL, "eps must be finite and >= 0");
+  if (!std::isfinite(p->momentum) || !std::isfinite(p->scale) || !std::isfinite(p->decay))
+    return fail(E2F_EINVAL, "momentum, scale and decay must be finite");
+  if (p->nesterov != 0 && p->nesterov != 1) return fail(E2F_EINVAL, "nesterov must be 0 or 1");
+  if (!dtype_ok((int)p->grad_dtype) || !dtype_ok((int)p->dtype)) return fail(E2F_EINVAL, "dtype");
+  for (int k = 0; k < 3 * p->steps; ++k) {
+    coefs->v[k] = p->coefs ? p->coefs[k] : kDefaultCoefs[k % 3];
+    if (!std::isfinite(coefs->v[k])) return fail(E2F_EINVAL, "coefs must be finite");
+  }
+  int x[kOrthoMaxSteps + 1], a[kOrthoMaxSteps], b[kOrthoMaxSteps];
+  if (!ortho_bounds(p->steps, coefs->v, x, a, b))
+    return fail(E2F_EINVAL, "coefs that do not keep the singular values bounded");
+  return E2F_OK;
+}
+
+// No output over another tensor, but over the input of its own number among those that it may replace
+struct TensorArray {
+  const void* const* at;
+  size_t bytes;
+  int replaces;  // which of the inputs' arrays (-1: none)
+};
+e2f_status check_array_overlaps(int32_t count, std::initializer_list<TensorArray> in,
+                                std::initializer_list<TensorArray> out, Span workspace) {
+  struct Range {
+    const char *lo, *hi;
+    int array, index;
+  };
+  try {
+    std::vector<Range> r;
+    int k = 0;
+    for (const TensorArray& o : out) {
+      if (o.at && o.bytes)
+        for (int i = 0; i < count; ++i) r.push_back({(const char*)o.at[i], (const char*)o.at[i] + o.bytes, k, i});
+      ++k;
+    }
+    if (workspace.at && workspace.bytes)
+      r.push_back({(const char*)workspace.at, (const char*)workspace.at + workspace.bytes, -1, -1});
+    auto less = [](const Range& a, const Range& b) { return a.lo < b.lo; };
+    if (!std::is_sorted(r.begin(), r.end(), less)) std::sort(r.begin(), r.end(), less);
+    for (size_t i = 1; i < r.size(); ++i)
+      if (r[i].lo < r[i - 1].hi) return fail(E2F_EINVAL, "two outputs overlap");
+    if (r.empty()) return E2F_OK;
+    int which = 0;
+    for (const TensorArray& a : in) {
+      if (a.at && a.bytes)
+        for (int i = 0; i < count; ++i) {
+          const char *lo = (const char*)a.at[i], *hi = lo + a.bytes;
+          if (hi <= r.front().lo || lo >= r.back().hi) continue;
+          // the outputs are disjoint: the last that begins before the input's end is the one that ends last
+          const auto next = std::lower_bound(r.begin(), r.end(), Range{hi, hi, 0, 0}, less);
+          if (next == r.begin() || (next - 1)->hi <= lo) continue;
+          const Range& o = *(next - 1);
+          if (o.lo == lo && o.hi == hi && o.index == i && o.array >= 0 && (out.begin() + o.array)->replaces == which) continue;
+          return fail(E2F_EINVAL, "an output overlaps an input");
+        }
+      ++which;
+    }
+  } catch (const std::exception&) {
+    return fail(E2F_ENOMEM, "host memory for %d tensors", count);
+  }
+  return E2F_OK;
+}
+
 }  // namespace
 
 e2f_status e2f_transpose_graph_workspace_size(e2f_ctx* ctx, int32_t n, int64_t n_edges, size_t* bytes) {
@@ -1861,6 +2002,174 @@ e2f_status e2f_grad_clip(e2f_ctx* ctx, int32_t count, const void* const* tensors
   hipStream_t s = (hipStream_t)stream;
   DeviceGuard g(ctx->device);
   E2F_TIMED("grad_clip", launch_grad_clip(count, tensors, outs, sizes, dtypes, total, sumsq, max_norm, s));
+  return E2F_OK;
+}
+
+e2f_status e2f_embedding_forward(e2f_ctx* ctx, const e2f_embedding_params* p, const void* table, const void* index,
+                                 int32_t n, void* out, void* stream) {
+  if (e2f_status rs = check_embedding(ctx, p, n); rs != E2F_OK) return rs;
+  if (n > 0 && (!table || !index || !out)) return fail(E2F_EINVAL, "table, index and out are required");
+  const EmbedArgs a = embedding_args(p, index, n);
+  const size_t te = bytes_of(p->table_dtype), oe = bytes_of(p->dtype);
+  if (!aligned(table, te) || !aligned(out, oe) || !aligned(index, p->index_bytes))
+    return fail(E2F_EINVAL, "alignment of an argument");
+  if (e2f_status rs = check_overlaps({{table, n ? te * (size_t)a.V * a.C : 0}, {index, (size_t)p->index_bytes * n}},
+                                     {{out, rows_bytes(n, a.ld, (int64_t)a.K * a.C, oe)}});
+      rs != E2F_OK)
+    return rs;
+  if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
+  if (n == 0) return E2F_OK;
+  hipStream_t s = (hipStream_t)stream;
+  DeviceGuard g(ctx->device);
+  E2F_TIMED("embedding", launch_embed_forward(a, table, out, s));
+  return E2F_OK;
+}
+
+e2f_status e2f_embedding_backward_workspace_size(e2f_ctx* ctx, const e2f_embedding_params* p, int32_t n,
+                                                 size_t* bytes) {
+  if (e2f_status rs = check_embedding(ctx, p, n); rs != E2F_OK) return rs;
+  if (!bytes) return fail(E2F_EINVAL, "bytes is NULL");
+  *bytes = embed_workspace(n, p->vocab, p->channels);
+  return E2F_OK;
+}
+
+e2f_status e2f_embedding_backward(e2f_ctx* ctx, const e2f_embedding_params* p, const void* index, int32_t n,
+                                  const void* grad_out, void* grad_table, void* workspace, size_t workspace_bytes,
+                                  void* stream) {
+  if (e2f_status rs = check_embedding(ctx, p, n); rs != E2F_OK) return rs;
+  if (!grad_table) return fail(E2F_EINVAL, "grad_table is required");
+  if (n > 0 && (!index || !grad_out)) return fail(E2F_EINVAL, "index and grad_out are required");
+  const EmbedArgs a = embedding_args(p, index, n);
+  const size_t te = bytes_of(p->table_dtype), oe = bytes_of(p->dtype);
+  if (!aligned(grad_table, te) || !aligned(grad_out, oe) || !aligned(index, p->index_bytes))
+    return fail(E2F_EINVAL, "alignment of an argument");
+  const size_t need = embed_workspace(n, p->vocab, p->channels);
+  if (e2f_status rs = check_workspace(workspace, workspace_bytes, need); rs != E2F_OK) return rs;
+  if (e2f_status rs = check_overlaps(
+          {{grad_out, rows_bytes(n, a.ld, (int64_t)a.K * a.C, oe)}, {index, (size_t)p->index_bytes * n}},
+          {{grad_table, te * (size_t)a.V * a.C}, {workspace, need}});
+      rs != E2F_OK)
+    return rs;
+  if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
+  hipStream_t s = (hipStream_t)stream;
+  DeviceGuard g(ctx->device);
+  E2F_TIMED("embedding_grad", launch_embed_backward(a, grad_out, grad_table, workspace, s));
+  return E2F_OK;
+}
+
+e2f_status e2f_layer_norm_forward(e2f_ctx* ctx, const e2f_layer_norm_params* p, const void* x, int32_t n, void* out,
+                                  void* stream) {
+  if (e2f_status rs = check_layer(ctx, p, n); rs != E2F_OK) return rs;
+  if (n > 0 && (!x || !out)) return fail(E2F_EINVAL, "x and out are required");
+  const LayerArgs a = layer_args(p, x, n);
+  const size_t el = bytes_of(p->dtype), w = n ? sizeof(float) * p->channels : 0;
+  const int64_t row = (int64_t)nk_of(p->lmax) * p->channels;
+  if (!aligned(x, el) || !aligned(out, el) || !aligned(p->weight, 4) || !aligned(p->bias, 4))
+    return fail(E2F_EINVAL, "alignment of an argument");
+  if (e2f_status rs = check_overlaps({{x, rows_bytes(n, a.ldx, row, el)}, {p->weight, w * (p->lmax + 1)}, {p->bias, w}},
+                                     {{out, el * (size_t)n * row}});
+      rs != E2F_OK)
+    return rs;
+  if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
+  if (n == 0) return E2F_OK;
+  hipStream_t s = (hipStream_t)stream;
+  DeviceGuard g(ctx->device);
+  E2F_TIMED("layer_norm", launch_layer_forward(p->lmax, p->dtype == E2F_BF16, a, out, s));
+  return E2F_OK;
+}
+
+e2f_status e2f_layer_norm_workspace_size(e2f_ctx* ctx, const e2f_layer_norm_params* p, int32_t n, size_t* bytes) {
+  if (e2f_status rs = check_layer(ctx, p, n); rs != E2F_OK) return rs;
+  if (!bytes) return fail(E2F_EINVAL, "bytes is NULL");
+  *bytes = al256(sizeof(float) * (size_t)layer_parts(p->lmax, p->channels, p->dtype == E2F_BF16, n) * (p->lmax + 2) *
+                 p->channels);
+  return E2F_OK;
+}
+
+e2f_status e2f_layer_norm_backward(e2f_ctx* ctx, const e2f_layer_norm_params* p, const void* x, int32_t n,
+                                   const void* grad_out, void* grad_x, float* grad_weight, float* grad_bias,
+                                   void* workspace, size_t workspace_bytes, void* stream) {
+  if (e2f_status rs = check_layer(ctx, p, n); rs != E2F_OK) return rs;
+  if (!grad_x && !grad_weight && !grad_bias) return fail(E2F_EINVAL, "no gradient is requested");
+  if (n > 0 && (!x || !grad_out)) return fail(E2F_EINVAL, "x and grad_out are required");
+  const bool weights = grad_weight || grad_bias;
+  size_t need = 0;
+  if (weights) {
+    if (e2f_status rs = e2f_layer_norm_workspace_size(ctx, p, n, &need); rs != E2F_OK) return rs;
+    if (e2f_status rs = check_workspace(workspace, workspace_bytes, need); rs != E2F_OK) return rs;
+  }
+  const LayerArgs a = layer_args(p, x, n);
+  const size_t el = bytes_of(p->dtype), w = sizeof(float) * p->channels;
+  const int64_t row = (int64_t)nk_of(p->lmax) * p->channels;
+  const size_t all = el * (size_t)n * row;
+  if (!aligned(x, el) || !aligned(grad_out, el) || !aligned(grad_x, el) || !aligned(p->weight, 4) ||
+      !aligned(p->bias, 4) || !aligned(grad_weight, 4) || !aligned(grad_bias, 4))
+    return fail(E2F_EINVAL, "alignment of an argument");
+  if (e2f_status rs = check_overlaps({{x, rows_bytes(n, a.ldx, row, el)}, {grad_out, all},
+                                      {p->weight, w * (p->lmax + 1)}, {p->bias, w}},
+                                     {{grad_x, all}, {grad_weight, w * (p->lmax + 1)}, {grad_bias, w}, {workspace, need}});
+      rs != E2F_OK)
+    return rs;
+  if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
+  hipStream_t s = (hipStream_t)stream;
+  DeviceGuard g(ctx->device);
+  const LayerGrad d{grad_out, grad_x, weights ? (float*)workspace : nullptr, grad_weight, grad_bias};
+  E2F_TIMED("layer_norm_grad", launch_layer_backward(p->lmax, p->dtype == E2F_BF16, a, d, s));
+  return E2F_OK;
+}
+
+e2f_status e2f_orthogonalize_workspace_size(e2f_ctx* ctx, const e2f_orthogonalize_params* p, int32_t count,
+                                            size_t* bytes) {
+  Coefs coefs;
+  if (e2f_status rs = check_orthogonalize(ctx, p, count, &coefs); rs != E2F_OK) return rs;
+  if (!bytes) return fail(E2F_EINVAL, "bytes is NULL");
+  *bytes = p->rows && p->cols && count ? ortho_workspace(p->rows, p->cols, count) : 0;
+  return E2F_OK;
+}
+
+e2f_status e2f_orthogonalize(e2f_ctx* ctx, const e2f_orthogonalize_params* p, int32_t count,
+                             const void* const* grads, const float* const* moments, float* const* new_moments,
+                             const void* const* weights, void* const* outs, void* workspace, size_t workspace_bytes,
+                             void* stream) {
+  Coefs coefs;
+  if (e2f_status rs = check_orthogonalize(ctx, p, count, &coefs); rs != E2F_OK) return rs;
+  const size_t size = (size_t)p->rows * p->cols;
+  const bool any = count > 0 && size > 0;
+  if (any && (!grads || !outs)) return fail(E2F_EINVAL, "grads and outs are required");
+  if (any && (moments != nullptr) != (new_moments != nullptr))
+    return fail(E2F_EINVAL, "moments and new_moments go together");
+  if (any && !weights && p->decay != 0.0f) return fail(E2F_EINVAL, "weights are required with decay");
+  const size_t ge = bytes_of(p->grad_dtype), we = bytes_of(p->dtype);
+  const void* const* w = p->decay != 0.0f ? weights : nullptr;
+  if (any) {
+    const struct {
+      const void* const* at;
+      size_t el;
+      const char* name;
+    } arrays[] = {{grads, ge, "grads"}, {(const void* const*)moments, 4, "moments"},
+                  {(const void* const*)new_moments, 4, "new_moments"}, {w, we, "weights"},
+                  {(const void* const*)outs, we, "outs"}};
+    for (const auto& a : arrays)
+      for (int i = 0; a.at && i < count; ++i)
+        if (!a.at[i] || !aligned(a.at[i], a.el)) return fail(E2F_EINVAL, "%s[%d] is NULL or not aligned", a.name, i);
+    const size_t need = ortho_workspace(p->rows, p->cols, count);
+    if (e2f_status rs = check_workspace(workspace, workspace_bytes, need); rs != E2F_OK) return rs;
+    if (e2f_status rs = check_array_overlaps(
+            count, {{grads, size * ge, -1}, {(const void* const*)moments, size * 4, -1}, {w, size * we, -1}},
+            {{(const void* const*)new_moments, size * 4, 1}, {(const void* const*)outs, size * we, 2}}, {workspace, need});
+        rs != E2F_OK)
+      return rs;
+  }
+  if (ctx->device < 0) return fail(E2F_EDEVICE, "context has no device");
+  if (!any) return E2F_OK;
+  OrthoArgs a{};
+  a.rows = p->rows, a.cols = p->cols, a.steps = p->steps, a.count = count;
+  a.grads = grads, a.moments = moments, a.news = new_moments, a.weights = w, a.outs = outs, a.coef = coefs.v;
+  a.eps = p->eps, a.mu = p->momentum, a.scale = p->scale, a.decay = p->decay;
+  a.nesterov = p->nesterov != 0, a.grad_bf16 = p->grad_dtype == E2F_BF16, a.bf16 = p->dtype == E2F_BF16;
+  hipStream_t s = (hipStream_t)stream;
+  DeviceGuard g(ctx->device);
+  E2F_TIMED("orthogonalize", launch_orthogonalize(a, workspace, s));
   return E2F_OK;
 }
 

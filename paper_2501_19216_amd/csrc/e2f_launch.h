@@ -1,5 +1,6 @@
 // Kernel launchers of libe2f (implemented in neighbor.hip, plan.hip, conv.hip,
-// attention.hip, graph_attention.hip, block_norm.hip and grad_clip.hip).
+// attention.hip, graph_attention.hip, block_norm.hip, layer_norm.hip, embedding.hip,
+// orthogonalize.hip and grad_clip.hip).
 // All sizes are checked by the callers in abi.cpp before these run.
 #pragma once
 
@@ -265,6 +266,58 @@ hipError_t launch_grad_norm(int count, const void* const* in, const int64_t* n, 
                             double* part, double* sumsq, float* norm, hipStream_t s);
 hipError_t launch_grad_clip(int count, const void* const* in, void* const* out, const int64_t* n,
                             const int32_t* dtype, int64_t total, const double* sumsq, float max_norm, hipStream_t s);
+
+// ---- layer norm of irrep features and of rows (layer_norm.hip)
+struct LayerArgs {
+  const void* x;      // row i from x + i ldx on
+  const float *w, *b; // [L + 1][C], [C], or NULL
+  int64_t ldx;
+  int n, C;
+  float eps;
+  bool silu;          // (L = 0)
+};
+struct LayerGrad {
+  const void* gout;
+  void* gx;
+  float* part;  // [layer_parts][L + 2][C]
+  float *gw, *gb;
+};
+constexpr int kLayerMaxRow = 8192;  // channels with L = 0
+int layer_parts(int L, int C, bool bf16, int n);
+hipError_t launch_layer_forward(int L, bool bf16, const LayerArgs& a, void* out, hipStream_t s);
+hipError_t launch_layer_backward(int L, bool bf16, const LayerArgs& a, const LayerGrad& g, hipStream_t s);
+
+// ---- rows of a table by their types, and the table's gradient (embedding.hip)
+struct EmbedArgs {
+  const void* index;  // int32 or int64
+  int64_t ld;         // elements between rows of out or of its gradient
+  int n, V, C, K;
+  float scale;
+  bool wide, table_bf16, bf16;
+};
+size_t embed_workspace(int n, int V, int C);
+hipError_t launch_embed_forward(const EmbedArgs& a, const void* table, void* out, hipStream_t s);
+hipError_t launch_embed_backward(const EmbedArgs& a, const void* gout, void* gtable, void* workspace, hipStream_t s);
+
+// ---- orthogonalised updates of matrices (orthogonalize.hip)
+struct OrthoArgs {
+  int rows, cols, steps, count;
+  const void* const* grads;  // host arrays of `count` addresses
+  const float* const* moments;  // or NULL
+  float* const* news;
+  const void* const* weights;   // or NULL
+  void* const* outs;
+  const float* coef;  // host [steps][3]
+  float eps, mu, scale, decay;
+  bool nesterov, grad_bf16, bf16;
+};
+// Bounds of the singular values before each step and of the polynomial's matrix, as the exponents of two by which the
+// matrices are scaled; false where the steps do not keep them bounded
+bool ortho_bounds(int steps, const float* coef, int* x_exp, int* a_exp, int* b_exp);
+constexpr int kOrthoMaxSteps = 64;
+int ortho_batch(int rows, int cols, int count);  // matrices at a time
+size_t ortho_workspace(int rows, int cols, int count);
+hipError_t launch_orthogonalize(const OrthoArgs& a, void* workspace, hipStream_t s);
 
 // ---- backward
 // Both per-edge backward products of the edges lo .. hi - 1 (either output may

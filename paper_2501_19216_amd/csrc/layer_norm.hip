@@ -1,0 +1,454 @@
+// The layer norm of irrep features [N][(L+1)^2][C]: the scalars by their mean and variance over the channels, all
+// higher degrees by one root mean square that rotations leave alone; one component is the plain layer norm of rows,
+// with the activation of a radial network behind it:
+//   m = mean_c x_0,  r0 = 1 / sqrt(mean_c (x_0 - m)^2 + eps),  h = (x_0 - m) r0,
+//   z = w_0 h + b,   y_0 = z, or z sigma(z),
+//   r1 = 1 / sqrt(mean over l >= 1 of the mean over (m, c) of x_l^2, plus eps),   y_l = w_l x_l r1,
+// and the gradients, with a_l = 1 / (L (2l+1) C) and g the gradient of y:
+//   dz = g_0, or g_0 sigma(z) (1 + z (1 - sigma(z))),   u = w_0 dz,
+//   dx_0 = r0 (u - mean u - h mean(u h)),   dw_0 = sum of dz h,   db = sum of dz  over the atoms,
+//   dx_l = r1 u_l - r1^3 a_l x_l (sum of u x),  u_l = w_l g_l,   dw_l = sum of g x r1 over (atom, m).
+// Every value is read once and written once.  A row stays in registers between its reductions; the variance is taken of the
+// differences from the mean, so that rows far from zero keep their digits.  The backward takes the row's statistics from x
+// again, which it reads anyway: nothing is kept from the forward.  Sums, statistics and everything between loads
+// and stores are float; outputs are rounded once.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "e2f_launch.h"
+#include "values.h"
+#include "wave.h"
+
+namespace e2f {
+namespace {
+
+// Sums of N values over the `tpr` threads of a row (a power of two, up to eight waves)
+template <int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], int tpr, float (*red)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = lanes_sum(v[i], tpr);
+  if (tpr <= 64) return;
+  const int wave = threadIdx.x >> 6, per = tpr >> 6, w0 = wave / per * per;
+  __syncthreads();  // (the sums before have been read)
+  if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) red[wave][i] = v[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = 0.0f;
+  for (int w = w0; w < w0 + per; ++w)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += red[w][i];
+}
+
+__device__ __forceinline__ float sigmoid(float x) {
+  const float e = expf(-fabsf(x));
+  return (x < 0.0f ? e : 1.0f) / (1.0f + e);
+}
+
+// Where a thread's values lie: V neighbouring channels of each of S pieces, which are the components (L > 0), or
+// stretches of tpr V channels of a row (L = 0), the last of them cut where the row ends.  The first S0 pieces hold
+// scalars; W sets of weights
+template <int L, int V, int J>
+struct Place {
+  static constexpr int S = L ? (L + 1) * (L + 1) : J, S0 = L ? 1 : J, W = L ? L + 1 : J;
+  int C, t, tpr;
+  __device__ __forceinline__ int channel(int s) const { return L ? t * V : (s * tpr + t) * V; }
+  __device__ __forceinline__ int offset(int s) const { return L ? s * C + t * V : (s * tpr + t) * V; }
+  // (weights: of a degree, of a stretch)
+  __device__ __forceinline__ int weight(int i) const { return L ? i * C + t * V : (i * tpr + t) * V; }
+};
+
+// The thread's values of a row as they are stored; what lies behind the row's end is zero
+template <typename T, int L, int V, int J, bool TAIL>
+struct Row {
+  typedef Place<L, V, J> P;
+  typename Raw<T, V>::type v[P::S];
+  float end[V];  // (TAIL: the values of the piece that the row's end cuts)
+  __device__ __forceinline__ void load(const T* p, const P& at) {
+#pragma unroll
+    for (int s = 0; s < P::S; ++s)
+      v[s] = at.channel(s) + V <= at.C ? Raw<T, V>::load((const char*)(p + at.offset(s))) : typename Raw<T, V>::type{};
+    if constexpr (TAIL) {
+      const int c = at.C / V * V;
+      if (c / V % at.tpr == at.t)
+#pragma unroll
+        for (int u = 0; u < V; ++u) end[u] = c + u < at.C ? part(Raw<T, 1>::load((const char*)(p + c + u)), 0) : 0.0f;
+    }
+  }
+  __device__ __forceinline__ void values(const P& at, float (&f)[P::S][V]) const {
+#pragma unroll
+    for (int s = 0; s < P::S; ++s) {
+      const bool cut = TAIL && at.channel(s) < at.C && at.channel(s) + V > at.C;
+#pragma unroll
+      for (int u = 0; u < V; ++u) f[s][u] = cut ? end[u] : part(v[s], u);
+    }
+  }
+};
+template <typename T, int L, int V, int J, bool TAIL>
+__device__ __forceinline__ void write_row(T* p, const Place<L, V, J>& at, const float (&f)[Place<L, V, J>::S][V]) {
+#pragma unroll
+  for (int s = 0; s < Place<L, V, J>::S; ++s) {
+    const int c = at.channel(s);
+    if (c + V <= at.C) {
+      typename Raw<T, V>::type v;
+      join(f[s], v);
+      Raw<T, V>::store((char*)(p + at.offset(s)), v);
+    } else if constexpr (TAIL) {
+#pragma unroll
+      for (int u = 0; u < V; ++u)
+        if (c + u < at.C) {
+          typename Raw<T, 1>::type v;
+          join(&f[s][u], v);
+          Raw<T, 1>::store((char*)(p + c + u), v);
+        }
+    }
+  }
+}
+
+// N sets of the thread's weights (`none` where there are none, 0 behind the row's end)
+template <int N, int L, int V, int J>
+__device__ __forceinline__ void read_weights(const float* w, float none, const Place<L, V, J>& at, float (&f)[N][V]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int u = 0; u < V; ++u)
+      f[i][u] = at.channel(i) + u >= at.C ? 0.0f : w ? w[at.weight(i) + u] : none;
+}
+
+// f(s, l) for the components above the scalars, of degree l, and end(l) after each degree
+template <int L, typename F, typename G>
+__device__ __forceinline__ void each_higher(F&& f, G&& end) {
+  each<L>([&](auto i) {
+    constexpr int l = i + 1;
+    each<2 * l + 1>([&](auto m) { f(l * l + m, l); });
+    end(l);
+  });
+}
+
+// The scalars' mean off them (0 behind the row's end)
+template <int L, int V, int J>
+__device__ __forceinline__ void centre(const Place<L, V, J>& at, float mean, float (&x)[Place<L, V, J>::S][V]) {
+#pragma unroll
+  for (int s = 0; s < Place<L, V, J>::S0; ++s)
+#pragma unroll
+    for (int u = 0; u < V; ++u) x[s][u] = at.channel(s) + u < at.C ? x[s][u] - mean : 0.0f;
+}
+
+template <int L, typename T, int V, int J, bool SILU, bool TAIL>
+__global__ __launch_bounds__(512) void k_layer_forward(LayerArgs a, int tpr, T* out) {
+  typedef Place<L, V, J> P;
+  __shared__ float red1[8][L ? 2 : 1], red2[8][1];
+  const int slot = threadIdx.x / tpr, slots = blockDim.x / tpr;
+  const int64_t first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * slots;
+  if (first >= a.n) return;  // (the last round's)
+  const int64_t row = min(first + slot, (int64_t)a.n - 1);
+  const P at{a.C, (int)threadIdx.x % tpr, tpr};
+  Row<T, L, V, J, TAIL> in;
+  in.load((const T*)a.x + row * a.ldx, at);
+  float x[P::S][V], w[P::W][V], b[P::S0][V];
+  read_weights(a.w, 1.0f, at, w);
+  read_weights(a.b, 0.0f, at, b);
+  in.values(at, x);
+  const float per = 1.0f / (float)a.C;
+  float s1[L ? 2 : 1] = {}, s2[1] = {}, t = 0.0f;
+#pragma unroll
+  for (int s = 0; s < P::S0; ++s)
+#pragma unroll
+    for (int u = 0; u < V; ++u) s1[0] += x[s][u];
+  each_higher<L>(
+      [&](int s, int) {
+#pragma unroll
+        for (int u = 0; u < V; ++u) t += x[s][u] * x[s][u];
+      },
+      [&](int l) { s1[L ? 1 : 0] += t * (1.0f / (2 * l + 1)), t = 0.0f; });
+  row_sums(s1, tpr, red1);
+  centre(at, s1[0] * per, x);
+#pragma unroll
+  for (int s = 0; s < P::S0; ++s)
+#pragma unroll
+    for (int u = 0; u < V; ++u) s2[0] += x[s][u] * x[s][u];
+  row_sums(s2, tpr, red2);
+  const float r0 = 1.0f / sqrtf(s2[0] * per + a.eps);
+#pragma unroll
+  for (int s = 0; s < P::S0; ++s)
+#pragma unroll
+    for (int u = 0; u < V; ++u) {
+      const float z = x[s][u] * r0 * w[s][u] + b[s][u];
+      x[s][u] = SILU ? z * sigmoid(z) : z;
+    }
+  if constexpr (L > 0) {
+    const float r1 = 1.0f / sqrtf(s1[1] * per * (1.0f / L) + a.eps);
+    each_higher<L>(
+        [&](int s, int l) {
+#pragma unroll
+          for (int u = 0; u < V; ++u) x[s][u] *= r1 * w[l][u];
+        },
+        [](int) {});
+  }
+  if (first + slot < a.n) write_row<T, L, V, J, TAIL>(out + row * (int64_t)(L ? P::S : 1) * a.C, at, x);
+}
+
+template <int L, typename T, int V, int J, bool SILU, bool TAIL>
+__global__ __launch_bounds__(512) void k_layer_backward(LayerArgs a, LayerGrad g, int tpr) {
+  typedef Place<L, V, J> P;
+  constexpr int N1 = L ? 3 : 1, N2 = SILU ? 1 : 3;
+  extern __shared__ float sums[];  // [W C + C], with more than one wave's rows a workgroup
+  __shared__ float red1[8][N1], red2[8][N2], red3[8][2];
+  const int slot = threadIdx.x / tpr, slots = blockDim.x / tpr;
+  const P at{a.C, (int)threadIdx.x % tpr, tpr};
+  const float per = 1.0f / (float)a.C;
+  float w[P::W][V], b[P::S0][V], aw[P::W][V] = {}, ab[P::S0][V] = {};
+  read_weights(a.w, 1.0f, at, w);
+  if constexpr (SILU) read_weights(a.b, 0.0f, at, b);
+  for (int64_t first = (int64_t)blockIdx.x * slots; first < a.n; first += (int64_t)gridDim.x * slots) {
+    const int64_t row = min(first + slot, (int64_t)a.n - 1), packed = row * (L ? P::S : 1) * a.C;
+    const bool on = first + slot < a.n;
+    Row<T, L, V, J, TAIL> in, gin;
+    in.load((const T*)a.x + row * a.ldx, at);
+    gin.load((const T*)g.gout + packed, at);
+    float x[P::S][V], d[P::S][V];
+    in.values(at, x);
+    gin.values(at, d);
+    float s1[N1] = {}, s2[N2] = {}, s3[2] = {}, t = 0.0f, v[V] = {};
+#pragma unroll
+    for (int s = 0; s < P::S0; ++s)
+#pragma unroll
+      for (int u = 0; u < V; ++u) s1[0] += x[s][u];
+    if constexpr (L > 0) {
+      float gx[P::W][V];  // sum over a degree's components of g x
+      each_higher<L>(
+          [&](int s, int) {
+#pragma unroll
+            for (int u = 0; u < V; ++u) t += x[s][u] * x[s][u], v[u] += d[s][u] * x[s][u];
+          },
+          [&](int l) {
+            s1[N1 > 1 ? 1 : 0] += t * (1.0f / (2 * l + 1)), t = 0.0f;
+#pragma unroll
+            for (int u = 0; u < V; ++u) s1[N1 - 1] += w[l][u] * v[u], gx[l][u] = v[u], v[u] = 0.0f;
+          });
+      row_sums(s1, tpr, red1);
+      const float r1 = 1.0f / sqrtf(s1[N1 > 1 ? 1 : 0] * per * (1.0f / (L ? L : 1)) + a.eps);
+      const float back = r1 * r1 * r1 * per * (1.0f / (L ? L : 1)) * s1[N1 - 1];
+      each_higher<L>(
+          [&](int s, int l) {
+#pragma unroll
+            for (int u = 0; u < V; ++u) d[s][u] = r1 * w[l][u] * d[s][u] - back * (1.0f / (2 * l + 1)) * x[s][u];
+          },
+          [&](int l) {
+#pragma unroll
+            for (int u = 0; u < V; ++u) aw[l][u] += on ? r1 * gx[l][u] : 0.0f;
+          });
+    } else {
+      row_sums(s1, tpr, red1);
+    }
+    centre(at, s1[0] * per, x);
+    // without an activation u needs no statistics: its sums go along with the variance's
+#pragma unroll
+    for (int s = 0; s < P::S0; ++s)
+#pragma unroll
+      for (int u = 0; u < V; ++u) {
+        s2[0] += x[s][u] * x[s][u];
+        if constexpr (!SILU) {
+          s2[N2 > 1 ? 1 : 0] += w[s][u] * d[s][u];
+          s2[N2 - 1] += w[s][u] * d[s][u] * x[s][u];
+        }
+      }
+    row_sums(s2, tpr, red2);
+    const float r0 = 1.0f / sqrtf(s2[0] * per + a.eps);
+    if constexpr (SILU) {
+#pragma unroll
+      for (int s = 0; s < P::S0; ++s)
+#pragma unroll
+        for (int u = 0; u < V; ++u) {
+          const float z = x[s][u] * r0 * w[s][u] + b[s][u], q = sigmoid(z);
+          d[s][u] *= q * (1.0f + z * (1.0f - q));
+          s3[0] += w[s][u] * d[s][u];
+          s3[1] += w[s][u] * d[s][u] * x[s][u];
+        }
+      row_sums(s3, tpr, red3);
+    } else {
+      s3[0] = s2[N2 > 1 ? 1 : 0], s3[1] = s2[N2 - 1];
+    }
+    const float mu = s3[0] * per, mh = s3[1] * per * r0;  // means of u and of u h
+#pragma unroll
+    for (int s = 0; s < P::S0; ++s)
+#pragma unroll
+      for (int u = 0; u < V; ++u) {
+        const float h = x[s][u] * r0, dz = d[s][u];
+        aw[s][u] += on ? dz * h : 0.0f;
+        ab[s][u] += on ? dz : 0.0f;
+        d[s][u] = r0 * (w[s][u] * dz - mu - h * mh);
+      }
+    if (on && g.gx) write_row<T, L, V, J, TAIL>((T*)g.gx + packed, at, d);
+  }
+  if (!g.part) return;
+  // the rows of a wave together, then the waves one after the other
+  const int width = (P::W > P::S0 ? (L + 1) * a.C : a.C);  // all weights, before the biases
+  float* mine_at = g.part + (int64_t)blockIdx.x * (width + a.C);
+  if (tpr < 64) {
+#pragma unroll
+    for (int i = 0; i < P::W; ++i)
+#pragma unroll
+      for (int u = 0; u < V; ++u) aw[i][u] = classes_all(aw[i][u], tpr, [](float p, float q) { return p + q; });
+#pragma unroll
+    for (int i = 0; i < P::S0; ++i)
+#pragma unroll
+      for (int u = 0; u < V; ++u) ab[i][u] = classes_all(ab[i][u], tpr, [](float p, float q) { return p + q; });
+  }
+  const int tpg = tpr < 64 ? 64 : tpr, group = threadIdx.x / tpg, groups = blockDim.x / tpg;
+  const bool one = threadIdx.x % tpg < tpr;  // one of the threads that hold the same sums
+  auto add = [&](int k, int at_, float s) {
+    s += k ? sums[at_] : 0.0f;
+    if (k + 1 < groups)
+      sums[at_] = s;
+    else
+      mine_at[at_] = s;
+  };
+  for (int k = 0; k < groups; ++k) {
+    if (groups > 1) __syncthreads();
+    if (k != group || !one) continue;
+#pragma unroll
+    for (int i = 0; i < P::W; ++i)
+#pragma unroll
+      for (int u = 0; u < V; ++u)
+        if (at.channel(i) + u < a.C) add(k, at.weight(i) + u, aw[i][u]);
+#pragma unroll
+    for (int i = 0; i < P::S0; ++i)
+#pragma unroll
+      for (int u = 0; u < V; ++u)
+        if (at.channel(i) + u < a.C) add(k, width + at.channel(i) + u, ab[i][u]);
+  }
+}
+
+// The weights' gradients from the workgroups' sums: 32 columns a workgroup
+__global__ __launch_bounds__(1024) void k_layer_weights(const float* __restrict__ part, int parts, int weights, int count,
+                                                        float* __restrict__ gw, float* __restrict__ gb) {
+  __shared__ double red[32][33];
+  const int c = blockIdx.x * 32 + (threadIdx.x & 31), s = threadIdx.x >> 5;
+  double v = 0.0;
+  if (c < count)
+    for (int b = s; b < parts; b += 32) v += part[(int64_t)b * count + c];
+  red[s][threadIdx.x & 31] = v;
+  __syncthreads();
+  if (s || c >= count) return;
+  for (int k = 1; k < 32; ++k) v += red[k][threadIdx.x];
+  if (c < weights) {
+    if (gw) gw[c] = (float)v;
+  } else if (gb) {
+    gb[c - weights] = (float)v;
+  }
+}
+
+struct Shape {
+  int V, J, tpr, threads;
+  bool tail;
+};
+// Channels of a thread: 16 bytes of plain rows in the forward and four values in the backward, as many pieces as a row
+// needs beyond a wave; of irrep features as many as keep a row's components in its registers
+Shape shape_of(int L, int C, bool bf16, bool back) {
+  Shape s{};
+  if (L) {
+    s.V = L <= 1 ? 4 : L <= 3 ? 2 : C > 512 ? 2 : 1;
+    s.J = 1;
+    s.tpr = 1;
+    while (s.tpr * s.V < C) s.tpr <<= 1;
+  } else {
+    s.V = bf16 && !back ? 8 : 4;
+    const int pieces = (C + s.V - 1) / s.V;
+    s.tpr = 1, s.J = 1;
+    while (s.tpr < 64 && s.tpr < pieces) s.tpr <<= 1;
+    while (s.tpr * s.J < pieces)
+      if (s.J < 2 || s.tpr == 512)
+        s.J <<= 1;
+      else
+        s.tpr <<= 1;
+    s.tail = C % s.V != 0;
+  }
+  s.threads = s.tpr <= 256 ? 256 : s.tpr;
+  return s;
+}
+
+}  // namespace
+
+int layer_parts(int L, int C, bool bf16, int n) {
+  const Shape s = shape_of(L, C, bf16, true);
+  const int slots = s.threads / s.tpr;
+  const int64_t want = ((int64_t)n + slots - 1) / slots, most = 512;
+  return (int)(want < most ? want : most);
+}
+
+// the kernel for the degree, type, size, activation and end: E2F_LAYER(L, T, V, J, silu, tail)
+#define E2F_LAYER_J(T, VV, JJ)                                            \
+  case JJ:                                                                \
+    if (a.silu) {                                                         \
+      if (s.tail) E2F_LAYER(0, T, VV, JJ, true, true);                    \
+      else E2F_LAYER(0, T, VV, JJ, true, false);                          \
+    } else {                                                              \
+      if (s.tail) E2F_LAYER(0, T, VV, JJ, false, true);                   \
+      else E2F_LAYER(0, T, VV, JJ, false, false);                         \
+    }                                                                     \
+    break;
+#define E2F_LAYER_L(LL, VV)                                               \
+  case LL:                                                                \
+    if (bf16) E2F_LAYER(LL, bf16_t, VV, 1, false, false);                 \
+    else E2F_LAYER(LL, float, VV, 1, false, false);                       \
+    break;
+#define E2F_LAYER_M(LL)                                                   \
+  case LL:                                                                \
+    if (s.V == 2) {                                                       \
+      if (bf16) E2F_LAYER(LL, bf16_t, 2, 1, false, false);                \
+      else E2F_LAYER(LL, float, 2, 1, false, false);                      \
+    } else {                                                              \
+      if (bf16) E2F_LAYER(LL, bf16_t, 1, 1, false, false);                \
+      else E2F_LAYER(LL, float, 1, 1, false, false);                      \
+    }                                                                     \
+    break;
+#define E2F_LAYER_SWITCH(VB)                                              \
+  if (L == 0 && bf16) {                                                   \
+    switch (s.J) {                                                        \
+      E2F_LAYER_J(bf16_t, VB, 1) E2F_LAYER_J(bf16_t, VB, 2) E2F_LAYER_J(bf16_t, VB, 4) \
+      default: return hipErrorInvalidValue;                               \
+    }                                                                     \
+  } else if (L == 0) {                                                    \
+    switch (s.J) {                                                        \
+      E2F_LAYER_J(float, 4, 1) E2F_LAYER_J(float, 4, 2) E2F_LAYER_J(float, 4, 4) \
+      default: return hipErrorInvalidValue;                               \
+    }                                                                     \
+  } else {                                                                \
+    switch (L) {                                                          \
+      E2F_LAYER_L(1, 4) E2F_LAYER_L(2, 2) E2F_LAYER_L(3, 2) E2F_LAYER_M(4) E2F_LAYER_M(5) E2F_LAYER_M(6) \
+      default: return hipErrorInvalidValue;                               \
+    }                                                                     \
+  }
+
+hipError_t launch_layer_forward(int L, bool bf16, const LayerArgs& a, void* out, hipStream_t st) {
+  if (a.n == 0) return hipSuccess;
+  const Shape s = shape_of(L, a.C, bf16, false);
+  const int slots = s.threads / s.tpr;
+  const Rounds r = rounds_of(((int64_t)a.n + slots - 1) / slots, s.threads);
+  const dim3 grid(r.x, r.rounds);
+#define E2F_LAYER(LL, T, VV, JJ, A, E) k_layer_forward<LL, T, VV, JJ, A, E><<<grid, s.threads, 0, st>>>(a, s.tpr, (T*)out)
+  E2F_LAYER_SWITCH(8)
+#undef E2F_LAYER
+  return hipGetLastError();
+}
+
+hipError_t launch_layer_backward(int L, bool bf16, const LayerArgs& a, const LayerGrad& g, hipStream_t st) {
+  const int weights = (L + 1) * a.C, count = weights + a.C, parts = a.n ? layer_parts(L, a.C, bf16, a.n) : 0;
+  if (a.n) {
+    const Shape s = shape_of(L, a.C, bf16, true);
+    const size_t lds = g.part && s.threads > s.tpr ? sizeof(float) * count : 0;
+#define E2F_LAYER(LL, T, VV, JJ, A, E) k_layer_backward<LL, T, VV, JJ, A, E><<<parts, s.threads, lds, st>>>(a, g, s.tpr)
+    E2F_LAYER_SWITCH(4)
+#undef E2F_LAYER
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (g.gw || g.gb) k_layer_weights<<<(count + 31) / 32, 1024, 0, st>>>(g.part, parts, weights, count, g.gw, g.gb);
+  return hipGetLastError();
+}
+
+}  // namespace e2f
