@@ -2029,7 +2029,7 @@ e2f_status e2f_embedding_backward_workspace_size(e2f_ctx* ctx, const e2f_embeddi
                                                  size_t* bytes) {
   if (e2f_status rs = check_embedding(ctx, p, n); rs != E2F_OK) return rs;
   if (!bytes) return fail(E2F_EINVAL, "bytes is NULL");
-  *bytes = embed_workspace(n, p->vocab, p->channels);
+  *bytes = embed_workspace(n, p->vocab, p->channels, p->dtype == E2F_BF16);
   return E2F_OK;
 }
 
@@ -2043,7 +2043,7 @@ e2f_status e2f_embedding_backward(e2f_ctx* ctx, const e2f_embedding_params* p, c
   const size_t te = bytes_of(p->table_dtype), oe = bytes_of(p->dtype);
   if (!aligned(grad_table, te) || !aligned(grad_out, oe) || !aligned(index, p->index_bytes))
     return fail(E2F_EINVAL, "alignment of an argument");
-  const size_t need = embed_workspace(n, p->vocab, p->channels);
+  const size_t need = embed_workspace(n, p->vocab, p->channels, p->dtype == E2F_BF16);
   if (e2f_status rs = check_workspace(workspace, workspace_bytes, need); rs != E2F_OK) return rs;
   if (e2f_status rs = check_overlaps(
           {{grad_out, rows_bytes(n, a.ld, (int64_t)a.K * a.C, oe)}, {index, (size_t)p->index_bytes * n}},

@@ -295,7 +295,7 @@ struct EmbedArgs {
   float scale;
   bool wide, table_bf16, bf16;
 };
-size_t embed_workspace(int n, int V, int C);
+size_t embed_workspace(int n, int V, int C, bool bf16);  // (bf16: of the rows' gradient)
 hipError_t launch_embed_forward(const EmbedArgs& a, const void* table, void* out, hipStream_t s);
 hipError_t launch_embed_backward(const EmbedArgs& a, const void* gout, void* gtable, void* workspace, hipStream_t s);
 

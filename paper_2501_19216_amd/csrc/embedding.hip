@@ -22,32 +22,59 @@ __device__ __forceinline__ int type_of(const void* index, int64_t i, int V) {
   return z >= 0 && z < (I)V ? (int)z : V;
 }
 
-// ------------------------------------------------------------------ forward
-// tpr threads a row, each V neighbouring values at a time (V divides C: a row's scalars end between two of them)
-template <typename TT, typename T, typename I, int V>
-__global__ __launch_bounds__(256) void k_embed(EmbedArgs a, const TT* __restrict__ table, T* __restrict__ out, int tpr) {
-  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (256 / tpr) + threadIdx.x / tpr;
-  if (row >= a.n) return;
-  const int z = type_of<I>(a.index, row, a.V);
-  T* to = out + row * a.ld;
-  const TT* from = table + (int64_t)z * a.C;
-  const int all = a.K * a.C, scalars = z < a.V ? a.C : 0;
-  for (int o = threadIdx.x % tpr * V; o < all; o += tpr * V) {
-    float f[V] = {};
-    if (o < scalars) {
-      const auto v = Raw<TT, V>::load((const char*)(from + o));
+// V neighbouring values, in pieces of up to 16 bytes
+template <typename T, int V>
+__device__ __forceinline__ void read_values(const T* p, float (&f)[V]) {
+  constexpr int Q = V * sizeof(T) > 16 ? 16 / sizeof(T) : V;
 #pragma unroll
-      for (int u = 0; u < V; ++u) f[u] = part(v, u) * a.scale;
+  for (int u = 0; u < V; u += Q) {
+    const auto v = Raw<T, Q>::load((const char*)(p + u));
+#pragma unroll
+    for (int k = 0; k < Q; ++k) f[u + k] = part(v, k);
+  }
+}
+template <typename T, int V>
+__device__ __forceinline__ void write_values(T* p, const float (&f)[V]) {
+  constexpr int Q = V * sizeof(T) > 16 ? 16 / sizeof(T) : V;
+#pragma unroll
+  for (int u = 0; u < V; u += Q) {
+    typename Raw<T, Q>::type v;
+    join(f + u, v);
+    Raw<T, Q>::store((char*)(p + u), v);
+  }
+}
+
+// ------------------------------------------------------------------ forward
+// tpr threads a row, each V neighbouring values at a time (V divides C: a row's scalars end between two of them); R
+// rows of a thread, side by side with the others' rows, all their loads in flight together
+template <typename TT, typename T, typename I, int V, int R>
+__global__ __launch_bounds__(256) void k_embed(EmbedArgs a, const TT* __restrict__ table, T* __restrict__ out, int tpr) {
+  const int slots = 256 / tpr, all = a.K * a.C;
+  const int64_t first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (slots * R) + threadIdx.x / tpr;
+  int z[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int64_t row = first + r * slots;
+    z[r] = row < a.n ? type_of<I>(a.index, row, a.V) : a.V;
+  }
+  for (int o = threadIdx.x % tpr * V; o < all; o += tpr * V) {
+    float f[R][V] = {};
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (o < a.C && z[r] < a.V) read_values(table + (int64_t)z[r] * a.C + o, f[r]);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t row = first + r * slots;
+      if (row >= a.n) continue;
+#pragma unroll
+      for (int u = 0; u < V; ++u) f[r][u] *= a.scale;
+      write_values(out + row * a.ld + o, f[r]);
     }
-    typename Raw<T, V>::type v;
-    join(f, v);
-    Raw<T, V>::store((char*)(to + o), v);
   }
 }
 
 // ------------------------------------------------------------------ rows by type
-constexpr int kSegments = 1024;  // waves that sort, at most: each a stretch of neighbouring rows
-constexpr int kSmall = 8192;     // rows that one workgroup sorts
+constexpr int kSmall = 8192;  // rows that one workgroup sorts
 
 // what lanes of this wave wrote to the LDS is there for its other lanes
 __device__ __forceinline__ void wave_sync() {
@@ -69,28 +96,34 @@ __device__ __forceinline__ int below(uint64_t m) {
   return __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0));
 }
 
-// Numbers of each digit in each wave's rows: counts [256][segments].  The first pass also clears the types' first rows
-template <typename I>
+// A workgroup's rows: R rounds of 64 for each of its four waves, neighbouring ones.  The type of lane's row of round r
+template <typename I, int R>
+__device__ __forceinline__ void read_types(const void* index, const int* keys, int n, int V, int64_t lo, int (&key)[R]) {
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int64_t at = min(lo + r * 64 + (threadIdx.x & 63), (int64_t)n - 1);
+    key[r] = keys ? keys[at] : type_of<I>(index, at, V);
+  }
+}
+
+// Numbers of each digit in each workgroup's rows: counts [256][workgroups].  The first pass also clears the types' first
+// rows
+template <typename I, int R>
 __global__ __launch_bounds__(256) void k_embed_count(const void* __restrict__ index, const int* __restrict__ keys, int n,
-                                                     int V, int shift, int per, int segments, int* __restrict__ counts,
-                                                     int* __restrict__ first) {
-  __shared__ int have[4][256];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, seg = blockIdx.x * 4 + wave;
+                                                     int V, int shift, int* __restrict__ counts, int* __restrict__ first) {
+  __shared__ int have[256];
   if (first)
     for (int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x; v < V; v += (int64_t)gridDim.x * 256) first[v] = -1;
-  for (int d = lane; d < 256; d += 64) have[wave][d] = 0;
-  wave_sync();
-  const int64_t lo = (int64_t)seg * per, hi = min(lo + per, (int64_t)n);
-  for (int64_t i = lo; i < hi; i += 64) {
-    const bool on = i + lane < hi;
-    const int64_t at = min(i + lane, hi - 1);
-    const int d = (keys ? keys[at] : type_of<I>(index, at, V)) >> shift & 255;
-    const uint64_t m = same_digit(d, on);
-    if (on && below(m) == 0) have[wave][d] += __popcll(m);
-    wave_sync();
-  }
-  if (seg < segments)
-    for (int d = lane; d < 256; d += 64) counts[d * segments + seg] = have[wave][d];
+  have[threadIdx.x] = 0;
+  const int64_t lo = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * (R * 64);
+  int key[R];
+  read_types<I, R>(index, keys, n, V, lo, key);
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (lo + r * 64 + (threadIdx.x & 63) < n) atomicAdd(&have[key[r] >> shift & 255], 1);  // (whole numbers: any order)
+  __syncthreads();
+  counts[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] = have[threadIdx.x];
 }
 
 // Sums of a workgroup's threads before each, and of all
@@ -114,48 +147,68 @@ __device__ __forceinline__ int scan(int v, int* waves, int& total) {
   return before + s - v;
 }
 
-// of each digit: the numbers before each segment (in place), and their total; segments <= 1024
-__global__ __launch_bounds__(256) void k_embed_scan(int* __restrict__ counts, int segments, int* __restrict__ totals) {
+// of each digit: the numbers before each workgroup (in place), and their total
+__global__ __launch_bounds__(256) void k_embed_scan(int* __restrict__ counts, int groups, int* __restrict__ totals) {
   __shared__ int waves[4];
-  int* row = counts + blockIdx.x * segments;
-  const int s0 = threadIdx.x * 4;
-  int v[4], t = 0, total;
+  int* row = counts + (int64_t)blockIdx.x * groups;
+  int before = 0;
+  for (int g0 = 0; g0 < groups; g0 += 1024) {
+    const int g = g0 + threadIdx.x * 4;
+    int v[4], t = 0, total;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) v[k] = s0 + k < segments ? row[s0 + k] : 0, t += v[k];
-  t = scan(t, waves, total);
+    for (int k = 0; k < 4; ++k) v[k] = g + k < groups ? row[g + k] : 0, t += v[k];
+    t = before + scan(t, waves, total);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if (s0 + k < segments) row[s0 + k] = t;
-    t += v[k];
+    for (int k = 0; k < 4; ++k) {
+      if (g + k < groups) row[g + k] = t;
+      t += v[k];
+    }
+    before += total;
   }
-  if (threadIdx.x == 0) totals[blockIdx.x] = total;
+  if (threadIdx.x == 0) totals[blockIdx.x] = before;
 }
 
-template <typename I>
+template <typename I, int R>
 __global__ __launch_bounds__(256) void k_embed_scatter(const void* __restrict__ index, const int* __restrict__ keys,
-                                                       const int* __restrict__ rows, int n, int V, int shift, int per,
-                                                       int segments, const int* __restrict__ counts,
-                                                       const int* __restrict__ totals, int* __restrict__ keys_out,
-                                                       int* __restrict__ rows_out) {
-  __shared__ int next[4][256], base[256], waves[4];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, seg = blockIdx.x * 4 + wave;
-  int total;
-  base[threadIdx.x] = scan(totals[threadIdx.x], waves, total);
+                                                       const int* __restrict__ rows, int n, int V, int shift,
+                                                       const int* __restrict__ counts, const int* __restrict__ totals,
+                                                       int* __restrict__ keys_out, int* __restrict__ rows_out) {
+  __shared__ int next[4][256], waves[4];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t lo = ((int64_t)blockIdx.x * 4 + wave) * (R * 64);
+  int key[R], row[R], total;
+  read_types<I, R>(index, keys, n, V, lo, key);
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int64_t at = lo + r * 64 + lane;
+    row[r] = rows ? rows[min(at, (int64_t)n - 1)] : (int)at;
+  }
+  const int before = counts[(int64_t)threadIdx.x * gridDim.x + blockIdx.x];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) next[w][threadIdx.x] = 0;
+  int base = scan(totals[threadIdx.x], waves, total) + before;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (lo + r * 64 + lane < n) atomicAdd(&next[wave][key[r] >> shift & 255], 1);
   __syncthreads();
-  if (seg < segments)
-    for (int d = lane; d < 256; d += 64) next[wave][d] = base[d] + counts[d * segments + seg];
-  wave_sync();
-  const int64_t lo = (int64_t)seg * per, hi = min(lo + per, (int64_t)n);
-  for (int64_t i = lo; i < hi; i += 64) {
-    const bool on = i + lane < hi;
-    const int64_t at = min(i + lane, hi - 1);
-    const int key = keys ? keys[at] : type_of<I>(index, at, V), d = key >> shift & 255;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {  // (a thread a digit)
+    const int v = next[w][threadIdx.x];
+    next[w][threadIdx.x] = base;
+    base += v;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    if (lo + r * 64 >= n) break;
+    const bool on = lo + r * 64 + lane < n;
+    const int d = key[r] >> shift & 255;
     const uint64_t m = same_digit(d, on);
     const int rank = below(m), to = next[wave][d] + rank;
     wave_sync();
     if (on) {
-      keys_out[to] = key;
-      rows_out[to] = rows ? rows[at] : (int)at;
+      keys_out[to] = key[r];
+      rows_out[to] = row[r];
       if (rank == 0) next[wave][d] = to + __popcll(m);
     }
     wave_sync();
@@ -216,39 +269,46 @@ __global__ __launch_bounds__(1024) void k_embed_sort(const void* __restrict__ in
 struct Sorted {
   const int *keys, *rows;
   int* range;   // [V] first place of a type in the sorted order, or -1, then [V] one past its last
-  float* part;  // [stretches][2][C]: of the type that began before the stretch, of the one that goes on behind it
-  int per, stretches;
+  float* part;  // [workgroups][2][C]: of the type that began before the workgroup's rows, of the one that goes on behind
+  int per, wide;  // rows of a stretch, of a workgroup
 };
 
-// tpr threads a stretch, each V neighbouring channels; blocks of tpr V channels along y
+// tpr threads a stretch, each V neighbouring channels; blocks of tpr V channels along y; a workgroup's stretches side by
+// side, joined in the LDS: of the parts that go on from one to the next only the workgroup's own two are left
 template <typename TT, typename T, int V>
 __global__ __launch_bounds__(256) void k_embed_sums(EmbedArgs a, const T* __restrict__ g, Sorted s, TT* __restrict__ gt,
                                                     int tpr) {
   constexpr int U = 8;  // rows in flight
-  const int64_t q = (int64_t)blockIdx.x * (256 / tpr) + threadIdx.x / tpr;
-  if (q >= s.stretches) return;
-  const int c = (blockIdx.y * tpr + threadIdx.x % tpr) * V;
-  const bool on = c < a.C;
-  const int at = on ? c : 0;
-  const bool lead = blockIdx.y == 0 && threadIdx.x % tpr == 0;
-  const int64_t lo = q * s.per;
-  const int hi = (int)min(lo + s.per, (int64_t)a.n);
+  __shared__ float part_of[2][256 * V];
+  __shared__ int key_of[2][256];  // the type of a stretch's first part (-1: none), and where it ends there; of its last
+  __shared__ bool ends[256];
+  const int slots = 256 / tpr, slot = threadIdx.x / tpr, t = threadIdx.x % tpr;
+  const int64_t start = (int64_t)blockIdx.x * s.wide, lo = min(start + (int64_t)slot * s.per, (int64_t)a.n);
+  const int c = (blockIdx.y * tpr + t) * V;
+  const bool on = c < a.C, lead = blockIdx.y == 0 && t == 0;
+  const int at = on ? c : 0, hi = (int)min(lo + s.per, (int64_t)a.n);
   float sum[V] = {};
   int key = lo ? s.keys[lo - 1] : -1;  // of the running sum
   bool before = true;                  // it began before the stretch
+  if (t == 0) key_of[0][slot] = key_of[1][slot] = -1;
+  auto write = [&](int v) {
+    float f[V];
+#pragma unroll
+    for (int u = 0; u < V; ++u) f[u] = sum[u] * a.scale;
+    if (on) write_values(gt + (int64_t)v * a.C + at, f);
+  };
   auto flush = [&](int p, int next) {  // the sum of `key` ends at place p (or the stretch does)
     const bool behind = p == hi && next == key;
     if (key >= 0 && key < a.V && (p > lo || !before)) {
       if (before || behind) {
-        float* to = s.part + (q * 2 + (before ? 0 : 1)) * a.C + at;
-        if (on) Raw<float, V>::store((char*)to, [&] { typename Raw<float, V>::type v; join(sum, v); return v; }());
-      } else if (on) {
-        float f[V];
+        if (t == 0) {
+          key_of[before ? 0 : 1][slot] = key;
+          if (before) ends[slot] = !behind;
+        }
 #pragma unroll
-        for (int u = 0; u < V; ++u) f[u] = sum[u] * a.scale;
-        typename Raw<TT, V>::type v;
-        join(f, v);
-        Raw<TT, V>::store((char*)(gt + (int64_t)key * a.C + at), v);
+        for (int u = 0; u < V; ++u) part_of[before ? 0 : 1][threadIdx.x * V + u] = sum[u];
+      } else {
+        write(key);
       }
     }
     if (lead && !behind && key >= 0 && key < a.V) s.range[a.V + key] = p;
@@ -256,14 +316,16 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedArgs a, const T* __rest
     for (int u = 0; u < V; ++u) sum[u] = 0.0f;
   };
   for (int p = (int)lo; p < hi; p += U) {
-    int k[U];
+    int k[U], row[U];
     typename Raw<T, V>::type v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = min(p + u, hi - 1);
-      k[u] = s.keys[i];
-      v[u] = Raw<T, V>::load((const char*)(g + (int64_t)s.rows[i] * a.ld + at));
+      k[u] = s.keys[i], row[u] = s.rows[i];
     }
+    // (rows outside of the table, the last ones, are read and their sum is dropped)
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = Raw<T, V>::load((const char*)(g + (int64_t)row[u] * a.ld + at));
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (p + u >= hi) break;
@@ -276,33 +338,109 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedArgs a, const T* __rest
       for (int x = 0; x < V; ++x) sum[x] += part(v[u], x);
     }
   }
-  flush(hi, hi < a.n ? s.keys[hi] : -1);
+  if (lo < hi) flush(hi, hi < a.n ? s.keys[hi] : -1);
+  __syncthreads();
+  if (slot) return;
+  // the parts in their order, by the first stretch's threads
+  int now = -1;
+  before = true;
+  auto store = [&]() {
+    if (on) write_values(s.part + ((int64_t)blockIdx.x * 2 + (before ? 0 : 1)) * a.C + at, sum);
+  };
+#pragma unroll
+  for (int u = 0; u < V; ++u) sum[u] = 0.0f;
+  for (int w = 0; w < slots; ++w) {
+    if (key_of[0][w] >= 0) {
+      now = key_of[0][w];
+#pragma unroll
+      for (int u = 0; u < V; ++u) sum[u] += part_of[0][(w * tpr + t) * V + u];
+      if (ends[w]) {
+        if (before)
+          store();
+        else
+          write(now);
+        now = -1;
+      }
+    }
+    if (key_of[1][w] >= 0) {
+      now = key_of[1][w], before = false;
+#pragma unroll
+      for (int u = 0; u < V; ++u) sum[u] = part_of[1][(w * tpr + t) * V + u];
+    }
+  }
+  if (now >= 0) store();
 }
 
-// What no stretch held whole: a workgroup a type and 64 channels, the parts of its stretches in 16 interleaved sums
-template <typename TT>
-__global__ __launch_bounds__(1024) void k_embed_join(EmbedArgs a, Sorted s, TT* __restrict__ gt) {
-  __shared__ float red[16][64];
-  const int64_t v = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-  if (v >= a.V) return;
-  const int first = s.range[v], end = first < 0 ? 0 : s.range[a.V + v];
-  const int q0 = first / s.per, q1 = first < 0 ? 0 : (end - 1) / s.per;
-  if (first >= 0 && q0 == q1) return;
-  const int slot = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  for (int c0 = blockIdx.z * 64; c0 < a.C; c0 += gridDim.z * 64) {
-    const int c = c0 + lane;
-    float sum = 0.0f;
-    if (first >= 0 && c < a.C)
-      for (int q = q0 + slot; q <= q1; q += 16) sum += s.part[((int64_t)q * 2 + (q == q0 ? 1 : 0)) * a.C + c];
-    __syncthreads();
-    red[slot][lane] = sum;
-    __syncthreads();
-    if (slot || c >= a.C) continue;
-    for (int k = 1; k < 16; ++k) sum += red[k][lane];
-    const float f[1] = {first < 0 ? 0.0f : sum * a.scale};
-    typename Raw<TT, 1>::type w;
-    join(f, w);
-    Raw<TT, 1>::store((char*)(gt + v * a.C + c), w);
+// What no workgroup held whole: zeros for a type without rows, and the parts of one that several workgroups hold, V
+// channels a lane.  A wave takes up to kEach types, taken far apart (types that many rows have stand side by side in
+// most numberings); where a type has more than kMany parts all threads of its workgroup add them, as many side by side as
+// the channels leave room for
+constexpr int kMany = 32, kEach = 8;
+template <typename TT, int V>
+__global__ __launch_bounds__(1024) void k_embed_join(EmbedArgs a, Sorted s, TT* __restrict__ gt, unsigned apart, int each,
+                                                     int tpr) {
+  __shared__ float red[1024 * V];
+  __shared__ int many[16 * kEach];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t group = (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
+  auto add = [&](int c, int q, int q0, float (&sum)[V]) {
+    float f[V];
+    read_values(s.part + ((int64_t)q * 2 + (q == q0 ? 1 : 0)) * a.C + c, f);
+#pragma unroll
+    for (int u = 0; u < V; ++u) sum[u] += f[u];
+  };
+  auto put = [&](int c, int64_t v, float (&sum)[V]) {
+#pragma unroll
+    for (int u = 0; u < V; ++u) sum[u] *= a.scale;
+    write_values(gt + v * a.C + c, sum);
+  };
+  // the ranges of the wave's `each` types, a lane one
+  const int64_t mine = group + ((int64_t)lane * 16 + wave) * apart;
+  const bool is = lane < each && group < apart && mine < a.V;
+  const int first = is ? s.range[mine] : 0, end = is && first >= 0 ? s.range[a.V + mine] : 0;
+  const int q0 = first < 0 ? 0 : first / s.wide, q1 = end > first ? (end - 1) / s.wide : q0;
+  if (lane < each) many[lane * 16 + wave] = is && q1 - q0 >= kMany;
+  const uint64_t todo = __ballot(is && (first < 0 || (q1 > q0 && q1 - q0 < kMany)));
+  for (int k = 0; k < each; ++k) {
+    if (!(todo >> k & 1)) continue;
+    const int64_t v = group + ((int64_t)k * 16 + wave) * apart;
+    const int f = __builtin_amdgcn_readlane(first, k), b = __builtin_amdgcn_readlane(q0, k), e = __builtin_amdgcn_readlane(q1, k);
+    for (int c = (blockIdx.y * 64 + lane) * V; c < a.C; c += gridDim.y * 64 * V) {
+      float sum[V] = {};
+      if (f >= 0) {
+#pragma unroll 4
+        for (int q = b; q <= e; ++q) add(c, q, b, sum);
+      }
+      put(c, v, sum);
+    }
+  }
+  __syncthreads();
+  const int slots = 1024 / tpr, slot = threadIdx.x / tpr, t = threadIdx.x % tpr;
+  for (int w = 0; w < 16 * each; ++w) {
+    if (!many[w]) continue;
+    const int64_t type = group + (int64_t)w * apart;
+    const int b = s.range[type] / s.wide, e = (s.range[a.V + type] - 1) / s.wide;
+    for (int c0 = blockIdx.y * tpr * V; c0 < a.C; c0 += gridDim.y * tpr * V) {
+      const int c = c0 + t * V;
+      float sum[V] = {};
+      if (c < a.C) {
+#pragma unroll 4
+        for (int q = b + slot; q <= e; q += slots) add(c, q, b, sum);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < V; ++u) red[threadIdx.x * V + u] = sum[u];
+      // halves of the threads, a fixed order
+      for (int k = slots >> 1; k > 0; k >>= 1) {
+        __syncthreads();
+        if (slot < k) {
+#pragma unroll
+          for (int u = 0; u < V; ++u) sum[u] += red[(threadIdx.x + k * tpr) * V + u], red[threadIdx.x * V + u] = sum[u];
+        }
+      }
+      if (slot == 0 && c < a.C) put(c, type, sum);
+      __syncthreads();
+    }
   }
 }
 
@@ -312,21 +450,31 @@ int pieces_of(int C, bool bf16) {  // values of a thread: 16 bytes of the narrow
   return V;
 }
 
+int lanes_of(int C, int V) {
+  int tpr = 1;
+  while (tpr < 64 && tpr < C / V) tpr <<= 1;
+  return tpr;
+}
+
 struct Layout {
-  int passes, per_wave, segments, per, stretches;
+  int passes, rounds, groups, tpr, per, wide, blocks;
   size_t keys[2], rows[2], counts, totals, range, part, total;
 };
-Layout layout_of(int n, int V, int C) {
+Layout layout_of(int n, int V, int C, bool bf16) {
   Layout l{};
   l.passes = 1;
   while (l.passes < 4 && (uint64_t)V >> (8 * l.passes)) ++l.passes;  // (types 0 .. V)
-  l.per_wave = (int)(((int64_t)n + kSegments - 1) / kSegments + 63) / 64 * 64;
-  if (l.per_wave < 64) l.per_wave = 64;
-  l.segments = (int)(((int64_t)n + l.per_wave - 1) / l.per_wave);
-  // rows of a stretch: enough stretches to fill the GPU
-  l.per = 16;
-  while (l.per < 256 && (int64_t)n * ((C + 255) / 256) / l.per > 8192) l.per <<= 1;
-  l.stretches = (int)(((int64_t)n + l.per - 1) / l.per);
+  // rounds of 64 rows a wave of the sort: up to 512 workgroups with one, then up to 2,048 with four, then 16
+  l.rounds = n <= 1 << 17 ? 1 : n <= 1 << 21 ? 4 : 16;
+  l.groups = (int)(((int64_t)n + 256 * l.rounds - 1) / (256 * l.rounds));
+  // rows of a stretch: 8 (all in flight) until the workgroups are 2,048, then up to 64
+  const int Q = pieces_of(C, bf16);
+  l.tpr = lanes_of(C, Q);
+  const int columns = (C / Q + l.tpr - 1) / l.tpr;
+  l.per = 8;
+  while (l.per < 64 && (int64_t)n * columns / ((int64_t)l.per * (256 / l.tpr)) > 2048) l.per <<= 1;
+  l.wide = l.per * (256 / l.tpr);
+  l.blocks = (int)(((int64_t)n + l.wide - 1) / l.wide);
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t was = at;
@@ -334,17 +482,16 @@ Layout layout_of(int n, int V, int C) {
     return was;
   };
   for (int k = 0; k < 2; ++k) l.keys[k] = take(sizeof(int) * (size_t)n), l.rows[k] = take(sizeof(int) * (size_t)n);
-  l.counts = take(sizeof(int) * 256 * (size_t)l.segments);
-  l.totals = take(sizeof(int) * 256);
+  if (n > kSmall) l.counts = take(sizeof(int) * 256 * (size_t)l.groups), l.totals = take(sizeof(int) * 256);
   l.range = take(sizeof(int) * 2 * (size_t)V);
-  l.part = take(sizeof(float) * 2 * (size_t)l.stretches * C);
+  l.part = take(sizeof(float) * 2 * (size_t)l.blocks * C);
   l.total = at;
   return l;
 }
 
 }  // namespace
 
-size_t embed_workspace(int n, int V, int C) { return layout_of(n, V, C).total; }
+size_t embed_workspace(int n, int V, int C, bool bf16) { return layout_of(n, V, C, bf16).total; }
 
 #define E2F_EMBED_V(TT, T)                    \
   switch (V) {                                \
@@ -362,30 +509,47 @@ size_t embed_workspace(int n, int V, int C) { return layout_of(n, V, C).total; }
 
 hipError_t launch_embed_forward(const EmbedArgs& a, const void* table, void* out, hipStream_t st) {
   if (a.n == 0) return hipSuccess;
-  const int V = pieces_of(a.C, a.table_bf16 && a.bf16);
+  const int V = pieces_of(a.C, a.bf16);
   const int64_t pieces = (int64_t)a.K * a.C / V;
   int tpr = 1;
   while (tpr < 64 && tpr < pieces) tpr <<= 1;
-  const Rounds r = rounds_of(((int64_t)a.n + 256 / tpr - 1) / (256 / tpr), 256);
+  // four rows a thread where a row is one round of its threads and there are enough to fill the GPU
+  const bool four = pieces <= 64 && (int64_t)a.n * tpr > 1 << 20;
+  const int64_t rows = 256 / tpr * (four ? 4 : 1);
+  const Rounds r = rounds_of(((int64_t)a.n + rows - 1) / rows, 256);
   const dim3 grid(r.x, r.rounds);
-#define E2F_EMBED(TT, T, VV)                                                                               \
-  a.wide ? k_embed<TT, T, int64_t, VV><<<grid, 256, 0, st>>>(a, (const TT*)table, (T*)out, tpr)            \
-         : k_embed<TT, T, int32_t, VV><<<grid, 256, 0, st>>>(a, (const TT*)table, (T*)out, tpr)
+#define E2F_EMBED_R(TT, T, I, VV)                                                                  \
+  four ? k_embed<TT, T, I, VV, 4><<<grid, 256, 0, st>>>(a, (const TT*)table, (T*)out, tpr)         \
+       : k_embed<TT, T, I, VV, 1><<<grid, 256, 0, st>>>(a, (const TT*)table, (T*)out, tpr)
+#define E2F_EMBED(TT, T, VV)                 \
+  if (a.wide)                                \
+    E2F_EMBED_R(TT, T, int64_t, VV);         \
+  else                                       \
+    E2F_EMBED_R(TT, T, int32_t, VV)
   if (a.table_bf16 && a.bf16) {
     E2F_EMBED_V(bf16_t, bf16_t)
   } else if (a.table_bf16) {
     E2F_EMBED_V4(bf16_t, float)
   } else if (a.bf16) {
-    E2F_EMBED_V4(float, bf16_t)
+    E2F_EMBED_V(float, bf16_t)
   } else {
     E2F_EMBED_V4(float, float)
   }
 #undef E2F_EMBED
+#undef E2F_EMBED_R
   return hipGetLastError();
 }
 
+template <typename I, int R>
+void sort_pass(const EmbedArgs& a, const Layout& l, const int* k, const int* r, int shift, int* counts, int* totals,
+               int* first, int* keys, int* rows, hipStream_t st) {
+  k_embed_count<I, R><<<l.groups, 256, 0, st>>>(a.index, k, a.n, a.V, shift, counts, first);
+  k_embed_scan<<<256, 256, 0, st>>>(counts, l.groups, totals);
+  k_embed_scatter<I, R><<<l.groups, 256, 0, st>>>(a.index, k, r, a.n, a.V, shift, counts, totals, keys, rows);
+}
+
 hipError_t launch_embed_backward(const EmbedArgs& a, const void* gout, void* gtable, void* workspace, hipStream_t st) {
-  const Layout l = layout_of(a.n, a.V, a.C);
+  const Layout l = layout_of(a.n, a.V, a.C, a.bf16);
   char* ws = (char*)workspace;
   int *keys[2] = {(int*)(ws + l.keys[0]), (int*)(ws + l.keys[1])}, *rows[2] = {(int*)(ws + l.rows[0]), (int*)(ws + l.rows[1])};
   int *counts = (int*)(ws + l.counts), *totals = (int*)(ws + l.totals), *range = (int*)(ws + l.range);
@@ -396,50 +560,47 @@ hipError_t launch_embed_backward(const EmbedArgs& a, const void* gout, void* gta
     else
       k_embed_sort<int32_t><<<1, 1024, 0, st>>>(a.index, a.n, a.V, l.passes, keys[0], rows[0], range);
   } else {
-    const int blocks = (l.segments + 3) / 4;
     for (int p = 0; p < l.passes; ++p, now ^= 1) {
       const int *k = p ? keys[now] : nullptr, *r = p ? rows[now] : nullptr;
       int* first = p ? nullptr : range;
-      if (a.wide) {
-        k_embed_count<int64_t><<<blocks, 256, 0, st>>>(a.index, k, a.n, a.V, 8 * p, l.per_wave, l.segments, counts, first);
-        k_embed_scan<<<256, 256, 0, st>>>(counts, l.segments, totals);
-        k_embed_scatter<int64_t><<<blocks, 256, 0, st>>>(a.index, k, r, a.n, a.V, 8 * p, l.per_wave, l.segments, counts,
-                                                         totals, keys[now ^ 1], rows[now ^ 1]);
-      } else {
-        k_embed_count<int32_t><<<blocks, 256, 0, st>>>(a.index, k, a.n, a.V, 8 * p, l.per_wave, l.segments, counts, first);
-        k_embed_scan<<<256, 256, 0, st>>>(counts, l.segments, totals);
-        k_embed_scatter<int32_t><<<blocks, 256, 0, st>>>(a.index, k, r, a.n, a.V, 8 * p, l.per_wave, l.segments, counts,
-                                                         totals, keys[now ^ 1], rows[now ^ 1]);
-      }
+      auto pass = a.wide ? (l.rounds == 1 ? sort_pass<int64_t, 1> : l.rounds == 4 ? sort_pass<int64_t, 4> : sort_pass<int64_t, 16>)
+                         : (l.rounds == 1 ? sort_pass<int32_t, 1> : l.rounds == 4 ? sort_pass<int32_t, 4> : sort_pass<int32_t, 16>);
+      pass(a, l, k, r, 8 * p, counts, totals, first, keys[now ^ 1], rows[now ^ 1], st);
     }
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const Sorted s{keys[now], rows[now], range, (float*)(ws + l.part), l.per, l.stretches};
+  const Sorted s{keys[now], rows[now], range, (float*)(ws + l.part), l.per, l.wide};
   if (a.n) {
-    const int V = pieces_of(a.C, false);
-    int tpr = 1;
-    while (tpr < 64 && tpr < a.C / V) tpr <<= 1;
-    const dim3 grid((unsigned)(((int64_t)l.stretches + 256 / tpr - 1) / (256 / tpr)), (unsigned)((a.C / V + tpr - 1) / tpr));
-#define E2F_EMBED(TT, T, VV) k_embed_sums<TT, T, VV><<<grid, 256, 0, st>>>(a, (const T*)gout, s, (TT*)gtable, tpr)
+    const int V = pieces_of(a.C, a.bf16);
+    const dim3 grid(l.blocks, (unsigned)((a.C / V + l.tpr - 1) / l.tpr));
+#define E2F_EMBED(TT, T, VV) k_embed_sums<TT, T, VV><<<grid, 256, 0, st>>>(a, (const T*)gout, s, (TT*)gtable, l.tpr)
     if (a.table_bf16 && a.bf16) {
-      E2F_EMBED_V4(bf16_t, bf16_t)
+      E2F_EMBED_V(bf16_t, bf16_t)
     } else if (a.table_bf16) {
       E2F_EMBED_V4(bf16_t, float)
     } else if (a.bf16) {
-      E2F_EMBED_V4(float, bf16_t)
+      E2F_EMBED_V(float, bf16_t)
     } else {
       E2F_EMBED_V4(float, float)
     }
 #undef E2F_EMBED
   }
-  const Rounds r = rounds_of(a.V, 1024);
-  const int columns = (a.C + 63) / 64;
-  const dim3 grid(r.x, r.rounds, a.V < 4096 ? columns : 1);
-  if (a.table_bf16)
-    k_embed_join<bf16_t><<<grid, 1024, 0, st>>>(a, s, (bf16_t*)gtable);
-  else
-    k_embed_join<float><<<grid, 1024, 0, st>>>(a, s, (float*)gtable);
+  // (the table's type alone: the parts are float)
+  const int V = pieces_of(a.C, a.table_bf16), tpr = lanes_of(a.C, V), columns = (a.C / V + 63) / 64;
+  // types of a wave: as many workgroups as the GPU holds at once, where there are that many types
+  int each = 1;
+  while (each < kEach && a.V / (16 * each) > 512) each <<= 1;
+  const unsigned apart = ((unsigned)a.V + 16 * each - 1) / (16 * each);
+  const Rounds r = rounds_of(apart, 1024);
+  const dim3 grid(r.x, apart < 512 ? columns : 1, r.rounds);
+#define E2F_EMBED(TT, T, VV) k_embed_join<TT, VV><<<grid, 1024, 0, st>>>(a, s, (TT*)gtable, apart, each, tpr)
+  if (a.table_bf16) {
+    E2F_EMBED_V(bf16_t, float)
+  } else {
+    E2F_EMBED_V4(float, float)
+  }
+#undef E2F_EMBED
   return hipGetLastError();
 }
 

@@ -43,9 +43,13 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int tpr, float (*red)[N]
     for (int i = 0; i < N; ++i) v[i] += red[w][i];
 }
 
+// (by the power of -|x|, whose argument keeps its low part: a shut gate keeps its digits, to 6 roundings down to 2^-126)
 __device__ __forceinline__ float sigmoid(float x) {
-  const float e = expf(-fabsf(x));
-  return (x < 0.0f ? e : 1.0f) / (1.0f + e);
+  constexpr float kLog2e = 1.44269504f, kLow = 1.92596299e-8f, kLn2 = 0.693147181f;
+  const float a = -fabsf(x), hi = a * kLog2e, lo = fmaf(a, kLog2e, -hi) + a * kLow;
+  float e = __builtin_amdgcn_exp2f(hi);
+  e = fmaf(e, hi > -INFINITY ? lo * kLn2 : 0.0f, e);
+  return (x < 0.0f ? e : 1.0f) * __builtin_amdgcn_rcpf(1.0f + e);
 }
 
 // Where a thread's values lie: V neighbouring channels of each of S pieces, which are the components (L > 0), or
@@ -57,6 +61,8 @@ struct Place {
   int C, t, tpr;
   __device__ __forceinline__ int channel(int s) const { return L ? t * V : (s * tpr + t) * V; }
   __device__ __forceinline__ int offset(int s) const { return L ? s * C + t * V : (s * tpr + t) * V; }
+  // whether the piece's value u lies before the row's end (pieces are whole unless the end cuts one)
+  __device__ __forceinline__ bool within(int s, int u, bool tail) const { return channel(s) + (tail ? u : 0) < C; }
   // (weights: of a degree, of a stretch)
   __device__ __forceinline__ int weight(int i) const { return L ? i * C + t * V : (i * tpr + t) * V; }
 };
@@ -109,13 +115,27 @@ __device__ __forceinline__ void write_row(T* p, const Place<L, V, J>& at, const 
 }
 
 // N sets of the thread's weights (`none` where there are none, 0 behind the row's end)
-template <int N, int L, int V, int J>
+template <bool TAIL, int N, int L, int V, int J>
 __device__ __forceinline__ void read_weights(const float* w, float none, const Place<L, V, J>& at, float (&f)[N][V]) {
+  constexpr int Q = V < 4 ? V : 4;
 #pragma unroll
-  for (int i = 0; i < N; ++i)
+  for (int i = 0; i < N; ++i) {
 #pragma unroll
-    for (int u = 0; u < V; ++u)
-      f[i][u] = at.channel(i) + u >= at.C ? 0.0f : w ? w[at.weight(i) + u] : none;
+    for (int u = 0; u < V; ++u) f[i][u] = at.within(i, u, TAIL) ? none : 0.0f;
+    if (!w || at.channel(i) >= at.C) continue;
+    if (!TAIL || at.channel(i) + V <= at.C) {
+#pragma unroll
+      for (int u = 0; u < V; u += Q) {
+        const auto v = Raw<float, Q>::load((const char*)(w + at.weight(i) + u));
+#pragma unroll
+        for (int k = 0; k < Q; ++k) f[i][u + k] = part(v, k);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < V; ++u)
+        if (at.within(i, u, TAIL)) f[i][u] = w[at.weight(i) + u];
+    }
+  }
 }
 
 // f(s, l) for the components above the scalars, of degree l, and end(l) after each degree
@@ -129,12 +149,12 @@ __device__ __forceinline__ void each_higher(F&& f, G&& end) {
 }
 
 // The scalars' mean off them (0 behind the row's end)
-template <int L, int V, int J>
+template <bool TAIL, int L, int V, int J>
 __device__ __forceinline__ void centre(const Place<L, V, J>& at, float mean, float (&x)[Place<L, V, J>::S][V]) {
 #pragma unroll
   for (int s = 0; s < Place<L, V, J>::S0; ++s)
 #pragma unroll
-    for (int u = 0; u < V; ++u) x[s][u] = at.channel(s) + u < at.C ? x[s][u] - mean : 0.0f;
+    for (int u = 0; u < V; ++u) x[s][u] = at.within(s, u, TAIL) ? x[s][u] - mean : 0.0f;
 }
 
 template <int L, typename T, int V, int J, bool SILU, bool TAIL>
@@ -142,53 +162,54 @@ __global__ __launch_bounds__(512) void k_layer_forward(LayerArgs a, int tpr, T* 
   typedef Place<L, V, J> P;
   __shared__ float red1[8][L ? 2 : 1], red2[8][1];
   const int slot = threadIdx.x / tpr, slots = blockDim.x / tpr;
-  const int64_t first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * slots;
-  if (first >= a.n) return;  // (the last round's)
-  const int64_t row = min(first + slot, (int64_t)a.n - 1);
   const P at{a.C, (int)threadIdx.x % tpr, tpr};
-  Row<T, L, V, J, TAIL> in;
-  in.load((const T*)a.x + row * a.ldx, at);
-  float x[P::S][V], w[P::W][V], b[P::S0][V];
-  read_weights(a.w, 1.0f, at, w);
-  read_weights(a.b, 0.0f, at, b);
-  in.values(at, x);
+  float w[P::W][V], b[P::S0][V];
+  read_weights<TAIL>(a.w, 1.0f, at, w);
+  read_weights<TAIL>(a.b, 0.0f, at, b);
   const float per = 1.0f / (float)a.C;
-  float s1[L ? 2 : 1] = {}, s2[1] = {}, t = 0.0f;
+  for (int64_t first = (int64_t)blockIdx.x * slots; first < a.n; first += (int64_t)gridDim.x * slots) {
+    const int64_t row = min(first + slot, (int64_t)a.n - 1);
+    Row<T, L, V, J, TAIL> in;
+    in.load((const T*)a.x + row * a.ldx, at);
+    float x[P::S][V];
+    in.values(at, x);
+    float s1[L ? 2 : 1] = {}, s2[1] = {}, t = 0.0f;
 #pragma unroll
-  for (int s = 0; s < P::S0; ++s)
+    for (int s = 0; s < P::S0; ++s)
 #pragma unroll
-    for (int u = 0; u < V; ++u) s1[0] += x[s][u];
-  each_higher<L>(
-      [&](int s, int) {
-#pragma unroll
-        for (int u = 0; u < V; ++u) t += x[s][u] * x[s][u];
-      },
-      [&](int l) { s1[L ? 1 : 0] += t * (1.0f / (2 * l + 1)), t = 0.0f; });
-  row_sums(s1, tpr, red1);
-  centre(at, s1[0] * per, x);
-#pragma unroll
-  for (int s = 0; s < P::S0; ++s)
-#pragma unroll
-    for (int u = 0; u < V; ++u) s2[0] += x[s][u] * x[s][u];
-  row_sums(s2, tpr, red2);
-  const float r0 = 1.0f / sqrtf(s2[0] * per + a.eps);
-#pragma unroll
-  for (int s = 0; s < P::S0; ++s)
-#pragma unroll
-    for (int u = 0; u < V; ++u) {
-      const float z = x[s][u] * r0 * w[s][u] + b[s][u];
-      x[s][u] = SILU ? z * sigmoid(z) : z;
-    }
-  if constexpr (L > 0) {
-    const float r1 = 1.0f / sqrtf(s1[1] * per * (1.0f / L) + a.eps);
+      for (int u = 0; u < V; ++u) s1[0] += x[s][u];
     each_higher<L>(
-        [&](int s, int l) {
+        [&](int s, int) {
 #pragma unroll
-          for (int u = 0; u < V; ++u) x[s][u] *= r1 * w[l][u];
+          for (int u = 0; u < V; ++u) t += x[s][u] * x[s][u];
         },
-        [](int) {});
+        [&](int l) { s1[L ? 1 : 0] += t * (1.0f / (2 * l + 1)), t = 0.0f; });
+    row_sums(s1, tpr, red1);
+    centre<TAIL>(at, s1[0] * per, x);
+#pragma unroll
+    for (int s = 0; s < P::S0; ++s)
+#pragma unroll
+      for (int u = 0; u < V; ++u) s2[0] += x[s][u] * x[s][u];
+    row_sums(s2, tpr, red2);
+    const float r0 = 1.0f / sqrtf(s2[0] * per + a.eps);
+#pragma unroll
+    for (int s = 0; s < P::S0; ++s)
+#pragma unroll
+      for (int u = 0; u < V; ++u) {
+        const float z = x[s][u] * r0 * w[s][u] + b[s][u];
+        x[s][u] = SILU ? z * sigmoid(z) : z;
+      }
+    if constexpr (L > 0) {
+      const float r1 = 1.0f / sqrtf(s1[1] * per * (1.0f / L) + a.eps);
+      each_higher<L>(
+          [&](int s, int l) {
+#pragma unroll
+            for (int u = 0; u < V; ++u) x[s][u] *= r1 * w[l][u];
+          },
+          [](int) {});
+    }
+    if (first + slot < a.n) write_row<T, L, V, J, TAIL>(out + row * (int64_t)(L ? P::S : 1) * a.C, at, x);
   }
-  if (first + slot < a.n) write_row<T, L, V, J, TAIL>(out + row * (int64_t)(L ? P::S : 1) * a.C, at, x);
 }
 
 template <int L, typename T, int V, int J, bool SILU, bool TAIL>
@@ -201,8 +222,8 @@ __global__ __launch_bounds__(512) void k_layer_backward(LayerArgs a, LayerGrad g
   const P at{a.C, (int)threadIdx.x % tpr, tpr};
   const float per = 1.0f / (float)a.C;
   float w[P::W][V], b[P::S0][V], aw[P::W][V] = {}, ab[P::S0][V] = {};
-  read_weights(a.w, 1.0f, at, w);
-  if constexpr (SILU) read_weights(a.b, 0.0f, at, b);
+  read_weights<TAIL>(a.w, 1.0f, at, w);
+  if constexpr (SILU) read_weights<TAIL>(a.b, 0.0f, at, b);
   for (int64_t first = (int64_t)blockIdx.x * slots; first < a.n; first += (int64_t)gridDim.x * slots) {
     const int64_t row = min(first + slot, (int64_t)a.n - 1), packed = row * (L ? P::S : 1) * a.C;
     const bool on = first + slot < a.n;
@@ -244,7 +265,7 @@ __global__ __launch_bounds__(512) void k_layer_backward(LayerArgs a, LayerGrad g
     } else {
       row_sums(s1, tpr, red1);
     }
-    centre(at, s1[0] * per, x);
+    centre<TAIL>(at, s1[0] * per, x);
     // without an activation u needs no statistics: its sums go along with the variance's
 #pragma unroll
     for (int s = 0; s < P::S0; ++s)
@@ -323,24 +344,29 @@ __global__ __launch_bounds__(512) void k_layer_backward(LayerArgs a, LayerGrad g
   }
 }
 
-// The weights' gradients from the workgroups' sums: 32 columns a workgroup
+// The weights' gradients from the workgroups' sums: 16 columns a workgroup, 64 sums of each side by side
 __global__ __launch_bounds__(1024) void k_layer_weights(const float* __restrict__ part, int parts, int weights, int count,
                                                         float* __restrict__ gw, float* __restrict__ gb) {
-  __shared__ double red[32][33];
-  const int c = blockIdx.x * 32 + (threadIdx.x & 31), s = threadIdx.x >> 5;
+  __shared__ double red[64][17];
+  const int c = blockIdx.x * 16 + (threadIdx.x & 15), s = threadIdx.x >> 4;
   double v = 0.0;
-  if (c < count)
-    for (int b = s; b < parts; b += 32) v += part[(int64_t)b * count + c];
-  red[s][threadIdx.x & 31] = v;
+  if (c < count) {
+#pragma unroll 4
+    for (int b = s; b < parts; b += 64) v += part[(int64_t)b * count + c];
+  }
+  red[s][threadIdx.x & 15] = v;
   __syncthreads();
   if (s || c >= count) return;
-  for (int k = 1; k < 32; ++k) v += red[k][threadIdx.x];
+#pragma unroll 8
+  for (int k = 1; k < 64; ++k) v += red[k][threadIdx.x];
   if (c < weights) {
     if (gw) gw[c] = (float)v;
   } else if (gb) {
     gb[c - weights] = (float)v;
   }
 }
+
+constexpr int kForwardBlocks = 4096;  // of a launch, which take rows in turn
 
 struct Shape {
   int V, J, tpr, threads;
@@ -356,7 +382,7 @@ Shape shape_of(int L, int C, bool bf16, bool back) {
     s.tpr = 1;
     while (s.tpr * s.V < C) s.tpr <<= 1;
   } else {
-    s.V = bf16 && !back ? 8 : 4;
+    s.V = bf16 && (!back || C <= 512) ? 8 : 4;
     const int pieces = (C + s.V - 1) / s.V;
     s.tpr = 1, s.J = 1;
     while (s.tpr < 64 && s.tpr < pieces) s.tpr <<= 1;
@@ -376,7 +402,10 @@ Shape shape_of(int L, int C, bool bf16, bool back) {
 int layer_parts(int L, int C, bool bf16, int n) {
   const Shape s = shape_of(L, C, bf16, true);
   const int slots = s.threads / s.tpr;
-  const int64_t want = ((int64_t)n + slots - 1) / slots, most = 512;
+  // two workgroups a CU; of long rows so few that their sums, written and read, stay a quarter of the rows' bytes
+  const int64_t want = ((int64_t)n + slots - 1) / slots;
+  int64_t most = 512;
+  if (L == 0 && want > 128 && want / 4 < most) most = want / 4 < 128 ? 128 : want / 4;
   return (int)(want < most ? want : most);
 }
 
@@ -409,7 +438,7 @@ int layer_parts(int L, int C, bool bf16, int n) {
 #define E2F_LAYER_SWITCH(VB)                                              \
   if (L == 0 && bf16) {                                                   \
     switch (s.J) {                                                        \
-      E2F_LAYER_J(bf16_t, VB, 1) E2F_LAYER_J(bf16_t, VB, 2) E2F_LAYER_J(bf16_t, VB, 4) \
+      E2F_LAYER_J(bf16_t, 8, 1) E2F_LAYER_J(bf16_t, VB, 2) E2F_LAYER_J(bf16_t, VB, 4) \
       default: return hipErrorInvalidValue;                               \
     }                                                                     \
   } else if (L == 0) {                                                    \
@@ -427,9 +456,8 @@ int layer_parts(int L, int C, bool bf16, int n) {
 hipError_t launch_layer_forward(int L, bool bf16, const LayerArgs& a, void* out, hipStream_t st) {
   if (a.n == 0) return hipSuccess;
   const Shape s = shape_of(L, a.C, bf16, false);
-  const int slots = s.threads / s.tpr;
-  const Rounds r = rounds_of(((int64_t)a.n + slots - 1) / slots, s.threads);
-  const dim3 grid(r.x, r.rounds);
+  const int64_t blocks = ((int64_t)a.n + s.threads / s.tpr - 1) / (s.threads / s.tpr);
+  const unsigned grid = (unsigned)(blocks < kForwardBlocks ? blocks : kForwardBlocks);
 #define E2F_LAYER(LL, T, VV, JJ, A, E) k_layer_forward<LL, T, VV, JJ, A, E><<<grid, s.threads, 0, st>>>(a, s.tpr, (T*)out)
   E2F_LAYER_SWITCH(8)
 #undef E2F_LAYER
@@ -447,7 +475,7 @@ hipError_t launch_layer_backward(int L, bool bf16, const LayerArgs& a, const Lay
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (g.gw || g.gb) k_layer_weights<<<(count + 31) / 32, 1024, 0, st>>>(g.part, parts, weights, count, g.gw, g.gb);
+  if (g.gw || g.gb) k_layer_weights<<<(count + 15) / 16, 1024, 0, st>>>(g.part, parts, weights, count, g.gw, g.gb);
   return hipGetLastError();
 }
 
