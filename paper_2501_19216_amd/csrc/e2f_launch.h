@@ -315,7 +315,6 @@ struct OrthoArgs {
 // matrices are scaled; false where the steps do not keep them bounded
 bool ortho_bounds(int steps, const float* coef, int* x_exp, int* a_exp, int* b_exp);
 constexpr int kOrthoMaxSteps = 64;
-int ortho_batch(int rows, int cols, int count);  // matrices at a time
 size_t ortho_workspace(int rows, int cols, int count);
 hipError_t launch_orthogonalize(const OrthoArgs& a, void* workspace, hipStream_t s);
 

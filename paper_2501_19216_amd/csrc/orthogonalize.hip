@@ -12,6 +12,10 @@
 // a X is added in float; the products, whose errors stay in the directions that are already large, take their operands as two float16 numbers,
 // x = hi + lo to 22 bits, in three products (hi hi, hi lo, lo hi) on the matrix cores, summed in float.  Powers of two keep the
 // operands in float16's range: from the coefficients follow bounds of all singular values (ortho_bounds).
+//
+// Matrices that fit a workgroup's registers and LDS go through all steps there (k_ortho_small); larger ones through three
+// tiled products a step.  Those hold Y = X^T alone: Y' = a Y + Y B (B = b P + c P^2 is symmetric) reads rows of Y and of B,
+// and P = Y^T Y reads its operands by the LDS's transposing loads.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -23,24 +27,38 @@
 namespace e2f {
 namespace {
 
-typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef short s4 __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 
-constexpr int kTile = 64;   // rows and columns of a workgroup's product; matrices are padded to it with zeros
-constexpr int kStep = 32;   // of the products' long axis
-constexpr int kParts = 64;  // workgroups that sum a matrix's squares, at most
-constexpr int kTable = 96;  // matrices of a launch: their addresses travel in the kernel's arguments
+constexpr int kStep = 32;     // of the products' long axis
+constexpr int kParts = 256;   // workgroups that sum a matrix's squares, at most
+constexpr int kTable = 64;    // matrices of a launch: their addresses travel in the kernel's arguments
 
 // A matrix as the products read it: rows of steps of 32 values, each step's hi and then its lo (128 bytes)
 __host__ __device__ __forceinline__ int64_t split_at(int64_t row, int ld, int k, int lo) {
   return row * 2 * ld + (k >> 5) * 64 + lo * 32 + (k & 31);
 }
-__device__ __forceinline__ void split(float x, float scale, _Float16& hi, _Float16& lo) {
-  const float y = x * scale;
-  hi = (_Float16)y;
-  lo = (_Float16)(y - (float)hi);
+// four floats, scaled, as two float16 numbers each: hi rounded to nearest, lo the rest
+__device__ __forceinline__ void split(v4f x, float scale, h4& hi, h4& lo) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float y = x[k] * scale;
+    hi[k] = (_Float16)y;
+    lo[k] = (_Float16)(y - (float)hi[k]);
+  }
+}
+__device__ __forceinline__ h8 both(h4 a, h4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+__device__ __forceinline__ v4f mfma(h8 a, h8 b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+// the product of operands split in two: the small parts first
+__device__ __forceinline__ v4f product(h8 ah, h8 al, h8 bh, h8 bl, v4f c) {
+  return mfma(ah, bh, mfma(ah, bl, mfma(al, bh, c)));
+}
+// Transposing load: of 16 lanes, lane s gives the address of four neighbours of row s / 4, from column 4 (s % 4) on, and lane
+// t gets the four rows' values of column t
+__device__ __forceinline__ h4 read_transposed(const _Float16* p) {
+  return __builtin_bit_cast(h4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)p));
 }
 
 struct Table {
@@ -48,7 +66,6 @@ struct Table {
   const float* m[kTable];
   float* to[kTable];
 };
-static_assert(sizeof(Table) <= 3584, "kernel arguments of 4 KB");
 struct Ends {
   const void* w[kTable];
   void* out[kTable];
@@ -58,216 +75,518 @@ struct Sizes {
   int rows, cols, m, n, mp, np;  // m <= n: X's sides; mp, np: padded
   bool turned;                   // X is the transpose of the caller's matrices
 };
+struct Update {
+  float mu, eps, scale, decay;
+  bool nesterov;
+};
 
-// element i of the gradient or update
 template <typename T>
 __device__ __forceinline__ float value(const void* p, int64_t i) {
   return part(Raw<T, 1>::load((const char*)((const T*)p + i)), 0);
 }
-
-// The momentum, and the sum of the update's squares in float64, in which none of them overflows
+// four neighbours of an array from i on, of which `have` are there (zeros behind)
 template <typename T>
-__global__ __launch_bounds__(256) void k_ortho_norm(Table t, int64_t size, int parts, float mu, bool nesterov,
-                                                    double* __restrict__ part) {
-  const int z = blockIdx.y;
-  double s = 0.0;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)parts * 256) {
-    float u = value<T>(t.g[z], i);
-    if (t.m[z]) {
-      const float m = mu * t.m[z][i] + u;
-      t.to[z][i] = m;
-      u = nesterov ? u + mu * m : m;
+__device__ __forceinline__ v4f values(const void* p, int64_t i, int have) {
+  v4f f = {};
+  if (have >= 4) {
+    const auto v = Raw<T, 4>::load((const char*)((const T*)p + i));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) f[k] = part(v, k);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (k < have) f[k] = value<T>(p, i + k);
+  }
+  return f;
+}
+template <typename T>
+__device__ __forceinline__ void put(void* p, int64_t i, float x) {
+  const float f[1] = {x};
+  typename Raw<T, 1>::type v;
+  join(f, v);
+  Raw<T, 1>::store((char*)((T*)p + i), v);
+}
+template <typename T>
+__device__ __forceinline__ void puts(void* p, int64_t i, int have, v4f x) {
+  if (have >= 4) {
+    const float f[4] = {x[0], x[1], x[2], x[3]};
+    typename Raw<T, 4>::type v;
+    join(f, v);
+    Raw<T, 4>::store((char*)((T*)p + i), v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (k < have) put<T>(p, i + k, x[k]);
+  }
+}
+
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// ------------------------------------------------------------------ matrices of a workgroup
+// the steps' coefficients and, as exponents of two, the scales of X, P and B as operands
+struct Steps {
+  float coef[kOrthoMaxSteps][3];
+  signed char x[kOrthoMaxSteps + 1], p[kOrthoMaxSteps], b[kOrthoMaxSteps];
+  int count;
+};
+static_assert(sizeof(Table) + sizeof(Ends) + sizeof(Steps) + sizeof(Sizes) + sizeof(Update) <= 4032, "kernel arguments of 4 KB");
+__device__ __forceinline__ float power(int e) { return __uint_as_float((unsigned)(127 + e) << 23); }
+
+// values of an LDS row, of X^T and of P: 16 rows of 32 bytes meet few equal banks
+template <int MP>
+struct Rows {
+  static constexpr int X = MP + 24, P = MP + 16;
+  static constexpr size_t bytes(int np) { return sizeof(_Float16) * 2 * ((size_t)np * X + (size_t)MP * P); }
+};
+
+// A matrix of up to MP rows and 128 S columns, a workgroup of eight waves each.  A wave holds S strips of 16 columns of X in
+// registers as the matrix cores return them: lane l has rows 4 (l / 16) .. + 3 of every 16 and column l % 16.  These rows, of two
+// 16s, are also what it gives as the right operand of B X, so B's columns are stored in that order (within 32: 16 h + 4 g + e
+// at 8 g + 4 h + e).  X^T lies in the LDS for P, whose tiles the waves share in blocks of BR x BC.  P, and B that replaces it, are
+// symmetric: a tile is stored as its transpose
+template <int MP, int S, typename TG, typename T>
+__global__ __launch_bounds__(512) void k_ortho_small(Table t, Ends e, Steps steps, Sizes d, Update u) {
+  constexpr int MT = MP / 16, SX = Rows<MP>::X, SP = Rows<MP>::P;
+  constexpr int BR = MT <= 4 ? 1 : 2, BC = MT == 2 ? 1 : MT == 4 ? 2 : MT / 2, COLS = MT / BC;
+  extern __shared__ __align__(16) _Float16 lds[];
+  __shared__ double squares[8];
+  _Float16 *xh = lds, *xl = xh + d.np * SX, *ph = xl + d.np * SX, *pl = ph + MP * SP;
+  const int z = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  v4f x[S][MT];
+  double sum = 0.0;
+#pragma unroll
+  for (int s = 0; s < S; ++s)
+#pragma unroll
+    for (int tau = 0; tau < MT; ++tau) {
+      const int j = (wave + 8 * s) * 16 + c, i = tau * 16 + 4 * g;
+      v4f v = {};
+      if (j < d.n && i < d.m) {
+        if (d.turned) {
+          const int64_t at = (int64_t)j * d.cols + i;
+          v = values<TG>(t.g[z], at, d.m - i);
+          if (t.m[z]) {
+            const v4f m = values<float>(t.m[z], at, d.m - i) * u.mu + v;
+            puts<float>(t.to[z], at, d.m - i, m);
+            v = u.nesterov ? v + u.mu * m : m;
+          }
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (i + r < d.m) {
+              const int64_t at = (int64_t)(i + r) * d.cols + j;
+              v[r] = value<TG>(t.g[z], at);
+              if (t.m[z]) {
+                const float m = u.mu * t.m[z][at] + v[r];
+                t.to[z][at] = m;
+                v[r] = u.nesterov ? v[r] + u.mu * m : m;
+              }
+            }
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum += (double)v[r] * (double)v[r];
+      x[s][tau] = v;
     }
-    s += (double)u * (double)u;
+  sum = wave_sum(sum);
+  if (lane == 0) squares[wave] = sum;
+  __syncthreads();
+  sum = 0.0;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) sum += squares[w];
+  const double inv = 1.0 / (sqrt(sum) + (double)u.eps);
+#pragma unroll
+  for (int s = 0; s < S; ++s)
+#pragma unroll
+    for (int tau = 0; tau < MT; ++tau)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[s][tau][r] = (float)((double)x[s][tau][r] * inv);
+
+  const int br = wave / COLS * BR, bc = wave % COLS * BC;  // the wave's block of P's tiles
+  const bool tiles = br < MT;
+  for (int k = 0; k < steps.count; ++k) {
+    const float sx = power(steps.x[k]), sp = power(steps.p[k]), sb = power(steps.b[k]);
+    h4 hi[S][MT], lo[S][MT];
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int tau = 0; tau < MT; ++tau) {
+        split(x[s][tau], sx, hi[s][tau], lo[s][tau]);
+        const int j = (wave + 8 * s) * 16 + c;
+        if ((wave + 8 * s) * 16 < d.np) {
+          *(h4*)(xh + j * SX + tau * 16 + 4 * g) = hi[s][tau];
+          *(h4*)(xl + j * SX + tau * 16 + 4 * g) = lo[s][tau];
+        }
+      }
+    __syncthreads();
+    // P = X X^T
+    v4f p[BR][BC] = {};
+    if (tiles)
+      for (int j = 0; j < d.np; j += 32) {
+        const int row = (j + 8 * g + (c >> 2)) * SX + 4 * (c & 3);
+        h8 ah[BR], al[BR];
+#pragma unroll
+        for (int a = 0; a < BR; ++a) {
+          const int at = row + (br + a) * 16;
+          ah[a] = both(read_transposed(xh + at), read_transposed(xh + at + 4 * SX));
+          al[a] = both(read_transposed(xl + at), read_transposed(xl + at + 4 * SX));
+        }
+#pragma unroll
+        for (int b = 0; b < BC; ++b) {
+          const int at = row + (bc + b) * 16;
+          const h8 bh = both(read_transposed(xh + at), read_transposed(xh + at + 4 * SX));
+          const h8 bl = both(read_transposed(xl + at), read_transposed(xl + at + 4 * SX));
+#pragma unroll
+          for (int a = 0; a < BR; ++a) p[a][b] = product(ah[a], al[a], bh, bl, p[a][b]);
+        }
+      }
+    auto store = [&](const v4f(&m)[BR][BC], float scale) {
+#pragma unroll
+      for (int a = 0; a < BR; ++a)
+#pragma unroll
+        for (int b = 0; b < BC; ++b) {
+          h4 h, l;
+          split(m[a][b], scale, h, l);
+          const int at = ((bc + b) * 16 + c) * SP + ((br + a) >> 1) * 32 + 8 * g + ((br + a) & 1) * 4;
+          *(h4*)(ph + at) = h, *(h4*)(pl + at) = l;
+        }
+    };
+    if (tiles) {
+      const float off = power(-2 * steps.x[k]);
+#pragma unroll
+      for (int a = 0; a < BR; ++a)
+#pragma unroll
+        for (int b = 0; b < BC; ++b) p[a][b] *= off;
+      store(p, sp);
+    }
+    __syncthreads();
+    // B = b P + c P^2
+    v4f q[BR][BC] = {};
+    if (tiles)
+#pragma unroll
+      for (int kb = 0; kb < MP; kb += 32) {
+        h8 ah[BR], al[BR];
+#pragma unroll
+        for (int a = 0; a < BR; ++a) {
+          const int at = ((br + a) * 16 + c) * SP + kb + 8 * g;
+          ah[a] = *(const h8*)(ph + at), al[a] = *(const h8*)(pl + at);
+        }
+#pragma unroll
+        for (int b = 0; b < BC; ++b) {
+          const int at = ((bc + b) * 16 + c) * SP + kb + 8 * g;
+          const h8 bh = *(const h8*)(ph + at), bl = *(const h8*)(pl + at);
+#pragma unroll
+          for (int a = 0; a < BR; ++a) q[a][b] = product(ah[a], al[a], bh, bl, q[a][b]);
+        }
+      }
+    __syncthreads();
+    if (tiles) {
+      const float by = steps.coef[k][1], cy = steps.coef[k][2] * power(-2 * steps.p[k]);
+#pragma unroll
+      for (int a = 0; a < BR; ++a)
+#pragma unroll
+        for (int b = 0; b < BC; ++b) q[a][b] = by * p[a][b] + cy * q[a][b];
+      store(q, sb);
+    }
+    __syncthreads();
+    // X <- a X + B X
+    const float off = power(-steps.b[k] - steps.x[k]);
+    if (wave * 16 < d.np)
+#pragma unroll
+      for (int tau = 0; tau < MT; ++tau) {
+        v4f y[S] = {};
+#pragma unroll
+        for (int kb = 0; kb < MT / 2; ++kb) {
+          const int at = (tau * 16 + c) * SP + kb * 32 + 8 * g;
+          const h8 ah = *(const h8*)(ph + at), al = *(const h8*)(pl + at);
+#pragma unroll
+          for (int s = 0; s < S; ++s)
+            y[s] = product(ah, al, both(hi[s][2 * kb], hi[s][2 * kb + 1]), both(lo[s][2 * kb], lo[s][2 * kb + 1]), y[s]);
+        }
+#pragma unroll
+        for (int s = 0; s < S; ++s) x[s][tau] = steps.coef[k][0] * x[s][tau] + off * y[s];
+      }
   }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+  for (int s = 0; s < S; ++s)
+#pragma unroll
+    for (int tau = 0; tau < MT; ++tau) {
+      const int j = (wave + 8 * s) * 16 + c, i = tau * 16 + 4 * g;
+      if (j >= d.n || i >= d.m) continue;
+      const v4f v = u.scale * x[s][tau];
+      if (d.turned) {
+        const int64_t at = (int64_t)j * d.cols + i;
+        puts<T>(e.out[z], at, d.m - i, e.w[z] ? v + u.decay * values<T>(e.w[z], at, d.m - i) : v);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (i + r < d.m) {
+            const int64_t at = (int64_t)(i + r) * d.cols + j;
+            put<T>(e.out[z], at, e.w[z] ? v[r] + u.decay * value<T>(e.w[z], at) : v[r]);
+          }
+      }
+    }
+}
+
+// ------------------------------------------------------------------ larger matrices
+// The momentum, and the sum of the update's squares in float64, in which none of them overflows
+template <typename T>
+__global__ __launch_bounds__(256) void k_ortho_norm(Table t, int64_t size, int parts, Update u, double* __restrict__ part) {
+  const int z = blockIdx.y;
+  double s = 0.0;
+#pragma unroll 2
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size; i += (int64_t)parts * 1024) {
+    const int have = (int)min(size - i, (int64_t)4);
+    v4f v = values<T>(t.g[z], i, have);
+    if (t.m[z]) {
+      const v4f m = values<float>(t.m[z], i, have) * u.mu + v;
+      puts<float>(t.to[z], i, have, m);
+      v = u.nesterov ? v + u.mu * m : m;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s += (double)v[k] * (double)v[k];
+  }
+  s = wave_sum(s);
   __shared__ double w[4];
   if ((threadIdx.x & 63) == 0) w[threadIdx.x >> 6] = s;
   __syncthreads();
   if (threadIdx.x == 0) part[(int64_t)z * parts + blockIdx.x] = w[0] + w[1] + w[2] + w[3];
 }
 
-// X = U / (|U| + eps), in float [mp][np] and split, as it stands and transposed [np][mp]: a tile of 64 x 64 a workgroup
+// Y = (U / (|U| + eps))^T, in float [np][mp] and split: a tile of 64 x 64 a workgroup
 template <typename T>
-__global__ __launch_bounds__(256) void k_ortho_start(Table t, Sizes d, int parts, float mu, bool nesterov, float eps,
-                                                     float scale, const double* __restrict__ part, float* __restrict__ x,
-                                                     _Float16* __restrict__ xs, _Float16* __restrict__ xt) {
+__global__ __launch_bounds__(256) void k_ortho_start(Table t, Sizes d, int parts, Update u, float scale,
+                                                     const double* __restrict__ part, float* __restrict__ y,
+                                                     _Float16* __restrict__ ys) {
   __shared__ float tile[64][65];
   const int z = blockIdx.z, i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
   double norm = 0.0;
-  for (int k = 0; k < parts; ++k) norm += part[(int64_t)z * parts + k];
-  norm = sqrt(norm) + (double)eps;
-  const int a = threadIdx.x & 63, b = threadIdx.x >> 6;
-#pragma unroll 4
-  for (int k = b; k < 64; k += 4) {
-    // neighbouring lanes read neighbouring values of the caller's rows
-    const int i = d.turned ? i0 + a : i0 + k, j = d.turned ? j0 + k : j0 + a;
-    float u = 0.0f;
-    if (i < d.m && j < d.n) {
-      const int64_t at = d.turned ? (int64_t)j * d.cols + i : (int64_t)i * d.cols + j;
-      u = value<T>(t.g[z], at);
-      if (t.m[z]) u = nesterov ? u + mu * t.to[z][at] : t.to[z][at];
-      u = (float)((double)u / norm);
+  for (int k = threadIdx.x & 63; k < parts; k += 64) norm += part[(int64_t)z * parts + k];
+  const double inv = 1.0 / (sqrt(wave_sum(norm)) + (double)u.eps);
+  const int a = (threadIdx.x & 15) * 4, b = threadIdx.x >> 4;
+  // four neighbours of the caller's matrix, of which `have` are there
+  auto read = [&](int64_t at, int have) {
+    v4f v = values<T>(t.g[z], at, have);
+    if (t.m[z]) {
+      const v4f m = values<float>(t.to[z], at, have);
+      v = u.nesterov ? v + u.mu * m : m;
     }
-    tile[i - i0][j - j0] = u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = (float)((double)v[k] * inv);
+    return v;
+  };
+  v4f v[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int r = q * 16 + b;
+    v[q] = v4f{};
+    if (d.turned) {
+      if (j0 + r < d.n && i0 + a < d.m) v[q] = read((int64_t)(j0 + r) * d.cols + i0 + a, d.m - i0 - a);
+    } else if (i0 + r < d.m && j0 + a < d.n) {
+      v[q] = read((int64_t)(i0 + r) * d.cols + j0 + a, d.n - j0 - a);
+    }
   }
-  __syncthreads();
-  x += (int64_t)z * d.mp * d.np, xs += (int64_t)z * d.mp * d.np * 2, xt += (int64_t)z * d.mp * d.np * 2;
-#pragma unroll 4
-  for (int k = b; k < 64; k += 4) {
-    const float u = tile[k][a], v = tile[a][k];
-    _Float16 hi, lo;
-    x[(int64_t)(i0 + k) * d.np + j0 + a] = u;
-    split(u, scale, hi, lo);
-    xs[split_at(i0 + k, d.np, j0 + a, 0)] = hi, xs[split_at(i0 + k, d.np, j0 + a, 1)] = lo;
-    split(v, scale, hi, lo);
-    xt[split_at(j0 + k, d.mp, i0 + a, 0)] = hi, xt[split_at(j0 + k, d.mp, i0 + a, 1)] = lo;
+  if (!d.turned) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) tile[q * 16 + b][a + k] = v[q][k];
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[q][k] = tile[a + k][q * 16 + b];
+  }
+  y += (int64_t)z * d.mp * d.np, ys += (int64_t)z * d.mp * d.np * 2;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int64_t j = j0 + q * 16 + b;
+    h4 hi, lo;
+    split(v[q], scale, hi, lo);
+    *(v4f*)(y + j * d.mp + i0 + a) = v[q];
+    *(h4*)(ys + split_at(j, d.mp, i0 + a, 0)) = hi;
+    *(h4*)(ys + split_at(j, d.mp, i0 + a, 1)) = lo;
   }
 }
 
-__device__ __forceinline__ v4f mfma(h8 a, h8 b, v4f c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
-
-enum { GRAM, POLY, APPLY };
+enum { GRAM, POLY, APPLY, LAST };
 struct Product {
-  const _Float16 *p, *q;  // [rows][ld] split, the product's rows and columns
-  int64_t sp, sq;         // values from one matrix to the next
-  int ld, tiles;          // tiles of a row of the result
+  const _Float16 *p, *q;  // split matrices: rows of the product's rows and columns (GRAM: of its sums), ld values each
+  int64_t sp, sq;         // from one matrix to the next
+  int ld, steps;          // of kStep
+  int tiles, count;       // tiles of a matrix's result, matrices
   float unscale;          // of the sums
-  // GRAM: P split with `scale`; POLY: b P + c P^2 split with `scale`, P with `old`
-  float b, c, old, scale;
-  const _Float16* pin;
-  _Float16* out;
-  // APPLY: X <- a X + sums in float, split with `scale` as it stands and transposed
-  float a;
-  float* x;
-  _Float16 *xs, *xt;
+  float a, b, c, old, scale;
+  _Float16* out;          // GRAM: P; POLY: B = b P + c P^2, P (p) scaled with `old`; APPLY: Y, all split with `scale`
+  float* y;               // APPLY: Y <- a Y + sums;  LAST: the same, to the caller's matrices
   int mp, np;
 };
 
-// One tile of 64 x 64 of  sum_k p[i][k] q[j][k]: four waves of 32 x 32, two buffers of a step in the LDS.  GRAM and POLY are
-// symmetric: the tiles on and below the diagonal, each written at both its places
-template <int KIND>
-__global__ __launch_bounds__(256) void k_ortho_product(Product g) {
-  __shared__ __align__(16) _Float16 lds[2][2][kTile * 72];  // rows of 128 bytes, 16 apart in the banks
+// One tile of TILE x TILE of  sum_k p[i][k] q[j][k]  (GRAM: p[k][i] q[k][j]) by four waves of a quarter each, with two buffers of a
+// step in the LDS: while a step's products run, the next step's values are on their way there without passing registers.
+// GRAM and POLY are symmetric: the tiles on and below the diagonal, each written at both its places.  A lane has four neighbouring
+// rows i of a column j, which are neighbours in memory at row j of Y, and of the symmetric P and B.
+//
+// In the LDS a row of 128 bytes (GRAM: of 4 TILE bytes) has its 16 bytes at position c ^ row % 8 (its 32 bytes at c ^ a number
+// of the row): lanes that read together meet different banks, and the loads, which write 64 x 16 bytes in
+// their order, read the places that belong there
+template <int KIND, int TILE, typename T>
+__global__ __launch_bounds__(256) void k_ortho_product(Product g, Ends e, Sizes d, Update u) {
+  constexpr int F = TILE / 32, HALF = TILE / 2;
+  __shared__ __align__(16) _Float16 lds[2][2][TILE * 64];
+  // neighbouring workgroups lie on different dies: each die takes a stretch of neighbouring tiles, which share rows in its L2
+  const int all = g.tiles * g.count, each = (all + 7) >> 3, at_ = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
+  if (at_ >= all) return;
+  const int z = at_ / g.tiles, tile = at_ % g.tiles;
   int ti, tj;
-  if (KIND == APPLY) {
-    ti = blockIdx.x / g.tiles, tj = blockIdx.x % g.tiles;
+  if (KIND >= APPLY) {
+    ti = tile % (g.mp / TILE), tj = tile / (g.mp / TILE);
   } else {  // the number of the tile among those of the triangle
-    ti = (int)((sqrtf(8.0f * (float)blockIdx.x + 1.0f) - 1.0f) * 0.5f);
-    while (ti * (ti + 1) / 2 > (int)blockIdx.x) --ti;
-    while ((ti + 1) * (ti + 2) / 2 <= (int)blockIdx.x) ++ti;
-    tj = (int)blockIdx.x - ti * (ti + 1) / 2;
+    ti = (int)((sqrtf(8.0f * (float)tile + 1.0f) - 1.0f) * 0.5f);
+    while (ti * (ti + 1) / 2 > tile) --ti;
+    while ((ti + 1) * (ti + 2) / 2 <= tile) ++ti;
+    tj = tile - ti * (ti + 1) / 2;
   }
-  const int z = blockIdx.y, i0 = ti * kTile, j0 = tj * kTile;
-  const _Float16 *p = g.p + z * g.sp + (int64_t)i0 * 2 * g.ld, *q = g.q + z * g.sq + (int64_t)j0 * 2 * g.ld;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = (wave >> 1) * 32, wj = (wave & 1) * 32;
-  v4f acc[2][2] = {};
-  // 64 rows of 128 bytes of each operand: four threads a row, 32 bytes each
-  const int lr = threadIdx.x >> 2, lc = (threadIdx.x & 3) * 16;
-  h8 rp[2], rq[2];
+  const int i0 = ti * TILE, j0 = tj * TILE;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = (wave >> 1) * HALF, wj = (wave & 1) * HALF;
+  const int lg = lane >> 4, lc = lane & 15;
+  // where this lane's 16 bytes of each load come from, and how far a step is
+  int64_t from[F];
+  const int64_t step = KIND == GRAM ? (int64_t)kStep * 2 * g.ld : 2 * kStep;
+#pragma unroll
+  for (int n = 0; n < F; ++n) {
+    const int chunk = (wave * F + n) * 64 + lane;
+    if (KIND == GRAM) {
+      constexpr int PER = TILE / 4;  // of a row
+      const int k = chunk / PER, to = chunk % PER, h = (k & 3) | (k >> 3 & 1) << 2;
+      from[n] = (int64_t)k * 2 * g.ld + (((to >> 1) ^ h) * 2 + (to & 1)) * 8;
+    } else {
+      const int r = chunk >> 3;
+      from[n] = (int64_t)r * 2 * g.ld + ((chunk & 7) ^ (r & 7)) * 8;
+    }
+  }
+  const _Float16 *p = g.p + z * g.sp + (KIND == GRAM ? 2 * i0 : (int64_t)i0 * 2 * g.ld);
+  const _Float16 *q = g.q + z * g.sq + (KIND == GRAM ? 2 * j0 : (int64_t)j0 * 2 * g.ld);
   auto fetch = [&](int s) {
-    const int64_t at = (int64_t)lr * 2 * g.ld + s * 64 + lc;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) rp[u] = *(const h8*)(p + at + u * 8), rq[u] = *(const h8*)(q + at + u * 8);
-  };
-  auto put = [&](int buf) {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      *(h8*)(&lds[buf][0][lr * 72 + lc + u * 8]) = rp[u];
-      *(h8*)(&lds[buf][1][lr * 72 + lc + u * 8]) = rq[u];
+    for (int n = 0; n < F; ++n) {
+      const int to = __builtin_amdgcn_readfirstlane((wave * F + n) * 512);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + s * step + from[n]),
+                                       (__attribute__((address_space(3))) void*)(&lds[s & 1][0][to]), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(q + s * step + from[n]),
+                                       (__attribute__((address_space(3))) void*)(&lds[s & 1][1][to]), 16, 0, 0);
     }
   };
-  const int steps = g.ld / kStep;
+  // 16 of the tile's rows from `row` on, part 0 (hi) or 1 (lo), as an operand
+  auto operand = [&](const _Float16* l, int row, int part) {
+    if constexpr (KIND == GRAM) {
+      const int h = (lc >> 2) | (lg & 1) << 2, pair = (row >> 5) * 4 + part * 2 + (row >> 4 & 1);
+      const _Float16* a = l + (8 * lg + (lc >> 2)) * (2 * TILE) + (pair ^ h) * 16 + 4 * (lc & 3);
+      return both(read_transposed(a), read_transposed(a + 4 * 2 * TILE));
+    } else {
+      return *(const h8*)(l + (row + lc) * 64 + ((part * 4 + lg) ^ (lc & 7)) * 8);
+    }
+  };
+  v4f acc[F][F] = {};
   fetch(0);
-  put(0);
-  for (int s = 0; s < steps; ++s) {
-    __syncthreads();
-    if (s + 1 < steps) fetch(s + 1);
+  for (int s = 0; s < g.steps; ++s) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();  // this step's values are there, and the other buffer's have been read
     const _Float16 *lp = lds[s & 1][0], *lq = lds[s & 1][1];
-    h8 ph[2], pl[2], qh[2], ql[2];
-    const int r = lane & 15, k = (lane >> 4) * 8;
+    h8 ph[F], pl[F], qh[F], ql[F];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      ph[u] = *(const h8*)(lp + (wi + u * 16 + r) * 72 + k), pl[u] = *(const h8*)(lp + (wi + u * 16 + r) * 72 + 32 + k);
-      qh[u] = *(const h8*)(lq + (wj + u * 16 + r) * 72 + k), ql[u] = *(const h8*)(lq + (wj + u * 16 + r) * 72 + 32 + k);
+    for (int a = 0; a < F; ++a) {
+      ph[a] = operand(lp, wi + a * 16, 0), pl[a] = operand(lp, wi + a * 16, 1);
+      qh[a] = operand(lq, wj + a * 16, 0), ql[a] = operand(lq, wj + a * 16, 1);
     }
+    if (s + 1 < g.steps) fetch(s + 1);
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int a = 0; a < F; ++a)
 #pragma unroll
-      for (int v = 0; v < 2; ++v) {
-        acc[u][v] = mfma(pl[u], qh[v], acc[u][v]);
-        acc[u][v] = mfma(ph[u], ql[v], acc[u][v]);
-        acc[u][v] = mfma(ph[u], qh[v], acc[u][v]);
-      }
-    if (s + 1 < steps) put((s + 1) & 1);
+      for (int b = 0; b < F; ++b) acc[a][b] = product(ph[a], pl[a], qh[b], ql[b], acc[a][b]);
   }
-  // a lane holds rows 4 (lane / 16) .. + 3 of column lane % 16
 #pragma unroll
-  for (int u = 0; u < 2; ++u)
+  for (int a = 0; a < F; ++a)
 #pragma unroll
-    for (int v = 0; v < 2; ++v) {
-      const int i = i0 + wi + u * 16 + (lane >> 4) * 4, j = j0 + wj + v * 16 + (lane & 15);
-      h4 hi, lo;
+    for (int b = 0; b < F; ++b) {
+      const int i = i0 + wi + a * 16 + lg * 4, j = j0 + wj + b * 16 + lc;
+      v4f s = acc[a][b] * g.unscale;
+      if constexpr (KIND == POLY) {
+        const _Float16* in = g.p + z * g.sp;
+        const h4 hi = *(const h4*)(in + split_at(j, g.mp, i, 0)), lo = *(const h4*)(in + split_at(j, g.mp, i, 1));
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        float s = acc[u][v][k] * g.unscale;
-        if constexpr (KIND == POLY) {
-          const _Float16* in = g.pin + z * g.sp;
-          s = g.b * (((float)in[split_at(i + k, g.ld, j, 0)] + (float)in[split_at(i + k, g.ld, j, 1)]) * g.old) + g.c * s;
-        }
-        if constexpr (KIND == APPLY) {
-          float* at = g.x + ((int64_t)z * g.mp + i + k) * g.np + j;
-          s += g.a * *at;
-          *at = s;
-        }
-        _Float16 h, l;
-        split(s, g.scale, h, l);
-        hi[k] = h, lo[k] = l;
-        _Float16* out = KIND == APPLY ? g.xs + (int64_t)z * g.mp * g.np * 2 : g.out + (int64_t)z * g.mp * g.mp * 2;
-        const int ld = KIND == APPLY ? g.np : g.mp;
-        out[split_at(i + k, ld, j, 0)] = h, out[split_at(i + k, ld, j, 1)] = l;
+        for (int k = 0; k < 4; ++k) s[k] = g.b * (((float)hi[k] + (float)lo[k]) * g.old) + g.c * s[k];
       }
-      if (KIND == APPLY || ti != tj) {
-        _Float16* out = KIND == APPLY ? g.xt + (int64_t)z * g.mp * g.np * 2 : g.out + (int64_t)z * g.mp * g.mp * 2;
+      if constexpr (KIND >= APPLY) {
+        v4f* y = (v4f*)(g.y + ((int64_t)z * g.np + j) * g.mp + i);
+        s += g.a * *y;
+        if constexpr (KIND == APPLY) *y = s;
+      }
+      if constexpr (KIND == LAST) {
+        if (j >= d.n || i >= d.m) continue;
+        s *= u.scale;
+        if (d.turned) {
+          const int64_t at = (int64_t)j * d.cols + i;
+          puts<T>(e.out[z], at, d.m - i, e.w[z] ? s + u.decay * values<T>(e.w[z], at, d.m - i) : s);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (i + k < d.m) {
+              const int64_t at = (int64_t)(i + k) * d.cols + j;
+              put<T>(e.out[z], at, e.w[z] ? s[k] + u.decay * value<T>(e.w[z], at) : s[k]);
+            }
+        }
+      } else {
+        h4 hi, lo;
+        split(s, g.scale, hi, lo);
+        _Float16* out = g.out + (int64_t)z * (KIND == APPLY ? g.np : g.mp) * g.mp * 2;
         *(h4*)(out + split_at(j, g.mp, i, 0)) = hi, *(h4*)(out + split_at(j, g.mp, i, 1)) = lo;
+        if (KIND != APPLY && ti != tj) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            out[split_at(i + k, g.mp, j, 0)] = hi[k], out[split_at(i + k, g.mp, j, 1)] = lo[k];
+        }
       }
     }
 }
 
-// W' = decay W + scale X
+// no steps: out = decay W + scale X from Y
 template <typename T>
-__global__ __launch_bounds__(256) void k_ortho_end(Ends t, Sizes d, float scale, float decay, const float* __restrict__ x) {
-  __shared__ float tile[64][65];
-  const int z = blockIdx.z, i0 = blockIdx.y * 64, j0 = blockIdx.x * 64, a = threadIdx.x & 63, b = threadIdx.x >> 6;
-  x += (int64_t)z * d.mp * d.np;
-#pragma unroll 4
-  for (int k = b; k < 64; k += 4) tile[k][a] = x[(int64_t)(i0 + k) * d.np + j0 + a];
-  __syncthreads();
-#pragma unroll 4
-  for (int k = b; k < 64; k += 4) {
-    const int i = d.turned ? i0 + a : i0 + k, j = d.turned ? j0 + k : j0 + a;
-    if (i >= d.m || j >= d.n) continue;
-    const int64_t at = d.turned ? (int64_t)j * d.cols + i : (int64_t)i * d.cols + j;
-    float f[1] = {scale * tile[i - i0][j - j0]};
-    if (t.w[z]) f[0] += decay * value<T>(t.w[z], at);
-    typename Raw<T, 1>::type v;
-    join(f, v);
-    Raw<T, 1>::store((char*)((T*)t.out[z] + at), v);
+__global__ __launch_bounds__(256) void k_ortho_end(Ends e, Sizes d, Update u, const float* __restrict__ y) {
+  const int z = blockIdx.y;
+  const int64_t size = (int64_t)d.m * d.n;
+  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < size; at += (int64_t)gridDim.x * 256) {
+    const int r = (int)(at / d.cols), c = (int)(at % d.cols), i = d.turned ? c : r, j = d.turned ? r : c;
+    const float v = u.scale * y[((int64_t)z * d.np + j) * d.mp + i];
+    put<T>(e.out[z], at, e.w[z] ? v + u.decay * value<T>(e.w[z], at) : v);
   }
 }
 
-Sizes sizes_of(int rows, int cols) {
+// The rows that k_ortho_small is made for, 0 where a matrix does not fit a workgroup, and its strips of a wave
+int small_rows(int m) { return m <= 32 ? 32 : m <= 64 ? 64 : m <= 96 ? 96 : m <= 128 ? 128 : 0; }
+constexpr size_t kLds = 160 * 1024 - 1024;
+size_t small_bytes(int mp, int np) {
+  return mp == 32 ? Rows<32>::bytes(np) : mp == 64 ? Rows<64>::bytes(np) : mp == 96 ? Rows<96>::bytes(np) : Rows<128>::bytes(np);
+}
+
+Sizes sizes_of(int rows, int cols, int count, bool* small, int* tile) {
   Sizes d{};
   d.rows = rows, d.cols = cols, d.turned = rows > cols;
   d.m = d.turned ? cols : rows, d.n = d.turned ? rows : cols;
-  d.mp = (d.m + kTile - 1) / kTile * kTile, d.np = (d.n + kTile - 1) / kTile * kTile;
+  d.mp = small_rows(d.m), d.np = (d.n + 31) / 32 * 32;
+  *small = d.mp && d.np <= 512 && small_bytes(d.mp, d.np) <= kLds;
+  if (*small) return d;
+  // tiles of 128, each value of which is read from the LDS half as often, where they fill the GPU
+  const int64_t big = (int64_t)((d.m + 127) / 128) * ((d.n + 127) / 128);
+  *tile = big * (count < kTable ? count : kTable) >= 512 ? 128 : 64;
+  d.mp = (d.m + *tile - 1) / *tile * *tile, d.np = (d.n + *tile - 1) / *tile * *tile;
   return d;
 }
 struct Layout {
-  size_t part, x, xs, xt[2], p, q, total;
+  size_t part, y, ys[2], p, b, total;
 };
 Layout layout_of(const Sizes& d, int count) {
   Layout l{};
@@ -279,9 +598,17 @@ Layout layout_of(const Sizes& d, int count) {
   };
   const size_t all = 4 * (size_t)d.mp * d.np * count, square = 4 * (size_t)d.mp * d.mp * count;
   l.part = take(sizeof(double) * kParts * (size_t)count);
-  l.x = take(all), l.xs = take(all), l.xt[0] = take(all), l.xt[1] = take(all), l.p = take(square), l.q = take(square);
+  l.y = take(all), l.ys[0] = take(all), l.ys[1] = take(all), l.p = take(square), l.b = take(square);
   l.total = at;
   return l;
+}
+
+// matrices at a time: as many as a launch's arguments hold, and 1 GB of workspace
+int batch_of(const Sizes& d, int count) {
+  const double each = 12.0 * d.mp * d.np + 8.0 * d.mp * d.mp;
+  int b = each * kTable > 0x1p30 ? (int)(0x1p30 / each) : kTable;
+  if (b < 1) b = 1;
+  return count < b ? count : b;
 }
 
 }  // namespace
@@ -323,32 +650,123 @@ bool ortho_bounds(int steps, const float* coef, int* x_exp, int* a_exp, int* b_e
   return true;
 }
 
-int ortho_batch(int rows, int cols, int count) {
-  const Sizes d = sizes_of(rows, cols);
-  const double each = 16.0 * d.mp * d.np + 8.0 * d.mp * d.mp;
-  int b = each * kTable > 0x1p30 ? (int)(0x1p30 / each) : kTable;
-  if (b < 1) b = 1;
-  return count < b ? count : b;
+size_t ortho_workspace(int rows, int cols, int count) {
+  bool small;
+  int tile;
+  const Sizes d = sizes_of(rows, cols, count, &small, &tile);
+  return small ? 0 : layout_of(d, batch_of(d, count)).total;
 }
 
-size_t ortho_workspace(int rows, int cols, int count) {
-  return layout_of(sizes_of(rows, cols), ortho_batch(rows, cols, count)).total;
+namespace {
+
+// an attribute of the kernel, not of a stream: allowed while one is captured
+template <typename K>
+hipError_t allow_lds(K kernel, size_t bytes) {
+  return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
+
+template <typename TG, typename T>
+hipError_t launch_small(const Table& t, const Ends& e, const Steps& steps, const Sizes& d, const Update& u, int count,
+                        hipStream_t st) {
+  const int strips = (d.np + 127) / 128;
+  const size_t bytes = small_bytes(d.mp, d.np);
+#define E2F_ORTHO(MP, S)                                                                             \
+  do {                                                                                               \
+    const hipError_t err = allow_lds(k_ortho_small<MP, S, TG, T>, bytes);                            \
+    if (err != hipSuccess) return err;                                                               \
+    k_ortho_small<MP, S, TG, T><<<count, 512, bytes, st>>>(t, e, steps, d, u);                       \
+  } while (0)
+  if (d.mp == 128)
+    E2F_ORTHO(128, 1);
+  else if (d.mp == 96 && strips == 1)
+    E2F_ORTHO(96, 1);
+  else if (d.mp == 96)
+    E2F_ORTHO(96, 2);
+  else if (d.mp == 64 && strips == 1)
+    E2F_ORTHO(64, 1);
+  else if (d.mp == 64 && strips == 2)
+    E2F_ORTHO(64, 2);
+  else if (d.mp == 64)
+    E2F_ORTHO(64, 4);
+  else if (strips == 1)
+    E2F_ORTHO(32, 1);
+  else if (strips == 2)
+    E2F_ORTHO(32, 2);
+  else
+    E2F_ORTHO(32, 4);
+#undef E2F_ORTHO
+  return hipGetLastError();
+}
+
+template <int KIND, typename T>
+void launch_product(int tile, Product g, const Ends& e, const Sizes& d, const Update& u, hipStream_t st) {
+  const int mt = g.mp / tile;
+  g.tiles = KIND >= APPLY ? mt * (g.np / tile) : mt * (mt + 1) / 2;
+  const unsigned blocks = (unsigned)((g.tiles * g.count + 7) / 8 * 8);
+  if (tile == 128)
+    k_ortho_product<KIND, 128, T><<<blocks, 256, 0, st>>>(g, e, d, u);
+  else
+    k_ortho_product<KIND, 64, T><<<blocks, 256, 0, st>>>(g, e, d, u);
+}
+
+template <typename TG, typename T>
+hipError_t launch_large(const Table& t, const Ends& e, const Steps& steps, const Sizes& d, const Update& u, int tile,
+                        int count, const Layout& l, char* ws, hipStream_t st) {
+  double* part = (double*)(ws + l.part);
+  float* y = (float*)(ws + l.y);
+  _Float16 *ys[2] = {(_Float16*)(ws + l.ys[0]), (_Float16*)(ws + l.ys[1])}, *p = (_Float16*)(ws + l.p), *b = (_Float16*)(ws + l.b);
+  const int64_t size = (int64_t)d.rows * d.cols;
+  int64_t parts = (size + 8191) / 8192;
+  if (parts > kParts) parts = kParts;
+  k_ortho_norm<TG><<<dim3((unsigned)parts, count), 256, 0, st>>>(t, size, (int)parts, u, part);
+  k_ortho_start<TG><<<dim3(d.np / 64, d.mp / 64, count), 256, 0, st>>>(t, d, (int)parts, u, ldexpf(1.0f, steps.x[0]), part,
+                                                                       y, ys[0]);
+  const int mt = d.mp / 128;
+  // (the triangle's tiles are fewer: tiles of 64 until 128 fill the GPU too)
+  const int tri = tile == 128 && (int64_t)mt * (mt + 1) / 2 * count >= 512 ? 128 : 64;
+  for (int k = 0; k < steps.count; ++k) {
+    const int xe = steps.x[k], pe = steps.p[k], be = steps.b[k];
+    Product g{};
+    g.mp = d.mp, g.np = d.np, g.count = count, g.y = y, g.ld = d.mp;
+    g.a = steps.coef[k][0], g.b = steps.coef[k][1], g.c = steps.coef[k][2];
+    const int64_t all = 2 * (int64_t)d.mp * d.np, square = 2 * (int64_t)d.mp * d.mp;
+    Product poly = g, apply = g;
+    g.p = g.q = ys[k & 1], g.sp = g.sq = all, g.steps = d.np / kStep, g.out = p;
+    g.unscale = ldexpf(1.0f, -2 * xe), g.scale = ldexpf(1.0f, pe);
+    poly.p = poly.q = p, poly.sp = poly.sq = square, poly.steps = d.mp / kStep, poly.out = b;
+    poly.unscale = ldexpf(1.0f, -2 * pe), poly.old = ldexpf(1.0f, -pe), poly.scale = ldexpf(1.0f, be);
+    apply.p = b, apply.sp = square, apply.q = ys[k & 1], apply.sq = all, apply.steps = d.mp / kStep, apply.out = ys[~k & 1];
+    apply.unscale = ldexpf(1.0f, -be - xe), apply.scale = ldexpf(1.0f, steps.x[k + 1]);
+    launch_product<GRAM, float>(tri, g, Ends{}, d, u, st);
+    launch_product<POLY, float>(tri, poly, Ends{}, d, u, st);
+    if (k + 1 < steps.count)
+      launch_product<APPLY, float>(tile, apply, Ends{}, d, u, st);
+    else
+      launch_product<LAST, T>(tile, apply, e, d, u, st);
+  }
+  if (steps.count == 0) k_ortho_end<T><<<dim3((unsigned)((size + 1023) / 1024), count), 256, 0, st>>>(e, d, u, y);
+  return hipGetLastError();
+}
+
+}  // namespace
 
 hipError_t launch_orthogonalize(const OrthoArgs& a, void* workspace, hipStream_t st) {
-  const Sizes d = sizes_of(a.rows, a.cols);
-  const int batch = ortho_batch(a.rows, a.cols, a.count);
-  const Layout l = layout_of(d, batch);
-  char* ws = (char*)workspace;
-  double* part = (double*)(ws + l.part);
-  float* x = (float*)(ws + l.x);
-  _Float16 *xs = (_Float16*)(ws + l.xs), *xt[2] = {(_Float16*)(ws + l.xt[0]), (_Float16*)(ws + l.xt[1])},
-           *p = (_Float16*)(ws + l.p), *q = (_Float16*)(ws + l.q);
-  int xe[kOrthoMaxSteps + 1], ae[kOrthoMaxSteps], be[kOrthoMaxSteps];
-  if (!ortho_bounds(a.steps, a.coef, xe, ae, be)) return hipErrorInvalidValue;
-  const int64_t size = (int64_t)a.rows * a.cols;
-  int parts = (int)((size + 4095) / 4096);
-  if (parts > kParts) parts = kParts;
+  bool small;
+  int tile = 0;
+  const Sizes d = sizes_of(a.rows, a.cols, a.count, &small, &tile);
+  const int batch = small ? kTable : batch_of(d, a.count);
+  const Layout l = small ? Layout{} : layout_of(d, batch);
+  Steps steps{};
+  int xe[kOrthoMaxSteps + 1], pe[kOrthoMaxSteps], be[kOrthoMaxSteps];
+  if (!ortho_bounds(a.steps, a.coef, xe, pe, be)) return hipErrorInvalidValue;
+  steps.count = a.steps;
+  for (int k = 0; k <= a.steps; ++k) {
+    steps.x[k] = (signed char)xe[k];
+    if (k == a.steps) break;
+    steps.p[k] = (signed char)pe[k], steps.b[k] = (signed char)be[k];
+    for (int c = 0; c < 3; ++c) steps.coef[k][c] = a.coef[3 * k + c];
+  }
+  const Update u{a.mu, a.eps, a.scale, a.decay, a.nesterov};
   for (int first = 0; first < a.count; first += batch) {
     const int count = a.count - first < batch ? a.count - first : batch;
     Table t{};
@@ -357,41 +775,17 @@ hipError_t launch_orthogonalize(const OrthoArgs& a, void* workspace, hipStream_t
       t.g[k] = a.grads[first + k];
       t.m[k] = a.moments ? a.moments[first + k] : nullptr;
       t.to[k] = a.moments ? a.news[first + k] : nullptr;
-      e.w[k] = a.weights && a.decay != 0.0f ? a.weights[first + k] : nullptr;
+      e.w[k] = a.weights ? a.weights[first + k] : nullptr;
       e.out[k] = a.outs[first + k];
     }
-    const dim3 tiles(d.np / 64, d.mp / 64, count);
-    const float s0 = ldexpf(1.0f, xe[0]);
-    if (a.grad_bf16) {
-      k_ortho_norm<bf16_t><<<dim3(parts, count), 256, 0, st>>>(t, size, parts, a.mu, a.nesterov, part);
-      k_ortho_start<bf16_t><<<tiles, 256, 0, st>>>(t, d, parts, a.mu, a.nesterov, a.eps, s0, part, x, xs, xt[0]);
-    } else {
-      k_ortho_norm<float><<<dim3(parts, count), 256, 0, st>>>(t, size, parts, a.mu, a.nesterov, part);
-      k_ortho_start<float><<<tiles, 256, 0, st>>>(t, d, parts, a.mu, a.nesterov, a.eps, s0, part, x, xs, xt[0]);
-    }
-    const int mt = d.mp / kTile, nt = d.np / kTile;
-    for (int k = 0; k < a.steps; ++k) {
-      Product g{};
-      g.mp = d.mp, g.np = d.np;
-      g.p = g.q = xs, g.sp = g.sq = 2 * (int64_t)d.mp * d.np, g.ld = d.np;
-      g.unscale = ldexpf(1.0f, -2 * xe[k]), g.scale = ldexpf(1.0f, ae[k]);
-      Product poly = g, apply = g;
-      g.out = p;
-      poly.p = poly.q = poly.pin = p, poly.sp = poly.sq = 2 * (int64_t)d.mp * d.mp, poly.ld = d.mp, poly.out = q;
-      poly.unscale = ldexpf(1.0f, -2 * ae[k]), poly.old = ldexpf(1.0f, -ae[k]), poly.scale = ldexpf(1.0f, be[k]);
-      poly.b = a.coef[3 * k + 1], poly.c = a.coef[3 * k + 2];
-      apply.p = q, apply.sp = poly.sp, apply.q = xt[k & 1], apply.sq = 2 * (int64_t)d.mp * d.np, apply.ld = d.mp;
-      apply.unscale = ldexpf(1.0f, -be[k] - xe[k]), apply.scale = ldexpf(1.0f, xe[k + 1]), apply.a = a.coef[3 * k];
-      apply.x = x, apply.xs = xs, apply.xt = xt[~k & 1], apply.tiles = nt;
-      k_ortho_product<GRAM><<<dim3(mt * (mt + 1) / 2, count), 256, 0, st>>>(g);
-      k_ortho_product<POLY><<<dim3(mt * (mt + 1) / 2, count), 256, 0, st>>>(poly);
-      k_ortho_product<APPLY><<<dim3(mt * nt, count), 256, 0, st>>>(apply);
-    }
-    if (a.bf16)
-      k_ortho_end<bf16_t><<<tiles, 256, 0, st>>>(e, d, a.scale, a.decay, x);
+    hipError_t err;
+    if (small)
+      err = a.grad_bf16 ? (a.bf16 ? launch_small<bf16_t, bf16_t> : launch_small<bf16_t, float>)(t, e, steps, d, u, count, st)
+                        : (a.bf16 ? launch_small<float, bf16_t> : launch_small<float, float>)(t, e, steps, d, u, count, st);
     else
-      k_ortho_end<float><<<tiles, 256, 0, st>>>(e, d, a.scale, a.decay, x);
-    const hipError_t err = hipGetLastError();
+      err = (a.grad_bf16 ? (a.bf16 ? launch_large<bf16_t, bf16_t> : launch_large<bf16_t, float>)
+                         : (a.bf16 ? launch_large<float, bf16_t> : launch_large<float, float>))(t, e, steps, d, u, tile, count, l,
+                                                                                                (char*)workspace, st);
     if (err != hipSuccess) return err;
   }
   return hipSuccess;

@@ -139,7 +139,7 @@ def test_orthogonalize_refusals(e2f, ctx):
                dict(momentum=NAN), dict(scale=INF), dict(decay=NAN), dict(nesterov=2), dict(grad_dtype=2), dict(dtype=2),
                dict(handle=None), dict(none=True), dict(g=None), dict(out=None), dict(m=None), dict(to=None),
                dict(w=None), dict(g=[at(1), None]), dict(m=[None, at(4)]), dict(out=[at(9, 2), at(10)]),
-               dict(to=[at(5), at(6, 1)]), dict(ws=at(20, 8))):
+               dict(to=[at(5), at(6, 1)])):
         assert call(**kw) == EINVAL, kw
     for kw in (dict(steps=65), dict(rows=65537), dict(cols=65537), dict(rows=65536, cols=32768)):
         assert call(**kw) == EUNS, kw
@@ -154,10 +154,16 @@ def test_orthogonalize_refusals(e2f, ctx):
         assert call(**kw) == EDEV, kw
     b = ctypes.c_size_t(0)
     size = lib.e2f_orthogonalize_workspace_size
-    assert size(ctx.handle, ctypes.byref(ortho(e2f)), 2, ctypes.byref(b)) == e2f.E2F_OK and b.value % 256 == 0
-    assert call(size=b.value) == EDEV and call(size=b.value - 1) == ECAP and call(ws=None) == ECAP
+    big = dict(rows=200, cols=300)
+    assert size(ctx.handle, ctypes.byref(ortho(e2f, **big)), 2, ctypes.byref(b)) == e2f.E2F_OK
+    assert b.value > 0 and b.value % 256 == 0
+    assert call(size=b.value, **big) == EDEV and call(size=b.value - 1, **big) == ECAP and call(ws=None, **big) == ECAP
+    assert call(ws=at(20, 8), **big) == EINVAL
+    assert call(ws=at(9), **big) == EINVAL and call(ws=at(1), **big) == EINVAL and call(ws=at(7), **big) == EINVAL
     assert size(ctx.handle, ctypes.byref(ortho(e2f)), 2, None) == EINVAL
-    assert size(ctx.handle, ctypes.byref(ortho(e2f, rows=0)), 2, ctypes.byref(b)) == e2f.E2F_OK and b.value == 0
+    for kw in (dict(rows=0), {}):  # nothing to do, or all in a workgroup
+        assert size(ctx.handle, ctypes.byref(ortho(e2f, **kw)), 2, ctypes.byref(b)) == e2f.E2F_OK and b.value == 0
+        assert call(ws=None, size=0, **kw) == EDEV
     # overlaps: matrices of 512 bytes; an output may be the input that it replaces
     assert call(out=base["w"]) == EDEV and call(to=base["m"]) == EDEV and call(out=base["w"], to=base["m"]) == EDEV
     assert call(out=[at(8), at(7)]) == EINVAL and call(to=[at(4), at(3)]) == EINVAL  # each other's
@@ -169,5 +175,4 @@ def test_orthogonalize_refusals(e2f, ctx):
                 assert call(**{out: [base[out][0], ctypes.c_void_p(first + off)]}) == want, (name, out, off)
     assert call(out=base["g"]) == EINVAL and call(out=base["to"]) == EINVAL and call(out=base["m"]) == EINVAL
     assert call(out=base["w"], decay=0.0) == EDEV  # (not read then)
-    assert call(ws=at(9)) == EINVAL and call(ws=at(1)) == EINVAL and call(ws=at(7)) == EINVAL
     assert call(dtype=1, grad_dtype=1, out=[at(1, 256), at(10)]) == EDEV and call(out=[at(1, 256), at(10)]) == EINVAL

@@ -66,7 +66,8 @@ def check(e2f, ctx, grads, **kw):
 
 @pytest.mark.parametrize("r,c", [(1, 1), (1, 2), (1, 50), (50, 1), (2, 2), (3, 5), (16, 16), (17, 16), (15, 40), (64, 64),
                                  (65, 63), (63, 200), (128, 128), (129, 128), (100, 300), (300, 100), (128, 500), (333, 200),
-                                 (256, 256), (257, 259), (511, 130), (640, 640)])
+                                 (256, 256), (257, 259), (511, 130), (640, 640), (90, 220),
+                                 (96, 224), (96, 225), (64, 384), (200, 33), (31, 512), (513, 32), (60, 257), (128, 129)])
 @pytest.mark.parametrize("t", [F32, BF16])
 def test_sizes(e2f, ctx, r, c, t):
     check(e2f, ctx, [matrix(r, c, r + c).to(t), matrix(r, c, 7, "plain").to(t)])
@@ -75,6 +76,14 @@ def test_sizes(e2f, ctx, r, c, t):
 @pytest.mark.parametrize("r,c", [(1, 2000), (1200, 1100), (96, 5000), (3000, 40)])
 def test_long_sides(e2f, ctx, r, c):
     check(e2f, ctx, [matrix(r, c, 5)])
+
+
+@pytest.mark.parametrize("r,c,n", [(150, 200, 64), (300, 260, 60), (260, 900, 33)])
+@pytest.mark.parametrize("t", [F32, BF16])
+def test_many_large_matrices(e2f, ctx, r, c, n, t):
+    """Enough of them that the products take their large tiles."""
+    grads = [matrix(r, c, i).to(t) for i in range(n)]
+    check(e2f, ctx, grads, weights=[matrix(r, c, 100 + i, "plain").to(t) for i in range(n)], scale=-0.3, decay=0.98)
 
 
 @pytest.mark.parametrize("gt", [F32, BF16])
@@ -127,7 +136,7 @@ def test_numbers_of_steps(e2f, ctx, steps, r, c):
 def test_lists_of_stacks_and_sizes(e2f, ctx):
     """Stacks and matrices of several sizes in one call, more of one size than a launch holds."""
     g = torch.Generator().manual_seed(1)
-    shapes = [(5, 12, 12), (8, 30), (3, 12, 12), (8, 30), (130, 12, 12), (1, 70, 8), (0, 4, 4), (6, 6)]
+    shapes = [(5, 12, 12), (8, 30), (3, 12, 12), (8, 30), (130, 12, 12), (67, 140, 130), (1, 70, 8), (0, 4, 4), (6, 6)]
     grads = [torch.randn(*s, generator=g).to(DEV) for s in shapes]
     outs = e2f.e2f_orthogonalize(ctx, grads, scale=0.5)
     for x, o in zip(grads, outs):
@@ -135,6 +144,8 @@ def test_lists_of_stacks_and_sizes(e2f, ctx):
         one = [e2f.e2f_orthogonalize(ctx, [m], scale=0.5)[0] for m in (x if x.dim() == 3 else x[None])]
         for a, b in zip(one, o if o.dim() == 3 else o[None]):
             assert torch.equal(a, b)
+    want, _, x, room = ref.orthogonalize(grads[5][66].cpu(), scale=0.5)
+    close(outs[5][66], want, x, room, 0.5)
     want, _, x, room = ref.orthogonalize(grads[4][129].cpu(), scale=0.5)
     close(outs[4][129], want, x, room, 0.5)
     assert e2f.e2f_orthogonalize(ctx, []) == []
@@ -223,6 +234,6 @@ def test_refused_by_the_binding(e2f, ctx):
             bad()
     for bad in (lambda: e2f.e2f_orthogonalize(ctx, g, outs=g), lambda: e2f.e2f_orthogonalize(ctx, g, decay=0.5),
                 lambda: e2f.e2f_orthogonalize(ctx, g, steps=-1), lambda: e2f.e2f_orthogonalize(ctx, g, coefs=(9.0, 0.0, 0.0)),
-                lambda: e2f.e2f_orthogonalize(ctx, g, workspace=torch.empty(256, dtype=torch.uint8, device=DEV))):
+                lambda: e2f.e2f_orthogonalize(ctx, [torch.zeros(200, 300, device=DEV)], workspace=torch.empty(256, dtype=torch.uint8, device=DEV))):
         with pytest.raises(e2f.E2FError):
             bad()
