@@ -776,8 +776,12 @@ def e2f_orthogonalize(ctx, grads, outs=None, weights=None, moments=None, new_mom
                 lists.append(None)
                 continue
             step = rows * cols * tensors[which[0]].element_size()
-            lists.append(array.array("Q", [t.data_ptr() + i * step for t in (tensors[k] for k in which)
-                                           for i in range(t.shape[0] if t.dim() == 3 else 1)]))
+            at = array.array("Q")
+            for k in which:
+                first = tensors[k].data_ptr()
+                many = len(tensors[k]) if tensors[k].dim() == 3 else 1
+                at.extend(range(first, first + many * step, step) if step else [first] * many)
+            lists.append(at)
         count = len(lists[0])
         prm = OrthogonalizeParams(rows, cols, steps, None if flat is None else flat.buffer_info()[0], eps, momentum,
                                   int(bool(nesterov)), scale, decay, _DTYPES[gt], _DTYPES[wt])

@@ -51,14 +51,37 @@ __device__ __forceinline__ void split(v4f x, float scale, h4& hi, h4& lo) {
 }
 __device__ __forceinline__ h8 both(h4 a, h4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 __device__ __forceinline__ v4f mfma(h8 a, h8 b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-// the product of operands split in two: the small parts first
-__device__ __forceinline__ v4f product(h8 ah, h8 al, h8 bh, h8 bl, v4f c) {
-  return mfma(ah, bh, mfma(ah, bl, mfma(al, bh, c)));
+// c += the products of operands split in two, the small parts first, and of all tiles one after the other: neighbours in the
+// matrix cores' queue wait for no result
+template <int A, int B>
+__device__ __forceinline__ void products(const h8 (&ah)[A], const h8 (&al)[A], const h8 (&bh)[B], const h8 (&bl)[B],
+                                         v4f (&c)[A][B]) {
+#pragma unroll
+  for (int i = 0; i < A; ++i)
+#pragma unroll
+    for (int j = 0; j < B; ++j) c[i][j] = mfma(al[i], bh[j], c[i][j]);
+#pragma unroll
+  for (int i = 0; i < A; ++i)
+#pragma unroll
+    for (int j = 0; j < B; ++j) c[i][j] = mfma(ah[i], bl[j], c[i][j]);
+#pragma unroll
+  for (int i = 0; i < A; ++i)
+#pragma unroll
+    for (int j = 0; j < B; ++j) c[i][j] = mfma(ah[i], bh[j], c[i][j]);
 }
 // Transposing load: of 16 lanes, lane s gives the address of four neighbours of row s / 4, from column 4 (s % 4) on, and lane
 // t gets the four rows' values of column t
 __device__ __forceinline__ h4 read_transposed(const _Float16* p) {
   return __builtin_bit_cast(h4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)p));
+}
+
+// 64 lanes' 16 bytes each to the LDS, lane after lane from `to` (the same for the wave) on, without passing registers.  By
+// hand: the compiler, which cannot tell the LDS's buffers apart, would wait for all such loads before any read of the LDS.
+// The instruction has no register for its result; who reads what it brings waits for vmcnt first, by hand as well.  (Nothing
+// else in a kernel that calls this uses m0.)
+__device__ __forceinline__ void load_past(const _Float16* from, _Float16* to) {
+  const unsigned at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) _Float16*)to);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory");
 }
 
 struct Table {
@@ -146,16 +169,39 @@ struct Rows {
 // A matrix of up to MP rows and 128 S columns, a workgroup of eight waves each.  A wave holds S strips of 16 columns of X in
 // registers as the matrix cores return them: lane l has rows 4 (l / 16) .. + 3 of every 16 and column l % 16.  These rows, of two
 // 16s, are also what it gives as the right operand of B X, so B's columns are stored in that order (within 32: 16 h + 4 g + e
-// at 8 g + 4 h + e).  X^T lies in the LDS for P, whose tiles the waves share in blocks of BR x BC.  P, and B that replaces it, are
-// symmetric: a tile is stored as its transpose
+// at 8 g + 4 h + e).  X^T lies in the LDS for P.  P, and B that replaces it, are symmetric: a tile is stored as
+// its transpose
 template <int MP, int S, typename TG, typename T>
 __global__ __launch_bounds__(512) void k_ortho_small(Table t, Ends e, Steps steps, Sizes d, Update u) {
   constexpr int MT = MP / 16, SX = Rows<MP>::X, SP = Rows<MP>::P;
-  constexpr int BR = MT <= 4 ? 1 : 2, BC = MT == 2 ? 1 : MT == 4 ? 2 : MT / 2, COLS = MT / BC;
+  // P's tiles of a wave, in a row: of six and eight rows of tiles the one on the diagonal and half of the row's others, in a
+  // circle, each written at both its places; of fewer all tiles, shared by the eight waves
+  constexpr bool BAND = MT >= 6;
+  constexpr int BC = BAND ? MT / 2 + 1 : MT / 2, COLS = MT / BC;
   extern __shared__ __align__(16) _Float16 lds[];
   __shared__ double squares[8];
   _Float16 *xh = lds, *xl = xh + d.np * SX, *ph = xl + d.np * SX, *pl = ph + MP * SP;
-  const int z = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  const int z = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  // the update's four neighbours of the caller's matrix from `at` on, of which `have` are there; the momentum on the way
+  auto update = [&](int64_t at, int have) {
+    v4f v = values<TG>(t.g[z], at, have);
+    if (t.m[z]) {
+      const v4f m = values<float>(t.m[z], at, have) * u.mu + v;
+      puts<float>(t.to[z], at, have, m);
+      v = u.nesterov ? v + u.mu * m : m;
+    }
+    return v;
+  };
+  // rows of the caller's matrix pass through the LDS where they are not X's columns: four neighbours a lane either way
+  float* stage = (float*)lds;  // [MP][SN], in X^T's place
+  const int SN = d.np + 4, quads = d.np / 4;
+  if (!d.turned) {
+    for (int k = threadIdx.x; k < MP * quads; k += 512) {
+      const int i = k / quads, j = k % quads * 4;
+      *(v4f*)(stage + i * SN + j) = i < d.m && j < d.n ? update((int64_t)i * d.cols + j, d.n - j) : v4f{};
+    }
+    __syncthreads();
+  }
   v4f x[S][MT];
   double sum = 0.0;
 #pragma unroll
@@ -164,28 +210,11 @@ __global__ __launch_bounds__(512) void k_ortho_small(Table t, Ends e, Steps step
     for (int tau = 0; tau < MT; ++tau) {
       const int j = (wave + 8 * s) * 16 + c, i = tau * 16 + 4 * g;
       v4f v = {};
-      if (j < d.n && i < d.m) {
-        if (d.turned) {
-          const int64_t at = (int64_t)j * d.cols + i;
-          v = values<TG>(t.g[z], at, d.m - i);
-          if (t.m[z]) {
-            const v4f m = values<float>(t.m[z], at, d.m - i) * u.mu + v;
-            puts<float>(t.to[z], at, d.m - i, m);
-            v = u.nesterov ? v + u.mu * m : m;
-          }
-        } else {
+      if (d.turned) {
+        if (j < d.n && i < d.m) v = update((int64_t)j * d.cols + i, d.m - i);
+      } else if (j < d.np) {
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (i + r < d.m) {
-              const int64_t at = (int64_t)(i + r) * d.cols + j;
-              v[r] = value<TG>(t.g[z], at);
-              if (t.m[z]) {
-                const float m = u.mu * t.m[z][at] + v[r];
-                t.to[z][at] = m;
-                v[r] = u.nesterov ? v[r] + u.mu * m : m;
-              }
-            }
-        }
+        for (int r = 0; r < 4; ++r) v[r] = stage[(i + r) * SN + j];
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) sum += (double)v[r] * (double)v[r];
@@ -205,8 +234,11 @@ __global__ __launch_bounds__(512) void k_ortho_small(Table t, Ends e, Steps step
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[s][tau][r] = (float)((double)x[s][tau][r] * inv);
 
-  const int br = wave / COLS * BR, bc = wave % COLS * BC;  // the wave's block of P's tiles
+  const int br = BAND ? wave : wave / COLS;
   const bool tiles = br < MT;
+  int bc[BC];
+#pragma unroll
+  for (int b = 0; b < BC; ++b) bc[b] = BAND ? (wave + b) % MT : wave % COLS * BC + b;
   for (int k = 0; k < steps.count; ++k) {
     const float sx = power(steps.x[k]), sp = power(steps.p[k]), sb = power(steps.b[k]);
     h4 hi[S][MT], lo[S][MT];
@@ -223,112 +255,110 @@ __global__ __launch_bounds__(512) void k_ortho_small(Table t, Ends e, Steps step
       }
     __syncthreads();
     // P = X X^T
-    v4f p[BR][BC] = {};
+    v4f p[1][BC] = {}, q[1][BC] = {};
     if (tiles)
       for (int j = 0; j < d.np; j += 32) {
         const int row = (j + 8 * g + (c >> 2)) * SX + 4 * (c & 3);
-        h8 ah[BR], al[BR];
+        auto read = [&](const _Float16* of, int tile) {
+          const _Float16* at = of + row + tile * 16;
+          return both(read_transposed(at), read_transposed(at + 4 * SX));
+        };
+        const h8 ah[1] = {read(xh, br)}, al[1] = {read(xl, br)};
+        h8 bh[BC], bl[BC];
 #pragma unroll
-        for (int a = 0; a < BR; ++a) {
-          const int at = row + (br + a) * 16;
-          ah[a] = both(read_transposed(xh + at), read_transposed(xh + at + 4 * SX));
-          al[a] = both(read_transposed(xl + at), read_transposed(xl + at + 4 * SX));
-        }
+        for (int b = 0; b < BC; ++b) bh[b] = read(xh, bc[b]), bl[b] = read(xl, bc[b]);
+        products<1, BC>(ah, al, bh, bl, p);
+      }
+    auto store = [&](const v4f(&m)[1][BC], float scale) {
 #pragma unroll
-        for (int b = 0; b < BC; ++b) {
-          const int at = row + (bc + b) * 16;
-          const h8 bh = both(read_transposed(xh + at), read_transposed(xh + at + 4 * SX));
-          const h8 bl = both(read_transposed(xl + at), read_transposed(xl + at + 4 * SX));
+      for (int b = 0; b < BC; ++b) {
+        if (BAND && b == MT / 2 && br >= MT / 2) continue;  // (the other of the two has it)
+        h4 h, l;
+        split(m[0][b], scale, h, l);
+        const int at = (bc[b] * 16 + c) * SP + (br >> 1) * 32 + 8 * g + (br & 1) * 4;
+        *(h4*)(ph + at) = h, *(h4*)(pl + at) = l;
+        if (BAND && b > 0) {
+          const int to = (br * 16 + 4 * g) * SP + (bc[b] >> 1) * 32 + 8 * (c >> 2) + (bc[b] & 1) * 4 + (c & 3);
 #pragma unroll
-          for (int a = 0; a < BR; ++a) p[a][b] = product(ah[a], al[a], bh, bl, p[a][b]);
+          for (int r = 0; r < 4; ++r) ph[to + r * SP] = h[r], pl[to + r * SP] = l[r];
         }
       }
-    auto store = [&](const v4f(&m)[BR][BC], float scale) {
-#pragma unroll
-      for (int a = 0; a < BR; ++a)
-#pragma unroll
-        for (int b = 0; b < BC; ++b) {
-          h4 h, l;
-          split(m[a][b], scale, h, l);
-          const int at = ((bc + b) * 16 + c) * SP + ((br + a) >> 1) * 32 + 8 * g + ((br + a) & 1) * 4;
-          *(h4*)(ph + at) = h, *(h4*)(pl + at) = l;
-        }
     };
     if (tiles) {
       const float off = power(-2 * steps.x[k]);
 #pragma unroll
-      for (int a = 0; a < BR; ++a)
-#pragma unroll
-        for (int b = 0; b < BC; ++b) p[a][b] *= off;
+      for (int b = 0; b < BC; ++b) p[0][b] *= off;
       store(p, sp);
     }
     __syncthreads();
     // B = b P + c P^2
-    v4f q[BR][BC] = {};
     if (tiles)
 #pragma unroll
       for (int kb = 0; kb < MP; kb += 32) {
-        h8 ah[BR], al[BR];
+        auto read = [&](const _Float16* of, int tile) { return *(const h8*)(of + (tile * 16 + c) * SP + kb + 8 * g); };
+        const h8 ah[1] = {read(ph, br)}, al[1] = {read(pl, br)};
+        h8 bh[BC], bl[BC];
 #pragma unroll
-        for (int a = 0; a < BR; ++a) {
-          const int at = ((br + a) * 16 + c) * SP + kb + 8 * g;
-          ah[a] = *(const h8*)(ph + at), al[a] = *(const h8*)(pl + at);
-        }
-#pragma unroll
-        for (int b = 0; b < BC; ++b) {
-          const int at = ((bc + b) * 16 + c) * SP + kb + 8 * g;
-          const h8 bh = *(const h8*)(ph + at), bl = *(const h8*)(pl + at);
-#pragma unroll
-          for (int a = 0; a < BR; ++a) q[a][b] = product(ah[a], al[a], bh, bl, q[a][b]);
-        }
+        for (int b = 0; b < BC; ++b) bh[b] = read(ph, bc[b]), bl[b] = read(pl, bc[b]);
+        products<1, BC>(ah, al, bh, bl, q);
       }
     __syncthreads();
     if (tiles) {
       const float by = steps.coef[k][1], cy = steps.coef[k][2] * power(-2 * steps.p[k]);
 #pragma unroll
-      for (int a = 0; a < BR; ++a)
-#pragma unroll
-        for (int b = 0; b < BC; ++b) q[a][b] = by * p[a][b] + cy * q[a][b];
+      for (int b = 0; b < BC; ++b) q[0][b] = by * p[0][b] + cy * q[0][b];
       store(q, sb);
     }
     __syncthreads();
     // X <- a X + B X
     const float off = power(-steps.b[k] - steps.x[k]);
+    constexpr int AT = MT % 4 ? 2 : 4;  // tiles side by side
     if (wave * 16 < d.np)
 #pragma unroll
-      for (int tau = 0; tau < MT; ++tau) {
-        v4f y[S] = {};
+      for (int tau = 0; tau < MT; tau += AT) {
+        v4f y[AT][S] = {};
 #pragma unroll
         for (int kb = 0; kb < MT / 2; ++kb) {
-          const int at = (tau * 16 + c) * SP + kb * 32 + 8 * g;
-          const h8 ah = *(const h8*)(ph + at), al = *(const h8*)(pl + at);
+          h8 ah[AT], al[AT], bh[S], bl[S];
+#pragma unroll
+          for (int a = 0; a < AT; ++a) {
+            const int at = ((tau + a) * 16 + c) * SP + kb * 32 + 8 * g;
+            ah[a] = *(const h8*)(ph + at), al[a] = *(const h8*)(pl + at);
+          }
 #pragma unroll
           for (int s = 0; s < S; ++s)
-            y[s] = product(ah, al, both(hi[s][2 * kb], hi[s][2 * kb + 1]), both(lo[s][2 * kb], lo[s][2 * kb + 1]), y[s]);
+            bh[s] = both(hi[s][2 * kb], hi[s][2 * kb + 1]), bl[s] = both(lo[s][2 * kb], lo[s][2 * kb + 1]);
+          products<AT, S>(ah, al, bh, bl, y);
         }
 #pragma unroll
-        for (int s = 0; s < S; ++s) x[s][tau] = steps.coef[k][0] * x[s][tau] + off * y[s];
+        for (int a = 0; a < AT; ++a)
+#pragma unroll
+          for (int s = 0; s < S; ++s) x[s][tau + a] = steps.coef[k][0] * x[s][tau + a] + off * y[a][s];
       }
   }
+  auto end = [&](int64_t at, int have, v4f v) {
+    v *= u.scale;
+    puts<T>(e.out[z], at, have, e.w[z] ? v + u.decay * values<T>(e.w[z], at, have) : v);
+  };
+  if (!d.turned) __syncthreads();  // (without steps what was staged is still read)
 #pragma unroll
   for (int s = 0; s < S; ++s)
 #pragma unroll
     for (int tau = 0; tau < MT; ++tau) {
       const int j = (wave + 8 * s) * 16 + c, i = tau * 16 + 4 * g;
-      if (j >= d.n || i >= d.m) continue;
-      const v4f v = u.scale * x[s][tau];
       if (d.turned) {
-        const int64_t at = (int64_t)j * d.cols + i;
-        puts<T>(e.out[z], at, d.m - i, e.w[z] ? v + u.decay * values<T>(e.w[z], at, d.m - i) : v);
-      } else {
+        if (j < d.n && i < d.m) end((int64_t)j * d.cols + i, d.m - i, x[s][tau]);
+      } else if (j < d.np) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (i + r < d.m) {
-            const int64_t at = (int64_t)(i + r) * d.cols + j;
-            put<T>(e.out[z], at, e.w[z] ? v[r] + u.decay * value<T>(e.w[z], at) : v[r]);
-          }
+        for (int r = 0; r < 4; ++r) stage[(i + r) * SN + j] = x[s][tau][r];
       }
     }
+  if (d.turned) return;
+  __syncthreads();
+  for (int k = threadIdx.x; k < MP * quads; k += 512) {
+    const int i = k / quads, j = k % quads * 4;
+    if (i < d.m && j < d.n) end((int64_t)i * d.cols + j, d.n - j, *(const v4f*)(stage + i * SN + j));
+  }
 }
 
 // ------------------------------------------------------------------ larger matrices
@@ -425,21 +455,23 @@ struct Product {
   int mp, np;
 };
 
-// One tile of TILE x TILE of  sum_k p[i][k] q[j][k]  (GRAM: p[k][i] q[k][j]) by four waves of a quarter each, with two buffers of a
-// step in the LDS: while a step's products run, the next step's values are on their way there without passing registers.
+// One tile of TILE x TILE of  sum_k p[i][k] q[j][k]  (GRAM: p[k][i] q[k][j]), WI x WJ waves, or WK times as many that take the
+// steps in turn and add their sums at the end, with ST buffers of a (WK) step(s) in the
+// LDS: the values of ST - 1 steps are on their way there, without passing registers, while one step's products run.
 // GRAM and POLY are symmetric: the tiles on and below the diagonal, each written at both its places.  A lane has four neighbouring
 // rows i of a column j, which are neighbours in memory at row j of Y, and of the symmetric P and B.
 //
 // In the LDS a row of 128 bytes (GRAM: of 4 TILE bytes) has its 16 bytes at position c ^ row % 8 (its 32 bytes at c ^ a number
 // of the row): lanes that read together meet different banks, and the loads, which write 64 x 16 bytes in
 // their order, read the places that belong there
-template <int KIND, int TILE, typename T>
-__global__ __launch_bounds__(256) void k_ortho_product(Product g, Ends e, Sizes d, Update u) {
-  constexpr int F = TILE / 32, HALF = TILE / 2;
-  __shared__ __align__(16) _Float16 lds[2][2][TILE * 64];
+template <int KIND, int TILE, int WI, int WJ, int WK, int ST, typename T>
+__global__ __launch_bounds__(64 * WI * WJ * WK) void k_ortho_product(Product g, Ends e, Sizes d, Update u) {
+  constexpr int FI = TILE / 16 / WI, FJ = TILE / 16 / WJ, N = TILE / 8 / (WI * WJ);  // N: loads of a wave and operand
+  __shared__ __align__(16) _Float16 lds[ST][WK][2][TILE * 64];
+  static_assert(sizeof(lds) >= sizeof(float) * TILE * TILE, "a tile of floats");
   // neighbouring workgroups lie on different dies: each die takes a stretch of neighbouring tiles, which share rows in its L2
   const int all = g.tiles * g.count, each = (all + 7) >> 3, at_ = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
-  if (at_ >= all) return;
+  if (at_ >= all || (int)(blockIdx.x >> 3) >= each) return;
   const int z = at_ / g.tiles, tile = at_ % g.tiles;
   int ti, tj;
   if (KIND >= APPLY) {
@@ -451,33 +483,34 @@ __global__ __launch_bounds__(256) void k_ortho_product(Product g, Ends e, Sizes 
     tj = tile - ti * (ti + 1) / 2;
   }
   const int i0 = ti * TILE, j0 = tj * TILE;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = (wave >> 1) * HALF, wj = (wave & 1) * HALF;
-  const int lg = lane >> 4, lc = lane & 15;
+  const int lane = threadIdx.x & 63, all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = all_waves % (WI * WJ), wk = all_waves / (WI * WJ);  // (and which of a round's steps it has)
+  const int wi = wave / WJ * (FI * 16), wj = wave % WJ * (FJ * 16), lg = lane >> 4, lc = lane & 15;
   // where this lane's 16 bytes of each load come from, and how far a step is
-  int64_t from[F];
   const int64_t step = KIND == GRAM ? (int64_t)kStep * 2 * g.ld : 2 * kStep;
+  const _Float16 *p[N], *q[N];
 #pragma unroll
-  for (int n = 0; n < F; ++n) {
-    const int chunk = (wave * F + n) * 64 + lane;
+  for (int n = 0; n < N; ++n) {
+    const int chunk = (wave * N + n) * 64 + lane;
+    int64_t from;
     if (KIND == GRAM) {
       constexpr int PER = TILE / 4;  // of a row
       const int k = chunk / PER, to = chunk % PER, h = (k & 3) | (k >> 3 & 1) << 2;
-      from[n] = (int64_t)k * 2 * g.ld + (((to >> 1) ^ h) * 2 + (to & 1)) * 8;
+      from = (int64_t)k * 2 * g.ld + (((to >> 1) ^ h) * 2 + (to & 1)) * 8;
     } else {
       const int r = chunk >> 3;
-      from[n] = (int64_t)r * 2 * g.ld + ((chunk & 7) ^ (r & 7)) * 8;
+      from = (int64_t)r * 2 * g.ld + ((chunk & 7) ^ (r & 7)) * 8;
     }
+    from += wk * step;
+    p[n] = g.p + z * g.sp + (KIND == GRAM ? 2 * i0 : (int64_t)i0 * 2 * g.ld) + from;
+    q[n] = g.q + z * g.sq + (KIND == GRAM ? 2 * j0 : (int64_t)j0 * 2 * g.ld) + from;
   }
-  const _Float16 *p = g.p + z * g.sp + (KIND == GRAM ? 2 * i0 : (int64_t)i0 * 2 * g.ld);
-  const _Float16 *q = g.q + z * g.sq + (KIND == GRAM ? 2 * j0 : (int64_t)j0 * 2 * g.ld);
-  auto fetch = [&](int s) {
+  auto fetch = [&](int buf) {
 #pragma unroll
-    for (int n = 0; n < F; ++n) {
-      const int to = __builtin_amdgcn_readfirstlane((wave * F + n) * 512);
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + s * step + from[n]),
-                                       (__attribute__((address_space(3))) void*)(&lds[s & 1][0][to]), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(q + s * step + from[n]),
-                                       (__attribute__((address_space(3))) void*)(&lds[s & 1][1][to]), 16, 0, 0);
+    for (int n = 0; n < N; ++n) {
+      load_past(p[n], &lds[buf][wk][0][(wave * N + n) * 512]);
+      load_past(q[n], &lds[buf][wk][1][(wave * N + n) * 512]);
+      p[n] += WK * step, q[n] += WK * step;
     }
   };
   // 16 of the tile's rows from `row` on, part 0 (hi) or 1 (lo), as an operand
@@ -490,67 +523,112 @@ __global__ __launch_bounds__(256) void k_ortho_product(Product g, Ends e, Sizes 
       return *(const h8*)(l + (row + lc) * 64 + ((part * 4 + lg) ^ (lc & 7)) * 8);
     }
   };
-  v4f acc[F][F] = {};
-  fetch(0);
-  for (int s = 0; s < g.steps; ++s) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();  // this step's values are there, and the other buffer's have been read
-    const _Float16 *lp = lds[s & 1][0], *lq = lds[s & 1][1];
-    h8 ph[F], pl[F], qh[F], ql[F];
+  v4f acc[FI][FJ] = {}, old[KIND >= APPLY ? FI : 1][KIND >= APPLY ? FJ : 1];
+  const int steps = g.steps / WK;
 #pragma unroll
-    for (int a = 0; a < F; ++a) {
-      ph[a] = operand(lp, wi + a * 16, 0), pl[a] = operand(lp, wi + a * 16, 1);
-      qh[a] = operand(lq, wj + a * 16, 0), ql[a] = operand(lq, wj + a * 16, 1);
-    }
-    if (s + 1 < g.steps) fetch(s + 1);
+  for (int s = 0; s + 1 < ST; ++s)
+    if (s < steps) fetch(s);
+  if constexpr (KIND >= APPLY) {  // Y, needed at the end
 #pragma unroll
-    for (int a = 0; a < F; ++a)
+    for (int a = 0; a < FI; ++a)
 #pragma unroll
-      for (int b = 0; b < F; ++b) acc[a][b] = product(ph[a], pl[a], qh[b], ql[b], acc[a][b]);
+      for (int b = 0; b < FJ; ++b)
+        old[a][b] = *(const v4f*)(g.y + ((int64_t)z * g.np + j0 + wj + b * 16 + lc) * g.mp + i0 + wi + a * 16 + lg * 4);
   }
+  int buf = 0, to = ST - 1;
+  for (int s = 0; s < steps; ++s) {
+    // this step's values are there (those of the steps behind it may be on their way), and the buffer that is filled next has
+    // been read by every wave
+    if (s + ST - 1 <= steps)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((ST - 2) * 2 * N) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const _Float16 *lp = lds[buf][wk][0], *lq = lds[buf][wk][1];
+    h8 ph[FI], pl[FI], qh[FJ], ql[FJ];
 #pragma unroll
-  for (int a = 0; a < F; ++a)
+    for (int a = 0; a < FI; ++a) ph[a] = operand(lp, wi + a * 16, 0), pl[a] = operand(lp, wi + a * 16, 1);
 #pragma unroll
-    for (int b = 0; b < F; ++b) {
-      const int i = i0 + wi + a * 16 + lg * 4, j = j0 + wj + b * 16 + lc;
-      v4f s = acc[a][b] * g.unscale;
-      if constexpr (KIND == POLY) {
-        const _Float16* in = g.p + z * g.sp;
-        const h4 hi = *(const h4*)(in + split_at(j, g.mp, i, 0)), lo = *(const h4*)(in + split_at(j, g.mp, i, 1));
+    for (int b = 0; b < FJ; ++b) qh[b] = operand(lq, wj + b * 16, 0), ql[b] = operand(lq, wj + b * 16, 1);
+    if (s + ST - 1 < steps) fetch(to);
+    products<FI, FJ>(ph, pl, qh, ql, acc);
+    buf = buf + 1 == ST ? 0 : buf + 1, to = to + 1 == ST ? 0 : to + 1;
+  }
+  float* turn = (float*)&lds[0][0][0][0];  // [TILE][TILE]
+  if constexpr (KIND == LAST || WK > 1) __syncthreads();  // (the last step's operands have been read)
+  if constexpr (WK > 1) {  // the sums of a tile's waves together, in their order
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s[k] = g.b * (((float)hi[k] + (float)lo[k]) * g.old) + g.c * s[k];
+    for (int w = 1; w < WK; ++w) {
+      if (wk == w) {
+#pragma unroll
+        for (int a = 0; a < FI; ++a)
+#pragma unroll
+          for (int b = 0; b < FJ; ++b) *(v4f*)(turn + (((wave * FI + a) * FJ + b) * 64 + lane) * 4) = acc[a][b];
       }
-      if constexpr (KIND >= APPLY) {
-        v4f* y = (v4f*)(g.y + ((int64_t)z * g.np + j) * g.mp + i);
-        s += g.a * *y;
-        if constexpr (KIND == APPLY) *y = s;
-      }
-      if constexpr (KIND == LAST) {
-        if (j >= d.n || i >= d.m) continue;
-        s *= u.scale;
-        if (d.turned) {
-          const int64_t at = (int64_t)j * d.cols + i;
-          puts<T>(e.out[z], at, d.m - i, e.w[z] ? s + u.decay * values<T>(e.w[z], at, d.m - i) : s);
-        } else {
+      __syncthreads();
+      if (wk == 0) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (i + k < d.m) {
-              const int64_t at = (int64_t)(i + k) * d.cols + j;
-              put<T>(e.out[z], at, e.w[z] ? s[k] + u.decay * value<T>(e.w[z], at) : s[k]);
-            }
-        }
-      } else {
-        h4 hi, lo;
-        split(s, g.scale, hi, lo);
-        _Float16* out = g.out + (int64_t)z * (KIND == APPLY ? g.np : g.mp) * g.mp * 2;
-        *(h4*)(out + split_at(j, g.mp, i, 0)) = hi, *(h4*)(out + split_at(j, g.mp, i, 1)) = lo;
-        if (KIND != APPLY && ti != tj) {
+        for (int a = 0; a < FI; ++a)
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            out[split_at(i + k, g.mp, j, 0)] = hi[k], out[split_at(i + k, g.mp, j, 1)] = lo[k];
-        }
+          for (int b = 0; b < FJ; ++b) acc[a][b] += *(const v4f*)(turn + (((wave * FI + a) * FJ + b) * 64 + lane) * 4);
       }
+      __syncthreads();
     }
+  }
+  if (wk == 0) {
+#pragma unroll
+    for (int a = 0; a < FI; ++a)
+#pragma unroll
+      for (int b = 0; b < FJ; ++b) {
+        const int i = i0 + wi + a * 16 + lg * 4, j = j0 + wj + b * 16 + lc;
+        v4f s = acc[a][b] * g.unscale;
+        if constexpr (KIND == POLY) {
+          const _Float16* in = g.p + z * g.sp;
+          const h4 hi = *(const h4*)(in + split_at(j, g.mp, i, 0)), lo = *(const h4*)(in + split_at(j, g.mp, i, 1));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) s[k] = g.b * (((float)hi[k] + (float)lo[k]) * g.old) + g.c * s[k];
+        }
+        if constexpr (KIND >= APPLY) {
+          s += g.a * old[a][b];
+          if constexpr (KIND == APPLY) *(v4f*)(g.y + ((int64_t)z * g.np + j) * g.mp + i) = s;
+        }
+        if constexpr (KIND == LAST) {
+          if (d.turned) {
+            if (j >= d.n || i >= d.m) continue;
+            const int64_t at = (int64_t)j * d.cols + i;
+            s *= u.scale;
+            puts<T>(e.out[z], at, d.m - i, e.w[z] ? s + u.decay * values<T>(e.w[z], at, d.m - i) : s);
+          } else {
+            // the caller's rows are i: by the LDS, 16 columns at a place that goes by the row (four lanes' rows meet other banks)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) turn[(i - i0 + k) * TILE + ((j - j0) ^ (lg * 16))] = s[k];
+          }
+        } else {
+          h4 hi, lo;
+          split(s, g.scale, hi, lo);
+          _Float16* out = g.out + (int64_t)z * (KIND == APPLY ? g.np : g.mp) * g.mp * 2;
+          *(h4*)(out + split_at(j, g.mp, i, 0)) = hi, *(h4*)(out + split_at(j, g.mp, i, 1)) = lo;
+          if (KIND != APPLY && ti != tj) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              out[split_at(i + k, g.mp, j, 0)] = hi[k], out[split_at(i + k, g.mp, j, 1)] = lo[k];
+          }
+        }
+      }
+  }
+  if constexpr (KIND == LAST) {
+    if (d.turned) return;
+    __syncthreads();
+#pragma unroll 4
+    for (int k = threadIdx.x; k < TILE * TILE / 4; k += 64 * WI * WJ * WK) {
+      const int r = k / (TILE / 4), c = k % (TILE / 4) * 4, i = i0 + r, j = j0 + c;
+      if (i >= d.m || j >= d.n) continue;
+      const v4f s = *(const v4f*)(turn + r * TILE + (c ^ (r >> 2 & 3) * 16)) * u.scale;
+      const int64_t at = (int64_t)i * d.cols + j;
+      puts<T>(e.out[z], at, d.n - j, e.w[z] ? s + u.decay * values<T>(e.w[z], at, d.n - j) : s);
+    }
+  }
 }
 
 // no steps: out = decay W + scale X from Y
@@ -574,7 +652,7 @@ size_t small_bytes(int mp, int np) {
 
 Sizes sizes_of(int rows, int cols, int count, bool* small, int* tile) {
   Sizes d{};
-  d.rows = rows, d.cols = cols, d.turned = rows > cols;
+  d.rows = rows, d.cols = cols, d.turned = rows >= cols;  // (of square ones the transpose, whose columns are rows in memory)
   d.m = d.turned ? cols : rows, d.n = d.turned ? rows : cols;
   d.mp = small_rows(d.m), d.np = (d.n + 31) / 32 * 32;
   *small = d.mp && d.np <= 512 && small_bytes(d.mp, d.np) <= kLds;
@@ -704,9 +782,11 @@ void launch_product(int tile, Product g, const Ends& e, const Sizes& d, const Up
   g.tiles = KIND >= APPLY ? mt * (g.np / tile) : mt * (mt + 1) / 2;
   const unsigned blocks = (unsigned)((g.tiles * g.count + 7) / 8 * 8);
   if (tile == 128)
-    k_ortho_product<KIND, 128, T><<<blocks, 256, 0, st>>>(g, e, d, u);
+    k_ortho_product<KIND, 128, 2, 4, 1, 2, T><<<blocks, 512, 0, st>>>(g, e, d, u);
+  else if (g.tiles * g.count <= 256)
+    k_ortho_product<KIND, 64, 2, 2, 2, 3, T><<<blocks, 512, 0, st>>>(g, e, d, u);
   else
-    k_ortho_product<KIND, 64, T><<<blocks, 256, 0, st>>>(g, e, d, u);
+    k_ortho_product<KIND, 64, 2, 2, 1, 3, T><<<blocks, 256, 0, st>>>(g, e, d, u);
 }
 
 template <typename TG, typename T>
