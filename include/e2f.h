@@ -286,8 +286,8 @@ e2f_status e2f_embedding_forward(e2f_ctx* ctx, const e2f_embedding_params* param
 /* The table's gradient for grad_out (like out; of its components only the scalars are read):
  *   grad_table[v][c] = scale sum over the i with index[i] = v of grad_out[i][0][c],
  * written whole, zeros for types that no row has; rows with an index outside [0, V) add
- * nothing and are not looked at.  The rows are sorted by type and summed in float32 in a fixed
- * order (up to 256 neighbours of the sorted rows at a time, then these sums), rounded once.
+ * nothing, whatever they hold.  Sums are float32, of stretches of rows and then of these, in
+ * a fixed order, rounded once.
  * workspace: e2f_embedding_backward_workspace_size bytes, 256-byte aligned (E2F_ECAPACITY
  * below).  Outputs must not overlap inputs (E2F_EINVAL).  Asynchronous, no allocation, can be
  * captured in a HIP graph; deterministic. */

@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import operator
 import os
 
 import torch
@@ -359,6 +360,7 @@ def _workspace(ctx, workspace, nbytes, device, stream):
 
 
 _DTYPES = {torch.float32: E2F_F32, torch.bfloat16: E2F_BF16}
+_SHAPE, _DTYPE = operator.attrgetter("shape"), operator.attrgetter("dtype")
 
 
 def e2f_transpose_graph(ctx, n, row_ptr, col_idx, workspace=None):
@@ -716,15 +718,22 @@ def e2f_layer_norm_backward(ctx, x, grad_out, lmax=0, weight=None, bias=None, ep
     return gx, gw, gb
 
 
-def _matrices(ctx, tensors, name, dtype=None, like=None):
-    """Checks a list of matrices [rows, cols] or stacks of them [batch, rows, cols] (contiguous, of one type)."""
-    if like is not None and len(tensors) != len(like):
-        raise ValueError("%s must have a tensor for every gradient" % name)
-    for k, t in enumerate(tensors):
-        if t.get_device() != ctx.device or not t.is_contiguous() or t.dtype != (dtype or t.dtype):
-            raise ValueError("%s must be contiguous tensors of one type on the context's device" % name)
-        if t.dim() not in (2, 3) or (like is not None and t.shape != like[k].shape):
-            raise ValueError("%s must be [rows, cols] or [batch, rows, cols], like the gradients" % name)
+def _matrices(ctx, tensors, name, dtype, shapes):
+    """Checks matrices [rows, cols] or stacks of them [batch, rows, cols] of these shapes (contiguous, of one type)."""
+    if list(map(_SHAPE, tensors)) != shapes:
+        raise ValueError("%s must have the gradients' shapes" % name)
+    if (not {dtype}.issuperset(map(_DTYPE, tensors)) or not all(map(torch.Tensor.is_contiguous, tensors)) or
+            not {ctx.device}.issuperset(map(torch.Tensor.get_device, tensors))):
+        raise ValueError("%s must be contiguous tensors of one type on the context's device" % name)
+
+
+def _addresses(tensors, many, step):
+    """Host array of the addresses of the tensors' matrices: many[k] of them in tensor k, `step` bytes each."""
+    first = list(map(torch.Tensor.data_ptr, tensors))
+    if step and len(set(many)) == 1:
+        offsets = range(0, many[0] * step, step)
+        return array.array("Q", [a + i for a in first for i in offsets])
+    return array.array("Q", [a + i * step for a, n in zip(first, many) for i in range(n)])
 
 
 def e2f_orthogonalize(ctx, grads, outs=None, weights=None, moments=None, new_moments=None, momentum=0.95,
@@ -739,23 +748,26 @@ def e2f_orthogonalize(ctx, grads, outs=None, weights=None, moments=None, new_mom
     moments themselves for new_moments; outs may be weights.  Returns outs."""
     if not grads:
         return [] if outs is None else outs
-    gt = grads[0].dtype
-    _matrices(ctx, grads, "grads", gt)
+    gt, shapes = grads[0].dtype, list(map(_SHAPE, grads))
+    if not {2, 3}.issuperset(map(len, shapes)):
+        raise ValueError("grads must be [rows, cols] or [batch, rows, cols]")
+    _matrices(ctx, grads, "grads", gt, shapes)
     if outs is None:
         outs = [torch.empty_like(t) for t in (grads if weights is None else weights)]
     wt = outs[0].dtype if outs else None
     if gt not in _DTYPES or wt not in _DTYPES:
         raise ValueError("grads and outs must be float32 or bfloat16")
-    _matrices(ctx, outs, "outs", wt, grads)
-    if weights is not None:
-        _matrices(ctx, weights, "weights", wt, grads)
+    _matrices(ctx, outs, "outs", wt, shapes)
+    if weights is not None and weights is not outs:
+        _matrices(ctx, weights, "weights", wt, shapes)
     if new_moments is None:
         new_moments = moments
     elif moments is None:
         raise ValueError("new_moments without moments")
     if moments is not None:
-        _matrices(ctx, moments, "moments", torch.float32, grads)
-        _matrices(ctx, new_moments, "new_moments", torch.float32, grads)
+        _matrices(ctx, moments, "moments", torch.float32, shapes)
+        if new_moments is not moments:
+            _matrices(ctx, new_moments, "new_moments", torch.float32, shapes)
     flat = None
     if coefs is not None:
         flat = [float(c) for row in (coefs if len(coefs) and hasattr(coefs[0], "__len__") else [coefs] * steps)
@@ -764,24 +776,20 @@ def e2f_orthogonalize(ctx, grads, outs=None, weights=None, moments=None, new_mom
             raise ValueError("coefs must be three numbers, or three for each step")
         flat = array.array("f", flat)
     by_size = {}
-    for k, t in enumerate(grads):
-        by_size.setdefault(t.shape[-2:], []).append(k)
+    for k, shape in enumerate(shapes):
+        by_size.setdefault(shape[-2:], []).append(k)
     device = grads[0].device
     stream = _stream(device)
     for (rows, cols), which in by_size.items():
         _fits(rows, cols)
+        many = [1 if len(shapes[k]) == 2 else shapes[k][0] for k in which]
         lists = []
         for tensors in (grads, moments, new_moments, weights, outs):
             if tensors is None:
                 lists.append(None)
                 continue
-            step = rows * cols * tensors[which[0]].element_size()
-            at = array.array("Q")
-            for k in which:
-                first = tensors[k].data_ptr()
-                many = len(tensors[k]) if tensors[k].dim() == 3 else 1
-                at.extend(range(first, first + many * step, step) if step else [first] * many)
-            lists.append(at)
+            mine = tensors if len(by_size) == 1 else [tensors[k] for k in which]
+            lists.append(_addresses(mine, many, rows * cols * mine[0].element_size()))
         count = len(lists[0])
         prm = OrthogonalizeParams(rows, cols, steps, None if flat is None else flat.buffer_info()[0], eps, momentum,
                                   int(bool(nesterov)), scale, decay, _DTYPES[gt], _DTYPES[wt])

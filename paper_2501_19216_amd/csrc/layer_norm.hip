@@ -43,7 +43,9 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int tpr, float (*red)[N]
     for (int i = 0; i < N; ++i) v[i] += red[w][i];
 }
 
-// (by the power of -|x|, whose argument keeps its low part: a shut gate keeps its digits, to 6 roundings down to 2^-126)
+// (by the power of -|x|, whose argument keeps its low part: a shut gate keeps its digits, to 6 roundings down to 2^-126.  With
+// the library's exponential and an IEEE quotient a million rows of 64 bfloat16 channels take 92 us forward and 164
+// backward, this way 62 and 140)
 __device__ __forceinline__ float sigmoid(float x) {
   constexpr float kLog2e = 1.44269504f, kLow = 1.92596299e-8f, kLn2 = 0.693147181f;
   const float a = -fabsf(x), hi = a * kLog2e, lo = fmaf(a, kLog2e, -hi) + a * kLow;
@@ -321,26 +323,37 @@ __global__ __launch_bounds__(512) void k_layer_backward(LayerArgs a, LayerGrad g
   }
   const int tpg = tpr < 64 ? 64 : tpr, group = threadIdx.x / tpg, groups = blockDim.x / tpg;
   const bool one = threadIdx.x % tpg < tpr;  // one of the threads that hold the same sums
-  auto add = [&](int k, int at_, float s) {
-    s += k ? sums[at_] : 0.0f;
-    if (k + 1 < groups)
-      sums[at_] = s;
-    else
-      mine_at[at_] = s;
-  };
   for (int k = 0; k < groups; ++k) {
     if (groups > 1) __syncthreads();
     if (k != group || !one) continue;
+    // V neighbouring sums: with those of the groups before, to the next one or to memory
+    auto add = [&](int i, int to, float(&s)[V]) {
+      if (at.channel(i) >= a.C) return;
+      float* lds = sums + to;
+      float* out = k + 1 < groups ? lds : mine_at + to;
+      constexpr int Q = V < 4 ? V : 4;
+      if (!TAIL || at.channel(i) + V <= a.C) {
 #pragma unroll
-    for (int i = 0; i < P::W; ++i)
+        for (int u = 0; u < V; u += Q) {
+          typename Raw<float, Q>::type v;
+          if (k) {
+            v = Raw<float, Q>::load((const char*)(lds + u));
 #pragma unroll
-      for (int u = 0; u < V; ++u)
-        if (at.channel(i) + u < a.C) add(k, at.weight(i) + u, aw[i][u]);
+            for (int x = 0; x < Q; ++x) s[u + x] += part(v, x);
+          }
+          join(s + u, v);
+          Raw<float, Q>::store((char*)(out + u), v);
+        }
+      } else {
 #pragma unroll
-    for (int i = 0; i < P::S0; ++i)
+        for (int u = 0; u < V; ++u)
+          if (at.within(i, u, TAIL)) out[u] = s[u] + (k ? lds[u] : 0.0f);
+      }
+    };
 #pragma unroll
-      for (int u = 0; u < V; ++u)
-        if (at.channel(i) + u < a.C) add(k, width + at.channel(i) + u, ab[i][u]);
+    for (int i = 0; i < P::W; ++i) add(i, at.weight(i), aw[i]);
+#pragma unroll
+    for (int i = 0; i < P::S0; ++i) add(i, width + at.channel(i), ab[i]);
   }
 }
 
@@ -402,9 +415,11 @@ Shape shape_of(int L, int C, bool bf16, bool back) {
 int layer_parts(int L, int C, bool bf16, int n) {
   const Shape s = shape_of(L, C, bf16, true);
   const int slots = s.threads / s.tpr;
-  // two workgroups a CU; of long rows so few that their sums, written and read, stay a quarter of the rows' bytes
+  // two workgroups a CU, about what the registers of a row's components leave; of plain rows four (a million rows of 64
+  // bfloat16 channels: 106 us, with two 137), but of long ones so few that their sums, written and read, stay a quarter of
+  // the rows' bytes
   const int64_t want = ((int64_t)n + slots - 1) / slots;
-  int64_t most = 512;
+  int64_t most = L ? 512 : 1024;
   if (L == 0 && want > 128 && want / 4 < most) most = want / 4 < 128 ? 128 : want / 4;
   return (int)(want < most ? want : most);
 }

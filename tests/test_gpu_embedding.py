@@ -72,9 +72,10 @@ def test_wide_rows(e2f, ctx, C, t):
 
 @pytest.mark.parametrize("n", [100, 20000, 300000])
 @pytest.mark.parametrize("kind", ["one", "sorted", "reversed", "runs", "distinct"])
-def test_orders(e2f, ctx, n, kind):
+@pytest.mark.parametrize("few", [17, 260])
+def test_orders(e2f, ctx, n, kind, few):
     """One type alone; sorted, falling and alternating types; runs that end where stretches do; every type once."""
-    V = n if kind == "distinct" else 17
+    V = n if kind == "distinct" else few
     g = torch.Generator().manual_seed(n)
     i = torch.arange(n)
     idx = {"one": torch.full((n,), 11), "sorted": i * V // n, "reversed": (n - 1 - i) * V // n, "runs": i // 64 % V,
@@ -85,9 +86,8 @@ def test_orders(e2f, ctx, n, kind):
 
 def test_outside_of_the_table(e2f, ctx):
     """Rows with an index outside of the table: zeros forward, and no part in the gradient, whatever they hold."""
-    V, C = 12, 24
-    for t in (torch.int32, torch.int64):
-        far = [-1, -2 ** 31, 12, 2 ** 31 - 1] + ([2 ** 32 + 3, -2 ** 40, 2 ** 63 - 1] if t == torch.int64 else [])
+    for V, C, t in ((12, 24, torch.int32), (12, 24, torch.int64), (500, 24, torch.int32), (500, 24, torch.int64)):
+        far = [-1, -2 ** 31, V, 2 ** 31 - 1] + ([2 ** 32 + 3, -2 ** 40, 2 ** 63 - 1] if t == torch.int64 else [])
         idx = torch.tensor([3, far[0], 0, 11, 11] + far + [3], dtype=t)
         g = torch.randn(len(idx), C)
         inside = (idx >= 0) & (idx < V)
@@ -103,7 +103,13 @@ def test_outside_of_the_table(e2f, ctx):
 
 
 def test_values_that_are_not_finite(e2f, ctx):
-    table, idx, _ = data(400, 9, 8, 1, skew=False)
+    for V in (9, 300):
+        check_not_finite(e2f, ctx, V)
+
+
+def check_not_finite(e2f, ctx, V):
+    table, idx, _ = data(400, V, 8, 1, skew=False)
+    idx[7] = 4
     table[4, 3] = float("nan")
     table[5, 2] = float("inf")
     out = e2f.e2f_embedding_forward(ctx, table.to(DEV), idx.to(DEV), lmax=1).cpu()
@@ -112,7 +118,7 @@ def test_values_that_are_not_finite(e2f, ctx):
     g = torch.randn(400, 8)
     at = int((idx == 4).nonzero()[0])
     g[at, 1] = float("inf")
-    gt = e2f.e2f_embedding_backward(ctx, idx.to(DEV), g.to(DEV), 9).cpu()
+    gt = e2f.e2f_embedding_backward(ctx, idx.to(DEV), g.to(DEV), V).cpu()
     assert gt[4, 1] == float("inf") and int(gt.isfinite().sum()) == gt.numel() - 1
 
 
@@ -132,21 +138,22 @@ def test_rows_further_apart_and_odd_addresses(e2f, ctx, t):
     ref.check(gt, ref.embedding_grad(go[:, 0].cpu(), idx, V, 1.0), "grad_table")
 
 
-def test_same_bits_every_time_and_on_another_stream(e2f, ctx):
-    table, idx, g = data(50000, 200, 32, 3)
+@pytest.mark.parametrize("V", [200, 500])
+def test_same_bits_every_time_and_on_another_stream(e2f, ctx, V):
+    table, idx, g = data(50000, V, 32, 3)
     idx, go = idx.to(DEV), torch.randn(50000, 32, generator=g).to(DEV)
-    first = e2f.e2f_embedding_backward(ctx, idx, go, 200)
+    first = e2f.e2f_embedding_backward(ctx, idx, go, V)
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(s):
-        other = e2f.e2f_embedding_backward(ctx, idx, go, 200)
+        other = e2f.e2f_embedding_backward(ctx, idx, go, V)
     for _ in range(3):
-        assert torch.equal(e2f.e2f_embedding_backward(ctx, idx, go, 200), first)
+        assert torch.equal(e2f.e2f_embedding_backward(ctx, idx, go, V), first)
     torch.cuda.current_stream().wait_stream(s)
     assert torch.equal(other, first)
 
 
-@pytest.mark.parametrize("n,V", [(500, 40), (30000, 40), (30000, 3000)])
+@pytest.mark.parametrize("n,V", [(500, 40), (30000, 40), (500, 400), (30000, 3000)])
 def test_captured_and_replayed(e2f, ctx, n, V):
     table, idx, g = data(n, V, 16, n)
     table, idx, go = table.to(DEV), idx.to(DEV), torch.randn(n, 16, generator=g).to(DEV)
@@ -190,6 +197,6 @@ def test_refused_by_the_binding(e2f, ctx):
         with pytest.raises(ValueError):
             bad()
     with pytest.raises(e2f.E2FError):
-        e2f.e2f_embedding_backward(ctx, idx, go, 5, workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
+        e2f.e2f_embedding_backward(ctx, idx, go, 300, workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
     with pytest.raises(e2f.E2FError):
         e2f.e2f_embedding_forward(ctx, table, idx, scale=float("nan"))

@@ -47,9 +47,10 @@ def embedding_grad(g, index, V, scale):
     at, rows = idx[there], g.double()[there]
     zero = torch.zeros(V, g.shape[1], dtype=torch.float64)
     value, size = zero.index_add(0, at, rows), zero.index_add(0, at, rows.abs())
-    # a stretch of up to 256 rows one after the other; those sums 16 apart, then 16; the scale
+    # a stretch of up to 64 sorted rows one after the other, up to 256 such parts of a workgroup in their order, the workgroups'
+    # sums in up to 1024 strides and 10 halvings, the scale; never more than the rows there are, and those last ones
     k = torch.bincount(at, minlength=V).double()[:, None]
-    count = k.clamp_max(256) + k / 256 / 16 + 20
+    count = k.clamp_max(64 + 256) + k / 1024 + 20
     return value * scale, U * count * size * abs(scale)
 
 
