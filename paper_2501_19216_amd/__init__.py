@@ -10,6 +10,7 @@ package raises: there is no fallback.
 from __future__ import annotations
 
 import array
+import bisect
 import ctypes
 import operator
 import os
@@ -184,7 +185,9 @@ def _ptr(t):
 
 
 def _stream(device=None):
-    return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+    """The handle of a device's current stream (without a stream object: 0.1 us instead of 2)."""
+    index = None if device is None else torch.device(device).index
+    return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if index is None else index))
 
 
 def _dev(t, dtype, name):
@@ -736,6 +739,18 @@ def _addresses(tensors, many, step):
     return array.array("Q", [a + i * step for a, n in zip(first, many) for i in range(n)])
 
 
+def _disjoint(outputs, inputs):
+    """Refuses lists of tensors in which an output lies over another tensor, but over one that it is."""
+    spans = lambda ts: [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in ts if t.numel()]  # noqa: E731
+    outs = sorted(s for ts in outputs for s in spans(ts))
+    if any(b[0] < a[1] for a, b in zip(outs, outs[1:])):
+        raise ValueError("two outputs overlap")
+    for lo, hi in (s for ts in inputs for s in spans(ts)):
+        k = bisect.bisect_left(outs, (hi, 0)) - 1  # the last that begins before the input's end
+        if k >= 0 and outs[k][1] > lo and outs[k] != (lo, hi):
+            raise ValueError("an output overlaps another tensor")
+
+
 def e2f_orthogonalize(ctx, grads, outs=None, weights=None, moments=None, new_moments=None, momentum=0.95,
                       nesterov=True, steps=5, coefs=None, scale=1.0, decay=0.0, eps=1e-7, workspace=None):
     """Orthogonalised updates of matrices (the step of the Muon optimiser):
@@ -778,6 +793,9 @@ def e2f_orthogonalize(ctx, grads, outs=None, weights=None, moments=None, new_mom
     by_size = {}
     for k, shape in enumerate(shapes):
         by_size.setdefault(shape[-2:], []).append(k)
+    if len(by_size) > 1:  # (the library sees the matrices of one size at a time)
+        _disjoint([t for t in (outs, new_moments) if t is not None],
+                  [t for t in (grads, moments, None if decay == 0 else weights) if t is not None])
     device = grads[0].device
     stream = _stream(device)
     for (rows, cols), which in by_size.items():

@@ -84,6 +84,16 @@ def test_orders(e2f, ctx, n, kind, few):
     both(e2f, ctx, table, idx, torch.randn(n, 20, generator=g).to(DEV), 0, 1.0, F32, F32)
 
 
+@pytest.mark.parametrize("n,V,C", [(700, 2000003, 4), (20000, 2000003, 4), (6000001, 50, 2), (2500000, 300, 1)])
+def test_large_tables_and_many_rows(e2f, ctx, n, V, C):
+    """Types of three digits; more workgroups of the sort than one round of its scan."""
+    g = torch.Generator(device=DEV).manual_seed(n)
+    idx = torch.randint(0, V, (n,), device=DEV, generator=g)
+    go = torch.randn(n, C, device=DEV, generator=g)
+    gt = e2f.e2f_embedding_backward(ctx, idx, go, V)
+    ref.check(gt, ref.embedding_grad(go.cpu(), idx.cpu(), V, 1.0), "grad_table")
+
+
 def test_outside_of_the_table(e2f, ctx):
     """Rows with an index outside of the table: zeros forward, and no part in the gradient, whatever they hold."""
     for V, C, t in ((12, 24, torch.int32), (12, 24, torch.int64), (500, 24, torch.int32), (500, 24, torch.int64)):

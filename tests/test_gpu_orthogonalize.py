@@ -158,6 +158,24 @@ def test_lists_of_stacks_and_sizes(e2f, ctx):
 
 
 @pytest.mark.parametrize("r,c", [(24, 40), (200, 140)])
+def test_in_place_of_several_sizes(e2f, ctx, r, c):
+    """Pieces of one buffer, matrices of several sizes, weights and momentum in place."""
+    shapes = [(r, c), (3, 5, 7), (r, c), (12, 9)]
+    sizes = [math.prod(s) for s in shapes]
+    g = torch.Generator().manual_seed(r)
+    flat = [torch.randn(sum(sizes), generator=g).to(DEV) for _ in range(3)]
+    cut = lambda t: [x.view(s) for x, s in zip(t.split(sizes), shapes)]  # noqa: E731
+    want = [t.clone() for t in flat]
+    kw = dict(scale=-0.1, decay=0.5)
+    for x, m, w in zip(cut(want[0]), cut(want[1]), cut(want[2])):
+        e2f.e2f_orthogonalize(ctx, [x], outs=[w], weights=[w], moments=[m], **kw)
+    grads, moments, weights = map(cut, flat)
+    e2f.e2f_orthogonalize(ctx, grads, outs=weights, weights=weights, moments=moments, **kw)
+    assert torch.equal(flat[0], want[0]) and torch.equal(flat[1], want[1])
+    assert float((flat[2] - want[2]).norm()) <= 1e-4 * float(want[2].norm())
+
+
+@pytest.mark.parametrize("r,c", [(24, 40), (200, 140)])
 def test_scales_of_the_gradient(e2f, ctx, r, c):
     """Values near the ends of the type's range; zeros; one value."""
     for s in (1e-30, 1e30, 1e37):
@@ -228,6 +246,7 @@ def test_same_bits_on_another_stream(e2f, ctx):
 
 def test_refused_by_the_binding(e2f, ctx):
     g = [torch.zeros(4, 6, device=DEV)]
+    flat, other = torch.zeros(49, device=DEV), torch.zeros(5, 5, device=DEV)
     for bad in (lambda: e2f.e2f_orthogonalize(ctx, [g[0].half()]), lambda: e2f.e2f_orthogonalize(ctx, [g[0].t()]),
                 lambda: e2f.e2f_orthogonalize(ctx, [g[0].cpu()]), lambda: e2f.e2f_orthogonalize(ctx, [g[0][0]]),
                 lambda: e2f.e2f_orthogonalize(ctx, [g[0], g[0].bfloat16()]),
@@ -235,6 +254,9 @@ def test_refused_by_the_binding(e2f, ctx):
                 lambda: e2f.e2f_orthogonalize(ctx, g, new_moments=[torch.zeros(4, 6, device=DEV)]),
                 lambda: e2f.e2f_orthogonalize(ctx, g, moments=[g[0].bfloat16()]),
                 lambda: e2f.e2f_orthogonalize(ctx, g, weights=[g[0].bfloat16()], outs=[torch.zeros(4, 6, device=DEV)]),
+                # (of matrices of two sizes)
+                lambda: e2f.e2f_orthogonalize(ctx, [flat[:24].view(4, 6), flat[24:].view(5, 5)], outs=[flat[20:44].view(4, 6), other]),
+                lambda: e2f.e2f_orthogonalize(ctx, [g[0], other], outs=[flat[:24].view(4, 6), flat[23:48].view(5, 5)]),
                 lambda: e2f.e2f_orthogonalize(ctx, g, coefs=(1.0, 2.0)), lambda: e2f.e2f_orthogonalize(ctx, g, coefs=[(1, 0, 0)] * 4)):
         with pytest.raises(ValueError):
             bad()
