@@ -399,11 +399,9 @@ Shape shape_of(int L, int C, bool bf16, bool back) {
     const int pieces = (C + s.V - 1) / s.V;
     s.tpr = 1, s.J = 1;
     while (s.tpr < 64 && s.tpr < pieces) s.tpr <<= 1;
-    while (s.tpr * s.J < pieces)
-      if (s.J < 2 || s.tpr == 512)
-        s.J <<= 1;
-      else
-        s.tpr <<= 1;
+    if (s.tpr < pieces) s.J = 2;
+    while (s.tpr < 512 && s.tpr * s.J < pieces) s.tpr <<= 1;
+    if (s.tpr * s.J < pieces) s.J = (pieces + s.tpr - 1) / s.tpr;  // (three or four)
     s.tail = C % s.V != 0;
   }
   s.threads = s.tpr <= 256 ? 256 : s.tpr;
@@ -416,11 +414,11 @@ int layer_parts(int L, int C, bool bf16, int n) {
   const Shape s = shape_of(L, C, bf16, true);
   const int slots = s.threads / s.tpr;
   // two workgroups a CU, about what the registers of a row's components leave; of plain rows four (a million rows of 64
-  // bfloat16 channels: 106 us, with two 137), but of long ones so few that their sums, written and read, stay a quarter of
-  // the rows' bytes
+  // bfloat16 channels: 106 us, with two 137), but of long ones one for two rows, whose sums, written and read, are then as
+  // many bytes as the rows' (517 rows of 5,001: 21 us with the sums' sum, 25 with one a row, 24 with one for four)
   const int64_t want = ((int64_t)n + slots - 1) / slots;
   int64_t most = L ? 512 : 1024;
-  if (L == 0 && want > 128 && want / 4 < most) most = want / 4 < 128 ? 128 : want / 4;
+  if (L == 0 && want > 128 && want / 2 < most) most = want / 2 < 128 ? 128 : want / 2;
   return (int)(want < most ? want : most);
 }
 
@@ -453,12 +451,12 @@ int layer_parts(int L, int C, bool bf16, int n) {
 #define E2F_LAYER_SWITCH(VB)                                              \
   if (L == 0 && bf16) {                                                   \
     switch (s.J) {                                                        \
-      E2F_LAYER_J(bf16_t, 8, 1) E2F_LAYER_J(bf16_t, VB, 2) E2F_LAYER_J(bf16_t, VB, 4) \
+      E2F_LAYER_J(bf16_t, 8, 1) E2F_LAYER_J(bf16_t, VB, 2) E2F_LAYER_J(bf16_t, VB, 3) E2F_LAYER_J(bf16_t, VB, 4) \
       default: return hipErrorInvalidValue;                               \
     }                                                                     \
   } else if (L == 0) {                                                    \
     switch (s.J) {                                                        \
-      E2F_LAYER_J(float, 4, 1) E2F_LAYER_J(float, 4, 2) E2F_LAYER_J(float, 4, 4) \
+      E2F_LAYER_J(float, 4, 1) E2F_LAYER_J(float, 4, 2) E2F_LAYER_J(float, 4, 3) E2F_LAYER_J(float, 4, 4) \
       default: return hipErrorInvalidValue;                               \
     }                                                                     \
   } else {                                                                \
