@@ -1,11 +1,18 @@
-// Rows of a table by the types of atoms (of edges, of tokens), as the scalars of irrep features, and the table's gradient:
+// Rows of a table by the types of atoms (of edges, of tokens), as the scalars of irrep features, and the table's
+// gradient:
 //   out[i][0][c] = s T[z_i][c],   out[i][k][c] = 0 for the components k >= 1,   0 for z_i outside of the table,
 //   dT[v][c] = s sum over the i with z_i = v of g[i][0][c].
-// The forward reads a row and writes one: memory.  The gradient sorts the rows by their types (a stable sort by digits of 8
-// bits, so that a type's rows keep their order) and sums them in stretches of the sorted order, as many rows each whatever
-// the types are: a type that holds half of all rows costs no more than many small ones.  A stretch writes the sums of the
-// types that begin and end in it; of one that goes on it keeps the part, and a last kernel adds a type's parts in
-// their order and writes zeros for types without rows.  No atomics: the same bits every time.
+// The forward reads a row and writes one: memory.  The gradient sorts the rows by their types (a stable sort by
+// digits of 8 bits, so that a type's rows keep their order) and sums them in stretches of the sorted order, as many
+// rows each whatever the types are: a type that holds half of all rows costs no more than many small ones.  A stretch
+// writes the sums of the types that begin and end in it; of one that goes on it keeps the part, and a last kernel
+// adds a type's parts in their order and writes zeros for types without rows.  No float atomics: the same bits every
+// time.
+//
+// 20,000 atoms of 100 types, L = 4, 128 channels: 49 us forward (256 MB at the rate of a copy), 25 backward in five
+// kernels of 4 to 8 us.  1.5 million rows of 64 bfloat16 channels of 100 types: 41 us forward, 97 backward, of which
+// the sort 25 and the sums 64 (192 MB of rows gathered at 3 TB/s, whatever the length of a stretch).  16,384 tokens
+// of 32,768 types, 1,024 bfloat16 channels: 9 us forward, 50 backward, of which 20 are the zeros of absent types.
 #include <hip/hip_runtime.h>
 
 #include "e2f_launch.h"
@@ -106,8 +113,8 @@ __device__ __forceinline__ void read_types(const void* index, const int* keys, i
   }
 }
 
-// Numbers of each digit in each workgroup's rows: counts [256][workgroups].  The first pass also clears the types' first
-// rows
+// Numbers of each digit in each workgroup's rows: counts [256][workgroups].  The first pass also clears the types'
+// first rows
 template <typename I, int R>
 __global__ __launch_bounds__(256) void k_embed_count(const void* __restrict__ index, const int* __restrict__ keys, int n,
                                                      int V, int shift, int* __restrict__ counts, int* __restrict__ first) {
@@ -273,8 +280,8 @@ struct Sorted {
   int per, wide;  // rows of a stretch, of a workgroup
 };
 
-// tpr threads a stretch, each V neighbouring channels; blocks of tpr V channels along y; a workgroup's stretches side by
-// side, joined in the LDS: of the parts that go on from one to the next only the workgroup's own two are left
+// tpr threads a stretch, each V neighbouring channels; blocks of tpr V channels along y; a workgroup's stretches side
+// by side, joined in the LDS: of the parts that go on from one to the next only the workgroup's own two are left
 template <typename TT, typename T, int V>
 __global__ __launch_bounds__(256) void k_embed_sums(EmbedArgs a, const T* __restrict__ g, Sorted s, TT* __restrict__ gt,
                                                     int tpr) {
@@ -373,8 +380,8 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedArgs a, const T* __rest
 
 // What no workgroup held whole: zeros for a type without rows, and the parts of one that several workgroups hold, V
 // channels a lane.  A wave takes up to kEach types, taken far apart (types that many rows have stand side by side in
-// most numberings); where a type has more than kMany parts all threads of its workgroup add them, as many side by side as
-// the channels leave room for
+// most numberings); where a type has more than kMany parts all threads of its workgroup add them, as many side by
+// side as the channels leave room for
 constexpr int kMany = 32, kEach = 8;
 template <typename TT, int V>
 __global__ __launch_bounds__(1024) void k_embed_join(EmbedArgs a, Sorted s, TT* __restrict__ gt, unsigned apart, int each,

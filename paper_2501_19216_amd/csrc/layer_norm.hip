@@ -8,10 +8,14 @@
 //   dz = g_0, or g_0 sigma(z) (1 + z (1 - sigma(z))),   u = w_0 dz,
 //   dx_0 = r0 (u - mean u - h mean(u h)),   dw_0 = sum of dz h,   db = sum of dz  over the atoms,
 //   dx_l = r1 u_l - r1^3 a_l x_l (sum of u x),  u_l = w_l g_l,   dw_l = sum of g x r1 over (atom, m).
-// Every value is read once and written once.  A row stays in registers between its reductions; the variance is taken of the
-// differences from the mean, so that rows far from zero keep their digits.  The backward takes the row's statistics from x
-// again, which it reads anyway: nothing is kept from the forward.  Sums, statistics and everything between loads
-// and stores are float; outputs are rounded once.
+// Every value is read once and written once.  A row stays in registers between its reductions; the variance is taken
+// of the differences from the mean, so that rows far from zero keep their digits.  The backward takes the row's
+// statistics from x again, which it reads anyway: nothing is kept from the forward.  Sums, statistics and everything
+// between loads and stores are float; outputs are rounded once.
+//
+// 20,000 atoms, L = 4, 128 float channels: 86 us forward, 154 backward and 5 for the weights' sums, the rate of a
+// copy (5.1 TB/s) for all that is read and written.  A million rows of 64 bfloat16 channels with their activation: 62
+// us forward (4.1 TB/s), 106 backward (3.6), where the activation's arithmetic begins to show.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -43,9 +47,9 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int tpr, float (*red)[N]
     for (int i = 0; i < N; ++i) v[i] += red[w][i];
 }
 
-// (by the power of -|x|, whose argument keeps its low part: a shut gate keeps its digits, to 6 roundings down to 2^-126.  With
-// the library's exponential and an IEEE quotient a million rows of 64 bfloat16 channels take 92 us forward and 164
-// backward, this way 62 and 140)
+// (by the power of -|x|, whose argument keeps its low part: a shut gate keeps its digits, to 6 roundings down to
+// 2^-126.  With the library's exponential and an IEEE quotient a million rows of 64 bfloat16 channels take 92 us
+// forward and 164 backward, this way 62 and 140)
 __device__ __forceinline__ float sigmoid(float x) {
   constexpr float kLog2e = 1.44269504f, kLow = 1.92596299e-8f, kLn2 = 0.693147181f;
   const float a = -fabsf(x), hi = a * kLog2e, lo = fmaf(a, kLog2e, -hi) + a * kLow;
@@ -413,9 +417,10 @@ Shape shape_of(int L, int C, bool bf16, bool back) {
 int layer_parts(int L, int C, bool bf16, int n) {
   const Shape s = shape_of(L, C, bf16, true);
   const int slots = s.threads / s.tpr;
-  // two workgroups a CU, about what the registers of a row's components leave; of plain rows four (a million rows of 64
-  // bfloat16 channels: 106 us, with two 137), but of long ones one for two rows, whose sums, written and read, are then as
-  // many bytes as the rows' (517 rows of 5,001: 21 us with the sums' sum, 25 with one a row, 24 with one for four)
+  // two workgroups a CU, about what the registers of a row's components leave; of plain rows four (a million rows of
+  // 64 bfloat16 channels: 106 us, with two 137), but of long ones one for two rows, whose sums, written and read, are
+  // then as many bytes as the rows' (517 rows of 5,001: 21 us with the sums' sum, 25 with one a row, 24 with one for
+  // four)
   const int64_t want = ((int64_t)n + slots - 1) / slots;
   int64_t most = L ? 512 : 1024;
   if (L == 0 && want > 128 && want / 2 < most) most = want / 2 < 128 ? 128 : want / 2;

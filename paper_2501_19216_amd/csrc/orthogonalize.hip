@@ -1,21 +1,31 @@
-// Orthogonalised updates of matrices (the update rule of the Muon optimiser): of the gradient G, or of what the momentum
-// makes of it,
+// Orthogonalised updates of matrices (the update rule of the Muon optimiser): of the gradient G, or of what the
+// momentum makes of it,
 //   M' = mu M + G,   U = G + mu M' (Nesterov) or M',
 // the matrix with U's singular vectors and singular values near one, by Newton-Schulz steps
 //   X = U / (|U|_F + eps),   P = X X^T,   X <- a X + (b P + c P^2) X,
 // and the weights W' = decay W + scale X.
 //
-// X stands with its shorter side as rows (m <= n), so that P is m x m: m^2 n + m^3 + 2 m^2 n operations a step, of which
-// the products of a matrix with its own transpose need one triangle.  The steps raise the smallest singular values by up to a^steps,
-// and with them whatever rounding the large ones left in their directions: products of 11 bits end 1e-3 from the exact
-// matrix and sums over a X of 22 bits 3e-5, where float gives 1e-5 (200 x 333, an eighth of the directions strong).  So X stays float and
-// a X is added in float; the products, whose errors stay in the directions that are already large, take their operands as two float16 numbers,
-// x = hi + lo to 22 bits, in three products (hi hi, hi lo, lo hi) on the matrix cores, summed in float.  Powers of two keep the
-// operands in float16's range: from the coefficients follow bounds of all singular values (ortho_bounds).
+// X stands with its shorter side as rows (m <= n), so that P is m x m: m^2 n + m^3 + 2 m^2 n operations a step, of
+// which the products of a matrix with its own transpose need one triangle.  The steps raise the smallest singular
+// values by up to a^steps, and with them whatever rounding the large ones left in their directions: products of 11
+// bits end 3e-4 from the exact matrix, of 22 bits with a X among them 2e-5, where float gives 1e-5 (200 x 333, a
+// sixteenth of the directions strong and the others a hundredth of them).  So X stays float and a X is added in
+// float, which gives 1e-5 too; the products, whose errors stay in the directions that are already large, take their
+// operands as two float16 numbers, x = hi + lo to 22 bits, in three products (hi hi, hi lo, lo hi) on the matrix
+// cores, summed in float.  Powers of two keep the operands in float16's range: from the coefficients follow bounds of
+// all singular values (ortho_bounds).
 //
-// Matrices that fit a workgroup's registers and LDS go through all steps there (k_ortho_small); larger ones through three
-// tiled products a step.  Those hold Y = X^T alone: Y' = a Y + Y B (B = b P + c P^2 is symmetric) reads rows of Y and of B,
-// and P = Y^T Y reads its operands by the LDS's transposing loads.
+// Matrices that fit a workgroup's registers and LDS go through all steps there (k_ortho_small); larger ones through
+// three tiled products a step.  Those hold Y = X^T alone: Y' = a Y + Y B (B = b P + c P^2 is symmetric) reads rows of
+// Y and of B, and P = Y^T Y reads its operands by the LDS's transposing loads.
+//
+// Sixty matrices of 128 x 128 with momentum and weights take 50 us in one launch (three tiled products a step 151, of
+// which launches are the most), of which a step is 7.4: matrix cores 3.3, reads of the LDS and four barriers between
+// the phases, two waves a SIMD.  Four of 1024 x 4096 take 1.15 ms, 244 TFLOP/s (library products in float 72): P 80
+// us a step, P^2 27, B X 118, the norm and the first Y 91.  B X is the sum of what its parts take alone: the matrix
+// cores 45, the loads to the LDS 60 (20 bytes a cycle and CU), the float and split Y 41; more buffers of a step,
+// tiles of 256, loads issued before the LDS is read, priorities of waves and other strides of memory left it where it
+// is.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -51,8 +61,8 @@ __device__ __forceinline__ void split(v4f x, float scale, h4& hi, h4& lo) {
 }
 __device__ __forceinline__ h8 both(h4 a, h4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 __device__ __forceinline__ v4f mfma(h8 a, h8 b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-// c += the products of operands split in two, the small parts first, and of all tiles one after the other: neighbours in the
-// matrix cores' queue wait for no result
+// c += the products of operands split in two, the small parts first, and of all tiles one after the other: neighbours
+// in the matrix cores' queue wait for no result
 template <int A, int B>
 __device__ __forceinline__ void products(const h8 (&ah)[A], const h8 (&al)[A], const h8 (&bh)[B], const h8 (&bl)[B],
                                          v4f (&c)[A][B]) {
@@ -69,16 +79,16 @@ __device__ __forceinline__ void products(const h8 (&ah)[A], const h8 (&al)[A], c
 #pragma unroll
     for (int j = 0; j < B; ++j) c[i][j] = mfma(ah[i], bh[j], c[i][j]);
 }
-// Transposing load: of 16 lanes, lane s gives the address of four neighbours of row s / 4, from column 4 (s % 4) on, and lane
-// t gets the four rows' values of column t
+// Transposing load: of 16 lanes, lane s gives the address of four neighbours of row s / 4, from column 4 (s % 4) on,
+// and lane t gets the four rows' values of column t
 __device__ __forceinline__ h4 read_transposed(const _Float16* p) {
   return __builtin_bit_cast(h4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)p));
 }
 
-// 64 lanes' 16 bytes each to the LDS, lane after lane from `to` (the same for the wave) on, without passing registers.  By
-// hand: the compiler, which cannot tell the LDS's buffers apart, would wait for all such loads before any read of the LDS.
-// The instruction has no register for its result; who reads what it brings waits for vmcnt first, by hand as well.  (Nothing
-// else in a kernel that calls this uses m0.)
+// 64 lanes' 16 bytes each to the LDS, lane after lane from `to` (the same for the wave) on, without passing
+// registers.  By hand: the compiler, which cannot tell the LDS's buffers apart, would wait for all such loads before
+// any read of the LDS. The instruction has no register for its result; who reads what it brings waits for vmcnt
+// first, by hand as well.  (Nothing else in a kernel that calls this uses m0.)
 __device__ __forceinline__ void load_past(const _Float16* from, _Float16* to) {
   const unsigned at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) _Float16*)to);
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory");
@@ -166,23 +176,24 @@ struct Rows {
   static constexpr size_t bytes(int np) { return sizeof(_Float16) * 2 * ((size_t)np * X + (size_t)MP * P); }
 };
 
-// A matrix of up to MP rows and 128 S columns, a workgroup of eight waves each.  A wave holds S strips of 16 columns of X in
-// registers as the matrix cores return them: lane l has rows 4 (l / 16) .. + 3 of every 16 and column l % 16.  These rows, of two
-// 16s, are also what it gives as the right operand of B X, so B's columns are stored in that order (within 32: 16 h + 4 g + e
-// at 8 g + 4 h + e).  X^T lies in the LDS for P.  P, and B that replaces it, are symmetric: a tile is stored as
-// its transpose
+// A matrix of up to MP rows and 128 S columns, a workgroup of eight waves each.  A wave holds S strips of 16 columns
+// of X in registers as the matrix cores return them: lane l has rows 4 (l / 16) .. + 3 of every 16 and column l %
+// 16.  These rows, of two 16s, are also what it gives as the right operand of B X, so B's columns are stored in that
+// order (within 32: 16 h + 4 g + e at 8 g + 4 h + e).  X^T lies in the LDS for P.  P, and B that replaces it, are
+// symmetric: a tile is stored as its transpose
 template <int MP, int S, typename TG, typename T>
 __global__ __launch_bounds__(512) void k_ortho_small(Table t, Ends e, Steps steps, Sizes d, Update u) {
   constexpr int MT = MP / 16, SX = Rows<MP>::X, SP = Rows<MP>::P;
-  // P's tiles of a wave, in a row: of six and eight rows of tiles the one on the diagonal and half of the row's others, in a
-  // circle, each written at both its places; of fewer all tiles, shared by the eight waves
+  // P's tiles of a wave, in a row: of six and eight rows of tiles the one on the diagonal and half of the row's
+  // others, in a circle, each written at both its places; of fewer all tiles, shared by the eight waves
   constexpr bool BAND = MT >= 6;
   constexpr int BC = BAND ? MT / 2 + 1 : MT / 2, COLS = MT / BC;
   extern __shared__ __align__(16) _Float16 lds[];
   __shared__ double squares[8];
   _Float16 *xh = lds, *xl = xh + d.np * SX, *ph = xl + d.np * SX, *pl = ph + MP * SP;
   const int z = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
-  // the update's four neighbours of the caller's matrix from `at` on, of which `have` are there; the momentum on the way
+  // the update's four neighbours of the caller's matrix from `at` on, of which `have` are there; the momentum on the
+  // way
   auto update = [&](int64_t at, int have) {
     v4f v = values<TG>(t.g[z], at, have);
     if (t.m[z]) {
@@ -455,21 +466,22 @@ struct Product {
   int mp, np;
 };
 
-// One tile of TILE x TILE of  sum_k p[i][k] q[j][k]  (GRAM: p[k][i] q[k][j]), WI x WJ waves, or WK times as many that take the
-// steps in turn and add their sums at the end, with ST buffers of a (WK) step(s) in the
-// LDS: the values of ST - 1 steps are on their way there, without passing registers, while one step's products run.
-// GRAM and POLY are symmetric: the tiles on and below the diagonal, each written at both its places.  A lane has four neighbouring
-// rows i of a column j, which are neighbours in memory at row j of Y, and of the symmetric P and B.
+// One tile of TILE x TILE of  sum_k p[i][k] q[j][k]  (GRAM: p[k][i] q[k][j]), WI x WJ waves, or WK times as many that
+// take the steps in turn and add their sums at the end, with ST buffers of a (WK) step(s) in the LDS: the values of
+// ST - 1 steps are on their way there, without passing registers, while one step's products run. GRAM and POLY are
+// symmetric: the tiles on and below the diagonal, each written at both its places.  A lane has four neighbouring rows
+// i of a column j, which are neighbours in memory at row j of Y, and of the symmetric P and B.
 //
-// In the LDS a row of 128 bytes (GRAM: of 4 TILE bytes) has its 16 bytes at position c ^ row % 8 (its 32 bytes at c ^ a number
-// of the row): lanes that read together meet different banks, and the loads, which write 64 x 16 bytes in
+// In the LDS a row of 128 bytes (GRAM: of 4 TILE bytes) has its 16 bytes at position c ^ row % 8 (its 32 bytes at c ^
+// a number of the row): lanes that read together meet different banks, and the loads, which write 64 x 16 bytes in
 // their order, read the places that belong there
 template <int KIND, int TILE, int WI, int WJ, int WK, int ST, typename T>
 __global__ __launch_bounds__(64 * WI * WJ * WK) void k_ortho_product(Product g, Ends e, Sizes d, Update u) {
   constexpr int FI = TILE / 16 / WI, FJ = TILE / 16 / WJ, N = TILE / 8 / (WI * WJ);  // N: loads of a wave and operand
   __shared__ __align__(16) _Float16 lds[ST][WK][2][TILE * 64];
   static_assert(sizeof(lds) >= sizeof(float) * TILE * TILE, "a tile of floats");
-  // neighbouring workgroups lie on different dies: each die takes a stretch of neighbouring tiles, which share rows in its L2
+  // neighbouring workgroups lie on different dies: each die takes a stretch of neighbouring tiles, which share rows
+  // in its L2
   const int all = g.tiles * g.count, each = (all + 7) >> 3, at_ = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
   if (at_ >= all || (int)(blockIdx.x >> 3) >= each) return;
   const int z = at_ / g.tiles, tile = at_ % g.tiles;
@@ -537,8 +549,8 @@ __global__ __launch_bounds__(64 * WI * WJ * WK) void k_ortho_product(Product g, 
   }
   int buf = 0, to = ST - 1;
   for (int s = 0; s < steps; ++s) {
-    // this step's values are there (those of the steps behind it may be on their way), and the buffer that is filled next has
-    // been read by every wave
+    // this step's values are there (those of the steps behind it may be on their way), and the buffer that is filled
+    // next has been read by every wave
     if (s + ST - 1 <= steps)
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((ST - 2) * 2 * N) : "memory");
     else
@@ -600,7 +612,8 @@ __global__ __launch_bounds__(64 * WI * WJ * WK) void k_ortho_product(Product g, 
             s *= u.scale;
             puts<T>(e.out[z], at, d.m - i, e.w[z] ? s + u.decay * values<T>(e.w[z], at, d.m - i) : s);
           } else {
-            // the caller's rows are i: by the LDS, 16 columns at a place that goes by the row (four lanes' rows meet other banks)
+            // the caller's rows are i: by the LDS, 16 columns at a place that goes by the row (four lanes' rows meet
+            // other banks)
 #pragma unroll
             for (int k = 0; k < 4; ++k) turn[(i - i0 + k) * TILE + ((j - j0) ^ (lg * 16))] = s[k];
           }
@@ -655,9 +668,11 @@ Sizes sizes_of(int rows, int cols, int count, bool* small, int* tile) {
   d.rows = rows, d.cols = cols, d.turned = rows >= cols;  // (of square ones the transpose, whose columns are rows in memory)
   d.m = d.turned ? cols : rows, d.n = d.turned ? rows : cols;
   d.mp = small_rows(d.m), d.np = (d.n + 31) / 32 * 32;
+  // (sixty of 128 x 128 46 us, by tiled products 96; one 44 and 77, 200 of them 180 and 367)
   *small = d.mp && d.np <= 512 && small_bytes(d.mp, d.np) <= kLds;
   if (*small) return d;
-  // tiles of 128, each value of which is read from the LDS half as often, where they fill the GPU
+  // tiles of 128, each value of which is loaded and read from the LDS half as often, where they fill the GPU (four
+  // matrices of 1024 x 4096 1.19 ms, with tiles of 64 1.32; 64 of 512 x 512 1.00 and 1.11)
   const int64_t big = (int64_t)((d.m + 127) / 128) * ((d.n + 127) / 128);
   *tile = big * (count < kTable ? count : kTable) >= 512 ? 128 : 64;
   d.mp = (d.m + *tile - 1) / *tile * *tile, d.np = (d.n + *tile - 1) / *tile * *tile;
@@ -783,7 +798,7 @@ void launch_product(int tile, Product g, const Ends& e, const Sizes& d, const Up
   const unsigned blocks = (unsigned)((g.tiles * g.count + 7) / 8 * 8);
   if (tile == 128)
     k_ortho_product<KIND, 128, 2, 4, 1, 2, T><<<blocks, 512, 0, st>>>(g, e, d, u);
-  else if (g.tiles * g.count <= 256)
+  else if (g.tiles * g.count <= 256 && g.steps >= 16)  // (300 x 3000 202 us, with four waves 245)
     k_ortho_product<KIND, 64, 2, 2, 2, 3, T><<<blocks, 512, 0, st>>>(g, e, d, u);
   else
     k_ortho_product<KIND, 64, 2, 2, 1, 3, T><<<blocks, 256, 0, st>>>(g, e, d, u);
