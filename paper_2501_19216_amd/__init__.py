@@ -186,7 +186,9 @@ def _ptr(t):
 
 def _stream(device=None):
     """The handle of a device's current stream (without a stream object: 0.1 us instead of 2)."""
-    index = None if device is None else torch.device(device).index
+    if device is not None and not isinstance(device, torch.device):
+        device = torch.device(device)
+    index = None if device is None else device.index
     return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if index is None else index))
 
 

@@ -136,7 +136,7 @@ def test_numbers_of_steps(e2f, ctx, steps, r, c):
 def test_lists_of_stacks_and_sizes(e2f, ctx):
     """Stacks and matrices of several sizes in one call, more of one size than a launch holds."""
     g = torch.Generator().manual_seed(1)
-    shapes = [(5, 12, 12), (8, 30), (3, 12, 12), (8, 30), (130, 12, 12), (67, 140, 130), (1, 70, 8), (0, 4, 4), (6, 6)]
+    shapes = [(5, 12, 12), (8, 30), (3, 12, 12), (8, 30), (130, 12, 12), (67, 140, 130), (1, 70, 8), (0, 4, 4), (6, 6), (0, 5), (5, 0), (2, 0, 3)]
     grads = [torch.randn(*s, generator=g).to(DEV) for s in shapes]
     outs = e2f.e2f_orthogonalize(ctx, grads, scale=0.5)
     for x, o in zip(grads, outs):
