@@ -671,10 +671,12 @@ Sizes sizes_of(int rows, int cols, int count, bool* small, int* tile) {
   // (sixty of 128 x 128 46 us, by tiled products 96; one 44 and 77, 200 of them 180 and 367)
   *small = d.mp && d.np <= 512 && small_bytes(d.mp, d.np) <= kLds;
   if (*small) return d;
-  // tiles of 128, each value of which is loaded and read from the LDS half as often, where they fill the GPU (four
-  // matrices of 1024 x 4096 1.19 ms, with tiles of 64 1.32; 64 of 512 x 512 1.00 and 1.11)
-  const int64_t big = (int64_t)((d.m + 127) / 128) * ((d.n + 127) / 128);
-  *tile = big * (count < kTable ? count : kTable) >= 512 ? 128 : 64;
+  // tiles of 128, each value of which is loaded and read from the LDS half as often, where they fill the GPU and pad
+  // little (four matrices of 1024 x 4096 1.19 ms, with tiles of 64 1.32; one 456 us and 498; 64 of 512 x 512 1.00 and 1.11
+  // ms; but 30 of 400 x 400, which become 512, 501 and 382 us)
+  const int64_t tiles = (int64_t)((d.m + 127) / 128) * ((d.n + 127) / 128);
+  const int64_t fine = (int64_t)((d.m + 63) / 64) * ((d.n + 63) / 64);
+  *tile = tiles * (count < kTable ? count : kTable) >= 256 && 40 * tiles <= 11 * fine ? 128 : 64;
   d.mp = (d.m + *tile - 1) / *tile * *tile, d.np = (d.n + *tile - 1) / *tile * *tile;
   return d;
 }

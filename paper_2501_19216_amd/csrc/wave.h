@@ -1,5 +1,5 @@
 // Sums and maxima over neighbouring lanes of a wave, the same bits in every lane
-// (block_norm.hip, graph_attention.hip): four exchanges inside a row of 16 lanes
+// (block_norm.hip, layer_norm.hip, graph_attention.hip): four exchanges inside a row of 16 lanes
 // by data-parallel moves and two across rows by permlane swaps, none of which
 // goes through the LDS.
 #pragma once
