@@ -275,7 +275,7 @@ __global__ __launch_bounds__(1024) void k_embed_sort(const void* __restrict__ in
 // ------------------------------------------------------------------ sums
 struct Sorted {
   const int *keys, *rows;
-  int* range;   // [V] first place of a type in the sorted order, or -1, then [V] one past its last
+  int *first, *end;  // [V] first place of a type in the sorted order, or -1, and [V] one past its last
   float* part;  // [workgroups][2][C]: of the type that began before the workgroup's rows, of the one that goes on behind
   int per, wide;  // rows of a stretch, of a workgroup
 };
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedArgs a, const T* __rest
         write(key);
       }
     }
-    if (lead && !behind && key >= 0 && key < a.V) s.range[a.V + key] = p;
+    if (lead && !behind && key >= 0 && key < a.V) s.end[key] = p;
 #pragma unroll
     for (int u = 0; u < V; ++u) sum[u] = 0.0f;
   };
@@ -339,7 +339,7 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedArgs a, const T* __rest
       if (k[u] != key) {
         flush(p + u, k[u]);
         key = k[u], before = false;
-        if (lead && key < a.V) s.range[key] = p + u;
+        if (lead && key < a.V) s.first[key] = p + u;
       }
 #pragma unroll
       for (int x = 0; x < V; ++x) sum[x] += part(v[u], x);
@@ -404,7 +404,7 @@ __global__ __launch_bounds__(1024) void k_embed_join(EmbedArgs a, Sorted s, TT* 
   // the ranges of the wave's `each` types, a lane one
   const int64_t mine = group + ((int64_t)lane * 16 + wave) * apart;
   const bool is = lane < each && group < apart && mine < a.V;
-  const int first = is ? s.range[mine] : 0, end = is && first >= 0 ? s.range[a.V + mine] : 0;
+  const int first = is ? s.first[mine] : 0, end = is && first >= 0 ? s.end[mine] : 0;
   const int q0 = first < 0 ? 0 : first / s.wide, q1 = end > first ? (end - 1) / s.wide : q0;
   if (lane < each) many[lane * 16 + wave] = is && q1 - q0 >= kMany;
   const uint64_t todo = __ballot(is && (first < 0 || (q1 > q0 && q1 - q0 < kMany)));
@@ -426,7 +426,7 @@ __global__ __launch_bounds__(1024) void k_embed_join(EmbedArgs a, Sorted s, TT* 
   for (int w = 0; w < 16 * each; ++w) {
     if (!many[w]) continue;
     const int64_t type = group + (int64_t)w * apart;
-    const int b = s.range[type] / s.wide, e = (s.range[a.V + type] - 1) / s.wide;
+    const int b = s.first[type] / s.wide, e = (s.end[type] - 1) / s.wide;
     for (int c0 = blockIdx.y * tpr * V; c0 < a.C; c0 += gridDim.y * tpr * V) {
       const int c = c0 + t * V;
       float sum[V] = {};
@@ -577,7 +577,7 @@ hipError_t launch_embed_backward(const EmbedArgs& a, const void* gout, void* gta
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const Sorted s{keys[now], rows[now], range, (float*)(ws + l.part), l.per, l.wide};
+  const Sorted s{keys[now], rows[now], range, range + a.V, (float*)(ws + l.part), l.per, l.wide};
   if (a.n) {
     const int V = pieces_of(a.C, a.bf16);
     const dim3 grid(l.blocks, (unsigned)((a.C / V + l.tpr - 1) / l.tpr));
