@@ -742,15 +742,19 @@ def _addresses(tensors, many, step):
 
 
 def _disjoint(outputs, inputs):
-    """Refuses lists of tensors in which an output lies over another tensor, but over one that it is."""
-    spans = lambda ts: [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in ts if t.numel()]  # noqa: E731
-    outs = sorted(s for ts in outputs for s in spans(ts))
+    """Refuses lists of tensors in which an output lies over another tensor, but over the one of its own number that it
+    replaces.  inputs: lists, or None; outputs: (a list, which of the inputs' lists it replaces, -1: none)."""
+    span = lambda t: (t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())  # noqa: E731
+    outs = sorted((*span(t), which, i) for ts, which in outputs for i, t in enumerate(ts) if t.numel())
     if any(b[0] < a[1] for a, b in zip(outs, outs[1:])):
         raise ValueError("two outputs overlap")
-    for lo, hi in (s for ts in inputs for s in spans(ts)):
-        k = bisect.bisect_left(outs, (hi, 0)) - 1  # the last that begins before the input's end
-        if k >= 0 and outs[k][1] > lo and outs[k] != (lo, hi):
-            raise ValueError("an output overlaps another tensor")
+    for which, ts in enumerate(inputs):
+        for i, t in enumerate(ts or ()):
+            lo, hi = span(t)
+            # (the outputs are disjoint: the last that begins before the input's end is the one that ends last)
+            k = bisect.bisect_left(outs, (hi,)) - 1
+            if lo < hi and k >= 0 and outs[k][1] > lo and outs[k] != (lo, hi, which, i):
+                raise ValueError("an output overlaps another tensor")
 
 
 def e2f_orthogonalize(ctx, grads, outs=None, weights=None, moments=None, new_moments=None, momentum=0.95,
@@ -796,8 +800,8 @@ def e2f_orthogonalize(ctx, grads, outs=None, weights=None, moments=None, new_mom
     for k, shape in enumerate(shapes):
         by_size.setdefault(shape[-2:], []).append(k)
     if len(by_size) > 1:  # (the library sees the matrices of one size at a time)
-        _disjoint([t for t in (outs, new_moments) if t is not None],
-                  [t for t in (grads, moments, None if decay == 0 else weights) if t is not None])
+        _disjoint([(outs, 2)] + ([] if new_moments is None else [(new_moments, 1)]),
+                  [grads, moments, None if decay == 0 else weights])
     device = grads[0].device
     stream = _stream(device)
     for (rows, cols), which in by_size.items():

@@ -1,0 +1,62 @@
+"""CPU-only checks of e2f_orthogonalize's lists of several sizes: which outputs may lie over which inputs, and that
+nothing is launched before every size is accepted.  The context has no device, so that the library checks its arguments
+and goes no further."""
+import ctypes
+
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def e2f():
+    import paper_2501_19216_amd as e
+    return e
+
+
+@pytest.fixture
+def call(e2f, monkeypatch):
+    """The binding with CPU tensors: "refused" where it or the library refuses, "accepted" where only the device is
+    missing."""
+    ctx = e2f.e2f_create(0, None)
+    monkeypatch.setattr(e2f, "_stream", lambda device=None: ctypes.c_void_p(0))
+
+    def run(grads, **kw):
+        kw.setdefault("workspace", torch.empty(256, dtype=torch.uint8))
+        try:
+            e2f.e2f_orthogonalize(ctx, grads, **kw)
+        except ValueError:
+            return "refused"
+        except e2f.E2FError as e:
+            return "accepted" if e.status == e2f.E2F_EDEVICE else "refused"
+    yield run
+    ctx.close()
+
+
+def test_outputs_over_tensors_of_another_size(call):
+    a, b, c, d = (torch.zeros(240) for _ in range(4))
+    two = lambda x, y: [x.view(8, 30), y.view(12, 20)]  # noqa: E731
+    grads, other = two(a, b), two(c, d)
+    e, f = torch.zeros(240), torch.zeros(240)
+    assert call(grads, outs=other) == "accepted"
+    # the other size's gradient, its own, the other size's weights and moments
+    assert call(grads, outs=two(b, c)) == "refused"
+    assert call(grads, outs=two(c, a)) == "refused"
+    assert call(grads, outs=grads) == "refused"
+    assert call(grads, outs=two(d, c), weights=two(c, d), decay=0.5) == "refused"
+    assert call(grads, outs=two(c, e), weights=two(e, d), decay=0.5) == "refused"
+    assert call(grads, outs=two(c, d), moments=two(d, e), new_moments=two(f, torch.zeros(240))) == "refused"
+    assert call(grads, outs=two(c, d), moments=two(e, f), new_moments=two(f, e)) == "refused"
+    assert call(grads, outs=two(c, d), moments=two(e, f), new_moments=two(e, b)) == "refused"
+    assert call(grads, outs=two(c, d), moments=two(e, f), new_moments=two(e, d)) == "refused"
+    # new moments where the weights are, and weights' outputs where the moments are
+    assert call(grads, outs=two(c, d), weights=two(e, f), decay=0.5, moments=two(c, d), new_moments=two(e, f)) == "refused"
+    # the tensors that they replace
+    assert call(grads, outs=other, weights=other, decay=0.5) == "accepted"
+    assert call(grads, outs=two(c, d), weights=two(c, d), decay=0.5) == "accepted"
+    assert call(grads, outs=other, weights=other, decay=0.5, moments=two(e, f)) == "accepted"
+    assert call(grads, outs=other, moments=two(e, f), new_moments=two(e, f)) == "accepted"
+    # weights given twice: in place for both, or for one that the other still needs
+    assert call(grads, outs=two(d, e), weights=two(c, c), decay=0.5) == "accepted"
+    assert call(grads, outs=two(c, e), weights=two(c, c), decay=0.5) == "refused"
+    # weights that are not read
+    assert call(grads, outs=two(d, c), weights=two(c, d)) == "accepted"
