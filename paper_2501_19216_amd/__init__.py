@@ -804,6 +804,8 @@ def e2f_orthogonalize(ctx, grads, outs=None, weights=None, moments=None, new_mom
                   [grads, moments, None if decay == 0 else weights])
     device = grads[0].device
     stream = _stream(device)
+    # every size is checked before the first is launched: a call that is refused has changed nothing
+    calls, need = [], 0
     for (rows, cols), which in by_size.items():
         _fits(rows, cols)
         many = [1 if len(shapes[k]) == 2 else shapes[k][0] for k in which]
@@ -814,14 +816,21 @@ def e2f_orthogonalize(ctx, grads, outs=None, weights=None, moments=None, new_mom
                 continue
             mine = tensors if len(by_size) == 1 else [tensors[k] for k in which]
             lists.append(_addresses(mine, many, rows * cols * mine[0].element_size()))
-        count = len(lists[0])
         prm = OrthogonalizeParams(rows, cols, steps, None if flat is None else flat.buffer_info()[0], eps, momentum,
                                   int(bool(nesterov)), scale, decay, _DTYPES[gt], _DTYPES[wt])
         b = ctypes.c_size_t(0)
-        _check(lib.e2f_orthogonalize_workspace_size(ctx.handle, ctypes.byref(prm), count, ctypes.byref(b)),
+        _check(lib.e2f_orthogonalize_workspace_size(ctx.handle, ctypes.byref(prm), len(lists[0]), ctypes.byref(b)),
                "e2f_orthogonalize_workspace_size")
-        space = _workspace(ctx, workspace, b.value, device, stream)
-        _check(lib.e2f_orthogonalize(ctx.handle, ctypes.byref(prm), count,
+        calls.append((prm, lists))
+        need = max(need, b.value)
+    space = _workspace(ctx, workspace, need, device, stream)
+    if len(calls) > 1 and need:
+        if space.numel() < need:
+            raise E2FError(E2F_ECAPACITY, "e2f_orthogonalize", "workspace of %d bytes is required" % need)
+        if space.data_ptr() % 256:
+            raise E2FError(E2F_EINVAL, "e2f_orthogonalize", "workspace must be 256-byte aligned")
+    for prm, lists in calls:
+        _check(lib.e2f_orthogonalize(ctx.handle, ctypes.byref(prm), len(lists[0]),
                                      *(None if a is None else a.buffer_info()[0] for a in lists), space.data_ptr(),
                                      space.numel(), stream), "e2f_orthogonalize")
     return outs

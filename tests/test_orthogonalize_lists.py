@@ -60,3 +60,52 @@ def test_outputs_over_tensors_of_another_size(call):
     assert call(grads, outs=two(c, e), weights=two(c, c), decay=0.5) == "refused"
     # weights that are not read
     assert call(grads, outs=two(d, c), weights=two(c, d)) == "accepted"
+
+
+class Counting:
+    """The library, with the launching calls counted."""
+
+    def __init__(self, lib):
+        self.lib, self.launches = lib, 0
+
+    def __getattr__(self, name):
+        if name == "e2f_orthogonalize":
+            self.launches += 1
+        return getattr(self.lib, name)
+
+
+def test_nothing_is_launched_before_every_size_is_accepted(call, e2f, monkeypatch):
+    lib = Counting(e2f.lib)
+    monkeypatch.setattr(e2f, "lib", lib)
+    small, large, larger = torch.zeros(8, 30), torch.zeros(200, 300), torch.zeros(300, 400)
+
+    def launches(grads, want, **kw):
+        lib.launches = 0
+        assert call(grads, outs=[torch.zeros_like(g) for g in grads], **kw) == want
+        return lib.launches
+
+    space = torch.empty((1 << 24) + 256, dtype=torch.uint8)
+    space = space[-space.data_ptr() % 256:]
+    assert launches([small, large, larger], "accepted", workspace=space) == 1  # (which says that there is no device)
+    sizes = []
+    for g in (large, larger):
+        b = ctypes.c_size_t(0)
+        prm = e2f.OrthogonalizeParams(*g.shape, 5, None, 1e-7, 0.95, 1, 1.0, 0.0, 0, 0)
+        ctx = e2f.e2f_create(0, None)
+        assert lib.e2f_orthogonalize_workspace_size(ctx.handle, ctypes.byref(prm), 1, ctypes.byref(b)) == e2f.E2F_OK
+        ctx.close()
+        sizes.append(b.value)
+    assert 0 < sizes[0] < sizes[1]
+    # enough for the first sizes only, in any order of them; not aligned; over a tensor of either size
+    for grads in ([small, large, larger], [large, larger, small], [larger, small, large]):
+        assert launches(grads, "accepted", workspace=space[:sizes[1]]) == 1
+        for n in (0, 255, sizes[0] - 1, sizes[0], sizes[1] - 1):
+            assert launches(grads, "refused", workspace=space[:n]) == 0, n
+        assert launches(grads, "refused", workspace=space[8:]) == 0
+    # matrices that fit a workgroup need none
+    assert launches([small, torch.zeros(5, 5)], "accepted", workspace=space[:0]) == 1
+    assert launches([small, torch.zeros(5, 5)], "accepted", workspace=space[8:]) == 1
+    # a size that is too large behind one that is not
+    huge = torch.zeros(1).expand(65537, 1)
+    assert launches([small, torch.zeros(65537, 1)], "refused", workspace=space) == 0
+    assert call([small, huge], workspace=space) == "refused"  # (not contiguous)
