@@ -799,9 +799,6 @@ def e2f_orthogonalize(ctx, grads, outs=None, weights=None, moments=None, new_mom
     by_size = {}
     for k, shape in enumerate(shapes):
         by_size.setdefault(shape[-2:], []).append(k)
-    if len(by_size) > 1:  # (the library sees the matrices of one size at a time)
-        _disjoint([(outs, 2)] + ([] if new_moments is None else [(new_moments, 1)]),
-                  [grads, moments, None if decay == 0 else weights])
     device = grads[0].device
     stream = _stream(device)
     # every size is checked before the first is launched: a call that is refused has changed nothing
@@ -824,11 +821,13 @@ def e2f_orthogonalize(ctx, grads, outs=None, weights=None, moments=None, new_mom
         calls.append((prm, lists))
         need = max(need, b.value)
     space = _workspace(ctx, workspace, need, device, stream)
-    if len(calls) > 1 and need:
+    if len(calls) > 1:  # (the library sees the matrices of one size at a time)
         if space.numel() < need:
             raise E2FError(E2F_ECAPACITY, "e2f_orthogonalize", "workspace of %d bytes is required" % need)
-        if space.data_ptr() % 256:
+        if need and space.data_ptr() % 256:
             raise E2FError(E2F_EINVAL, "e2f_orthogonalize", "workspace must be 256-byte aligned")
+        _disjoint([(outs, 2), ([space[:need]], -1)] + ([] if new_moments is None else [(new_moments, 1)]),
+                  [grads, moments, None if decay == 0 else weights])
     for prm, lists in calls:
         _check(lib.e2f_orthogonalize(ctx.handle, ctypes.byref(prm), len(lists[0]),
                                      *(None if a is None else a.buffer_info()[0] for a in lists), space.data_ptr(),

@@ -109,3 +109,24 @@ def test_nothing_is_launched_before_every_size_is_accepted(call, e2f, monkeypatc
     huge = torch.zeros(1).expand(65537, 1)
     assert launches([small, torch.zeros(65537, 1)], "refused", workspace=space) == 0
     assert call([small, huge], workspace=space) == "refused"  # (not contiguous)
+
+
+def test_a_workspace_over_a_tensor_of_any_size(call, e2f, monkeypatch):
+    lib = Counting(e2f.lib)
+    monkeypatch.setattr(e2f, "lib", lib)
+    space = torch.empty((1 << 24) + 256, dtype=torch.uint8)
+    space = space[-space.data_ptr() % 256:]
+    small, large = torch.zeros(8, 30), torch.zeros(200, 300)
+    at = space[1 << 20:(1 << 20) + 960].view(torch.float32).view(8, 30)
+    new = lambda: [torch.zeros(8, 30), torch.zeros(200, 300)]  # noqa: E731
+    for kw in (dict(outs=[at, new()[1]]), dict(outs=new(), moments=[at, new()[1]]),
+               dict(outs=new(), weights=[at, new()[1]], decay=0.5)):
+        for turn in (slice(None), slice(None, None, -1)):
+            lists = {k: v[turn] if isinstance(v, list) else v for k, v in kw.items()}
+            lib.launches = 0
+            assert call([small, large][turn], workspace=space, **lists) == "refused", kw
+            assert lib.launches == 0
+    assert call([at, large], outs=new(), workspace=space) == "refused"
+    # behind what the call needs of it
+    behind = space[1 << 23:(1 << 23) + 960].view(torch.float32).view(8, 30)
+    assert call([behind, large], outs=new(), workspace=space) == "accepted"
