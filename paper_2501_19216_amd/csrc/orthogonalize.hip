@@ -153,6 +153,12 @@ __device__ __forceinline__ void puts(void* p, int64_t i, int have, v4f x) {
   }
 }
 
+// What U is multiplied with, from the sum of its squares: NaN where a value is not finite, so that the others, which
+// its reciprocal would make zeros, are NaN without a step as well
+__device__ __forceinline__ double inverse_norm(double sum, float eps) {
+  return sum < INFINITY ? 1.0 / (sqrt(sum) + (double)eps) : NAN;
+}
+
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
@@ -237,7 +243,7 @@ __global__ __launch_bounds__(512) void k_ortho_small(Table t, Ends e, Steps step
   sum = 0.0;
 #pragma unroll
   for (int w = 0; w < 8; ++w) sum += squares[w];
-  const double inv = 1.0 / (sqrt(sum) + (double)u.eps);
+  const double inv = inverse_norm(sum, u.eps);
 #pragma unroll
   for (int s = 0; s < S; ++s)
 #pragma unroll
@@ -406,7 +412,7 @@ __global__ __launch_bounds__(256) void k_ortho_start(Table t, Sizes d, int parts
   const int z = blockIdx.z, i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
   double norm = 0.0;
   for (int k = threadIdx.x & 63; k < parts; k += 64) norm += part[(int64_t)z * parts + k];
-  const double inv = 1.0 / (sqrt(wave_sum(norm)) + (double)u.eps);
+  const double inv = inverse_norm(wave_sum(norm), u.eps);
   const int a = (threadIdx.x & 15) * 4, b = threadIdx.x >> 4;
   // four neighbours of the caller's matrix, of which `have` are there
   auto read = [&](int64_t at, int have) {
