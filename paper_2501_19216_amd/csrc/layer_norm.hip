@@ -258,11 +258,12 @@ __global__ __launch_bounds__(512) void k_layer_backward(LayerArgs a, LayerGrad g
           });
       row_sums(s1, tpr, red1);
       const float r1 = 1.0f / sqrtf(s1[N1 > 1 ? 1 : 0] * per * (1.0f / (L ? L : 1)) + a.eps);
-      const float back = r1 * r1 * r1 * per * (1.0f / (L ? L : 1)) * s1[N1 - 1];
+      // (a power of r1 at a time: its cube leaves float's range from values of 10^13 on)
+      const float back = r1 * (r1 * s1[N1 - 1]) * per * (1.0f / (L ? L : 1));
       each_higher<L>(
           [&](int s, int l) {
 #pragma unroll
-            for (int u = 0; u < V; ++u) d[s][u] = r1 * w[l][u] * d[s][u] - back * (1.0f / (2 * l + 1)) * x[s][u];
+            for (int u = 0; u < V; ++u) d[s][u] = r1 * w[l][u] * d[s][u] - back * (1.0f / (2 * l + 1)) * (r1 * x[s][u]);
           },
           [&](int l) {
 #pragma unroll
