@@ -88,10 +88,15 @@ __device__ __forceinline__ h4 read_transposed(const _Float16* p) {
 // 64 lanes' 16 bytes each to the LDS, lane after lane from `to` (the same for the wave) on, without passing
 // registers.  By hand: the compiler, which cannot tell the LDS's buffers apart, would wait for all such loads before
 // any read of the LDS. The instruction has no register for its result; who reads what it brings waits for vmcnt
-// first, by hand as well.  (Nothing else in a kernel that calls this uses m0.)
+// first, by hand as well.  It takes the LDS's address from m0 when it is issued; m0, which cannot be declared as
+// changed, is what it was afterwards.
 __device__ __forceinline__ void load_past(const _Float16* from, _Float16* to) {
   const unsigned at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) _Float16*)to);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory");
+  unsigned was;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
+               : "=&s"(was)
+               : "s"(at), "v"(from)
+               : "memory");
 }
 
 struct Table {
