@@ -354,9 +354,9 @@ typedef struct {
  *   out = decay weight + scale X.
  * grads, moments, new_moments, weights, outs: host arrays of `count` device addresses (an
  * element's alignment), read before the call returns.  moments (float32) and new_moments go together and may be NULL;
- * new_moments[t] may be moments[t].  weights may be NULL with decay = 0; outs[t] may be weights[t].  Apart
- * from these no output may overlap another tensor (E2F_EINVAL), and with decay = 0 and
- * momentum = 0 an input is still one.  X and the sums of the products are float32; the products'
+ * new_moments[t] may be moments[t]; outs[t] may be weights[t].  Apart from these no output may overlap another
+ * tensor (E2F_EINVAL).  With decay = 0 the weights are not looked at: they may be NULL or lie anywhere; with
+ * momentum = 0 the moments are still read.  X and the sums of the products are float32; the products'
  * operands have 22 bits (two float16 parts, scaled by bounds of the singular values that follow from the
  * coefficients: those for which they leave [0, 64], or |b t + c t^2| 4096, are refused, E2F_EINVAL).
  * A matrix with a value that is not finite becomes NaN; one of zeros stays zero (with eps > 0).

@@ -766,7 +766,9 @@ def e2f_orthogonalize(ctx, grads, outs=None, weights=None, moments=None, new_mom
     or stacks [batch, rows, cols] of any sizes; grads of one type, weights and outs of one
     (float32 or bfloat16), moments float32.  Without moments the gradients
     themselves are orthogonalised.  None: new tensors like weights (or grads) for outs, and
-    moments themselves for new_moments; outs may be weights.  Returns outs."""
+    moments themselves for new_moments; outs may be weights; apart from these no output may lie over another tensor.  A call that is
+    refused has changed nothing.  Under graph capture a workspace must be given, as for every operator with one, also
+    where no matrix needs it.  Returns outs."""
     if not grads:
         return [] if outs is None else outs
     gt, shapes = grads[0].dtype, list(map(_SHAPE, grads))

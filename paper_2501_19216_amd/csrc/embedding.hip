@@ -9,10 +9,14 @@
 // adds a type's parts in their order and writes zeros for types without rows.  No float atomics: the same bits every
 // time.
 //
-// 20,000 atoms of 100 types, L = 4, 128 channels: 49 us forward (256 MB at the rate of a copy), 25 backward in five
-// kernels of 4 to 8 us.  1.5 million rows of 64 bfloat16 channels of 100 types: 41 us forward, 97 backward, of which
-// the sort 25 and the sums 64 (192 MB of rows gathered at 3 TB/s, whatever the length of a stretch).  16,384 tokens
-// of 32,768 types, 1,024 bfloat16 channels: 9 us forward, 50 backward, of which 20 are the zeros of absent types.
+// 20,000 atoms of 100 types, L = 4, 128 channels: 51 us forward (256 MB at the rate of a copy; 34 where the last pass's
+// rows are written over), 23 backward in five kernels of 4 to 8 us.  1.5 million rows of 64 bfloat16 channels of 100
+// types: 60 us forward (41 over the last pass's rows), 81 backward, of which the sums 64 by themselves (192 MB of rows
+// gathered at 3 TB/s, whatever the length of a stretch) and the sort 25.  16,384 tokens of 32,768 types, 1,024 bfloat16
+// channels: 14 us forward (9 over the last pass's), 47 backward, of which 20 are the zeros of absent types.
+//
+// Times at the rules below are of whole gradients (at the forward's of forwards) on the same rows over and over, types
+// as often as atoms have them.
 #include <hip/hip_runtime.h>
 
 #include "e2f_launch.h"
@@ -81,7 +85,8 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs a, const TT* __restrict
 }
 
 // ------------------------------------------------------------------ rows by type
-constexpr int kSmall = 2048;  // rows that one workgroup sorts (7,680: the whole gradient 28 us against 20)
+// rows that one workgroup sorts (2,000 rows of 128 channels: 17.7 us, by many 18.9; 4,000 21.3 and 19.8; 7,680 28 and 20)
+constexpr int kSmall = 2048;
 
 // what lanes of this wave wrote to the LDS is there for its other lanes
 __device__ __forceinline__ void wave_sync() {
@@ -381,7 +386,10 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedArgs a, const T* __rest
 // What no workgroup held whole: zeros for a type without rows, and the parts of one that several workgroups hold, V
 // channels a lane.  A wave takes up to kEach types, taken far apart (types that many rows have stand side by side in
 // most numberings); where a type has more than kMany parts all threads of its workgroup add them, as many side by
-// side as the channels leave room for
+// side as the channels leave room for.
+// (kMany: 20,000 rows of 128 channels 20.8 us, with 8 20.8, with 128 24.4; 1.5 million of 64 bfloat16 ones 69.2, 69.9 and
+// 73.0.  kEach: 20,000 rows of 2,000,000 types, 4 channels: one type a wave 867 us, two 665, eight 504, 32 486; 16,384 rows
+// of 32,768 types, 1,024 channels: 55.2, 52.9, 53.1, 53.1)
 constexpr int kMany = 32, kEach = 8;
 template <typename TT, int V>
 __global__ __launch_bounds__(1024) void k_embed_join(EmbedArgs a, Sorted s, TT* __restrict__ gt, unsigned apart, int each,
@@ -471,10 +479,14 @@ Layout layout_of(int n, int V, int C, bool bf16) {
   Layout l{};
   l.passes = 1;
   while (l.passes < 4 && (uint64_t)V >> (8 * l.passes)) ++l.passes;  // (types 0 .. V)
-  // rounds of 64 rows a wave of the sort: up to 512 workgroups with one, then up to 2,048 with four, then 16
+  // rounds of 64 rows a wave of the sort: up to 512 workgroups with one, then up to 2,048 with four, then 16 (130,000 rows
+  // of 64 bfloat16 channels: one 27.8 us, four 28.3, 16 37.5; 262,144 rows 36.0, 33.8, 45.1; 1.5 million 86.7, 69.6, 76.7;
+  // six million of 16 channels 290, 212, 200)
   l.rounds = n <= 1 << 17 ? 1 : n <= 1 << 21 ? 4 : 16;
   l.groups = (int)(((int64_t)n + 256 * l.rounds - 1) / (256 * l.rounds));
-  // rows of a stretch: 8 (all in flight) until the workgroups are 2,048, then up to 64
+  // rows of a stretch: 8 (all in flight) until the workgroups are 2,048, then up to 64 (20,000 rows of 128 channels: 8
+  // rows 20.8 us, 16 20.9, 32 22.1, 64 24.4; 400,000 of 64 bfloat16 ones 40.0, 39.2, 38.0, 39.8; 1.5 million 76.5, 70.2,
+  // 69.2, 70.0)
   const int Q = pieces_of(C, bf16);
   l.tpr = lanes_of(C, Q);
   const int columns = (C / Q + l.tpr - 1) / l.tpr;
@@ -520,7 +532,8 @@ hipError_t launch_embed_forward(const EmbedArgs& a, const void* table, void* out
   const int64_t pieces = (int64_t)a.K * a.C / V;
   int tpr = 1;
   while (tpr < 64 && tpr < pieces) tpr <<= 1;
-  // four rows a thread where a row is one round of its threads and there are enough to fill the GPU
+  // four rows a thread where a row is one round of its threads and there are enough to fill the GPU (64 bfloat16
+  // channels: 60,000 rows 4.6 us with one, 5.2 with four; 262,144 10.0 and 10.4; 1.5 million 39.6 and 35.0)
   const bool four = pieces <= 64 && (int64_t)a.n * tpr > 1 << 20;
   const int64_t rows = 256 / tpr * (four ? 4 : 1);
   const Rounds r = rounds_of(((int64_t)a.n + rows - 1) / rows, 256);
@@ -595,7 +608,9 @@ hipError_t launch_embed_backward(const EmbedArgs& a, const void* gout, void* gta
   }
   // (the table's type alone: the parts are float)
   const int V = pieces_of(a.C, a.table_bf16), tpr = lanes_of(a.C, V), columns = (a.C / V + 63) / 64;
-  // types of a wave: as many workgroups as the GPU holds at once, where there are that many types
+  // types of a wave: as many workgroups as the GPU holds at once, where there are that many types; where there are
+  // fewer, a type's channels side by side as well (1,024 channels: 2,000 rows of 200 types 16.0 us, one after the other
+  // 18.2; 20,000 of 4,000 types 44.2 and 41.9; but 16,384 of 32,768 types 69.2 and 53.1)
   int each = 1;
   while (each < kEach && a.V / (16 * each) > 512) each <<= 1;
   const unsigned apart = ((unsigned)a.V + 16 * each - 1) / (16 * each);

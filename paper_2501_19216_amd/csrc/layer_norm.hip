@@ -13,9 +13,10 @@
 // statistics from x again, which it reads anyway: nothing is kept from the forward.  Sums, statistics and everything
 // between loads and stores are float; outputs are rounded once.
 //
-// 20,000 atoms, L = 4, 128 float channels: 86 us forward, 154 backward and 5 for the weights' sums, the rate of a
-// copy (5.1 TB/s) for all that is read and written.  A million rows of 64 bfloat16 channels with their activation: 62
-// us forward (4.1 TB/s), 106 backward (3.6), where the activation's arithmetic begins to show.
+// 20,000 atoms, L = 4, 128 float channels: 87 us forward, 155 backward and 5 for the weights' sums, the rate of a
+// copy (5.1 TB/s) for all that is read and written.  A million rows of 64 bfloat16 channels with their activation: 64
+// us forward (4.0 TB/s), 104 backward (3.7), where the activation's arithmetic begins to show.  Times at the rules below
+// are of the forward, or of the backward with the weights' sums, on the same rows over and over.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -48,8 +49,8 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int tpr, float (*red)[N]
 }
 
 // (by the power of -|x|, whose argument keeps its low part: a shut gate keeps its digits, to 6 roundings down to
-// 2^-126.  With the library's exponential and an IEEE quotient a million rows of 64 bfloat16 channels take 92 us
-// forward and 164 backward, this way 62 and 140)
+// 2^-126.  With the library's exponential and an IEEE quotient a million rows of 64 bfloat16 channels take 77 us
+// forward and 129 backward, this way 55 and 111)
 __device__ __forceinline__ float sigmoid(float x) {
   constexpr float kLog2e = 1.44269504f, kLow = 1.92596299e-8f, kLn2 = 0.693147181f;
   const float a = -fabsf(x), hi = a * kLog2e, lo = fmaf(a, kLog2e, -hi) + a * kLow;
@@ -384,14 +385,25 @@ __global__ __launch_bounds__(1024) void k_layer_weights(const float* __restrict_
   }
 }
 
-constexpr int kForwardBlocks = 4096;  // of a launch, which take rows in turn
+// of a launch, which take rows in turn (a million rows of 64 bfloat16 channels: 63.8 us, of 1,024 workgroups 67.8, of
+// 16,384 67.6, of a row each 74.5; 20,000 atoms, L = 4, 128 channels: 94.9, 97.7, 91.4, 91.6; 200,000 rows of 512 floats:
+// 155, 149, 141, 136)
+constexpr int kForwardBlocks = 4096;
 
 struct Shape {
   int V, J, tpr, threads;
   bool tail;
 };
-// Channels of a thread: 16 bytes of plain rows in the forward and four values in the backward, as many pieces as a row
-// needs beyond a wave; of irrep features as many as keep a row's components in its registers
+// Channels of a thread.  Plain rows: 16 bytes in the forward, and in the backward up to 512 channels (a million rows of 64
+// bfloat16 ones with activation 107 us, with four a thread 129; 100,000 of 512 64.5 and 65.1), above four values
+// (50,000 rows of 1,024 73.0 us, but with eight 62.3); beyond a wave two pieces and more (50,000 rows of 512 floats: backward
+// 57.4 us, in one piece 62.3, in four 70.0; 20,000 of 2,048 bfloat16 61.9, 99.9, 61.2).
+// Irrep features: four, two (L = 2, 3) or one, so that the backward holds both rows of components in registers (128
+// channels: 40,000 atoms, L = 1: 43.5 us, with two 46.7; 20,000, L = 2: 48.9, with four 49.9, with one 56.5; L = 3: 99.1,
+// 100.0, 93.6; L = 4: 150.9, with two 151.1; 10,000, L = 6: 148, with two 388).  Two things this does not reach: one
+// bfloat16 a thread, loads of two bytes, is slow in the backward (20,000 atoms, L = 4: 288 us, with two 81), and above 512 channels
+// with L >= 4 a thread has two, whose backward spills at L = 5 (32 registers, bfloat16 38; 5,000 atoms of 1,024 channels 589
+// us, 10,000 of 512 412) and at L = 6 (120; 1,467 and 565)
 Shape shape_of(int L, int C, bool bf16, bool back) {
   Shape s{};
   if (L) {

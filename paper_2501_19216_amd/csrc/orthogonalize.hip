@@ -12,17 +12,19 @@
 // sixteenth of the directions strong and the others a hundredth of them).  So X stays float and a X is added in
 // float, which gives 1e-5 too; the products, whose errors stay in the directions that are already large, take their
 // operands as two float16 numbers, x = hi + lo to 22 bits, in three products (hi hi, hi lo, lo hi) on the matrix
-// cores, summed in float.  Powers of two keep the operands in float16's range: from the coefficients follow bounds of
+// cores, summed in float.  In all X ends 0.7e-6 to 2.2e-6 from the exact matrix (17 sizes from 16 x 16 to
+// 1270 x 380, three spectra), 0.3 to 1.3 of where library products in float end; the operands' rounding alone, with exact
+// sums, is 0.5e-6 to 0.7e-6 of it.  Powers of two keep the operands in float16's range: from the coefficients follow bounds of
 // all singular values (ortho_bounds).
 //
 // Matrices that fit a workgroup's registers and LDS go through all steps there (k_ortho_small); larger ones through
 // three tiled products a step.  Those hold Y = X^T alone: Y' = a Y + Y B (B = b P + c P^2 is symmetric) reads rows of
 // Y and of B, and P = Y^T Y reads its operands by the LDS's transposing loads.
 //
-// Sixty matrices of 128 x 128 with momentum and weights take 50 us in one launch (three tiled products a step 151, of
-// which launches are the most), of which a step is 7.4: matrix cores 3.3, reads of the LDS and four barriers between
-// the phases, two waves a SIMD.  Four of 1024 x 4096 take 1.15 ms, 244 TFLOP/s (library products in float 72): P 80
-// us a step, P^2 27, B X 118, the norm and the first Y 91.  B X is the sum of what its parts take alone: the matrix
+// Sixty matrices of 128 x 128 with momentum and weights take 50 us in one launch (without both 45; by three tiled
+// products a step 94), of which a step is 7.4: matrix cores 3.3, reads of the LDS and four barriers between
+// the phases, two waves a SIMD.  Four of 1024 x 4096 take 1.16 ms, 241 TFLOP/s (library products in float 72): P 84
+// us a step, P^2 28, B X 120, the norm and the first Y 91.  B X is the sum of what its parts take alone: the matrix
 // cores 45, the loads to the LDS 60 (20 bytes a cycle and CU), the float and split Y 41; more buffers of a step,
 // tiles of 256, loads issued before the LDS is read, priorities of waves and other strides of memory left it where it
 // is.
@@ -679,12 +681,13 @@ Sizes sizes_of(int rows, int cols, int count, bool* small, int* tile) {
   d.rows = rows, d.cols = cols, d.turned = rows >= cols;  // (of square ones the transpose, whose columns are rows in memory)
   d.m = d.turned ? cols : rows, d.n = d.turned ? rows : cols;
   d.mp = small_rows(d.m), d.np = (d.n + 31) / 32 * 32;
-  // (sixty of 128 x 128 46 us, by tiled products 96; one 44 and 77, 200 of them 180 and 367)
+  // (without momentum and weights, as all times here: sixty of 128 x 128 45 us, by tiled products 94; one 44 and 76, 200 of
+  // them 177 and 365; sixty of 64 x 384, whose four strips of a wave leave four registers in memory, 45 and 107)
   *small = d.mp && d.np <= 512 && small_bytes(d.mp, d.np) <= kLds;
   if (*small) return d;
   // tiles of 128, each value of which is loaded and read from the LDS half as often, where they fill the GPU and pad
-  // little (four matrices of 1024 x 4096 1.19 ms, with tiles of 64 1.32; one 456 us and 498; 64 of 512 x 512 1.00 and 1.11
-  // ms; but 30 of 400 x 400, which become 512, 501 and 382 us)
+  // little (four matrices of 1024 x 4096 1.10 ms, with tiles of 64 1.25; one 397 us and 414; 64 of 512 x 512 0.97 and 1.04
+  // ms; but 30 of 400 x 400, which become 512, 428 and 371 us, and one of 1024 x 1024, 64 tiles, 281 and 190)
   const int64_t tiles = (int64_t)((d.m + 127) / 128) * ((d.n + 127) / 128);
   const int64_t fine = (int64_t)((d.m + 63) / 64) * ((d.n + 63) / 64);
   *tile = tiles * (count < kTable ? count : kTable) >= 256 && 40 * tiles <= 11 * fine ? 128 : 64;
@@ -811,7 +814,9 @@ void launch_product(int tile, Product g, const Ends& e, const Sizes& d, const Up
   const unsigned blocks = (unsigned)((g.tiles * g.count + 7) / 8 * 8);
   if (tile == 128)
     k_ortho_product<KIND, 128, 2, 4, 1, 2, T><<<blocks, 512, 0, st>>>(g, e, d, u);
-  else if (g.tiles * g.count <= 256 && g.steps >= 16)  // (300 x 3000 202 us, with four waves 245)
+  // (300 x 3000 204 us, with four waves 250; 1024 x 1024 190 and 219; six of 517 x 200 119 and 126.  Beyond the bounds it
+  // makes no difference: 12 of 300 x 3000 404 us and 409, one of 200 x 200 93.5 and 95.0)
+  else if (g.tiles * g.count <= 256 && g.steps >= 16)
     k_ortho_product<KIND, 64, 2, 2, 2, 3, T><<<blocks, 512, 0, st>>>(g, e, d, u);
   else
     k_ortho_product<KIND, 64, 2, 2, 1, 3, T><<<blocks, 256, 0, st>>>(g, e, d, u);
@@ -830,8 +835,8 @@ hipError_t launch_large(const Table& t, const Ends& e, const Steps& steps, const
   k_ortho_start<TG><<<dim3(d.np / 64, d.mp / 64, count), 256, 0, st>>>(t, d, (int)parts, u, ldexpf(1.0f, steps.x[0]), part,
                                                                        y, ys[0]);
   const int mt = d.mp / 128;
-  // (the triangle's tiles are fewer: tiles of 64 until 512 of 128 are there.  One matrix of 4096 x 4096, 528 of them, 4.41
-  // ms against 5.29 with 64; four of 1024 x 4096, 144 of them, 1.27 ms against 1.21)
+  // (the triangle's tiles are fewer: tiles of 64 until 512 of 128 are there.  One matrix of 4096 x 4096, 528 of them, 4.36
+  // ms against 5.26 with 64; four of 1024 x 4096, 144 of them, 1.21 ms against 1.09)
   const int tri = tile == 128 && (int64_t)mt * (mt + 1) / 2 * count >= 512 ? 128 : 64;
   for (int k = 0; k < steps.count; ++k) {
     const int xe = steps.x[k], pe = steps.p[k], be = steps.b[k];
